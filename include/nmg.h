@@ -58,7 +58,7 @@
  *   - Arguments are validated on the host before anything is launched; on an
  *     error nothing is enqueued and no output is written.
  *   - Floating-point inputs must be finite for the product; the selection is
- *     defined for every input, NaN included.
+ *     defined for every input, NaN included (attention: see there).
  */
 #ifndef NMG_H
 #define NMG_H
@@ -491,6 +491,128 @@ int64_t nmg_p_spmm_workspace_bytes(const nmg_p_layout *layout, nmg_kernel kernel
 /* Chunked layout -> dense W_out (M x K, leading dimension ldw >= K). */
 nmg_status nmg_p_densify(const nmg_p_layout *layout, const void *values, const uint8_t *index,
                          void *W_out, int64_t ldw, hipStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * ATTENTION BETWEEN SPARSE PROJECTIONS.  What stands between the products of a
+ * transformer layer, on the same activations: features x tokens, row-major, a
+ * row per feature, tokens contiguous, any leading dimension >= the number of
+ * tokens.  Head h of a matrix of heads is rows [h D, h D + D).
+ *
+ * Inputs may hold infinities and NaN: they reach the outputs that the formulas
+ * below make them reach, and no others.
+ * ---------------------------------------------------------------------- */
+
+/* Position rotation.  The first `dim` = R rows of every head are R / 2 pairs;
+ * pair i of a token at position p turns by the table's angle:
+ *     a' = a c - b s,  b' = a s + b c,   c = table[i][p], s = table[R/2 + i][p]
+ * rows >= R are copied.  Tables are binary32, R x length: R / 2 rows of cosines,
+ * then R / 2 of sines. */
+typedef enum nmg_rotary_pairs {
+    NMG_ROTARY_HALF = 0,        /* pair i: rows i and i + R/2    */
+    NMG_ROTARY_INTERLEAVED = 1  /* pair i: rows 2 i and 2 i + 1  */
+} nmg_rotary_pairs;
+
+typedef struct nmg_rotary_desc {
+    int32_t dim;                /* R: rows of a head that turn, even, 0 .. D (0: none) */
+    nmg_rotary_pairs pairs;
+    int64_t length;             /* positions in the table                              */
+    const float *table;         /* R x length, device; may be NULL when dim is 0       */
+    const int32_t *positions;   /* position of every token, device; a position outside
+                                   [0, length) is taken as the nearest one inside
+                                   (may be NULL when dim is 0)                         */
+} nmg_rotary_desc;
+
+/* How the frequencies f_i = base^(-2i/R) are changed for contexts longer than
+ * the `original` length a model was trained on, by a factor `factor`:
+ *   LINEAR  f_i / factor
+ *   NTK     base becomes base * factor^(R / (R - 2))
+ *   PARTS   a pair that turns r = original f_i / 2 pi times over the original
+ *           length keeps its frequency for r >= fast, takes f_i / factor for
+ *           r <= slow, and a blend linear in r between them */
+typedef enum nmg_rotary_scaling {
+    NMG_ROTARY_PLAIN = 0,
+    NMG_ROTARY_LINEAR = 1,
+    NMG_ROTARY_NTK = 2,
+    NMG_ROTARY_PARTS = 3
+} nmg_rotary_scaling;
+
+/* table (dim x length, device): magnitude * cos(p f_i) and magnitude * sin(p f_i)
+ * for p = 0 .. length - 1, computed in binary64 and rounded once.  factor >= 1
+ * unless PLAIN; original > 0 and fast > slow >= 0 for PARTS; dim even, >= 2 (>= 4 for
+ * NTK); base > 0. */
+nmg_status nmg_rotary_table(int32_t dim, int64_t length, double base, nmg_rotary_scaling scaling,
+                            double factor, double original, double slow, double fast,
+                            double magnitude, float *table, hipStream_t stream);
+
+/* Y = the rotation of X: `heads` heads of `head_dim` rows, N tokens.  Computed in
+ * binary32, rounded once.  Y may be X (ldy = ldx); else they do not overlap. */
+nmg_status nmg_rotary(nmg_dtype dtype, int32_t heads, int32_t head_dim,
+                      const nmg_rotary_desc *rotary, const void *X, int64_t ldx, int64_t N,
+                      void *Y, int64_t ldy, hipStream_t stream);
+
+/* Queries and keys of one layer in one pass: every head's column x (head_dim
+ * values of one token) becomes the rotation of
+ *     x[d] * w[d] / sqrt(sum_d x[d]^2 / head_dim + eps)
+ * with w = q_weight for the q_heads heads of Q, k_weight for the k_heads of K
+ * (binary32, head_dim values; NULL: ones).  binary32 throughout, rounded once.
+ * k_heads may be 0 (K, YK unused).  YQ may be Q and YK may be K. */
+nmg_status nmg_qk_norm_rotary(nmg_dtype dtype, int32_t q_heads, int32_t k_heads, int32_t head_dim,
+                              const nmg_rotary_desc *rotary, const float *q_weight,
+                              const float *k_weight, float eps, const void *Q, int64_t ldq,
+                              const void *K, int64_t ldk, int64_t N, void *YQ, int64_t ldyq,
+                              void *YK, int64_t ldyk, hipStream_t stream);
+
+/* Heads of an attention: query head h reads key head h / (heads / kv_heads). */
+typedef struct nmg_heads {
+    int32_t heads, kv_heads;    /* heads a multiple of kv_heads       */
+    int32_t head_dim;           /* 1 .. 256                           */
+    nmg_dtype dtype;
+} nmg_heads;
+
+/* Sequences: ranges of columns, int32 on the device (read when the kernels run,
+ * so a captured call follows their contents).  Sequence b has the query columns
+ * [q_offsets[b], q_offsets[b+1]) and the key columns [kv_begin[b], kv_end[b]).
+ * Query ranges follow one another; key ranges may be anywhere, also the same
+ * for several sequences.  Ranges are cut to the matrices' columns; query
+ * columns of no sequence are not written. */
+typedef struct nmg_sequences {
+    int32_t count;
+    const int32_t *q_offsets;   /* count + 1, ascending */
+    const int32_t *kv_begin;    /* count                */
+    const int32_t *kv_end;      /* count                */
+} nmg_sequences;
+
+/* O = softmax(scale Q^T K) V^T of every sequence and head, features x tokens:
+ * Q, O heads * head_dim x Nq, K, V kv_heads * head_dim x Nk.  A sequence's query
+ * columns attend to its key columns j with key_mask[j] != 0 (Nk bytes; NULL: to
+ * all).  What other columns of K and V hold never matters.  A query with no
+ * key, or all of whose scores are minus infinity, gives 0.  scale > 0.
+ * Statistics and sums are binary32; binary16 weights are rounded to binary16
+ * for the product with V.  O overlaps no input.  Nk may be 0 (K, V unused).
+ *
+ * workspace (may be NULL; 256-byte aligned): lets few queries over many keys be
+ * split over the GPU.  Too little of it: fewer splits, none with 0.  The number
+ * of splits, and with it the order of sums, depends on the sizes and on
+ * workspace_bytes alone.  nmg_attention_workspace_bytes: the most a call uses
+ * (pure host code; 0 when it would not split, -1 for invalid arguments). */
+nmg_status nmg_attention(const nmg_heads *heads, const nmg_sequences *sequences, const void *Q,
+                         int64_t ldq, int64_t Nq, const void *K, int64_t ldk, const void *V,
+                         int64_t ldv, int64_t Nk, const uint8_t *key_mask, float scale, void *O,
+                         int64_t ldo, void *workspace, int64_t workspace_bytes,
+                         hipStream_t stream);
+
+/* nmg_attention for a tree of drafted tokens behind a cache: a sequence's n
+ * query columns are drafted tokens, whose keys and values are the last n columns
+ * of its key range.  Token t (query column c) attends to every earlier column
+ * of the range, and to drafted token i exactly if i < width and tree[c * ldtree +
+ * i] != 0 (bytes, Nq x width, ldtree >= width). */
+nmg_status nmg_tree_attention(const nmg_heads *heads, const nmg_sequences *sequences,
+                              const void *Q, int64_t ldq, int64_t Nq, const void *K, int64_t ldk,
+                              const void *V, int64_t ldv, int64_t Nk, const uint8_t *tree,
+                              int64_t ldtree, int64_t width, float scale, void *O, int64_t ldo,
+                              void *workspace, int64_t workspace_bytes, hipStream_t stream);
+int64_t nmg_attention_workspace_bytes(const nmg_heads *heads, int32_t sequences, int64_t Nq,
+                                      int64_t Nk);
 
 /* Static description of a status code; never NULL. */
 const char *nmg_status_str(nmg_status status);

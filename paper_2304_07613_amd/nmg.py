@@ -27,6 +27,8 @@ KERNELS = {"auto": 0, "valu": 1, "mfma": 2, "mfma_general": 3, "mfma_scalar": 4,
            "mfma_expand": 11, "sparse": 12}
 _KERNEL_NAME = {v: k for k, v in KERNELS.items()}
 EPILOGUES = {"none": 0, "gelu": 1, "add": 2}
+ROTARY_PAIRS = {"half": 0, "interleaved": 1}
+ROTARY_SCALING = {"none": 0, "linear": 1, "ntk": 2, "parts": 3}
 
 OK, ERR_NULL, ERR_PARAM, ERR_SHAPE, ERR_DTYPE, ERR_ALIGN, ERR_LAUNCH, ERR_UNSUPPORTED, ERR_CAPACITY = \
     range(9)
@@ -44,6 +46,21 @@ class _Layout(ctypes.Structure):
     _fields_ = [("M", ctypes.c_int32), ("K", ctypes.c_int32), ("n", ctypes.c_int32),
                 ("m", ctypes.c_int32), ("g", ctypes.c_int32), ("C", ctypes.c_int32),
                 ("dtype", ctypes.c_int)]
+
+
+class _Rotary(ctypes.Structure):
+    _fields_ = [("dim", ctypes.c_int32), ("pairs", ctypes.c_int), ("length", ctypes.c_int64),
+                ("table", ctypes.c_void_p), ("positions", ctypes.c_void_p)]
+
+
+class _Heads(ctypes.Structure):
+    _fields_ = [("heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int)]
+
+
+class _Sequences(ctypes.Structure):
+    _fields_ = [("count", ctypes.c_int32), ("q_offsets", ctypes.c_void_p),
+                ("kv_begin", ctypes.c_void_p), ("kv_end", ctypes.c_void_p)]
 
 
 class _PLayout(ctypes.Structure):
@@ -74,6 +91,8 @@ def _load():
     L = ctypes.CDLL(LIB_PATH)
     vp, i64, i32, lp = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32, ctypes.POINTER(_Layout)
     pp = ctypes.POINTER(_PLayout)
+    rp, hp, sp = (ctypes.POINTER(t) for t in (_Rotary, _Heads, _Sequences))
+    f32, f64 = ctypes.c_float, ctypes.c_double
     sig = {
         "nmg_layout_init": ([lp, i32, i32, i32, i32, i32, ctypes.c_int], ctypes.c_int),
         "nmg_values_numel": ([lp], i64),
@@ -109,6 +128,16 @@ def _load():
         "nmg_spmm_x16": ([lp, vp, vp, i64, i64, vp, i64, vp], ctypes.c_int),
         "nmg_spmm_x16_epilogue": ([lp, vp, ctypes.c_int, vp, i64, i64, vp, i64, vp, i64, vp],
                                   ctypes.c_int),
+        "nmg_rotary_table": ([i32, i64, f64, ctypes.c_int, f64, f64, f64, f64, f64, vp, vp],
+                             ctypes.c_int),
+        "nmg_rotary": ([ctypes.c_int, i32, i32, rp, vp, i64, i64, vp, i64, vp], ctypes.c_int),
+        "nmg_qk_norm_rotary": ([ctypes.c_int, i32, i32, i32, rp, vp, vp, f32, vp, i64, vp, i64, i64,
+                                vp, i64, vp, i64, vp], ctypes.c_int),
+        "nmg_attention": ([hp, sp, vp, i64, i64, vp, i64, vp, i64, i64, vp, f32, vp, i64, vp, i64,
+                           vp], ctypes.c_int),
+        "nmg_tree_attention": ([hp, sp, vp, i64, i64, vp, i64, vp, i64, i64, vp, i64, i64, f32, vp,
+                                i64, vp, i64, vp], ctypes.c_int),
+        "nmg_attention_workspace_bytes": ([hp, i32, i64, i64], i64),
         "nmg_status_str": ([ctypes.c_int], ctypes.c_char_p),
         "nmg_version": ([], ctypes.c_char_p),
     }
@@ -517,3 +546,158 @@ def p_refine(W: torch.Tensor, index: torch.Tensor, layout: PLayout):
     _check(lib().nmg_p_refine(layout.c, W.data_ptr(), _rows(W, "W"), values.data_ptr(),
                               idx.data_ptr(), _stream(W)), "nmg_p_refine")
     return values, idx
+
+
+# ---------------------------------------- attention between sparse projections
+
+def rotary_table(length: int, dim: int, base: float = 10000.0, scaling: str = "none",
+                 factor: float = 1.0, original: float = 0.0, slow: float = 1.0, fast: float = 32.0,
+                 magnitude: float = 1.0, device="cuda") -> torch.Tensor:
+    """``nmg_rotary_table``: (2, dim / 2, length) binary32, cosines then sines
+    of every position's angles; made once for a model and a length.  scaling
+    "linear", "ntk" and "parts" stretch it to `factor` times the context,
+    "parts" from the `original` length."""
+    if scaling not in ROTARY_SCALING:
+        raise ValueError(f"unknown scaling {scaling!r}")
+    if dim < 2 or dim % 2 or length < 1:
+        raise ValueError("dim must be even and length positive")
+    table = torch.empty((2, dim // 2, length), dtype=torch.float32, device=device)
+    _need_cuda(table)
+    _check(lib().nmg_rotary_table(dim, length, base, ROTARY_SCALING[scaling], factor, original,
+                                  slow, fast, magnitude, table.data_ptr(), _stream(table)),
+           "nmg_rotary_table")
+    return table
+
+
+def _rotary_desc(table, positions, pairs: str, N: int) -> _Rotary:
+    code = ROTARY_PAIRS.get(pairs)
+    if code is None:
+        raise ValueError(f"unknown rotary layout {pairs!r}")
+    if table is None:
+        return _Rotary(0, code, 0, None, None)
+    shape = table.shape
+    if len(shape) != 3 or shape[0] != 2 or table.dtype != torch.float32 or not table.is_contiguous():
+        raise ValueError("table must be a contiguous float32 (2, dim / 2, length) tensor")
+    if positions.dtype != torch.int32 or positions.shape != (N,) or not positions.is_contiguous():
+        raise ValueError("positions must be N contiguous int32 values")
+    _need_cuda(table, positions)
+    return _Rotary(2 * shape[1], code, shape[2], table.data_ptr(), positions.data_ptr())
+
+
+def _head_rows(t: torch.Tensor, heads: int, name: str) -> int:
+    """Rows of one head of a features x tokens matrix."""
+    rows = t.shape[0]
+    if heads < 1 or rows % heads or not rows:
+        raise ValueError(f"{name} must have a whole number of rows for each of {heads} heads")
+    return rows // heads
+
+
+def _out_like(t: torch.Tensor, out, name: str) -> torch.Tensor:
+    if out is None:
+        return t.new_empty(t.shape)
+    if out.dtype != t.dtype or out.shape != t.shape:
+        raise ValueError(f"{name} must have the shape and dtype of its input")
+    return out
+
+
+def rotary(X, heads: int, table, positions, layout: str = "half", out=None):
+    """``nmg_rotary``: the first 2 * table.shape[1] rows of each of the `heads`
+    heads of X (features x tokens) turned by their tokens' positions, the
+    others copied.  out may be X."""
+    code = _DTYPE_CODE.get(X.dtype)
+    if code is None:
+        raise TypeError(f"unsupported dtype {X.dtype}")
+    ldx, N = _rows(X, "X"), X.shape[1]
+    D = _head_rows(X, heads, "X")
+    out = _out_like(X, out, "out")
+    _need_cuda(X, out)
+    desc = _rotary_desc(table, positions, layout, N)
+    _check(lib().nmg_rotary(code, heads, D, desc, X.data_ptr(), ldx, N, out.data_ptr(),
+                            _rows(out, "out"), _stream(X)), "nmg_rotary")
+    return out
+
+
+def qk_norm_rotary(Q, K, heads: int, kv_heads: int, q_weight, k_weight, table=None, positions=None,
+                   layout: str = "half", eps: float = 1e-6, out=None):
+    """``nmg_qk_norm_rotary``: RMS norm of every head's column of Q and K
+    (weights float32 of head_dim, or None) and the rotation (none without a
+    table).  out: (Q's, K's), which may be Q and K.  Returns both."""
+    code = _DTYPE_CODE.get(Q.dtype)
+    if code is None or K.dtype != Q.dtype:
+        raise TypeError("Q and K must be float32 or float16, of one dtype")
+    ldq, ldk, N = _rows(Q, "Q"), _rows(K, "K"), Q.shape[1]
+    D = _head_rows(Q, heads, "Q")
+    if _head_rows(K, kv_heads, "K") != D or K.shape[1] != N:
+        raise ValueError("Q and K must have heads of one size and the same tokens")
+    yq, yk = (None, None) if out is None else out
+    yq, yk = _out_like(Q, yq, "out[0]"), _out_like(K, yk, "out[1]")
+    _need_cuda(Q, K, yq, yk)
+    for w in (q_weight, k_weight):
+        if w is not None:
+            if w.dtype != torch.float32 or w.shape != (D,) or not w.is_contiguous():
+                raise ValueError("norm weights must be head_dim contiguous float32 values")
+            _need_cuda(w)
+    desc = _rotary_desc(table, positions, layout, N)
+    _check(lib().nmg_qk_norm_rotary(
+        code, heads, kv_heads, D, desc, None if q_weight is None else q_weight.data_ptr(),
+        None if k_weight is None else k_weight.data_ptr(), eps, Q.data_ptr(), ldq, K.data_ptr(), ldk,
+        N, yq.data_ptr(), _rows(yq, "out[0]"), yk.data_ptr(), _rows(yk, "out[1]"), _stream(Q)),
+        "nmg_qk_norm_rotary")
+    return yq, yk
+
+
+def _attend(fn, Q, K, V, heads, kv_heads, q_offsets, kv_begin, kv_end, extra, scale, out):
+    code = _DTYPE_CODE.get(Q.dtype)
+    if code is None or K.dtype != Q.dtype or V.dtype != Q.dtype:
+        raise TypeError("Q, K and V must be float32 or float16, of one dtype")
+    ldq, Nq, Nk = _rows(Q, "Q"), Q.shape[1], K.shape[1]
+    D = _head_rows(Q, heads, "Q")
+    if _head_rows(K, kv_heads, "K") != D or V.shape != K.shape:
+        raise ValueError("K and V must have kv_heads heads of Q's head size, and the same tokens")
+    B = kv_begin.shape[0]
+    for t, n, name in ((q_offsets, B + 1, "q_offsets"), (kv_begin, B, "kv_begin"), (kv_end, B, "kv_end")):
+        if t.dtype != torch.int32 or t.shape != (n,) or not t.is_contiguous():
+            raise ValueError(f"{name} must be {n} contiguous int32 values")
+    out = _out_like(Q, out, "out")
+    _need_cuda(Q, K, V, out, q_offsets, kv_begin, kv_end)
+    L = lib()
+    h = _Heads(heads, kv_heads, D, code)
+    s = _Sequences(B, q_offsets.data_ptr(), kv_begin.data_ptr(), kv_end.data_ptr())
+    ws, wp, wb = _workspace(L.nmg_attention_workspace_bytes(h, B, Nq, Nk), Q)
+    _check(getattr(L, fn)(h, s, Q.data_ptr(), ldq, Nq, K.data_ptr(), _rows(K, "K"), V.data_ptr(),
+                          _rows(V, "V"), Nk, *extra, D ** -0.5 if scale is None else scale,
+                          out.data_ptr(), _rows(out, "out"), wp, wb, _stream(Q)), fn)
+    return out
+
+
+def attention(Q, K, V, heads: int, kv_heads: int, q_offsets, kv_begin, kv_end, key_mask=None,
+              scale: float | None = None, out=None):
+    """``nmg_attention``: every sequence's query columns of Q (features x tokens)
+    attend to its key columns of K and V; sequence b has queries q_offsets[b] ..
+    q_offsets[b + 1] - 1 and keys kv_begin[b] .. kv_end[b] - 1 (int32 tensors on
+    the device).  key_mask: uint8 or bool for every key column, 0 leaves it out.
+    scale: head_dim ** -0.5 by default.  Scratch memory from torch's
+    allocator."""
+    mask = None
+    if key_mask is not None:
+        if key_mask.dtype not in (torch.uint8, torch.bool) or key_mask.shape != (K.shape[1],) or \
+                not key_mask.is_contiguous():
+            raise ValueError("key_mask must be contiguous uint8 or bool, one for every key column")
+        _need_cuda(key_mask)
+        mask = key_mask.data_ptr()
+    return _attend("nmg_attention", Q, K, V, heads, kv_heads, q_offsets, kv_begin, kv_end, (mask,),
+                   scale, out)
+
+
+def tree_attention(Q, K, V, heads: int, kv_heads: int, q_offsets, kv_begin, kv_end, tree,
+                   scale: float | None = None, out=None):
+    """``nmg_tree_attention``: the query columns are drafted tokens, whose keys and
+    values are the last columns of their sequence's key range; tree (uint8 or
+    bool, a row per query column) says which drafted tokens of its sequence each
+    one attends to, itself included; all earlier columns it attends to."""
+    if tree.dtype not in (torch.uint8, torch.bool) or len(tree.shape) != 2 or \
+            tree.shape[0] != Q.shape[1]:
+        raise ValueError("tree must be uint8 or bool with a row for every query column")
+    _need_cuda(tree)
+    return _attend("nmg_tree_attention", Q, K, V, heads, kv_heads, q_offsets, kv_begin, kv_end,
+                   (tree.data_ptr(), _rows(tree, "tree"), tree.shape[1]), scale, out)

@@ -1,0 +1,719 @@
+// attention_mfma.hpp -- attention on the matrix cores, features x tokens, one
+// pass over the keys with a running maximum and sum.
+//
+// Orientation.  With a head's K as D x keys and Q as D x rows, both products
+// have the rows as their columns:
+//     S^T = K^T Q   (keys x rows),     O^T = V P^T   (D x rows)
+// on 32 x 32 tiles.  A lane then holds, of one row (lane % 32), half of the
+// keys of every 32 (half h = lane / 32), so maxima and sums over keys are sums
+// over its own registers and one exchange between the halves, and O^T is
+// stored as rows of tokens.
+//
+// P never moves.  The lane holds S^T[key][row] for some keys, and the second
+// product wants P^T's keys of a contraction step in the lane.  Which key of a
+// tile stands at which place of the contraction is free, as long as both
+// operands agree:
+//   binary16 (32 x 32 x 16): the places of S^T's rows are permuted by where the
+//     transposing LDS read of K fetches its 4-key segments, so that half h
+//     holds keys 16 c + 8 h + 0..7 of step c: 16 consecutive bytes of V's row.
+//   binary32 (32 x 32 x 2): register i of half h is key 8 (i/4) + 4 h + i%4;
+//     step i takes that key from each half: also 16 consecutive bytes of V.
+//
+// Key tiles are rows of 128 bytes (64 binary16 or 32 binary32 keys) of K and of
+// V in LDS, in the matrices' own layout.  16-byte chunks of a row are permuted
+// (chunk ^ swizzle(row)) so that the reads of both operands touch every bank
+// once: V's reads take one chunk of 16 consecutive rows, K's (binary16) four
+// chunks of 4 rows.  Tiles come with buffer loads that write LDS, which take
+// any address that is a multiple of 4 bytes; others are staged through registers.
+//
+// Two kernels:
+//   k_attn_shared  4 waves of 32 rows share key tiles: two LDS buffers, one
+//                  barrier per tile, the next tile in flight.
+//   k_attn_split   for few rows: the waves of a workgroup hold the same 32 rows
+//                  and each walks its own key tiles, without barriers; their
+//                  results are joined in LDS.
+// Either may take a part of every key range (splits > 1); k_attn_join adds the
+// parts.
+#pragma once
+
+#include "attention.hpp"
+
+namespace {
+
+typedef float f16v __attribute__((ext_vector_type(16)));
+typedef _Float16 h8 __attribute__((ext_vector_type(8)));
+typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+typedef short s4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) char lds_char;
+
+constexpr int kRowBytes = 128;  // of a staged row
+constexpr float kLog2e = 1.4426950408889634f;
+
+// What differs between the element types.  kLift: weights are 2^kLift times
+// exp(s - m), and m may lag kSlack (in powers of 2) behind the true maximum: the
+// largest binary16 weight is 2^15, and weights stay normal numbers down to
+// 2^-21 of the largest.
+template <typename T> struct Elem;
+template <> struct Elem<_Float16> {
+    static constexpr int keys = 64, per_chunk = 8;
+    static constexpr float lift = 7.f, slack = 8.f;
+};
+template <> struct Elem<float> {
+    static constexpr int keys = 32, per_chunk = 4;
+    static constexpr float lift = 0.f, slack = 16.f;
+};
+
+template <typename T, bool V>
+__device__ __forceinline__ int chunk_swizzle(int row) {
+    if (V) return (row >> 1) & 7;
+    return sizeof(T) == 2 ? ((row >> 1) & 1) * 4 : 0;
+}
+
+// One row tile and the keys its sequence has
+struct RowTile {
+    int q0, n;        // first query column, query columns
+    int begin, end;   // keys
+    int64_t row0;     // first row
+};
+
+// Row tile `t` of a key head, wave-uniform: the sequences' tile counts summed 64
+// at a time.  False when there are fewer tiles.
+template <int TR>
+__device__ __forceinline__ bool find_rows(const AttnArgs &a, int t, RowTile &r) {
+    const int lane = threadIdx.x & 63;
+    for (int b0 = 0; b0 < a.sequences; b0 += 64) {
+        const int b = b0 + lane;
+        int lo = 0, hi = 0;
+        if (b < a.sequences) {
+            lo = min(max(a.q_offsets[b], 0), a.Nq);
+            hi = min(max(a.q_offsets[b + 1], lo), a.Nq);
+        }
+        const int tiles = (int)(((int64_t)(hi - lo) * a.share + TR - 1) / TR);
+        int upto = tiles;
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) {
+            const int v = __shfl_up(upto, d);
+            if (lane >= d) upto += v;
+        }
+        const uint64_t hit = __ballot(upto > t);
+        if (hit) {
+            const int w = __builtin_ctzll(hit);
+            r.q0 = __builtin_amdgcn_readlane(lo, w);
+            r.n = __builtin_amdgcn_readlane(hi, w) - r.q0;
+            r.row0 = (int64_t)(t - __builtin_amdgcn_readlane(upto - tiles, w)) * TR;
+            const int at = b0 + w;
+            r.begin = min(max(a.kv_begin[at], 0), a.Nk);
+            r.end = max(min(a.kv_end[at], a.Nk), r.begin);
+            return true;
+        }
+        t -= __builtin_amdgcn_readlane(upto, 63);
+    }
+    return false;
+}
+
+// The lane's row of a tile: which query column and head.  Rows past the last
+// are read as the first.
+struct RowAt {
+    bool valid;
+    int g, column;
+};
+template <int TR>
+__device__ __forceinline__ RowAt row_at(const AttnArgs &a, const RowTile &r, int i) {
+    const int64_t row = r.row0 + i;
+    RowAt x;
+    x.valid = row >= 0 && row < (int64_t)r.n * a.share;
+    x.g = x.valid ? (int)(row / r.n) : 0;
+    x.column = r.q0 + (x.valid ? (int)(row - (int64_t)x.g * r.n) : 0);
+    return x;
+}
+
+__device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32); }
+
+__device__ __forceinline__ float exp2_fast(float v) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    return __builtin_amdgcn_exp2f(v);
+#else
+    return v;
+#endif
+}
+
+__device__ __forceinline__ f16v mfma(h8 a, h8 b, f16v c) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+#else
+    return c;
+#endif
+}
+__device__ __forceinline__ f16v mfma(float a, float b, f16v c) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    return __builtin_amdgcn_mfma_f32_32x32x2f32(a, b, c, 0, 0, 0);
+#else
+    return c;
+#endif
+}
+__device__ __forceinline__ s4 read_tr(lds_char *p) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s4 *)p);
+#else
+    return s4{};
+#endif
+}
+__device__ __forceinline__ u4 read16(lds_char *p) {
+    return *(__attribute__((address_space(3))) u4 *)p;
+}
+__device__ __forceinline__ float read4(lds_char *p) {
+    return *(__attribute__((address_space(3))) float *)p;
+}
+__device__ __forceinline__ void write16(lds_char *p, u4 v) {
+    *(__attribute__((address_space(3))) u4 *)p = v;
+}
+
+// Wait until at most n vector-memory operations of this wave are in flight
+template <int n>
+__device__ __forceinline__ void wait_vm() {
+#if defined(__HIP_DEVICE_COMPILE__)
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(n) : "memory");
+#endif
+}
+// ... and until its LDS operations are done
+__device__ __forceinline__ void wait_lds() {
+#if defined(__HIP_DEVICE_COMPILE__)
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#endif
+}
+
+// Rows of one matrix of keys or values on their way into LDS.  `step` waves
+// share a tile, this one takes every step-th group of 8 rows (1024 bytes).
+template <typename T, int DP, bool V, bool REGS, int STEP>
+struct Stager {
+    static constexpr int kGroups = DP / 8 / STEP;
+    const T *base;    // column `first` of the head's first row
+    int64_t ld;
+    int D, cols;      // rows of the head, columns from `first` on
+    buf_rsrc_t rsrc;
+    uint32_t off[REGS || STEP % 2 == 0 ? 1 : 2];  // of the lane's chunk in the wave's even and odd
+                                                  // groups (groups of one parity: one)
+    u4 hold[REGS ? kGroups : 1];
+
+    __device__ __forceinline__ void init(const void *matrix, int64_t ld_, int head, int D_, int Nk,
+                                         int first, int wave) {
+        ld = ld_;
+        D = D_;
+        cols = Nk - first;
+        base = (const T *)matrix + (int64_t)head * D * ld + first;
+        if constexpr (!REGS) {
+            const uint32_t bytes = (uint32_t)(((int64_t)(D - 1) * ld + cols) * sizeof(T));
+            rsrc = buf_rsrc(base, (bytes + 3) & ~3u);
+            const int lane = threadIdx.x & 63, row = lane >> 3;
+#pragma unroll
+            for (int i = 0; i < (STEP % 2 ? 2 : 1); ++i)
+                off[i] = (uint32_t)(row * ld * sizeof(T)) +
+                         16 * ((lane & 7) ^ chunk_swizzle<T, V>(8 * (STEP * i + wave) + row));
+        }
+    }
+
+    // Ask for the tile that starts `at` columns behind `first`; !REGS: into `lds`
+    __device__ __forceinline__ void ask(int at, lds_char *lds, int wave) {
+#pragma unroll
+        for (int i = 0; i < kGroups; ++i) {
+            const int group = STEP * i + wave;
+            if constexpr (!REGS) {
+                const uint32_t o = off[STEP % 2 ? i & 1 : 0] +
+                                   (uint32_t)(8 * group * ld * sizeof(T)) +
+                                   (uint32_t)at * (uint32_t)sizeof(T);
+                lds_copy16_buf(rsrc, o, (void *)(lds + 1024 * group));
+            } else {
+                constexpr int E = Elem<T>::per_chunk;
+                const int lane = threadIdx.x & 63, row = 8 * group + (lane >> 3);
+                const int c = at + E * ((lane & 7) ^ chunk_swizzle<T, V>(row));
+                u4 v = {0, 0, 0, 0};
+                if (row < D) {
+                    const T *p = base + row * ld + c;
+                    if (c + E <= cols) {
+                        __builtin_memcpy(&v, p, 16);
+                    } else {
+                        T e[E];
+                        for (int k = 0; k < E; ++k) e[k] = c + k < cols ? p[k] : (T)0;
+                        __builtin_memcpy(&v, e, 16);
+                    }
+                }
+                hold[i] = v;
+            }
+        }
+    }
+    // REGS: what was asked for, into `lds`
+    __device__ __forceinline__ void put(lds_char *lds, int wave) {
+        if constexpr (REGS) {
+            const int lane = threadIdx.x & 63;
+#pragma unroll
+            for (int i = 0; i < kGroups; ++i)
+                write16(lds + 1024 * (STEP * i + wave) + 16 * lane, hold[i]);
+        }
+    }
+};
+
+// 32 rows of a tile in one wave
+template <typename T, int DP>
+struct Rows {
+    static constexpr int KT = Elem<T>::keys, KB = KT / 32;
+    static constexpr int QF = sizeof(T) == 2 ? DP / 16 : DP / 2;
+    typedef typename std::conditional<sizeof(T) == 2, h8, float>::type QFrag;
+    QFrag q[QF];
+    f16v o[DP / 32];
+    f16v s[KB];
+    float m, l;        // running maximum (of scores times log2 e), sum of the lane's weights
+    float scale2;      // scale * log2 e
+
+    __device__ __forceinline__ void init(const AttnArgs &a, int kv_head, const RowAt &r) {
+        const int h = (threadIdx.x & 63) >> 5;
+        const T *src = (const T *)a.Q + (int64_t)(kv_head * a.share + r.g) * a.D * a.ldq + r.column;
+        auto at = [&](int d) { return d < a.D ? src[d * a.ldq] : (T)0; };
+#pragma unroll
+        for (int c = 0; c < QF; ++c) {
+            if constexpr (sizeof(T) == 2) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) q[c][e] = at(16 * c + 8 * h + e);
+            } else {
+                q[c] = at(2 * c + h);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < DP / 32; ++i) o[i] = f16v{};
+        m = -INFINITY;
+        l = 0.f;
+        scale2 = a.scale * kLog2e;
+    }
+
+    // The tile's place of register i of block kb
+    static __device__ __forceinline__ int key_of(int kb, int i, int h) {
+        return sizeof(T) == 2 ? 32 * kb + 16 * (i >> 3) + 8 * h + (i & 7)
+                              : 8 * (i >> 2) + 4 * h + (i & 3);
+    }
+
+    __device__ __forceinline__ void scores(lds_char *k) {
+        const int lane = threadIdx.x & 63, h = lane >> 5;
+#pragma unroll
+        for (int b = 0; b < KB; ++b) s[b] = f16v{};
+        if constexpr (sizeof(T) == 2) {
+            // segment lane % 4 of its 16 keys: 0, 8, 4, 12 (see the file's comment)
+            const int row = 8 * h + ((lane & 15) >> 2), x = (lane >> 3) & 1;
+            const int at = row * kRowBytes + 16 * (2 * ((lane >> 4) & 1) + (lane & 1)) + 64 * x +
+                           8 * ((lane >> 1) & 1);
+            lds_char *p0 = k + at, *p1 = k + (at ^ 64);
+#pragma unroll
+            for (int c = 0; c < QF; ++c) {
+#pragma unroll
+                for (int b = 0; b < KB; ++b) {
+                    lds_char *p = (b ? p1 : p0) + 16 * kRowBytes * c;
+                    struct { s4 x, y; } f = {read_tr(p), read_tr(p + 4 * kRowBytes)};
+                    s[b] = mfma(__builtin_bit_cast(h8, f), q[c], s[b]);
+                }
+            }
+        } else {
+            lds_char *p = k + h * kRowBytes + 4 * (lane & 31);
+#pragma unroll
+            for (int c = 0; c < QF; ++c) s[0] = mfma(read4(p + 2 * kRowBytes * c), q[c], s[0]);
+        }
+    }
+
+    // Leave keys out: bit j of `valid` is key j of the tile
+    __device__ __forceinline__ void mask(uint64_t valid) {
+        const int h = (threadIdx.x & 63) >> 5;
+        const uint64_t mine = valid >> (sizeof(T) == 2 ? 8 * h : 4 * h);
+#pragma unroll
+        for (int b = 0; b < KB; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                s[b][i] = (mine >> key_of(b, i, 0)) & 1 ? s[b][i] : -INFINITY;
+    }
+    // ... of the drafted tokens (key `drafted` of the tile is the first), those
+    // that the lane's query does not see
+    __device__ __forceinline__ void mask_tree(const AttnArgs &a, int64_t column, int drafted) {
+        const int h = (threadIdx.x & 63) >> 5;
+        const uint8_t *see = a.tree + column * a.ldtree;
+#pragma unroll
+        for (int b = 0; b < KB; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int at = key_of(b, i, h) - drafted;
+                if (at >= 0 && (at >= a.width || !see[at])) s[b][i] = -INFINITY;
+            }
+    }
+
+    // Scores to weights: the running maximum moves when a row's grew by more than
+    // Elem::slack powers of 2
+    __device__ __forceinline__ void weigh() {
+        float top = s[0][0];
+#pragma unroll
+        for (int b = 0; b < KB; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) top = fmaxf(top, s[b][i]);
+        top = fmaxf(top, other_half(top)) * scale2;
+        if (__any(top - m > Elem<T>::slack)) {  // (nothing seen yet: m is -inf)
+            const float next = fmaxf(m, top);
+            const float keep = m == next ? 1.f : exp2_fast(m - next);
+            l *= keep;
+#pragma unroll
+            for (int i = 0; i < DP / 32; ++i) o[i] *= keep;
+            m = next;
+        }
+        const float base = m == -INFINITY ? 0.f : m - Elem<T>::lift;
+#pragma unroll
+        for (int b = 0; b < KB; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[b][i] = exp2_fast(fmaf(s[b][i], scale2, -base));
+    }
+
+    // O^T += V P^T; MASKED: values of keys left out count as 0 whatever they hold
+    template <bool MASKED>
+    __device__ __forceinline__ void values(lds_char *v, uint64_t valid) {
+        const int lane = threadIdx.x & 63, h = lane >> 5, row = lane & 31;
+        const int swz = chunk_swizzle<T, true>(row);
+        if constexpr (sizeof(T) == 2) {
+#pragma unroll
+            for (int c = 0; c < KT / 16; ++c) {
+                h8 p;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) p[e] = (_Float16)s[c >> 1][8 * (c & 1) + e];
+                // the sum of the rounded weights: what the product divides by
+#pragma unroll
+                for (int e = 0; e < 8; e += 2)
+                    l = __builtin_amdgcn_fdot2(h2{p[e], p[e + 1]}, h2{(_Float16)1, (_Float16)1}, l,
+                                               false);
+                lds_char *at = v + row * kRowBytes + 16 * ((2 * c + h) ^ swz);
+                u4 keep;
+                if constexpr (MASKED) {
+                    const uint32_t bits = (uint32_t)(valid >> (16 * c + 8 * h));
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        keep[e] = ((bits >> (2 * e)) & 1 ? 0xffffu : 0u) |
+                                  ((bits >> (2 * e + 1)) & 1 ? 0xffff0000u : 0u);
+                }
+#pragma unroll
+                for (int d = 0; d < DP / 32; ++d) {
+                    u4 x = read16(at + 32 * kRowBytes * d);
+                    if constexpr (MASKED) x &= keep;
+                    o[d] = mfma(__builtin_bit_cast(h8, x), p, o[d]);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int b = 0; b < 4; ++b) {
+#pragma unroll
+                for (int r = 0; r < 4; ++r) l += s[0][4 * b + r];
+                lds_char *at = v + row * kRowBytes + 16 * ((2 * b + h) ^ swz);
+                const uint32_t bits = (uint32_t)(valid >> (8 * b + 4 * h));
+#pragma unroll
+                for (int d = 0; d < DP / 32; ++d) {
+                    v4f x = __builtin_bit_cast(v4f, read16(at + 32 * kRowBytes * d));
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const float e = !MASKED || (bits >> r & 1) ? x[r] : 0.f;
+                        o[d] = mfma(e, s[0][4 * b + r], o[d]);
+                    }
+                }
+            }
+        }
+    }
+};
+
+// Which keys of the tile at column t0 take part (bit j: column t0 + j);
+// `mask_byte`: the lane's key's
+template <typename T>
+__device__ __forceinline__ uint64_t valid_keys(int64_t t0, const RowTile &r, uint8_t mask_byte) {
+    const int lane = threadIdx.x & 63;
+    const int64_t c = t0 + lane;
+    return __ballot(lane < Elem<T>::keys && c >= r.begin && c < r.end && mask_byte);
+}
+
+// One key tile of a wave: `k` is staged; wait_v() returns when `v` is
+template <typename T, int DP, typename Between, typename WaitV>
+__device__ __forceinline__ void attend_tile(const AttnArgs &a, Rows<T, DP> &w, const RowTile &r,
+                                            const RowAt &mine, int64_t t0, uint8_t mask_byte,
+                                            lds_char *k, lds_char *v, Between between,
+                                            WaitV wait_v) {
+    w.scores(k);
+    between();
+    const uint64_t valid = valid_keys<T>(t0, r, mask_byte);
+    const bool full = valid == (Elem<T>::keys == 64 ? ~0ull : 0xffffffffull);
+    if (!full) w.mask(valid);
+    if (a.tree && t0 + Elem<T>::keys > (int64_t)r.end - r.n)
+        w.mask_tree(a, mine.column, (int)((int64_t)r.end - r.n - t0));
+    w.weigh();
+    wait_v();
+    if (full)
+        w.template values<false>(v, valid);
+    else
+        w.template values<true>(v, valid);
+}
+
+// The mask byte of the lane's key of the tile at t0 (1 without a mask)
+__device__ __forceinline__ uint8_t mask_at(const AttnArgs &a, int64_t t0) {
+    if (!a.key_mask) return 1;
+    const int64_t c = t0 + (threadIdx.x & 63);
+    return c < a.Nk ? a.key_mask[c] : 0;
+}
+
+// Workgroup -> (row tile, part, key head); tiles of one (head, part) adjacent,
+// on one XCD: they read the same keys
+struct Place {
+    int tile, part, head;
+};
+__device__ __forceinline__ Place place_of(const AttnArgs &a) {
+    int id = xcd_tile(blockIdx.x, gridDim.x);
+    Place p;
+    p.tile = id % a.tiles;
+    id /= a.tiles;
+    p.part = id % a.splits;
+    p.head = id / a.splits;
+    return p;
+}
+
+// Parts in the workspace: sums (padded D x rows), then maxima and totals, of every
+// (part, head, tile)
+template <int DP, int TR>
+__device__ __forceinline__ float *part_at(const AttnArgs &a, int part, int head, int tile) {
+    return a.part + ((int64_t)(part * a.kv_heads + head) * a.tiles + tile) * ((DP + 2) * TR);
+}
+
+template <typename T, int DP, bool REGS>
+__global__ __launch_bounds__(256, DP <= (REGS ? 96 : 128) ? 2 : 1) void k_attn_shared(AttnArgs a) {
+    constexpr int TR = kAttnSharedRows, KT = Elem<T>::keys, kTile = DP * kRowBytes;
+    __shared__ __attribute__((aligned(1024))) char lds_mem[2][2 * kTile];
+    const Place at = place_of(a);
+    RowTile r;
+    if (!find_rows<TR>(a, at.tile, r)) return;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const RowAt mine = row_at<TR>(a, r, 32 * wave + (lane & 31));
+    Rows<T, DP> w;
+    w.init(a, at.head, mine);
+
+    const int first = r.begin - r.begin % a.align;
+    const int tiles = r.end > r.begin ? (r.end - first + KT - 1) / KT : 0;
+    const int lo = (int)((int64_t)tiles * at.part / a.splits);
+    const int hi = (int)((int64_t)tiles * (at.part + 1) / a.splits);
+    if (lo < hi) {
+        Stager<T, DP, false, REGS, 4> ks;
+        Stager<T, DP, true, REGS, 4> vs;
+        ks.init(a.K, a.ldk, at.head, a.D, a.Nk, first, wave);
+        vs.init(a.V, a.ldv, at.head, a.D, a.Nk, first, wave);
+        lds_char *buf0 = (lds_char *)lds_mem[0], *buf1 = (lds_char *)lds_mem[1];
+        uint8_t byte = mask_at(a, (int64_t)first + (int64_t)lo * KT);
+        ks.ask(lo * KT, buf0, wave);
+        vs.ask(lo * KT, buf0 + kTile, wave);
+        ks.put(buf0, wave);
+        vs.put(buf0 + kTile, wave);
+        for (int t = lo; t < hi; ++t) {
+            lds_char *cur = (t - lo) & 1 ? buf1 : buf0, *nxt = (t - lo) & 1 ? buf0 : buf1;
+            __syncthreads();  // this tile has landed, the other buffer is free
+            const int64_t t0 = (int64_t)first + (int64_t)t * KT;
+            const uint8_t now = byte;
+            if (t + 1 < hi) {
+                byte = mask_at(a, t0 + KT);
+                ks.ask((t + 1) * KT, nxt, wave);
+                vs.ask((t + 1) * KT, nxt + kTile, wave);
+            }
+            attend_tile<T, DP>(a, w, r, mine, t0, now, cur, cur + kTile, [] {}, [] {});
+            if (REGS && t + 1 < hi) {
+                ks.put(nxt, wave);
+                vs.put(nxt + kTile, wave);
+            }
+        }
+    }
+
+    const int h = lane >> 5;
+    const float total = w.l + other_half(w.l);
+    if (a.splits > 1) {
+        float *part = part_at<DP, TR>(a, at.part, at.head, at.tile) + 32 * wave + (lane & 31);
+#pragma unroll
+        for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                part[(32 * d + 8 * (i >> 2) + 4 * h + (i & 3)) * TR] = w.o[d][i];
+        if (h == 0) {
+            part[DP * TR] = w.m;
+            part[(DP + 1) * TR] = total;
+        }
+        return;
+    }
+    if (!mine.valid) return;
+    const float inv = total == 0.f ? 0.f : 1.f / total;
+    T *out = (T *)a.O + (int64_t)(at.head * a.share + mine.g) * a.D * a.ldo + mine.column;
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int row = 32 * d + 8 * (i >> 2) + 4 * h + (i & 3);
+            if (row < a.D) out[row * a.ldo] = (T)(w.o[d][i] * inv);
+        }
+}
+
+// Waves of a workgroup that splits the keys: as many as 128 KB hold tiles of
+template <int DP> constexpr int split_waves() { return DP <= 64 ? 8 : DP <= 128 ? 4 : 2; }
+
+template <typename T, int DP, bool REGS>
+__global__ __launch_bounds__(64 * split_waves<DP>(), 1) void k_attn_split(AttnArgs a) {
+    constexpr int TR = kAttnSplitRows, KT = Elem<T>::keys, kTile = DP * kRowBytes;
+    constexpr int W = split_waves<DP>();
+    __shared__ __attribute__((aligned(1024))) char lds_mem[W][2 * kTile];
+    __shared__ float tops[W][TR], totals[W][TR];
+    const Place at = place_of(a);
+    RowTile r;
+    if (!find_rows<TR>(a, at.tile, r)) return;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const RowAt mine = row_at<TR>(a, r, lane & 31);
+    Rows<T, DP> w;
+    w.init(a, at.head, mine);
+
+    const int first = r.begin - r.begin % a.align;
+    const int tiles = r.end > r.begin ? (r.end - first + KT - 1) / KT : 0;
+    const int lo = (int)((int64_t)tiles * at.part / a.splits) + wave;
+    const int hi = (int)((int64_t)tiles * (at.part + 1) / a.splits);
+    lds_char *k = (lds_char *)lds_mem[wave], *v = k + kTile;
+    if (lo < hi) {
+        Stager<T, DP, false, REGS, 1> ks;
+        Stager<T, DP, true, REGS, 1> vs;
+        constexpr int kCopies = DP / 8;
+        ks.init(a.K, a.ldk, at.head, a.D, a.Nk, first, 0);
+        vs.init(a.V, a.ldv, at.head, a.D, a.Nk, first, 0);
+        uint8_t byte = mask_at(a, (int64_t)first + (int64_t)lo * KT);
+        ks.ask(lo * KT, k, 0);
+        ks.put(k, 0);
+        vs.ask(lo * KT, v, 0);
+        for (int t = lo; t < hi; t += W) {
+            const int64_t t0 = (int64_t)first + (int64_t)t * KT;
+            const bool more = t + W < hi;
+            const uint8_t now = byte;
+            if (!REGS) wait_vm<kCopies>();  // K has landed; V may still be in flight
+            attend_tile<T, DP>(
+                a, w, r, mine, t0, now, k, v,
+                [&] {
+                    wait_lds();  // K's tile has been read
+                    vs.put(v, 0);
+                    if (more) {
+                        byte = mask_at(a, t0 + (int64_t)W * KT);
+                        ks.ask((t + W) * KT, k, 0);
+                    }
+                },
+                [&] {
+                    if (!REGS) {
+                        if (more)
+                            wait_vm<kCopies>();
+                        else
+                            wait_vm<0>();
+                    }
+                });
+            wait_lds();  // V's too
+            if (more) {
+                ks.put(k, 0);
+                vs.ask((t + W) * KT, v, 0);
+            }
+        }
+    }
+
+    // join the waves: maxima, then sums at the common maximum
+    const int h = lane >> 5, row = lane & 31;
+    const float total = w.l + other_half(w.l);
+    if (h == 0) tops[wave][row] = w.m;
+    __syncthreads();
+    float top = tops[0][row];
+#pragma unroll
+    for (int i = 1; i < W; ++i) top = fmaxf(top, tops[i][row]);
+    const float f = w.m == -INFINITY ? 0.f : exp2_fast(w.m - top);
+    if (h == 0) totals[wave][row] = f * total;
+    float *sums = (float *)lds_mem[wave];
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            sums[(32 * d + 8 * (i >> 2) + 4 * h + (i & 3)) * TR + row] = f * w.o[d][i];
+    __syncthreads();
+    float all = totals[0][row];
+#pragma unroll
+    for (int i = 1; i < W; ++i) all += totals[i][row];
+    float *part = part_at<DP, TR>(a, at.part, at.head, at.tile) + row;
+    if (a.splits > 1 && threadIdx.x < TR) {
+        part[DP * TR] = top;
+        part[(DP + 1) * TR] = all;
+    }
+    const float inv = all == 0.f ? 0.f : 1.f / all;
+    T *out = (T *)a.O + (int64_t)(at.head * a.share + mine.g) * a.D * a.ldo + mine.column;
+    for (int d = threadIdx.x / TR; d < DP; d += 2 * W) {
+        float x = 0.f;
+#pragma unroll
+        for (int i = 0; i < W; ++i) x += ((float *)lds_mem[i])[d * TR + row];
+        if (a.splits > 1)
+            part[d * TR] = x;
+        else if (mine.valid && d < a.D)
+            out[d * a.ldo] = (T)(x * inv);
+    }
+}
+
+// Parts of every key range, in their order, to outputs: a workgroup per (tile,
+// head, 8 rows of the head)
+template <typename T, int DP, int TR>
+__global__ __launch_bounds__(kBlock) void k_attn_join(AttnArgs a) {
+    RowTile r;
+    const int tile = blockIdx.x, head = blockIdx.y;
+    if (!find_rows<TR>(a, tile, r)) return;
+    const int i = threadIdx.x % TR;
+    const RowAt mine = row_at<TR>(a, r, i);
+    if (!mine.valid) return;
+    const int64_t step = (int64_t)a.kv_heads * a.tiles * ((DP + 2) * TR);
+    const float *part = part_at<DP, TR>(a, 0, head, tile) + i;
+    float top = -INFINITY, all = 0.f;
+    for (int s = 0; s < a.splits; ++s) top = fmaxf(top, part[s * step + DP * TR]);
+    auto weight = [&](int s) {
+        const float m = part[s * step + DP * TR];
+        return m == -INFINITY ? 0.f : exp2_fast(m - top);
+    };
+    for (int s = 0; s < a.splits; ++s) all += weight(s) * part[s * step + (DP + 1) * TR];
+    const float inv = all == 0.f ? 0.f : 1.f / all;
+    T *out = (T *)a.O + (int64_t)(head * a.share + mine.g) * a.D * a.ldo + mine.column;
+    constexpr int kAtOnce = kBlock / TR;
+    const int d0 = blockIdx.z * 8;
+    for (int d = d0 + threadIdx.x / TR; d < d0 + 8 && d < a.D; d += kAtOnce) {
+        float x = 0.f;
+        for (int s = 0; s < a.splits; ++s) x += weight(s) * part[s * step + d * TR];
+        out[d * a.ldo] = (T)(x * inv);
+    }
+}
+
+template <typename T, int DP>
+nmg_status launch_attn_dim(const AttnArgs &a, bool shared, bool regs, hipStream_t stream) {
+    const dim3 grid((unsigned)(a.tiles * a.splits * a.kv_heads));
+    if (shared && regs)
+        hipLaunchKernelGGL((k_attn_shared<T, DP, true>), grid, dim3(256), 0, stream, a);
+    else if (shared)
+        hipLaunchKernelGGL((k_attn_shared<T, DP, false>), grid, dim3(256), 0, stream, a);
+    else if (regs)
+        hipLaunchKernelGGL((k_attn_split<T, DP, true>), grid, dim3(64 * split_waves<DP>()), 0,
+                           stream, a);
+    else
+        hipLaunchKernelGGL((k_attn_split<T, DP, false>), grid, dim3(64 * split_waves<DP>()), 0,
+                           stream, a);
+    if (a.splits > 1) {
+        const dim3 join((unsigned)a.tiles, (unsigned)a.kv_heads, (unsigned)((a.D + 7) / 8));
+        if (shared)
+            hipLaunchKernelGGL((k_attn_join<T, DP, kAttnSharedRows>), join, dim3(kBlock), 0,
+                               stream, a);
+        else
+            hipLaunchKernelGGL((k_attn_join<T, DP, kAttnSplitRows>), join, dim3(kBlock), 0, stream,
+                               a);
+    }
+    return launched();
+}
+
+template <typename T>
+nmg_status launch_attn(const AttnArgs &a, bool shared, bool regs, hipStream_t stream) {
+    switch (attn_padded_dim(a.D)) {
+        case 32: return launch_attn_dim<T, 32>(a, shared, regs, stream);
+        case 64: return launch_attn_dim<T, 64>(a, shared, regs, stream);
+        case 96: return launch_attn_dim<T, 96>(a, shared, regs, stream);
+        case 128: return launch_attn_dim<T, 128>(a, shared, regs, stream);
+        default: return launch_attn_dim<T, 256>(a, shared, regs, stream);
+    }
+}
+
+}  // namespace

@@ -1,0 +1,66 @@
+// attention_plan.hip -- how one attention call is laid over the GPU: the kernel,
+// its row tiles, and into how many parts every key range is split.
+#include "attention.hpp"
+
+namespace nmg_internal {
+
+namespace {
+
+struct Plan {
+    bool shared;
+    int64_t tiles;   // of one key head: an upper bound, the sequences' lengths are on the device
+    int splits;      // wanted
+    int64_t part_bytes;  // of one part of every range
+};
+
+Plan plan_of(nmg_dtype dtype, const AttnArgs &a) {
+    Plan p;
+    const int64_t rows = (int64_t)a.Nq * a.share;
+    // one wave's rows cover the average sequence: split the keys over the waves
+    p.shared = rows > (int64_t)kAttnSplitRows * a.sequences;
+    const int tr = p.shared ? kAttnSharedRows : kAttnSplitRows;
+    // sum of ceil(rows_b / tr) over sequences that hold `rows` rows together
+    p.tiles = std::min(rows / tr + a.sequences, rows);
+    const int dp = attn_padded_dim(a.D);
+    const int kt = dtype == NMG_F16 ? 64 : 32;
+    const int64_t keys = (a.Nk + a.sequences - 1) / a.sequences;  // of a sequence, if they share Nk
+    const int64_t kt_tiles = (keys + kt - 1) / kt;
+    const int64_t blocks = p.tiles * a.kv_heads;
+    const int64_t slots = (int64_t)device_cus() * (p.shared ? 2 : 1);
+    // at least 4 key tiles for every wave
+    const int64_t most = kt_tiles / (p.shared ? 4 : 4 * (dp <= 64 ? 8 : dp <= 128 ? 4 : 2));
+    p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(std::min(slots / blocks, most), 256));
+    p.part_bytes = blocks * (dp + 2) * tr * (int64_t)sizeof(float);
+    return p;
+}
+
+}  // namespace
+
+int64_t attention_workspace_bytes(nmg_dtype dtype, const AttnArgs &a) {
+    const Plan p = plan_of(dtype, a);
+    return p.splits > 1 ? p.splits * p.part_bytes : 0;
+}
+
+nmg_status launch_attention(nmg_dtype dtype, const AttnArgs &args, void *workspace,
+                            int64_t workspace_bytes, hipStream_t stream) {
+    AttnArgs a = args;
+    const Plan p = plan_of(dtype, a);
+    int64_t splits = std::min<int64_t>(p.splits, workspace_bytes / p.part_bytes);
+    if (splits < 2) splits = 1;
+    if (p.tiles * splits * a.kv_heads > INT32_MAX || a.kv_heads > 65535) return NMG_ERR_UNSUPPORTED;
+    a.tiles = (int32_t)p.tiles;
+    a.splits = (int32_t)splits;
+    a.part = (float *)workspace;
+    const int64_t es = (int64_t)elem_size(dtype);
+    auto rows_at = [&](int64_t to) {  // rows of K and V start at multiples of `to` bytes
+        return aligned(a.K, to) && aligned(a.V, to) && a.ldk * es % to == 0 && a.ldv * es % to == 0;
+    };
+    // direct copies: addresses a multiple of 4 bytes, offsets within a head in 31 bits
+    const int64_t head = std::max(a.ldk, a.ldv) * es * attn_padded_dim(a.D);
+    const bool regs = !rows_at(4) || head > INT32_MAX - 4096;
+    a.align = (int32_t)(regs ? 1 : rows_at(16) ? 16 / es : std::max<int64_t>(4 / es, 1));
+    return dtype == NMG_F16 ? launch_attention_f16(a, p.shared, regs, stream)
+                            : launch_attention_f32(a, p.shared, regs, stream);
+}
+
+}  // namespace nmg_internal

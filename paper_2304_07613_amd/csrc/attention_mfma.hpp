@@ -77,37 +77,71 @@ struct RowTile {
     int64_t row0;     // first row
 };
 
-// Row tile `t` of a key head, wave-uniform: the sequences' tile counts summed 64
-// at a time.  False when there are fewer tiles.
+// 64 sequences from b0 on, one a lane: their query columns, row tiles, and the
+// tiles of those up to each
 template <int TR>
-__device__ __forceinline__ bool find_rows(const AttnArgs &a, int t, RowTile &r) {
-    const int lane = threadIdx.x & 63;
-    for (int b0 = 0; b0 < a.sequences; b0 += 64) {
-        const int b = b0 + lane;
-        int lo = 0, hi = 0;
+struct Sequences64 {
+    int lo, hi, tiles, upto;
+    __device__ __forceinline__ void read(const AttnArgs &a, int b0) {
+        const int lane = threadIdx.x & 63, b = b0 + lane;
+        lo = hi = 0;
         if (b < a.sequences) {
             lo = min(max(a.q_offsets[b], 0), a.Nq);
             hi = min(max(a.q_offsets[b + 1], lo), a.Nq);
         }
-        const int tiles = (int)(((int64_t)(hi - lo) * a.share + TR - 1) / TR);
-        int upto = tiles;
+        tiles = upto = (int)(((int64_t)(hi - lo) * a.share + TR - 1) / TR);
 #pragma unroll
         for (int d = 1; d < 64; d *= 2) {
             const int v = __shfl_up(upto, d);
             if (lane >= d) upto += v;
         }
-        const uint64_t hit = __ballot(upto > t);
+    }
+    __device__ __forceinline__ int total() const { return __builtin_amdgcn_readlane(upto, 63); }
+};
+
+// A workgroup's row tile of a key head, and its part of the keys
+struct Place {
+    int tile, part, head;
+    RowTile rows;
+};
+
+// Workgroup `id` of the launch -> its place, wave-uniform; false when there is
+// none (the launch has room for the most tiles that sequences of any lengths
+// have).  The tiles there are go to the XCDs in equal shares, those of one
+// (head, part) adjacent on one XCD: they read the same keys.
+template <int TR>
+__device__ __forceinline__ bool find_place(const AttnArgs &a, int id, Place &p) {
+    Sequences64<TR> s;
+    s.read(a, 0);
+    int total = s.total();
+    for (int b0 = 64; b0 < a.sequences; b0 += 64) {
+        s.read(a, b0);
+        total += s.total();
+    }
+    total = min(total, a.tiles);
+    const int groups = a.splits * a.kv_heads;
+    if (id >= total * groups) return false;
+    id = xcd_tile(id, total * groups);
+    p.tile = id % total;
+    id /= total;
+    p.part = id % a.splits;
+    p.head = id / a.splits;
+    int t = p.tile;
+    for (int b0 = 0; b0 < a.sequences; b0 += 64) {
+        if (a.sequences > 64) s.read(a, b0);
+        const uint64_t hit = __ballot(s.upto > t);
         if (hit) {
             const int w = __builtin_ctzll(hit);
-            r.q0 = __builtin_amdgcn_readlane(lo, w);
-            r.n = __builtin_amdgcn_readlane(hi, w) - r.q0;
-            r.row0 = (int64_t)(t - __builtin_amdgcn_readlane(upto - tiles, w)) * TR;
+            RowTile &r = p.rows;
+            r.q0 = __builtin_amdgcn_readlane(s.lo, w);
+            r.n = __builtin_amdgcn_readlane(s.hi, w) - r.q0;
+            r.row0 = (int64_t)(t - __builtin_amdgcn_readlane(s.upto - s.tiles, w)) * TR;
             const int at = b0 + w;
             r.begin = min(max(a.kv_begin[at], 0), a.Nk);
             r.end = max(min(a.kv_end[at], a.Nk), r.begin);
             return true;
         }
-        t -= __builtin_amdgcn_readlane(upto, 63);
+        t -= s.total();
     }
     return false;
 }
@@ -128,7 +162,17 @@ __device__ __forceinline__ RowAt row_at(const AttnArgs &a, const RowTile &r, int
     return x;
 }
 
-__device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32); }
+// Over a row's two lanes, lane and lane ^ 32
+__device__ __forceinline__ float larger_of_halves(float v) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false,
+                                                    false);
+    return fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1]));
+#else
+    return v;
+#endif
+}
+__device__ __forceinline__ float sum_of_halves(float v) { return v + __shfl_xor(v, 32); }
 
 __device__ __forceinline__ float exp2_fast(float v) {
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -173,13 +217,17 @@ __device__ __forceinline__ void write16(lds_char *p, u4 v) {
 template <int n>
 __device__ __forceinline__ void wait_vm() {
 #if defined(__HIP_DEVICE_COMPILE__)
-    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(n) : "memory");
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt((n & 0xf) | (n >> 4) << 14 | 0x7 << 4 | 0xf << 8);
+    asm volatile("" ::: "memory");
 #endif
 }
 // ... and until its LDS operations are done
 __device__ __forceinline__ void wait_lds() {
 #if defined(__HIP_DEVICE_COMPILE__)
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0xf | 0x3 << 14 | 0x7 << 4);
+    asm volatile("" ::: "memory");
 #endif
 }
 
@@ -219,10 +267,11 @@ struct Stager {
         for (int i = 0; i < kGroups; ++i) {
             const int group = STEP * i + wave;
             if constexpr (!REGS) {
-                const uint32_t o = off[STEP % 2 ? i & 1 : 0] +
-                                   (uint32_t)(8 * group * ld * sizeof(T)) +
-                                   (uint32_t)at * (uint32_t)sizeof(T);
-                lds_copy16_buf(rsrc, o, (void *)(lds + 1024 * group));
+                // one scalar for the group and tile (kept from becoming an offset register
+                // for every group)
+                const uint32_t u = __builtin_amdgcn_readfirstlane(
+                    (uint32_t)(8 * group * ld * sizeof(T)) + (uint32_t)at * (uint32_t)sizeof(T));
+                lds_copy16_buf(rsrc, off[STEP % 2 ? i & 1 : 0] + u, (void *)(lds + 1024 * group));
             } else {
                 constexpr int E = Elem<T>::per_chunk;
                 const int lane = threadIdx.x & 63, row = 8 * group + (lane >> 3);
@@ -259,16 +308,25 @@ struct Rows {
     static constexpr int KT = Elem<T>::keys, KB = KT / 32;
     static constexpr int QF = sizeof(T) == 2 ? DP / 16 : DP / 2;
     typedef typename std::conditional<sizeof(T) == 2, h8, float>::type QFrag;
+    // One tile's scores, then its weights (binary32: the scores' registers)
+    struct Scores {
+        f16v s[KB];
+    };
+    struct Weights {
+        h8 p[KT / 16];
+    };
     QFrag q[QF];
     f16v o[DP / 32];
-    f16v s[KB];
     float m, l;        // running maximum (of scores times log2 e), sum of the lane's weights
     float scale2;      // scale * log2 e
 
     __device__ __forceinline__ void init(const AttnArgs &a, int kv_head, const RowAt &r) {
         const int h = (threadIdx.x & 63) >> 5;
         const T *src = (const T *)a.Q + (int64_t)(kv_head * a.share + r.g) * a.D * a.ldq + r.column;
-        auto at = [&](int d) { return d < a.D ? src[d * a.ldq] : (T)0; };
+        auto at = [&](int d) {
+            const T v = src[min(d, a.D - 1) * a.ldq];
+            return d < a.D ? v : (T)0;
+        };
 #pragma unroll
         for (int c = 0; c < QF; ++c) {
             if constexpr (sizeof(T) == 2) {
@@ -291,14 +349,15 @@ struct Rows {
                               : 8 * (i >> 2) + 4 * h + (i & 3);
     }
 
-    __device__ __forceinline__ void scores(lds_char *k) {
+    // S^T of the tile at k
+    __device__ __forceinline__ void scores(Scores &x, lds_char *k) const {
         const int lane = threadIdx.x & 63, h = lane >> 5;
 #pragma unroll
-        for (int b = 0; b < KB; ++b) s[b] = f16v{};
+        for (int b = 0; b < KB; ++b) x.s[b] = f16v{};
         if constexpr (sizeof(T) == 2) {
             // segment lane % 4 of its 16 keys: 0, 8, 4, 12 (see the file's comment)
-            const int row = 8 * h + ((lane & 15) >> 2), x = (lane >> 3) & 1;
-            const int at = row * kRowBytes + 16 * (2 * ((lane >> 4) & 1) + (lane & 1)) + 64 * x +
+            const int row = 8 * h + ((lane & 15) >> 2), odd = (lane >> 3) & 1;
+            const int at = row * kRowBytes + 16 * (2 * ((lane >> 4) & 1) + (lane & 1)) + 64 * odd +
                            8 * ((lane >> 1) & 1);
             lds_char *p0 = k + at, *p1 = k + (at ^ 64);
 #pragma unroll
@@ -307,49 +366,35 @@ struct Rows {
                 for (int b = 0; b < KB; ++b) {
                     lds_char *p = (b ? p1 : p0) + 16 * kRowBytes * c;
                     struct { s4 x, y; } f = {read_tr(p), read_tr(p + 4 * kRowBytes)};
-                    s[b] = mfma(__builtin_bit_cast(h8, f), q[c], s[b]);
+                    x.s[b] = mfma(__builtin_bit_cast(h8, f), q[c], x.s[b]);
                 }
             }
         } else {
             lds_char *p = k + h * kRowBytes + 4 * (lane & 31);
 #pragma unroll
-            for (int c = 0; c < QF; ++c) s[0] = mfma(read4(p + 2 * kRowBytes * c), q[c], s[0]);
+            for (int c = 0; c < QF; ++c) x.s[0] = mfma(read4(p + 2 * kRowBytes * c), q[c], x.s[0]);
         }
     }
 
-    // Leave keys out: bit j of `valid` is key j of the tile
-    __device__ __forceinline__ void mask(uint64_t valid) {
+    // Leave keys out: bit j of `valid` (the lane's own) is key j of the tile
+    __device__ __forceinline__ void mask(Scores &x, uint64_t valid) const {
         const int h = (threadIdx.x & 63) >> 5;
         const uint64_t mine = valid >> (sizeof(T) == 2 ? 8 * h : 4 * h);
 #pragma unroll
         for (int b = 0; b < KB; ++b)
 #pragma unroll
             for (int i = 0; i < 16; ++i)
-                s[b][i] = (mine >> key_of(b, i, 0)) & 1 ? s[b][i] : -INFINITY;
-    }
-    // ... of the drafted tokens (key `drafted` of the tile is the first), those
-    // that the lane's query does not see
-    __device__ __forceinline__ void mask_tree(const AttnArgs &a, int64_t column, int drafted) {
-        const int h = (threadIdx.x & 63) >> 5;
-        const uint8_t *see = a.tree + column * a.ldtree;
-#pragma unroll
-        for (int b = 0; b < KB; ++b)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const int at = key_of(b, i, h) - drafted;
-                if (at >= 0 && (at >= a.width || !see[at])) s[b][i] = -INFINITY;
-            }
+                x.s[b][i] = (mine >> key_of(b, i, 0)) & 1 ? x.s[b][i] : -INFINITY;
     }
 
-    // Scores to weights: the running maximum moves when a row's grew by more than
-    // Elem::slack powers of 2
-    __device__ __forceinline__ void weigh() {
-        float top = s[0][0];
+    // The running maximum moves when a row's grew by more than Elem::slack powers of 2
+    __device__ __forceinline__ void raise(const Scores &x) {
+        float top = x.s[0][0];
 #pragma unroll
         for (int b = 0; b < KB; ++b)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) top = fmaxf(top, s[b][i]);
-        top = fmaxf(top, other_half(top)) * scale2;
+            for (int i = 0; i < 16; ++i) top = fmaxf(top, x.s[b][i]);
+        top = larger_of_halves(top) * scale2;
         if (__any(top - m > Elem<T>::slack)) {  // (nothing seen yet: m is -inf)
             const float next = fmaxf(m, top);
             const float keep = m == next ? 1.f : exp2_fast(m - next);
@@ -358,60 +403,53 @@ struct Rows {
             for (int i = 0; i < DP / 32; ++i) o[i] *= keep;
             m = next;
         }
+    }
+
+    // Scores to weights, and their sum
+    __device__ __forceinline__ void weigh(Scores &x, Weights &w) {
         const float base = m == -INFINITY ? 0.f : m - Elem<T>::lift;
 #pragma unroll
         for (int b = 0; b < KB; ++b)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) s[b][i] = exp2_fast(fmaf(s[b][i], scale2, -base));
+            for (int i = 0; i < 16; ++i) x.s[b][i] = exp2_fast(fmaf(x.s[b][i], scale2, -base));
+        if constexpr (sizeof(T) == 2) {
+#pragma unroll
+            for (int c = 0; c < KT / 16; ++c) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) w.p[c][e] = (_Float16)x.s[c >> 1][8 * (c & 1) + e];
+                // the sum of the rounded weights: what the product divides by
+#pragma unroll
+                for (int e = 0; e < 8; e += 2)
+                    l = __builtin_amdgcn_fdot2(h2{w.p[c][e], w.p[c][e + 1]},
+                                               h2{(_Float16)1, (_Float16)1}, l, false);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) l += x.s[0][i];
+        }
     }
 
-    // O^T += V P^T; MASKED: values of keys left out count as 0 whatever they hold
-    template <bool MASKED>
-    __device__ __forceinline__ void values(lds_char *v, uint64_t valid) {
+    // O^T += V P^T
+    __device__ __forceinline__ void values(const Scores &x, const Weights &w, lds_char *v) {
         const int lane = threadIdx.x & 63, h = lane >> 5, row = lane & 31;
         const int swz = chunk_swizzle<T, true>(row);
         if constexpr (sizeof(T) == 2) {
 #pragma unroll
             for (int c = 0; c < KT / 16; ++c) {
-                h8 p;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) p[e] = (_Float16)s[c >> 1][8 * (c & 1) + e];
-                // the sum of the rounded weights: what the product divides by
-#pragma unroll
-                for (int e = 0; e < 8; e += 2)
-                    l = __builtin_amdgcn_fdot2(h2{p[e], p[e + 1]}, h2{(_Float16)1, (_Float16)1}, l,
-                                               false);
                 lds_char *at = v + row * kRowBytes + 16 * ((2 * c + h) ^ swz);
-                u4 keep;
-                if constexpr (MASKED) {
-                    const uint32_t bits = (uint32_t)(valid >> (16 * c + 8 * h));
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        keep[e] = ((bits >> (2 * e)) & 1 ? 0xffffu : 0u) |
-                                  ((bits >> (2 * e + 1)) & 1 ? 0xffff0000u : 0u);
-                }
-#pragma unroll
-                for (int d = 0; d < DP / 32; ++d) {
-                    u4 x = read16(at + 32 * kRowBytes * d);
-                    if constexpr (MASKED) x &= keep;
-                    o[d] = mfma(__builtin_bit_cast(h8, x), p, o[d]);
-                }
+                for (int d = 0; d < DP / 32; ++d)
+                    o[d] = mfma(__builtin_bit_cast(h8, read16(at + 32 * kRowBytes * d)), w.p[c], o[d]);
             }
         } else {
 #pragma unroll
             for (int b = 0; b < 4; ++b) {
-#pragma unroll
-                for (int r = 0; r < 4; ++r) l += s[0][4 * b + r];
                 lds_char *at = v + row * kRowBytes + 16 * ((2 * b + h) ^ swz);
-                const uint32_t bits = (uint32_t)(valid >> (8 * b + 4 * h));
 #pragma unroll
                 for (int d = 0; d < DP / 32; ++d) {
-                    v4f x = __builtin_bit_cast(v4f, read16(at + 32 * kRowBytes * d));
+                    const v4f y = __builtin_bit_cast(v4f, read16(at + 32 * kRowBytes * d));
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const float e = !MASKED || (bits >> r & 1) ? x[r] : 0.f;
-                        o[d] = mfma(e, s[0][4 * b + r], o[d]);
-                    }
+                    for (int r = 0; r < 4; ++r) o[d] = mfma(y[r], x.s[0][4 * b + r], o[d]);
                 }
             }
         }
@@ -427,25 +465,62 @@ __device__ __forceinline__ uint64_t valid_keys(int64_t t0, const RowTile &r, uin
     return __ballot(lane < Elem<T>::keys && c >= r.begin && c < r.end && mask_byte);
 }
 
-// One key tile of a wave: `k` is staged; wait_v() returns when `v` is
-template <typename T, int DP, typename Between, typename WaitV>
-__device__ __forceinline__ void attend_tile(const AttnArgs &a, Rows<T, DP> &w, const RowTile &r,
-                                            const RowAt &mine, int64_t t0, uint8_t mask_byte,
-                                            lds_char *k, lds_char *v, Between between,
-                                            WaitV wait_v) {
-    w.scores(k);
-    between();
-    const uint64_t valid = valid_keys<T>(t0, r, mask_byte);
-    const bool full = valid == (Elem<T>::keys == 64 ? ~0ull : 0xffffffffull);
-    if (!full) w.mask(valid);
-    if (a.tree && t0 + Elem<T>::keys > (int64_t)r.end - r.n)
-        w.mask_tree(a, mine.column, (int)((int64_t)r.end - r.n - t0));
-    w.weigh();
-    wait_v();
-    if (full)
-        w.template values<false>(v, valid);
-    else
-        w.template values<true>(v, valid);
+// Values of keys left out become 0 in LDS, whatever they hold (their weight is 0,
+// but 0 x NaN is not).  Every wave that reads the tile does it for itself: they
+// write the same bytes.
+template <typename T, int DP>
+__device__ __forceinline__ void clear_values(lds_char *v, uint64_t valid) {
+    const int lane = threadIdx.x & 63;
+    for (int i = 0; i < DP / 8; ++i) {
+        const int row = 8 * i + (lane >> 3);
+        const int key = Elem<T>::per_chunk * ((lane & 7) ^ chunk_swizzle<T, true>(row));
+        const uint32_t bits = (uint32_t)(valid >> key);
+        lds_char *at = v + 1024 * i + 16 * lane;
+        u4 x = read16(at);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if constexpr (sizeof(T) == 2)
+                x[e] &= ((bits >> (2 * e)) & 1 ? 0xffffu : 0u) |
+                        ((bits >> (2 * e + 1)) & 1 ? 0xffff0000u : 0u);
+            else
+                x[e] = (bits >> e) & 1 ? x[e] : 0u;
+        }
+        write16(at, x);
+    }
+}
+
+// Drafted tokens seen by each row (bit j: key j of the tile, whose key `drafted`
+// is the first drafted token; keys before it: 1): a lane loads its key's byte of
+// every row's line of the tree, a ballot makes the row's bits.
+template <typename T>
+__device__ __forceinline__ uint64_t seen_keys(const AttnArgs &a, int column, int drafted) {
+    const int lane = threadIdx.x & 63, at = lane - drafted;
+    const int from = min(max(at, 0), a.width - 1);
+    uint64_t mine = 0;
+#pragma unroll 8
+    for (int i = 0; i < 32; ++i) {
+        const int64_t c = __builtin_amdgcn_readlane(column, i);
+        const int seen = a.tree[c * a.ldtree + from] | (at < 0 ? 1 : 0);
+        const uint64_t bits = __ballot((seen != 0) & (at < a.width));
+        if ((lane & 31) == i) mine = bits;
+    }
+    return mine;
+}
+
+// Scores of keys that take no part in a tile at t0 become -inf; true when there
+// are keys whose values have to be cleared
+template <typename T, int DP>
+__device__ __forceinline__ bool settle(const AttnArgs &a, const Rows<T, DP> &w,
+                                       typename Rows<T, DP>::Scores &x, const RowTile &r,
+                                       const RowAt &mine, int64_t t0, uint64_t valid) {
+    constexpr int KT = Elem<T>::keys;
+    const bool full = valid == (KT == 64 ? ~0ull : 0xffffffffull);
+    const bool tree = a.tree && t0 + KT > (int64_t)r.end - r.n;
+    if (!full || tree) {
+        const int64_t drafted = max((int64_t)r.end - r.n - t0, -(int64_t)INT32_MAX);
+        w.mask(x, tree ? valid & seen_keys<T>(a, mine.column, (int)drafted) : valid);
+    }
+    return !full;
 }
 
 // The mask byte of the lane's key of the tile at t0 (1 without a mask)
@@ -455,19 +530,28 @@ __device__ __forceinline__ uint8_t mask_at(const AttnArgs &a, int64_t t0) {
     return c < a.Nk ? a.key_mask[c] : 0;
 }
 
-// Workgroup -> (row tile, part, key head); tiles of one (head, part) adjacent,
-// on one XCD: they read the same keys
-struct Place {
-    int tile, part, head;
-};
-__device__ __forceinline__ Place place_of(const AttnArgs &a) {
-    int id = xcd_tile(blockIdx.x, gridDim.x);
-    Place p;
-    p.tile = id % a.tiles;
-    id /= a.tiles;
-    p.part = id % a.splits;
-    p.head = id / a.splits;
-    return p;
+// The order of a step's instructions: the next scores' matrix instructions
+// between the weights' vector instructions, LDS reads ahead of their use, then
+// the product with V
+template <typename T, int DP>
+__device__ __forceinline__ void interleave() {
+#if defined(__HIP_DEVICE_COMPILE__)
+    if constexpr (sizeof(T) == 2) {
+        constexpr int kScores = DP / 16 * 2, kValues = DP / 32 * 4, kVector = 96 / kScores;
+        __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);
+#pragma unroll
+        for (int i = 0; i < kScores; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x002, kVector, 0);
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+        }
+#pragma unroll
+        for (int i = 0; i < kValues; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        }
+    }
+#endif
 }
 
 // Parts in the workspace: sums (padded D x rows), then maxima and totals, of every
@@ -480,10 +564,15 @@ __device__ __forceinline__ float *part_at(const AttnArgs &a, int part, int head,
 template <typename T, int DP, bool REGS>
 __global__ __launch_bounds__(256, DP <= (REGS ? 96 : 128) ? 2 : 1) void k_attn_shared(AttnArgs a) {
     constexpr int TR = kAttnSharedRows, KT = Elem<T>::keys, kTile = DP * kRowBytes;
-    __shared__ __attribute__((aligned(1024))) char lds_mem[2][2 * kTile];
-    const Place at = place_of(a);
-    RowTile r;
-    if (!find_rows<TR>(a, at.tile, r)) return;
+    // variables of their own: the compiler sees that reads of one do not touch
+    // copies into another still in flight
+    __shared__ __attribute__((aligned(1024))) char lds_k0[kTile];
+    __shared__ __attribute__((aligned(1024))) char lds_k1[kTile];
+    __shared__ __attribute__((aligned(1024))) char lds_v0[kTile];
+    __shared__ __attribute__((aligned(1024))) char lds_v1[kTile];
+    Place at;
+    if (!find_place<TR>(a, blockIdx.x, at)) return;
+    const RowTile &r = at.rows;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const RowAt mine = row_at<TR>(a, r, 32 * wave + (lane & 31));
     Rows<T, DP> w;
@@ -498,32 +587,67 @@ __global__ __launch_bounds__(256, DP <= (REGS ? 96 : 128) ? 2 : 1) void k_attn_s
         Stager<T, DP, true, REGS, 4> vs;
         ks.init(a.K, a.ldk, at.head, a.D, a.Nk, first, wave);
         vs.init(a.V, a.ldv, at.head, a.D, a.Nk, first, wave);
-        lds_char *buf0 = (lds_char *)lds_mem[0], *buf1 = (lds_char *)lds_mem[1];
-        uint8_t byte = mask_at(a, (int64_t)first + (int64_t)lo * KT);
-        ks.ask(lo * KT, buf0, wave);
-        vs.ask(lo * KT, buf0 + kTile, wave);
-        ks.put(buf0, wave);
-        vs.put(buf0 + kTile, wave);
-        for (int t = lo; t < hi; ++t) {
-            lds_char *cur = (t - lo) & 1 ? buf1 : buf0, *nxt = (t - lo) & 1 ? buf0 : buf1;
-            __syncthreads();  // this tile has landed, the other buffer is free
-            const int64_t t0 = (int64_t)first + (int64_t)t * KT;
-            const uint8_t now = byte;
-            if (t + 1 < hi) {
-                byte = mask_at(a, t0 + KT);
-                ks.ask((t + 1) * KT, nxt, wave);
-                vs.ask((t + 1) * KT, nxt + kTile, wave);
+        uint8_t byte;
+        // The scores of tile t + 1 are taken while tile t's become weights: matrix
+        // and vector instructions of one wave side by side.
+        typename Rows<T, DP>::Scores s0, s1;
+        typename Rows<T, DP>::Weights p;
+        auto valid_at = [&](int t, uint8_t b) {
+            return valid_keys<T>((int64_t)first + (int64_t)t * KT, r, b);
+        };
+        // K of tile t + 1 and V of tile t are under way
+        auto step = [&](auto more, int t, typename Rows<T, DP>::Scores &cur,
+                        typename Rows<T, DP>::Scores &nxt, lds_char *k_cur, lds_char *k_nxt,
+                        lds_char *v_cur, lds_char *v_nxt) {
+            __syncthreads();  // they have landed; the buffers of K of tile t, V of t - 1 are free
+            const uint64_t valid = valid_at(t, byte);
+            if (more) {
+                byte = mask_at(a, (int64_t)first + (int64_t)(t + 1) * KT);
+                if (t + 2 < hi) ks.ask((t + 2) * KT, k_cur, wave);
+                vs.ask((t + 1) * KT, v_nxt, wave);
             }
-            attend_tile<T, DP>(a, w, r, mine, t0, now, cur, cur + kTile, [] {}, [] {});
-            if (REGS && t + 1 < hi) {
-                ks.put(nxt, wave);
-                vs.put(nxt + kTile, wave);
+            if (settle(a, w, cur, r, mine, (int64_t)first + (int64_t)t * KT, valid))
+                clear_values<T, DP>(v_cur, valid);
+            w.raise(cur);
+            if (more) w.scores(nxt, k_nxt);
+            w.weigh(cur, p);
+            w.values(cur, p, v_cur);
+            if (more) interleave<T, DP>();
+            if (REGS && more) {
+                if (t + 2 < hi) ks.put(k_cur, wave);
+                vs.put(v_nxt, wave);
             }
+        };
+        lds_char *k0 = (lds_char *)lds_k0, *k1 = (lds_char *)lds_k1;
+        lds_char *v0 = (lds_char *)lds_v0, *v1 = (lds_char *)lds_v1;
+        ks.ask(lo * KT, k0, wave);
+        ks.put(k0, wave);
+        byte = mask_at(a, (int64_t)first + (int64_t)lo * KT);
+        __syncthreads();
+        if (lo + 1 < hi) ks.ask((lo + 1) * KT, k1, wave);
+        vs.ask(lo * KT, v0, wave);
+        w.scores(s0, k0);
+        if (REGS) {
+            if (lo + 1 < hi) ks.put(k1, wave);
+            vs.put(v0, wave);
+        }
+        constexpr std::true_type on{};
+        constexpr std::false_type off{};
+        int t = lo;
+        for (; t + 2 < hi; t += 2) {
+            step(on, t, s0, s1, k0, k1, v0, v1);
+            step(on, t + 1, s1, s0, k1, k0, v1, v0);
+        }
+        if (t + 1 < hi) {
+            step(on, t, s0, s1, k0, k1, v0, v1);
+            step(off, t + 1, s1, s0, k1, k0, v1, v0);
+        } else {
+            step(off, t, s0, s1, k0, k1, v0, v1);
         }
     }
 
     const int h = lane >> 5;
-    const float total = w.l + other_half(w.l);
+    const float total = sum_of_halves(w.l);
     if (a.splits > 1) {
         float *part = part_at<DP, TR>(a, at.part, at.head, at.tile) + 32 * wave + (lane & 31);
 #pragma unroll
@@ -556,11 +680,12 @@ template <typename T, int DP, bool REGS>
 __global__ __launch_bounds__(64 * split_waves<DP>(), 1) void k_attn_split(AttnArgs a) {
     constexpr int TR = kAttnSplitRows, KT = Elem<T>::keys, kTile = DP * kRowBytes;
     constexpr int W = split_waves<DP>();
-    __shared__ __attribute__((aligned(1024))) char lds_mem[W][2 * kTile];
+    __shared__ __attribute__((aligned(1024))) char lds_k[W * kTile];
+    __shared__ __attribute__((aligned(1024))) char lds_v[W * kTile];
     __shared__ float tops[W][TR], totals[W][TR];
-    const Place at = place_of(a);
-    RowTile r;
-    if (!find_rows<TR>(a, at.tile, r)) return;
+    Place at;
+    if (!find_place<TR>(a, blockIdx.x, at)) return;
+    const RowTile &r = at.rows;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const RowAt mine = row_at<TR>(a, r, lane & 31);
     Rows<T, DP> w;
@@ -570,7 +695,7 @@ __global__ __launch_bounds__(64 * split_waves<DP>(), 1) void k_attn_split(AttnAr
     const int tiles = r.end > r.begin ? (r.end - first + KT - 1) / KT : 0;
     const int lo = (int)((int64_t)tiles * at.part / a.splits) + wave;
     const int hi = (int)((int64_t)tiles * (at.part + 1) / a.splits);
-    lds_char *k = (lds_char *)lds_mem[wave], *v = k + kTile;
+    lds_char *k = (lds_char *)lds_k + wave * kTile, *v = (lds_char *)lds_v + wave * kTile;
     if (lo < hi) {
         Stager<T, DP, false, REGS, 1> ks;
         Stager<T, DP, true, REGS, 1> vs;
@@ -586,24 +711,27 @@ __global__ __launch_bounds__(64 * split_waves<DP>(), 1) void k_attn_split(AttnAr
             const bool more = t + W < hi;
             const uint8_t now = byte;
             if (!REGS) wait_vm<kCopies>();  // K has landed; V may still be in flight
-            attend_tile<T, DP>(
-                a, w, r, mine, t0, now, k, v,
-                [&] {
-                    wait_lds();  // K's tile has been read
-                    vs.put(v, 0);
-                    if (more) {
-                        byte = mask_at(a, t0 + (int64_t)W * KT);
-                        ks.ask((t + W) * KT, k, 0);
-                    }
-                },
-                [&] {
-                    if (!REGS) {
-                        if (more)
-                            wait_vm<kCopies>();
-                        else
-                            wait_vm<0>();
-                    }
-                });
+            typename Rows<T, DP>::Scores x;
+            typename Rows<T, DP>::Weights p;
+            w.scores(x, k);
+            wait_lds();  // K's tile has been read
+            vs.put(v, 0);
+            if (more) {
+                byte = mask_at(a, t0 + (int64_t)W * KT);
+                ks.ask((t + W) * KT, k, 0);
+            }
+            const uint64_t valid = valid_keys<T>(t0, r, now);
+            const bool clear = settle(a, w, x, r, mine, t0, valid);
+            w.raise(x);
+            w.weigh(x, p);
+            if (!REGS) {
+                if (more)
+                    wait_vm<kCopies>();
+                else
+                    wait_vm<0>();
+            }
+            if (clear) clear_values<T, DP>(v, valid);
+            w.values(x, p, v);
             wait_lds();  // V's too
             if (more) {
                 ks.put(k, 0);
@@ -614,7 +742,7 @@ __global__ __launch_bounds__(64 * split_waves<DP>(), 1) void k_attn_split(AttnAr
 
     // join the waves: maxima, then sums at the common maximum
     const int h = lane >> 5, row = lane & 31;
-    const float total = w.l + other_half(w.l);
+    const float total = sum_of_halves(w.l);
     if (h == 0) tops[wave][row] = w.m;
     __syncthreads();
     float top = tops[0][row];
@@ -622,7 +750,8 @@ __global__ __launch_bounds__(64 * split_waves<DP>(), 1) void k_attn_split(AttnAr
     for (int i = 1; i < W; ++i) top = fmaxf(top, tops[i][row]);
     const float f = w.m == -INFINITY ? 0.f : exp2_fast(w.m - top);
     if (h == 0) totals[wave][row] = f * total;
-    float *sums = (float *)lds_mem[wave];
+    static_assert(DP * TR * 4 == kTile, "a wave's sums take the place of its keys");
+    float *sums = (float *)(lds_k + wave * kTile);
 #pragma unroll
     for (int d = 0; d < DP / 32; ++d)
 #pragma unroll
@@ -642,7 +771,7 @@ __global__ __launch_bounds__(64 * split_waves<DP>(), 1) void k_attn_split(AttnAr
     for (int d = threadIdx.x / TR; d < DP; d += 2 * W) {
         float x = 0.f;
 #pragma unroll
-        for (int i = 0; i < W; ++i) x += ((float *)lds_mem[i])[d * TR + row];
+        for (int i = 0; i < W; ++i) x += ((const float *)(lds_k + i * kTile))[d * TR + row];
         if (a.splits > 1)
             part[d * TR] = x;
         else if (mine.valid && d < a.D)
@@ -654,9 +783,12 @@ __global__ __launch_bounds__(64 * split_waves<DP>(), 1) void k_attn_split(AttnAr
 // head, 8 rows of the head)
 template <typename T, int DP, int TR>
 __global__ __launch_bounds__(kBlock) void k_attn_join(AttnArgs a) {
-    RowTile r;
-    const int tile = blockIdx.x, head = blockIdx.y;
-    if (!find_rows<TR>(a, tile, r)) return;
+    AttnArgs one = a;
+    one.splits = 1;
+    Place at;
+    if (!find_place<TR>(one, blockIdx.x, at)) return;
+    const RowTile &r = at.rows;
+    const int tile = at.tile, head = at.head;
     const int i = threadIdx.x % TR;
     const RowAt mine = row_at<TR>(a, r, i);
     if (!mine.valid) return;
@@ -672,7 +804,7 @@ __global__ __launch_bounds__(kBlock) void k_attn_join(AttnArgs a) {
     const float inv = all == 0.f ? 0.f : 1.f / all;
     T *out = (T *)a.O + (int64_t)(head * a.share + mine.g) * a.D * a.ldo + mine.column;
     constexpr int kAtOnce = kBlock / TR;
-    const int d0 = blockIdx.z * 8;
+    const int d0 = blockIdx.y * 8;
     for (int d = d0 + threadIdx.x / TR; d < d0 + 8 && d < a.D; d += kAtOnce) {
         float x = 0.f;
         for (int s = 0; s < a.splits; ++s) x += weight(s) * part[s * step + d * TR];
@@ -694,7 +826,7 @@ nmg_status launch_attn_dim(const AttnArgs &a, bool shared, bool regs, hipStream_
         hipLaunchKernelGGL((k_attn_split<T, DP, false>), grid, dim3(64 * split_waves<DP>()), 0,
                            stream, a);
     if (a.splits > 1) {
-        const dim3 join((unsigned)a.tiles, (unsigned)a.kv_heads, (unsigned)((a.D + 7) / 8));
+        const dim3 join((unsigned)(a.tiles * a.kv_heads), (unsigned)((a.D + 7) / 8));
         if (shared)
             hipLaunchKernelGGL((k_attn_join<T, DP, kAttnSharedRows>), join, dim3(kBlock), 0,
                                stream, a);

@@ -19,17 +19,32 @@ Plan plan_of(nmg_dtype dtype, const AttnArgs &a) {
     // one wave's rows cover the average sequence: split the keys over the waves
     p.shared = rows > (int64_t)kAttnSplitRows * a.sequences;
     const int tr = p.shared ? kAttnSharedRows : kAttnSplitRows;
-    // sum of ceil(rows_b / tr) over sequences that hold `rows` rows together
-    p.tiles = std::min(rows / tr + a.sequences, rows);
+    // sum of ceil(rows_b / tr) over sequences that hold `rows` rows together: at most ...
+    p.tiles = a.sequences == 1 ? (rows + tr - 1) / tr : std::min(rows / tr + a.sequences, rows);
+    // ... and for equal lengths
+    const int64_t each = (rows + a.sequences - 1) / a.sequences;
+    const int64_t items = std::min((each + tr - 1) / tr * a.sequences, p.tiles) * a.kv_heads;
     const int dp = attn_padded_dim(a.D);
     const int kt = dtype == NMG_F16 ? 64 : 32;
     const int64_t keys = (a.Nk + a.sequences - 1) / a.sequences;  // of a sequence, if they share Nk
-    const int64_t kt_tiles = (keys + kt - 1) / kt;
-    const int64_t blocks = p.tiles * a.kv_heads;
+    const int waves = p.shared ? 1 : dp <= 64 ? 8 : dp <= 128 ? 4 : 2;  // that split a part's keys
+    const int64_t steps = (keys + (int64_t)kt * waves - 1) / (kt * waves);
     const int64_t slots = (int64_t)device_cus() * (p.shared ? 2 : 1);
-    // at least 4 key tiles for every wave
-    const int64_t most = kt_tiles / (p.shared ? 4 : 4 * (dp <= 64 ? 8 : dp <= 128 ? 4 : 2));
-    p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(std::min(slots / blocks, most), 256));
+    // The split that ends first, in steps of one key tile: rounds of workgroups
+    // times (its steps + about 2 to start), and with parts their traffic (an
+    // item's sums written and read: for 512 of 128 rows about 8 steps) and a launch.
+    p.splits = 1;
+    int64_t best = INT64_MAX;
+    for (int64_t s = 1; s <= 64 && (s == 1 || steps / s >= 4); ++s) {
+        const int64_t rounds = (items * s + slots - 1) / slots;
+        const int64_t cost = 8 * rounds * ((steps + s - 1) / s + 2) +
+                             (s > 1 ? items * s * (p.shared ? 64 : 16) / slots + 40 : 0);
+        if (cost < best) {
+            best = cost;
+            p.splits = (int)s;
+        }
+    }
+    const int64_t blocks = p.tiles * a.kv_heads;
     p.part_bytes = blocks * (dp + 2) * tr * (int64_t)sizeof(float);
     return p;
 }

@@ -1,45 +1,148 @@
 // k_rotary.hip -- position rotation of heads, alone or behind the norm of
 // queries and keys (features x tokens), and its tables.
 //
-//   k_rotary        a thread per (token, head): the column's sum of squares,
-//                   then its pairs.
-//   k_rotary_table  cosines and sines in binary64.
+// k_rotary.  A head's rows come in units: the R / 2 pairs that turn, then the
+// other rows by twos.  A workgroup covers a run of tokens (lanes, so every load
+// and store is a run of a row) and all units of a head, dealt over its
+// slices; a thread keeps its units of `tokens` tokens in registers from the
+// load to the store, so a head is read once and written once, whether the sum
+// of squares (added over the slices by lane exchanges and LDS) comes between
+// or not.  Cosines and sines are the same for every head: a workgroup keeps
+// them in registers for a run of heads, as many as leave about four workgroups
+// for every compute unit.
+//
+// k_rotary_table  cosines and sines in binary64.
 #include "rotary.hpp"
 
 namespace {
 
-template <typename T, bool NORM>
-__global__ __launch_bounds__(kBlock) void k_rotary(RotaryArgs a) {
-    const int64_t t = (int64_t)blockIdx.x * kBlock + threadIdx.x;
-    if (t >= a.N) return;
-    const int which = (int)blockIdx.y >= a.part[0].heads;
-    const RotaryRows &r = a.part[which];
-    const int h = (int)blockIdx.y - (which ? a.part[0].heads : 0);
-    const T *x = (const T *)r.X + (int64_t)h * a.D * r.ldx + t;
-    T *y = (T *)r.Y + (int64_t)h * a.D * r.ldy + t;
-    float s = 1.f;
-    if (NORM) {
-        float sum = 0.f;
-        for (int d = 0; d < a.D; ++d) {
-            const float v = (float)x[d * r.ldx];
-            sum = fmaf(v, v, sum);
+// N: tokens a thread, U: units a thread
+template <typename T, bool NORM, int N, int U>
+__global__ __launch_bounds__(kBlock, N == 4 && U <= 4 ? 4 : 1) void k_rotary(RotaryArgs a) {
+    __shared__ float sums[2][kBlock / 64][64 * N];
+    const int lanes = a.lanes, slices = kBlock / lanes;  // of tokens
+    const int x = threadIdx.x % lanes, slice = threadIdx.x / lanes;
+    // neighbouring runs of tokens on one XCD: rows rarely start on a cache line,
+    // and the line two workgroups share is put together in its L2
+    const int id = xcd_tile(blockIdx.x, gridDim.x), run = id / a.blocks;
+    const int64_t t = ((int64_t)(id - run * a.blocks) * lanes + x) * N;
+    const bool here = t < a.N, whole = t + N <= a.N;
+    const int which = run >= a.groups0;
+    const RotaryRows r = a.part[which];
+    const int h0 = (run - (which ? a.groups0 : 0)) * a.run;
+    const int h1 = min(h0 + a.run, r.heads);
+
+    const int half = a.R / 2, units = half + (a.D - a.R + 1) / 2;
+    int row[U][2];       // of unit i; -1: none
+    float c[U][N], s[U][N], w[U][2];
+    int64_t p[N];
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        p[n] = 0;
+        if (a.R && t + n < a.N) p[n] = min(max((int64_t)a.positions[t + n], (int64_t)0), a.length - 1);
+    }
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+        const int u = slice + i * slices;
+        row[i][0] = row[i][1] = -1;
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            c[i][n] = 1.f;
+            s[i][n] = 0.f;
         }
-        s = 1.f / sqrtf(sum / (float)a.D + a.eps);
+        if (u < half) {
+            row[i][0] = a.interleaved ? 2 * u : u;
+            row[i][1] = a.interleaved ? 2 * u + 1 : u + half;
+#pragma unroll
+            for (int n = 0; n < N; ++n) {
+                c[i][n] = a.table[u * a.length + p[n]];
+                s[i][n] = a.table[(half + u) * a.length + p[n]];
+            }
+        } else if (u < units) {
+            row[i][0] = a.R + 2 * (u - half);
+            row[i][1] = row[i][0] + 1 < a.D ? row[i][0] + 1 : -1;
+        }
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+            w[i][e] = NORM && r.weight && row[i][e] >= 0 ? r.weight[row[i][e]] : 1.f;
     }
-    auto at = [&](int d) {
-        const float v = (float)x[d * r.ldx];
-        return NORM ? v * s * (r.weight ? r.weight[d] : 1.f) : v;
-    };
-    int64_t p = 0;
-    if (a.R) p = min(max((int64_t)a.positions[t], (int64_t)0), a.length - 1);
-    for (int i = 0; i < a.R / 2; ++i) {
-        const int da = a.interleaved ? 2 * i : i, db = a.interleaved ? 2 * i + 1 : i + a.R / 2;
-        const float c = a.table[i * a.length + p], n = a.table[(a.R / 2 + i) * a.length + p];
-        const float u = at(da), v = at(db);
-        y[da * r.ldy] = (T)(u * c - v * n);
-        y[db * r.ldy] = (T)(u * n + v * c);
+
+    typedef T TN __attribute__((ext_vector_type(N)));
+    for (int h = h0; h < h1; ++h) {
+        const T *src = (const T *)r.X + (int64_t)h * a.D * r.ldx + t;
+        T *dst = (T *)r.Y + (int64_t)h * a.D * r.ldy + t;
+        float v[U][2][N];
+#pragma unroll
+        for (int i = 0; i < U; ++i)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                TN y = {};
+                if (row[i][e] >= 0 && here) {
+                    const T *q = src + row[i][e] * r.ldx;
+                    if (whole) {
+                        __builtin_memcpy(&y, q, sizeof y);
+                    } else {
+#pragma unroll
+                        for (int n = 0; n < N; ++n)
+                            if (t + n < a.N) y[n] = q[n];
+                    }
+                }
+#pragma unroll
+                for (int n = 0; n < N; ++n) v[i][e][n] = (float)y[n];
+            }
+        float scale[N];
+        if constexpr (NORM) {
+#pragma unroll
+            for (int n = 0; n < N; ++n) {
+                float sum = 0.f;
+#pragma unroll
+                for (int i = 0; i < U; ++i)
+                    sum = fmaf(v[i][0][n], v[i][0][n], fmaf(v[i][1][n], v[i][1][n], sum));
+                for (int d = lanes; d < 64; d *= 2) sum += __shfl_xor(sum, d);
+                scale[n] = sum;
+            }
+            // two sets of sums: a wave may be a head ahead of another's reads
+            auto &mine = sums[(h - h0) & 1];
+            if ((threadIdx.x & 63) < lanes)
+#pragma unroll
+                for (int n = 0; n < N; ++n) mine[threadIdx.x / 64][x * N + n] = scale[n];
+            __syncthreads();
+#pragma unroll
+            for (int n = 0; n < N; ++n) {
+                float sum = 0.f;
+#pragma unroll
+                for (int i = 0; i < kBlock / 64; ++i) sum += mine[i][x * N + n];
+                scale[n] = 1.f / sqrtf(sum / (float)a.D + a.eps);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            TN out[2];
+#pragma unroll
+            for (int n = 0; n < N; ++n) {
+                float f = v[i][0][n], g = v[i][1][n];
+                if (NORM) {
+                    f = f * scale[n] * w[i][0];
+                    g = g * scale[n] * w[i][1];
+                }
+                const bool turns = slice + i * slices < half;
+                out[0][n] = (T)(turns ? f * c[i][n] - g * s[i][n] : f);
+                out[1][n] = (T)(turns ? f * s[i][n] + g * c[i][n] : g);
+            }
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                if (row[i][e] < 0 || !here) continue;
+                T *q = dst + row[i][e] * r.ldy;
+                if (whole) {
+                    __builtin_memcpy(q, &out[e], sizeof(TN));
+                } else {
+#pragma unroll
+                    for (int n = 0; n < N; ++n)
+                        if (t + n < a.N) q[n] = out[e][n];
+                }
+            }
+        }
     }
-    for (int d = a.R; d < a.D; ++d) y[d * r.ldy] = (T)at(d);
 }
 
 __global__ __launch_bounds__(kBlock) void k_rotary_table(RotaryTableArgs a) {
@@ -63,18 +166,54 @@ __global__ __launch_bounds__(kBlock) void k_rotary_table(RotaryTableArgs a) {
 
 namespace nmg_internal {
 
-nmg_status launch_rotary(nmg_dtype dtype, const RotaryArgs &a, bool norm, hipStream_t stream) {
-    const int64_t heads = (int64_t)a.part[0].heads + a.part[1].heads;
-    if (heads > 65535) return NMG_ERR_UNSUPPORTED;
-    const dim3 grid((unsigned)((a.N + kBlock - 1) / kBlock), (unsigned)heads);
-    if (dtype == NMG_F32 && norm)
-        hipLaunchKernelGGL((k_rotary<float, true>), grid, dim3(kBlock), 0, stream, a);
-    else if (dtype == NMG_F32)
-        hipLaunchKernelGGL((k_rotary<float, false>), grid, dim3(kBlock), 0, stream, a);
-    else if (norm)
-        hipLaunchKernelGGL((k_rotary<_Float16, true>), grid, dim3(kBlock), 0, stream, a);
+namespace {
+
+template <typename T, bool NORM>
+void launch(const RotaryArgs &a, int tokens, int units, dim3 grid, hipStream_t stream) {
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kBlock), 0, stream, a); };
+    if (tokens == 1 && units <= 1)
+        go(k_rotary<T, NORM, 1, 1>);
+    else if (tokens == 1 && units <= 4)
+        go(k_rotary<T, NORM, 1, 4>);
+    else if (tokens == 1)
+        go(k_rotary<T, NORM, 1, 16>);
+    else if (units <= 2)
+        go(k_rotary<T, NORM, 4, 2>);
+    else if (units <= 4)
+        go(k_rotary<T, NORM, 4, 4>);
     else
-        hipLaunchKernelGGL((k_rotary<_Float16, false>), grid, dim3(kBlock), 0, stream, a);
+        go(k_rotary<T, NORM, 4, 8>);
+}
+
+}  // namespace
+
+nmg_status launch_rotary(nmg_dtype dtype, const RotaryArgs &args, bool norm, hipStream_t stream) {
+    RotaryArgs a = args;
+    const int units = a.R / 2 + (a.D - a.R + 1) / 2;
+    auto per_thread = [&] { return (units * a.lanes + kBlock - 1) / kBlock; };
+    // 4 tokens a thread for 128 or more: 256 bytes of a row at a time (at any alignment)
+    int tokens = a.N >= 128 ? 4 : 1;
+    const int most_lanes = tokens == 1 ? 64 : dtype == NMG_F16 ? 32 : 16;
+    a.lanes = 1;
+    while (a.lanes < most_lanes && (int64_t)a.lanes * tokens < a.N) a.lanes *= 2;
+    while (a.lanes > 1 && per_thread() > (tokens == 1 ? 16 : 8)) a.lanes /= 2;
+    if (per_thread() > 8) tokens = 1;
+    if (per_thread() > 16) return NMG_ERR_UNSUPPORTED;
+    const int64_t width = (int64_t)a.lanes * tokens, blocks = (a.N + width - 1) / width;
+    const int64_t heads = (int64_t)a.part[0].heads + a.part[1].heads;
+    a.run = (int)std::max<int64_t>(1, std::min<int64_t>(8, blocks * heads / (4 * device_cus())));
+    a.groups0 = (a.part[0].heads + a.run - 1) / a.run;
+    const int64_t groups = a.groups0 + (a.part[1].heads + a.run - 1) / a.run;
+    if (blocks * groups > INT32_MAX) return NMG_ERR_UNSUPPORTED;
+    a.blocks = (int)blocks;
+    const dim3 grid((unsigned)(blocks * groups));
+    const int u = per_thread();
+    if (dtype == NMG_F32)
+        norm ? launch<float, true>(a, tokens, u, grid, stream)
+             : launch<float, false>(a, tokens, u, grid, stream);
+    else
+        norm ? launch<_Float16, true>(a, tokens, u, grid, stream)
+             : launch<_Float16, false>(a, tokens, u, grid, stream);
     return launched();
 }
 

@@ -22,6 +22,11 @@ struct RotaryArgs {
     const float *table;
     const int32_t *positions;
     float eps;
+    // the plan of the launch
+    int32_t lanes;    // threads of a workgroup along the tokens
+    int32_t blocks;   // workgroups along the tokens
+    int32_t run;      // heads a workgroup takes one after another
+    int32_t groups0;  // runs of part[0]
 };
 
 nmg_status launch_rotary(nmg_dtype dtype, const RotaryArgs &a, bool norm, hipStream_t stream);

@@ -198,16 +198,13 @@ def _stream(t: torch.Tensor) -> int:
 def _need_cuda(*ts):
     """Every tensor on the current GPU: the library launches on the current
     HIP device, on that device's current stream."""
-    cur = -1
+    cur = torch._C._cuda_getDevice() if ts[0].is_cuda else -1
     for t in ts:
-        dev = t.get_device()
-        if dev < 0 or not t.is_cuda:
-            raise ValueError("libnmg works on GPU tensors only")
-        if cur < 0:
-            cur = torch._C._cuda_getDevice()
-        if dev != cur:
-            raise ValueError(f"tensor on {t.device}, but the current device is cuda:{cur} "
-                             "(select it with torch.cuda.device)")
+        if t.get_device() != cur or cur < 0:
+            if not t.is_cuda:
+                raise ValueError("libnmg works on GPU tensors only")
+            raise ValueError(f"tensor on {t.device}, but the current device is "
+                             f"cuda:{torch._C._cuda_getDevice()} (select it with torch.cuda.device)")
 
 
 def _rows(t: torch.Tensor, name: str) -> int:
@@ -569,6 +566,24 @@ def rotary_table(length: int, dim: int, base: float = 10000.0, scaling: str = "n
     return table
 
 
+# These calls are made once a layer and step, for single tokens too, so their
+# checks are few attribute reads each.
+
+def _matrix(t: torch.Tensor, name: str):
+    """(rows, columns, leading dimension) of a 2-D row-major tensor."""
+    shape, st = t.shape, t.stride()
+    if len(st) != 2 or st[1] != 1:
+        raise ValueError(f"{name} must be a 2-D tensor with unit column stride")
+    return shape[0], shape[1], st[0]
+
+
+def _ints(t: torch.Tensor, n: int, name: str) -> int:
+    """Pointer of n contiguous int32 values."""
+    if t.dtype is not torch.int32 or t.dim() != 1 or t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"{name} must be {n} contiguous int32 values")
+    return t.data_ptr()
+
+
 def _rotary_desc(table, positions, pairs: str, N: int) -> _Rotary:
     code = ROTARY_PAIRS.get(pairs)
     if code is None:
@@ -576,25 +591,22 @@ def _rotary_desc(table, positions, pairs: str, N: int) -> _Rotary:
     if table is None:
         return _Rotary(0, code, 0, None, None)
     shape = table.shape
-    if len(shape) != 3 or shape[0] != 2 or table.dtype != torch.float32 or not table.is_contiguous():
+    if len(shape) != 3 or shape[0] != 2 or table.dtype is not torch.float32 or \
+            not table.is_contiguous():
         raise ValueError("table must be a contiguous float32 (2, dim / 2, length) tensor")
-    if positions.dtype != torch.int32 or positions.shape != (N,) or not positions.is_contiguous():
-        raise ValueError("positions must be N contiguous int32 values")
-    _need_cuda(table, positions)
-    return _Rotary(2 * shape[1], code, shape[2], table.data_ptr(), positions.data_ptr())
+    return _Rotary(2 * shape[1], code, shape[2], table.data_ptr(), _ints(positions, N, "positions"))
 
 
-def _head_rows(t: torch.Tensor, heads: int, name: str) -> int:
+def _head_rows(rows: int, heads: int, name: str) -> int:
     """Rows of one head of a features x tokens matrix."""
-    rows = t.shape[0]
-    if heads < 1 or rows % heads or not rows:
+    if heads < 1 or rows < 1 or rows % heads:
         raise ValueError(f"{name} must have a whole number of rows for each of {heads} heads")
     return rows // heads
 
 
-def _out_like(t: torch.Tensor, out, name: str) -> torch.Tensor:
+def _out_for(t: torch.Tensor, out, name: str) -> torch.Tensor:
     if out is None:
-        return t.new_empty(t.shape)
+        return torch.empty_like(t)
     if out.dtype != t.dtype or out.shape != t.shape:
         raise ValueError(f"{name} must have the shape and dtype of its input")
     return out
@@ -607,13 +619,18 @@ def rotary(X, heads: int, table, positions, layout: str = "half", out=None):
     code = _DTYPE_CODE.get(X.dtype)
     if code is None:
         raise TypeError(f"unsupported dtype {X.dtype}")
-    ldx, N = _rows(X, "X"), X.shape[1]
-    D = _head_rows(X, heads, "X")
-    out = _out_like(X, out, "out")
-    _need_cuda(X, out)
+    M, N, ldx = _matrix(X, "X")
+    D = _head_rows(M, heads, "X")
     desc = _rotary_desc(table, positions, layout, N)
-    _check(lib().nmg_rotary(code, heads, D, desc, X.data_ptr(), ldx, N, out.data_ptr(),
-                            _rows(out, "out"), _stream(X)), "nmg_rotary")
+    if table is None:
+        _need_cuda(X)
+    else:
+        _need_cuda(X, table, positions)
+    out = _out_for(X, out, "out")
+    if out.get_device() != X.get_device():
+        _need_cuda(X, out)
+    _check((_lib or _load()).nmg_rotary(code, heads, D, desc, X.data_ptr(), ldx, N, out.data_ptr(),
+                                        _matrix(out, "out")[2], _stream(X)), "nmg_rotary")
     return out
 
 
@@ -623,50 +640,60 @@ def qk_norm_rotary(Q, K, heads: int, kv_heads: int, q_weight, k_weight, table=No
     (weights float32 of head_dim, or None) and the rotation (none without a
     table).  out: (Q's, K's), which may be Q and K.  Returns both."""
     code = _DTYPE_CODE.get(Q.dtype)
-    if code is None or K.dtype != Q.dtype:
+    if code is None or K.dtype is not Q.dtype:
         raise TypeError("Q and K must be float32 or float16, of one dtype")
-    ldq, ldk, N = _rows(Q, "Q"), _rows(K, "K"), Q.shape[1]
-    D = _head_rows(Q, heads, "Q")
-    if _head_rows(K, kv_heads, "K") != D or K.shape[1] != N:
+    M, N, ldq = _matrix(Q, "Q")
+    Mk, Nk, ldk = _matrix(K, "K")
+    D = _head_rows(M, heads, "Q")
+    if Nk != N or _head_rows(Mk, kv_heads, "K") != D:
         raise ValueError("Q and K must have heads of one size and the same tokens")
-    yq, yk = (None, None) if out is None else out
-    yq, yk = _out_like(Q, yq, "out[0]"), _out_like(K, yk, "out[1]")
-    _need_cuda(Q, K, yq, yk)
-    for w in (q_weight, k_weight):
-        if w is not None:
-            if w.dtype != torch.float32 or w.shape != (D,) or not w.is_contiguous():
-                raise ValueError("norm weights must be head_dim contiguous float32 values")
-            _need_cuda(w)
     desc = _rotary_desc(table, positions, layout, N)
-    _check(lib().nmg_qk_norm_rotary(
-        code, heads, kv_heads, D, desc, None if q_weight is None else q_weight.data_ptr(),
-        None if k_weight is None else k_weight.data_ptr(), eps, Q.data_ptr(), ldq, K.data_ptr(), ldk,
-        N, yq.data_ptr(), _rows(yq, "out[0]"), yk.data_ptr(), _rows(yk, "out[1]"), _stream(Q)),
-        "nmg_qk_norm_rotary")
+    used = [Q, K]
+    weights = [None, None]
+    for i, w in enumerate((q_weight, k_weight)):
+        if w is not None:
+            if w.dtype is not torch.float32 or w.dim() != 1 or w.numel() != D or not w.is_contiguous():
+                raise ValueError("norm weights must be head_dim contiguous float32 values")
+            weights[i] = w.data_ptr()
+            used.append(w)
+    if table is not None:
+        used += (table, positions)
+    _need_cuda(*used)
+    if out is None:
+        yq, yk = torch.empty_like(Q), torch.empty_like(K)
+    else:
+        yq, yk = _out_for(Q, out[0], "out[0]"), _out_for(K, out[1], "out[1]")
+        _need_cuda(Q, yq, yk)
+    _check((_lib or _load()).nmg_qk_norm_rotary(
+        code, heads, kv_heads, D, desc, weights[0], weights[1], eps, Q.data_ptr(), ldq, K.data_ptr(),
+        ldk, N, yq.data_ptr(), _matrix(yq, "out[0]")[2], yk.data_ptr(), _matrix(yk, "out[1]")[2],
+        _stream(Q)), "nmg_qk_norm_rotary")
     return yq, yk
 
 
 def _attend(fn, Q, K, V, heads, kv_heads, q_offsets, kv_begin, kv_end, extra, scale, out):
     code = _DTYPE_CODE.get(Q.dtype)
-    if code is None or K.dtype != Q.dtype or V.dtype != Q.dtype:
+    if code is None or K.dtype is not Q.dtype or V.dtype is not Q.dtype:
         raise TypeError("Q, K and V must be float32 or float16, of one dtype")
-    ldq, Nq, Nk = _rows(Q, "Q"), Q.shape[1], K.shape[1]
-    D = _head_rows(Q, heads, "Q")
-    if _head_rows(K, kv_heads, "K") != D or V.shape != K.shape:
+    M, Nq, ldq = _matrix(Q, "Q")
+    Mk, Nk, ldk = _matrix(K, "K")
+    Mv, Nv, ldv = _matrix(V, "V")
+    D = _head_rows(M, heads, "Q")
+    if Mk != Mv or Nk != Nv or _head_rows(Mk, kv_heads, "K") != D:
         raise ValueError("K and V must have kv_heads heads of Q's head size, and the same tokens")
-    B = kv_begin.shape[0]
-    for t, n, name in ((q_offsets, B + 1, "q_offsets"), (kv_begin, B, "kv_begin"), (kv_end, B, "kv_end")):
-        if t.dtype != torch.int32 or t.shape != (n,) or not t.is_contiguous():
-            raise ValueError(f"{name} must be {n} contiguous int32 values")
-    out = _out_like(Q, out, "out")
-    _need_cuda(Q, K, V, out, q_offsets, kv_begin, kv_end)
-    L = lib()
+    B = kv_begin.numel()
+    s = _Sequences(B, _ints(q_offsets, B + 1, "q_offsets"), _ints(kv_begin, B, "kv_begin"),
+                   _ints(kv_end, B, "kv_end"))
+    _need_cuda(Q, K, V, q_offsets, kv_begin, kv_end)
+    out = _out_for(Q, out, "out")
+    if out.get_device() != Q.get_device():
+        _need_cuda(Q, out)
+    L = _lib or _load()
     h = _Heads(heads, kv_heads, D, code)
-    s = _Sequences(B, q_offsets.data_ptr(), kv_begin.data_ptr(), kv_end.data_ptr())
     ws, wp, wb = _workspace(L.nmg_attention_workspace_bytes(h, B, Nq, Nk), Q)
-    _check(getattr(L, fn)(h, s, Q.data_ptr(), ldq, Nq, K.data_ptr(), _rows(K, "K"), V.data_ptr(),
-                          _rows(V, "V"), Nk, *extra, D ** -0.5 if scale is None else scale,
-                          out.data_ptr(), _rows(out, "out"), wp, wb, _stream(Q)), fn)
+    _check(getattr(L, fn)(h, s, Q.data_ptr(), ldq, Nq, K.data_ptr(), ldk, V.data_ptr(), ldv, Nk, *extra,
+                          D ** -0.5 if scale is None else scale, out.data_ptr(),
+                          _matrix(out, "out")[2], wp, wb, _stream(Q)), fn)
     return out
 
 

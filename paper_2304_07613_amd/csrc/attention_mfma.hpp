@@ -231,6 +231,19 @@ __device__ __forceinline__ void wait_lds() {
 #endif
 }
 
+// This wave's copies into LDS have landed and its LDS accesses are done, then the
+// workgroup barrier.  The wait is spelled out: the one the compiler puts before
+// __syncthreads() counts copies into LDS among other memory operations, and at
+// the head of a loop that count can leave copies of the loop's end in flight.
+__device__ __forceinline__ void landed_barrier() {
+#if defined(__HIP_DEVICE_COMPILE__)
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0x7 << 4);  // vmcnt(0) lgkmcnt(0)
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+#endif
+}
+
 // Rows of one matrix of keys or values on their way into LDS.  `step` waves
 // share a tile, this one takes every step-th group of 8 rows (1024 bytes).
 template <typename T, int DP, bool V, bool REGS, int STEP>
@@ -599,7 +612,7 @@ __global__ __launch_bounds__(256, DP <= (REGS ? 96 : 128) ? 2 : 1) void k_attn_s
         auto step = [&](auto more, int t, typename Rows<T, DP>::Scores &cur,
                         typename Rows<T, DP>::Scores &nxt, lds_char *k_cur, lds_char *k_nxt,
                         lds_char *v_cur, lds_char *v_nxt) {
-            __syncthreads();  // they have landed; the buffers of K of tile t, V of t - 1 are free
+            landed_barrier();  // they have landed; the buffers of K of tile t, V of t - 1 are free
             const uint64_t valid = valid_at(t, byte);
             if (more) {
                 byte = mask_at(a, (int64_t)first + (int64_t)(t + 1) * KT);
@@ -623,7 +636,7 @@ __global__ __launch_bounds__(256, DP <= (REGS ? 96 : 128) ? 2 : 1) void k_attn_s
         ks.ask(lo * KT, k0, wave);
         ks.put(k0, wave);
         byte = mask_at(a, (int64_t)first + (int64_t)lo * KT);
-        __syncthreads();
+        landed_barrier();
         if (lo + 1 < hi) ks.ask((lo + 1) * KT, k1, wave);
         vs.ask(lo * KT, v0, wave);
         w.scores(s0, k0);

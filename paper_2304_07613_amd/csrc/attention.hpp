@@ -38,6 +38,7 @@ nmg_status launch_attention(nmg_dtype dtype, const AttnArgs &a, void *workspace,
                             int64_t workspace_bytes, hipStream_t stream);
 int64_t attention_workspace_bytes(nmg_dtype dtype, const AttnArgs &a);
 
+constexpr int kAttnMostSplits = 64;   // parts of a key range
 constexpr int kAttnSharedRows = 128;  // rows of a tile whose waves share key tiles
 constexpr int kAttnSplitRows = 32;    // ... whose waves split the keys
 

@@ -77,24 +77,40 @@ struct RowTile {
     int64_t row0;     // first row
 };
 
-// 64 sequences from b0 on, one a lane: their query columns, row tiles, and the
-// tiles of those up to each
+// The sum of v over the lanes up to each, by data-parallel moves (row shifts of 1,
+// 2, 4, 8 lanes, then the last lane of a row of 16 and of 32 to those after it)
+__device__ __forceinline__ int sum_upto(int v) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);
+#endif
+    return v;
+}
+
+// 64 sequences from b0 on, one a lane: their query columns, keys, row tiles, and
+// the tiles of those up to each
 template <int TR>
 struct Sequences64 {
-    int lo, hi, tiles, upto;
+    int lo, hi, begin, end, tiles, upto;
     __device__ __forceinline__ void read(const AttnArgs &a, int b0) {
         const int lane = threadIdx.x & 63, b = b0 + lane;
-        lo = hi = 0;
+        lo = hi = begin = end = 0;
         if (b < a.sequences) {
-            lo = min(max(a.q_offsets[b], 0), a.Nq);
-            hi = min(max(a.q_offsets[b + 1], lo), a.Nq);
+            lo = a.q_offsets[b];
+            hi = a.q_offsets[b + 1];
+            begin = a.kv_begin[b];
+            end = a.kv_end[b];
         }
-        tiles = upto = (int)(((int64_t)(hi - lo) * a.share + TR - 1) / TR);
-#pragma unroll
-        for (int d = 1; d < 64; d *= 2) {
-            const int v = __shfl_up(upto, d);
-            if (lane >= d) upto += v;
-        }
+        lo = min(max(lo, 0), a.Nq);
+        hi = min(max(hi, lo), a.Nq);
+        begin = min(max(begin, 0), a.Nk);
+        end = max(min(end, a.Nk), begin);
+        tiles = (int)(((int64_t)(hi - lo) * a.share + TR - 1) / TR);
+        upto = sum_upto(tiles);
     }
     __device__ __forceinline__ int total() const { return __builtin_amdgcn_readlane(upto, 63); }
 };
@@ -136,9 +152,8 @@ __device__ __forceinline__ bool find_place(const AttnArgs &a, int id, Place &p) 
             r.q0 = __builtin_amdgcn_readlane(s.lo, w);
             r.n = __builtin_amdgcn_readlane(s.hi, w) - r.q0;
             r.row0 = (int64_t)(t - __builtin_amdgcn_readlane(s.upto - s.tiles, w)) * TR;
-            const int at = b0 + w;
-            r.begin = min(max(a.kv_begin[at], 0), a.Nk);
-            r.end = max(min(a.kv_end[at], a.Nk), r.begin);
+            r.begin = __builtin_amdgcn_readlane(s.begin, w);
+            r.end = __builtin_amdgcn_readlane(s.end, w);
             return true;
         }
         t -= s.total();
@@ -157,8 +172,18 @@ __device__ __forceinline__ RowAt row_at(const AttnArgs &a, const RowTile &r, int
     const int64_t row = r.row0 + i;
     RowAt x;
     x.valid = row >= 0 && row < (int64_t)r.n * a.share;
-    x.g = x.valid ? (int)(row / r.n) : 0;
-    x.column = r.q0 + (x.valid ? (int)(row - (int64_t)x.g * r.n) : 0);
+    x.g = 0;
+    int t = x.valid ? (int)row : 0;
+    if (a.share > 1) {  // (64-bit division is slow, and rows that need it rare)
+        if ((int64_t)r.n * a.share <= INT32_MAX) {
+            x.g = (int)((uint32_t)t / (uint32_t)r.n);
+            t -= x.g * r.n;
+        } else if (x.valid) {
+            x.g = (int)(row / r.n);
+            t = (int)(row - (int64_t)x.g * r.n);
+        }
+    }
+    x.column = r.q0 + t;
     return x;
 }
 
@@ -213,6 +238,13 @@ __device__ __forceinline__ void write16(lds_char *p, u4 v) {
     *(__attribute__((address_space(3))) u4 *)p = v;
 }
 
+template <int n>
+__device__ __forceinline__ void wave_priority() {
+#if defined(__HIP_DEVICE_COMPILE__)
+    __builtin_amdgcn_s_setprio(n);
+#endif
+}
+
 // Wait until at most n vector-memory operations of this wave are in flight
 template <int n>
 __device__ __forceinline__ void wait_vm() {
@@ -231,14 +263,15 @@ __device__ __forceinline__ void wait_lds() {
 #endif
 }
 
-// This wave's copies into LDS have landed and its LDS accesses are done, then the
-// workgroup barrier.  The wait is spelled out: the one the compiler puts before
+// All but the last n of this wave's copies into LDS have landed and its LDS
+// accesses are done, then the workgroup barrier.  The wait is spelled out: the one the compiler puts before
 // __syncthreads() counts copies into LDS among other memory operations, and at
 // the head of a loop that count can leave copies of the loop's end in flight.
+template <int n = 0>
 __device__ __forceinline__ void landed_barrier() {
 #if defined(__HIP_DEVICE_COMPILE__)
     asm volatile("" ::: "memory");
-    __builtin_amdgcn_s_waitcnt(0x7 << 4);  // vmcnt(0) lgkmcnt(0)
+    __builtin_amdgcn_s_waitcnt((n & 0xf) | (n >> 4) << 14 | 0x7 << 4);  // vmcnt(n) lgkmcnt(0)
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
 #endif
@@ -303,6 +336,8 @@ struct Stager {
                 hold[i] = v;
             }
         }
+        // waits count copies, so their order stays as written
+        asm volatile("" ::: "memory");
     }
     // REGS: what was asked for, into `lds`
     __device__ __forceinline__ void put(lds_char *lds, int wave) {
@@ -333,6 +368,13 @@ struct Rows {
     float m, l;        // running maximum (of scores times log2 e), sum of the lane's weights
     float scale2;      // scale * log2 e
 
+    __device__ __forceinline__ void clear(const AttnArgs &a) {
+#pragma unroll
+        for (int i = 0; i < DP / 32; ++i) o[i] = f16v{};
+        m = -INFINITY;
+        l = 0.f;
+        scale2 = a.scale * kLog2e;
+    }
     __device__ __forceinline__ void init(const AttnArgs &a, int kv_head, const RowAt &r) {
         const int h = (threadIdx.x & 63) >> 5;
         const T *src = (const T *)a.Q + (int64_t)(kv_head * a.share + r.g) * a.D * a.ldq + r.column;
@@ -349,11 +391,6 @@ struct Rows {
                 q[c] = at(2 * c + h);
             }
         }
-#pragma unroll
-        for (int i = 0; i < DP / 32; ++i) o[i] = f16v{};
-        m = -INFINITY;
-        l = 0.f;
-        scale2 = a.scale * kLog2e;
     }
 
     // The tile's place of register i of block kb
@@ -472,10 +509,13 @@ struct Rows {
 // Which keys of the tile at column t0 take part (bit j: column t0 + j);
 // `mask_byte`: the lane's key's
 template <typename T>
-__device__ __forceinline__ uint64_t valid_keys(int64_t t0, const RowTile &r, uint8_t mask_byte) {
-    const int lane = threadIdx.x & 63;
-    const int64_t c = t0 + lane;
-    return __ballot(lane < Elem<T>::keys && c >= r.begin && c < r.end && mask_byte);
+__device__ __forceinline__ uint64_t valid_keys(const AttnArgs &a, int64_t t0, const RowTile &r,
+                                               uint8_t mask_byte) {
+    constexpr int KT = Elem<T>::keys;
+    const int from = (int)max((int64_t)r.begin - t0, (int64_t)0);  // t0 is within KT of the range
+    const int upto = (int)min((int64_t)r.end - t0, (int64_t)KT);
+    const uint64_t in = (~0ull >> (64 - upto)) & (~0ull << from);
+    return a.key_mask ? in & __ballot(mask_byte != 0) : in;
 }
 
 // Values of keys left out become 0 in LDS, whatever they hold (their weight is 0,
@@ -589,7 +629,7 @@ __global__ __launch_bounds__(256, DP <= (REGS ? 96 : 128) ? 2 : 1) void k_attn_s
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const RowAt mine = row_at<TR>(a, r, 32 * wave + (lane & 31));
     Rows<T, DP> w;
-    w.init(a, at.head, mine);
+    w.clear(a);
 
     const int first = r.begin - r.begin % a.align;
     const int tiles = r.end > r.begin ? (r.end - first + KT - 1) / KT : 0;
@@ -606,7 +646,7 @@ __global__ __launch_bounds__(256, DP <= (REGS ? 96 : 128) ? 2 : 1) void k_attn_s
         typename Rows<T, DP>::Scores s0, s1;
         typename Rows<T, DP>::Weights p;
         auto valid_at = [&](int t, uint8_t b) {
-            return valid_keys<T>((int64_t)first + (int64_t)t * KT, r, b);
+            return valid_keys<T>(a, (int64_t)first + (int64_t)t * KT, r, b);
         };
         // K of tile t + 1 and V of tile t are under way
         auto step = [&](auto more, int t, typename Rows<T, DP>::Scores &cur,
@@ -622,10 +662,14 @@ __global__ __launch_bounds__(256, DP <= (REGS ? 96 : 128) ? 2 : 1) void k_attn_s
             if (settle(a, w, cur, r, mine, (int64_t)first + (int64_t)t * KT, valid))
                 clear_values<T, DP>(v_cur, valid);
             w.raise(cur);
+            // before the other wave of the SIMD while the matrix pipe has work for
+            // this one (4096 x 16384 at 128: 546 -> 515 us)
+            wave_priority<1>();
             if (more) w.scores(nxt, k_nxt);
             w.weigh(cur, p);
             w.values(cur, p, v_cur);
             if (more) interleave<T, DP>();
+            wave_priority<0>();
             if (REGS && more) {
                 if (t + 2 < hi) ks.put(k_cur, wave);
                 vs.put(v_nxt, wave);
@@ -633,16 +677,24 @@ __global__ __launch_bounds__(256, DP <= (REGS ? 96 : 128) ? 2 : 1) void k_attn_s
         };
         lds_char *k0 = (lds_char *)lds_k0, *k1 = (lds_char *)lds_k1;
         lds_char *v0 = (lds_char *)lds_v0, *v1 = (lds_char *)lds_v1;
+        // K of the first tile and Q on the way together, then the copies that the
+        // first step waits for
         ks.ask(lo * KT, k0, wave);
-        ks.put(k0, wave);
+        w.init(a, at.head, mine);
         byte = mask_at(a, (int64_t)first + (int64_t)lo * KT);
-        landed_barrier();
-        if (lo + 1 < hi) ks.ask((lo + 1) * KT, k1, wave);
+        ks.put(k0, wave);
         vs.ask(lo * KT, v0, wave);
+        if (!REGS && lo + 1 < hi) {
+            ks.ask((lo + 1) * KT, k1, wave);
+            landed_barrier<2 * decltype(ks)::kGroups>();
+        } else {
+            landed_barrier<REGS ? 0 : decltype(vs)::kGroups>();
+        }
         w.scores(s0, k0);
         if (REGS) {
-            if (lo + 1 < hi) ks.put(k1, wave);
             vs.put(v0, wave);
+            if (lo + 1 < hi) ks.ask((lo + 1) * KT, k1, wave);
+            if (lo + 1 < hi) ks.put(k1, wave);
         }
         constexpr std::true_type on{};
         constexpr std::false_type off{};
@@ -702,7 +754,7 @@ __global__ __launch_bounds__(64 * split_waves<DP>(), 1) void k_attn_split(AttnAr
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const RowAt mine = row_at<TR>(a, r, lane & 31);
     Rows<T, DP> w;
-    w.init(a, at.head, mine);
+    w.clear(a);
 
     const int first = r.begin - r.begin % a.align;
     const int tiles = r.end > r.begin ? (r.end - first + KT - 1) / KT : 0;
@@ -715,8 +767,9 @@ __global__ __launch_bounds__(64 * split_waves<DP>(), 1) void k_attn_split(AttnAr
         constexpr int kCopies = DP / 8;
         ks.init(a.K, a.ldk, at.head, a.D, a.Nk, first, 0);
         vs.init(a.V, a.ldv, at.head, a.D, a.Nk, first, 0);
-        uint8_t byte = mask_at(a, (int64_t)first + (int64_t)lo * KT);
         ks.ask(lo * KT, k, 0);
+        w.init(a, at.head, mine);
+        uint8_t byte = mask_at(a, (int64_t)first + (int64_t)lo * KT);
         ks.put(k, 0);
         vs.ask(lo * KT, v, 0);
         for (int t = lo; t < hi; t += W) {
@@ -733,7 +786,7 @@ __global__ __launch_bounds__(64 * split_waves<DP>(), 1) void k_attn_split(AttnAr
                 byte = mask_at(a, t0 + (int64_t)W * KT);
                 ks.ask((t + W) * KT, k, 0);
             }
-            const uint64_t valid = valid_keys<T>(t0, r, now);
+            const uint64_t valid = valid_keys<T>(a, t0, r, now);
             const bool clear = settle(a, w, x, r, mine, t0, valid);
             w.raise(x);
             w.weigh(x, p);
@@ -793,7 +846,8 @@ __global__ __launch_bounds__(64 * split_waves<DP>(), 1) void k_attn_split(AttnAr
 }
 
 // Parts of every key range, in their order, to outputs: a workgroup per (tile,
-// head, 8 rows of the head)
+// head, kJoinRows rows of the head)
+constexpr int kJoinRows = 16;
 template <typename T, int DP, int TR>
 __global__ __launch_bounds__(kBlock) void k_attn_join(AttnArgs a) {
     AttnArgs one = a;
@@ -802,26 +856,32 @@ __global__ __launch_bounds__(kBlock) void k_attn_join(AttnArgs a) {
     if (!find_place<TR>(one, blockIdx.x, at)) return;
     const RowTile &r = at.rows;
     const int tile = at.tile, head = at.head;
+    __shared__ float weights[kAttnMostSplits][TR], inverse[TR];
+    const int64_t step = (int64_t)a.kv_heads * a.tiles * ((DP + 2) * TR);
+    const float *part = part_at<DP, TR>(a, 0, head, tile);
+    if (threadIdx.x < TR) {
+        const int i = threadIdx.x;
+        float top = -INFINITY, all = 0.f;
+        for (int s = 0; s < a.splits; ++s) top = fmaxf(top, part[s * step + DP * TR + i]);
+        for (int s = 0; s < a.splits; ++s) {
+            const float m = part[s * step + DP * TR + i];
+            const float f = m == -INFINITY ? 0.f : exp2_fast(m - top);
+            weights[s][i] = f;
+            all += f * part[s * step + (DP + 1) * TR + i];
+        }
+        inverse[i] = all == 0.f ? 0.f : 1.f / all;
+    }
+    __syncthreads();
     const int i = threadIdx.x % TR;
     const RowAt mine = row_at<TR>(a, r, i);
     if (!mine.valid) return;
-    const int64_t step = (int64_t)a.kv_heads * a.tiles * ((DP + 2) * TR);
-    const float *part = part_at<DP, TR>(a, 0, head, tile) + i;
-    float top = -INFINITY, all = 0.f;
-    for (int s = 0; s < a.splits; ++s) top = fmaxf(top, part[s * step + DP * TR]);
-    auto weight = [&](int s) {
-        const float m = part[s * step + DP * TR];
-        return m == -INFINITY ? 0.f : exp2_fast(m - top);
-    };
-    for (int s = 0; s < a.splits; ++s) all += weight(s) * part[s * step + (DP + 1) * TR];
-    const float inv = all == 0.f ? 0.f : 1.f / all;
     T *out = (T *)a.O + (int64_t)(head * a.share + mine.g) * a.D * a.ldo + mine.column;
-    constexpr int kAtOnce = kBlock / TR;
-    const int d0 = blockIdx.y * 8;
-    for (int d = d0 + threadIdx.x / TR; d < d0 + 8 && d < a.D; d += kAtOnce) {
+    const int d0 = blockIdx.y * kJoinRows;
+    for (int d = d0 + threadIdx.x / TR; d < d0 + kJoinRows && d < a.D; d += kBlock / TR) {
         float x = 0.f;
-        for (int s = 0; s < a.splits; ++s) x += weight(s) * part[s * step + d * TR];
-        out[d * a.ldo] = (T)(x * inv);
+#pragma unroll 8
+        for (int s = 0; s < a.splits; ++s) x += weights[s][i] * part[s * step + d * TR + i];
+        out[d * a.ldo] = (T)(x * inverse[i]);
     }
 }
 
@@ -839,7 +899,7 @@ nmg_status launch_attn_dim(const AttnArgs &a, bool shared, bool regs, hipStream_
         hipLaunchKernelGGL((k_attn_split<T, DP, false>), grid, dim3(64 * split_waves<DP>()), 0,
                            stream, a);
     if (a.splits > 1) {
-        const dim3 join((unsigned)(a.tiles * a.kv_heads), (unsigned)((a.D + 7) / 8));
+        const dim3 join((unsigned)(a.tiles * a.kv_heads), (unsigned)((a.D + kJoinRows - 1) / kJoinRows));
         if (shared)
             hipLaunchKernelGGL((k_attn_join<T, DP, kAttnSharedRows>), join, dim3(kBlock), 0,
                                stream, a);

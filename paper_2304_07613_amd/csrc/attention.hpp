@@ -29,10 +29,13 @@ struct AttnArgs {
     float *part;                     // splits > 1: sums, maxima and totals of every part
 };
 
-// Workgroups that share key tiles (128 rows) or split them (32 rows); `regs`:
-// key tiles staged through registers
-nmg_status launch_attention_f16(const AttnArgs &a, bool shared, bool regs, hipStream_t stream);
-nmg_status launch_attention_f32(const AttnArgs &a, bool shared, bool regs, hipStream_t stream);
+// How rows of K and V are read: one buffer a head; 64-bit addresses, for heads that
+// span 2^31 bytes or more; the same for binary16 rows that do not all start on 4 bytes
+enum AttnRows { kAttnNarrow, kAttnWide, kAttnShift };
+
+// Workgroups that share key tiles (128 rows) or split them (32 rows)
+nmg_status launch_attention_f16(const AttnArgs &a, bool shared, AttnRows how, hipStream_t stream);
+nmg_status launch_attention_f32(const AttnArgs &a, bool shared, AttnRows how, hipStream_t stream);
 
 nmg_status launch_attention(nmg_dtype dtype, const AttnArgs &a, void *workspace,
                             int64_t workspace_bytes, hipStream_t stream);

@@ -24,7 +24,8 @@
 // (chunk ^ swizzle(row)) so that the reads of both operands touch every bank
 // once: V's reads take one chunk of 16 consecutive rows, K's (binary16) four
 // chunks of 4 rows.  Tiles come with buffer loads that write LDS, which take
-// any address that is a multiple of 4 bytes; others are staged through registers.
+// any address that is a multiple of 4 bytes; binary16 rows that start between go
+// through registers.
 //
 // Two kernels:
 //   k_attn_shared  4 waves of 32 rows share key tiles: two LDS buffers, one
@@ -187,6 +188,15 @@ __device__ __forceinline__ RowAt row_at(const AttnArgs &a, const RowTile &r, int
     return x;
 }
 
+// v, for code that few tiles run: what is computed from it is computed there, not
+// kept in registers over the whole loop
+__device__ __forceinline__ int rarely(int v) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    asm volatile("" : "+v"(v));
+#endif
+    return v;
+}
+
 // Over a row's two lanes, lane and lane ^ 32
 __device__ __forceinline__ float larger_of_halves(float v) {
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -245,6 +255,22 @@ __device__ __forceinline__ void wave_priority() {
 #endif
 }
 
+// 16 or 4 bytes at byte offset `off` (a multiple of 4) of a buffer, 0 past its end
+__device__ __forceinline__ u4 load16_buf(buf_rsrc_t r, uint32_t off) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    return __builtin_bit_cast(u4, __builtin_amdgcn_raw_buffer_load_b128(r, (int)off, 0, 0));
+#else
+    return u4{};
+#endif
+}
+__device__ __forceinline__ uint32_t load4_buf(buf_rsrc_t r, uint32_t off) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    return __builtin_amdgcn_raw_buffer_load_b32(r, (int)off, 0, 0);
+#else
+    return 0;
+#endif
+}
+
 // Wait until at most n vector-memory operations of this wave are in flight
 template <int n>
 __device__ __forceinline__ void wait_vm() {
@@ -277,93 +303,122 @@ __device__ __forceinline__ void landed_barrier() {
 #endif
 }
 
-// Rows of one matrix of keys or values on their way into LDS.  `step` waves
-// share a tile, this one takes every step-th group of 8 rows (1024 bytes).
-template <typename T, int DP, bool V, bool REGS, int STEP>
-struct Stager {
-    static constexpr int kGroups = DP / 8 / STEP;
-    const T *base;    // column `first` of the head's first row
-    int64_t ld;
-    int D, cols;      // rows of the head, columns from `first` on
-    buf_rsrc_t rsrc;
-    uint32_t off[REGS || STEP % 2 == 0 ? 1 : 2];  // of the lane's chunk in the wave's even and odd
-                                                  // groups (groups of one parity: one)
-    u4 hold[REGS ? kGroups : 1];
-
-    __device__ __forceinline__ void init(const void *matrix, int64_t ld_, int head, int D_, int Nk,
-                                         int first, int wave) {
-        ld = ld_;
-        D = D_;
-        cols = Nk - first;
-        base = (const T *)matrix + (int64_t)head * D * ld + first;
-        if constexpr (!REGS) {
-            const uint32_t bytes = (uint32_t)(((int64_t)(D - 1) * ld + cols) * sizeof(T));
-            rsrc = buf_rsrc(base, (bytes + 3) & ~3u);
-            const int lane = threadIdx.x & 63, row = lane >> 3;
-#pragma unroll
-            for (int i = 0; i < (STEP % 2 ? 2 : 1); ++i)
-                off[i] = (uint32_t)(row * ld * sizeof(T)) +
-                         16 * ((lane & 7) ^ chunk_swizzle<T, V>(8 * (STEP * i + wave) + row));
-        }
+// One head of K or V from column `first` on, read through buffers: what lies past
+// its last row or element is read as 0.  (A word that holds any byte of the head
+// counts as inside.)  A head that spans less than 2^31 bytes is one buffer; WIDE:
+// every 8 rows of a tile are (64-bit addresses, 32-bit offsets among the 8 rows).
+template <bool WIDE>
+struct HeadRows {
+    const char *base;       // on 4 bytes
+    int64_t end, ld;        // bytes to the end of the last row, and from row to row
+    buf_rsrc_t whole;
+    __device__ __forceinline__ int init(const AttnArgs &a, const void *matrix, int64_t ld_,
+                                        int head, int first, int es) {
+        ld = ld_ * es;
+        base = (const char *)matrix + head * (int64_t)a.D * ld + (int64_t)first * es;
+        const int odd = (int)((uintptr_t)base & 3);  // bytes past a multiple of 4
+        base -= odd;
+        end = (a.D - 1) * ld + (int64_t)(a.Nk - first) * es + odd;
+        whole = part(0);
+        return odd;
     }
-
-    // Ask for the tile that starts `at` columns behind `first`; !REGS: into `lds`
-    __device__ __forceinline__ void ask(int at, lds_char *lds, int wave) {
-#pragma unroll
-        for (int i = 0; i < kGroups; ++i) {
-            const int group = STEP * i + wave;
-            if constexpr (!REGS) {
-                // one scalar for the group and tile (kept from becoming an offset register
-                // for every group)
-                const uint32_t u = __builtin_amdgcn_readfirstlane(
-                    (uint32_t)(8 * group * ld * sizeof(T)) + (uint32_t)at * (uint32_t)sizeof(T));
-                lds_copy16_buf(rsrc, off[STEP % 2 ? i & 1 : 0] + u, (void *)(lds + 1024 * group));
-            } else {
-                constexpr int E = Elem<T>::per_chunk;
-                const int lane = threadIdx.x & 63, row = 8 * group + (lane >> 3);
-                const int c = at + E * ((lane & 7) ^ chunk_swizzle<T, V>(row));
-                u4 v = {0, 0, 0, 0};
-                if (row < D) {
-                    const T *p = base + row * ld + c;
-                    if (c + E <= cols) {
-                        __builtin_memcpy(&v, p, 16);
-                    } else {
-                        T e[E];
-                        for (int k = 0; k < E; ++k) e[k] = c + k < cols ? p[k] : (T)0;
-                        __builtin_memcpy(&v, e, 16);
-                    }
-                }
-                hold[i] = v;
-            }
-        }
-        // waits count copies, so their order stays as written
-        asm volatile("" ::: "memory");
+    // from byte `from` on
+    __device__ __forceinline__ buf_rsrc_t part(int64_t from) const {
+        const int64_t left = min(max(end - from, (int64_t)0), (int64_t)0x7ffffff0);
+        return buf_rsrc(base + from, ((uint32_t)left + 3) & ~3u);
     }
-    // REGS: what was asked for, into `lds`
-    __device__ __forceinline__ void put(lds_char *lds, int wave) {
-        if constexpr (REGS) {
-            const int lane = threadIdx.x & 63;
+    // f(i, buffer, offset of its first row, bytes) for a wave's groups of 8 rows of
+    // the tile at byte `at`: the first is `wave`, then every STEP-th
+    template <int N, int STEP, typename F>
+    __device__ __forceinline__ void groups(int64_t at, int wave, F f) const {
+        if constexpr (!WIDE) {
 #pragma unroll
-            for (int i = 0; i < kGroups; ++i)
-                write16(lds + 1024 * (STEP * i + wave) + 16 * lane, hold[i]);
+            for (int i = 0; i < N; ++i)
+                // one scalar for the group and tile, not an offset register for every group
+                f(i, whole, __builtin_amdgcn_readfirstlane(
+                                (uint32_t)(8 * (STEP * i + wave)) * (uint32_t)ld + (uint32_t)at));
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i) f(i, part(8 * (STEP * i + wave) * ld + at), 0u);
         }
     }
 };
 
-// 32 rows of a tile in one wave
-template <typename T, int DP>
-struct Rows {
-    static constexpr int KT = Elem<T>::keys, KB = KT / 32;
-    static constexpr int QF = sizeof(T) == 2 ? DP / 16 : DP / 2;
-    typedef typename std::conditional<sizeof(T) == 2, h8, float>::type QFrag;
-    // One tile's scores, then its weights (binary32: the scores' registers)
+// Rows of one matrix of keys or values on their way into LDS.  STEP waves share
+// a tile, this one takes every STEP-th group of 8 rows (1024 bytes).  HOW: see
+// AttnRows; kAttnShift: words into registers, shifted
+// by an element where the row's start is odd, and from there into LDS.
+template <typename T, int DP, bool V, AttnRows HOW, int STEP>
+struct Stager {
+    static constexpr bool SHIFT = HOW == kAttnShift;
+    static constexpr int kGroups = DP / 8 / STEP;
+    // SHIFT: with few enough words to hold, a tile waits in registers from ask to
+    // put; else ask takes it into LDS, 4 groups at a time
+    static constexpr bool kHolds = SHIFT && DP <= 128;
+    HeadRows<HOW != kAttnNarrow> rows;
+    uint32_t off[STEP % 2 ? 2 : 1];  // of the lane's chunk in the wave's even and odd groups
+                                     // (groups of one parity: one)
+    uint32_t shift;                  // bits
+    u4 hold[kHolds ? kGroups : 4];
+    uint32_t next[kHolds ? kGroups : 4];
+
+    __device__ __forceinline__ void init(const AttnArgs &a, const void *matrix, int64_t ld,
+                                         int head, int first, int wave) {
+        const int odd = rows.init(a, matrix, ld, head, first, sizeof(T));
+        const int lane = threadIdx.x & 63, row = lane >> 3;
+        const uint32_t at = (uint32_t)(row * rows.ld) + odd;
+        shift = SHIFT ? (at & 2) * 8 : 0;
+#pragma unroll
+        for (int i = 0; i < (STEP % 2 ? 2 : 1); ++i)
+            off[i] = (at & ~3u) + 16 * ((lane & 7) ^ chunk_swizzle<T, V>(8 * (STEP * i + wave) + row));
+    }
+
+    // Ask for the tile that starts `at` columns behind `first`; !kHolds: into `lds`
+    __device__ __forceinline__ void ask(int at, lds_char *lds, int wave) {
+        rows.template groups<kGroups, STEP>(
+            (int64_t)at * (int64_t)sizeof(T), wave, [&](int i, buf_rsrc_t r, uint32_t row) {
+                const uint32_t o = off[STEP % 2 ? i & 1 : 0] + row;
+                if constexpr (!SHIFT) {
+                    lds_copy16_buf(r, o, (void *)(lds + 1024 * (STEP * i + wave)));
+                } else {
+                    const int j = kHolds ? i : i % 4;
+                    hold[j] = load16_buf(r, o);
+                    next[j] = load4_buf(r, o + 16);
+                    if (!kHolds && j == 3) {
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) put_group(lds, i - 3 + k, k, wave);
+                        asm volatile("" ::: "memory");
+                    }
+                }
+            });
+        // waits count copies, so their order stays as written
+        asm volatile("" ::: "memory");
+    }
+    __device__ __forceinline__ void put_group(lds_char *lds, int i, int j, int wave) {
+        const int lane = threadIdx.x & 63;
+        const u4 x = hold[j];
+        const u4 y = {__builtin_amdgcn_alignbit(x[1], x[0], shift),
+                      __builtin_amdgcn_alignbit(x[2], x[1], shift),
+                      __builtin_amdgcn_alignbit(x[3], x[2], shift),
+                      __builtin_amdgcn_alignbit(next[j], x[3], shift)};
+        write16(lds + 1024 * (STEP * i + wave) + 16 * lane, y);
+    }
+    // kHolds: what was asked for, into `lds`
+    __device__ __forceinline__ void put(lds_char *lds, int wave) {
+        if constexpr (kHolds) {
+#pragma unroll
+            for (int i = 0; i < kGroups; ++i) put_group(lds, i, i, wave);
+        }
+    }
+};
+
+// The running sums of 32 rows in one wave, and one tile's scores: KB blocks of 32
+// keys.  WIDE: the places of keys that contraction steps of 16 want.
+template <int DP, int KB, bool WIDE>
+struct RowSums {
     struct Scores {
         f16v s[KB];
     };
-    struct Weights {
-        h8 p[KT / 16];
-    };
-    QFrag q[QF];
     f16v o[DP / 32];
     float m, l;        // running maximum (of scores times log2 e), sum of the lane's weights
     float scale2;      // scale * log2 e
@@ -375,6 +430,66 @@ struct Rows {
         l = 0.f;
         scale2 = a.scale * kLog2e;
     }
+
+    // The tile's place of register i of block kb
+    static __device__ __forceinline__ int key_of(int kb, int i, int h) {
+        return WIDE ? 32 * kb + 16 * (i >> 3) + 8 * h + (i & 7) : 8 * (i >> 2) + 4 * h + (i & 3);
+    }
+
+    // Leave keys out: bit j of `valid` (the lane's own) is key j of the tile
+    __device__ __forceinline__ void mask(Scores &x, uint64_t valid) const {
+        const int h = (threadIdx.x & 63) >> 5;
+        const uint64_t mine = valid >> (WIDE ? 8 * h : 4 * h);
+#pragma unroll
+        for (int b = 0; b < KB; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                x.s[b][i] = (mine >> key_of(b, i, 0)) & 1 ? x.s[b][i] : -INFINITY;
+    }
+
+    // The running maximum moves when a row's grew by more than `slack` powers of 2
+    __device__ __forceinline__ void raise(const Scores &x, float slack) {
+        float top = x.s[0][0];
+#pragma unroll
+        for (int b = 0; b < KB; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) top = fmaxf(top, x.s[b][i]);
+        top = larger_of_halves(top) * scale2;
+        if (__any(top - m > slack)) {  // (nothing seen yet: m is -inf)
+            const float next = fmaxf(m, top);
+            const float keep = m == next ? 1.f : exp2_fast(m - next);
+            l *= keep;
+#pragma unroll
+            for (int i = 0; i < DP / 32; ++i) o[i] *= keep;
+            m = next;
+        }
+    }
+
+    // exp2(score - m + lift); 0 for a row that has seen nothing
+    __device__ __forceinline__ void exponentials(Scores &x, float lift) const {
+        const float base = m == -INFINITY ? 0.f : m - lift;
+#pragma unroll
+        for (int b = 0; b < KB; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x.s[b][i] = exp2_fast(fmaf(x.s[b][i], scale2, -base));
+    }
+};
+
+// 32 rows of a tile in one wave
+template <typename T, int DP>
+struct Rows : RowSums<DP, Elem<T>::keys / 32, sizeof(T) == 2> {
+    static constexpr int KT = Elem<T>::keys, KB = KT / 32;
+    static constexpr int QF = sizeof(T) == 2 ? DP / 16 : DP / 2;
+    typedef typename std::conditional<sizeof(T) == 2, h8, float>::type QFrag;
+    typedef RowSums<DP, KB, sizeof(T) == 2> Sums;
+    using Sums::l;
+    using Sums::o;
+    using typename Sums::Scores;
+    struct Weights {
+        h8 p[KT / 16];
+    };
+    QFrag q[QF];
+
     __device__ __forceinline__ void init(const AttnArgs &a, int kv_head, const RowAt &r) {
         const int h = (threadIdx.x & 63) >> 5;
         const T *src = (const T *)a.Q + (int64_t)(kv_head * a.share + r.g) * a.D * a.ldq + r.column;
@@ -391,12 +506,6 @@ struct Rows {
                 q[c] = at(2 * c + h);
             }
         }
-    }
-
-    // The tile's place of register i of block kb
-    static __device__ __forceinline__ int key_of(int kb, int i, int h) {
-        return sizeof(T) == 2 ? 32 * kb + 16 * (i >> 3) + 8 * h + (i & 7)
-                              : 8 * (i >> 2) + 4 * h + (i & 3);
     }
 
     // S^T of the tile at k
@@ -426,42 +535,9 @@ struct Rows {
         }
     }
 
-    // Leave keys out: bit j of `valid` (the lane's own) is key j of the tile
-    __device__ __forceinline__ void mask(Scores &x, uint64_t valid) const {
-        const int h = (threadIdx.x & 63) >> 5;
-        const uint64_t mine = valid >> (sizeof(T) == 2 ? 8 * h : 4 * h);
-#pragma unroll
-        for (int b = 0; b < KB; ++b)
-#pragma unroll
-            for (int i = 0; i < 16; ++i)
-                x.s[b][i] = (mine >> key_of(b, i, 0)) & 1 ? x.s[b][i] : -INFINITY;
-    }
-
-    // The running maximum moves when a row's grew by more than Elem::slack powers of 2
-    __device__ __forceinline__ void raise(const Scores &x) {
-        float top = x.s[0][0];
-#pragma unroll
-        for (int b = 0; b < KB; ++b)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) top = fmaxf(top, x.s[b][i]);
-        top = larger_of_halves(top) * scale2;
-        if (__any(top - m > Elem<T>::slack)) {  // (nothing seen yet: m is -inf)
-            const float next = fmaxf(m, top);
-            const float keep = m == next ? 1.f : exp2_fast(m - next);
-            l *= keep;
-#pragma unroll
-            for (int i = 0; i < DP / 32; ++i) o[i] *= keep;
-            m = next;
-        }
-    }
-
     // Scores to weights, and their sum
     __device__ __forceinline__ void weigh(Scores &x, Weights &w) {
-        const float base = m == -INFINITY ? 0.f : m - Elem<T>::lift;
-#pragma unroll
-        for (int b = 0; b < KB; ++b)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) x.s[b][i] = exp2_fast(fmaf(x.s[b][i], scale2, -base));
+        this->exponentials(x, Elem<T>::lift);
         if constexpr (sizeof(T) == 2) {
 #pragma unroll
             for (int c = 0; c < KT / 16; ++c) {
@@ -523,7 +599,7 @@ __device__ __forceinline__ uint64_t valid_keys(const AttnArgs &a, int64_t t0, co
 // write the same bytes.
 template <typename T, int DP>
 __device__ __forceinline__ void clear_values(lds_char *v, uint64_t valid) {
-    const int lane = threadIdx.x & 63;
+    const int lane = rarely(threadIdx.x & 63);
     for (int i = 0; i < DP / 8; ++i) {
         const int row = 8 * i + (lane >> 3);
         const int key = Elem<T>::per_chunk * ((lane & 7) ^ chunk_swizzle<T, true>(row));
@@ -547,25 +623,31 @@ __device__ __forceinline__ void clear_values(lds_char *v, uint64_t valid) {
 // every row's line of the tree, a ballot makes the row's bits.
 template <typename T>
 __device__ __forceinline__ uint64_t seen_keys(const AttnArgs &a, int column, int drafted) {
-    const int lane = threadIdx.x & 63, at = lane - drafted;
+    const int lane = rarely(threadIdx.x & 63), at = lane - drafted;
     const int from = min(max(at, 0), a.width - 1);
     uint64_t mine = 0;
-#pragma unroll 8
-    for (int i = 0; i < 32; ++i) {
-        const int64_t c = __builtin_amdgcn_readlane(column, i);
-        const int seen = a.tree[c * a.ldtree + from] | (at < 0 ? 1 : 0);
-        const uint64_t bits = __ballot((seen != 0) & (at < a.width));
-        if ((lane & 31) == i) mine = bits;
+    for (int i0 = 0; i0 < 32; i0 += 16) {
+        int seen[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int64_t c = __builtin_amdgcn_readlane(column, i0 + i);
+            seen[i] = a.tree[c * a.ldtree + from] | (at < 0 ? 1 : 0);
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const uint64_t bits = __ballot((seen[i] != 0) & (at < a.width));
+            if ((lane & 31) == i0 + i) mine = bits;
+        }
     }
     return mine;
 }
 
 // Scores of keys that take no part in a tile at t0 become -inf; true when there
 // are keys whose values have to be cleared
-template <typename T, int DP>
-__device__ __forceinline__ bool settle(const AttnArgs &a, const Rows<T, DP> &w,
-                                       typename Rows<T, DP>::Scores &x, const RowTile &r,
-                                       const RowAt &mine, int64_t t0, uint64_t valid) {
+template <typename T, typename W>
+__device__ __forceinline__ bool settle(const AttnArgs &a, const W &w, typename W::Scores &x,
+                                       const RowTile &r, const RowAt &mine, int64_t t0,
+                                       uint64_t valid) {
     constexpr int KT = Elem<T>::keys;
     const bool full = valid == (KT == 64 ? ~0ull : 0xffffffffull);
     const bool tree = a.tree && t0 + KT > (int64_t)r.end - r.n;
@@ -583,30 +665,6 @@ __device__ __forceinline__ uint8_t mask_at(const AttnArgs &a, int64_t t0) {
     return c < a.Nk ? a.key_mask[c] : 0;
 }
 
-// The order of a step's instructions: the next scores' matrix instructions
-// between the weights' vector instructions, LDS reads ahead of their use, then
-// the product with V
-template <typename T, int DP>
-__device__ __forceinline__ void interleave() {
-#if defined(__HIP_DEVICE_COMPILE__)
-    if constexpr (sizeof(T) == 2) {
-        constexpr int kScores = DP / 16 * 2, kValues = DP / 32 * 4, kVector = 96 / kScores;
-        __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);
-#pragma unroll
-        for (int i = 0; i < kScores; ++i) {
-            __builtin_amdgcn_sched_group_barrier(0x002, kVector, 0);
-            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-            __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
-        }
-#pragma unroll
-        for (int i = 0; i < kValues; ++i) {
-            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-        }
-    }
-#endif
-}
-
 // Parts in the workspace: sums (padded D x rows), then maxima and totals, of every
 // (part, head, tile)
 template <int DP, int TR>
@@ -614,103 +672,12 @@ __device__ __forceinline__ float *part_at(const AttnArgs &a, int part, int head,
     return a.part + ((int64_t)(part * a.kv_heads + head) * a.tiles + tile) * ((DP + 2) * TR);
 }
 
-template <typename T, int DP, bool REGS>
-__global__ __launch_bounds__(256, DP <= (REGS ? 96 : 128) ? 2 : 1) void k_attn_shared(AttnArgs a) {
-    constexpr int TR = kAttnSharedRows, KT = Elem<T>::keys, kTile = DP * kRowBytes;
-    // variables of their own: the compiler sees that reads of one do not touch
-    // copies into another still in flight
-    __shared__ __attribute__((aligned(1024))) char lds_k0[kTile];
-    __shared__ __attribute__((aligned(1024))) char lds_k1[kTile];
-    __shared__ __attribute__((aligned(1024))) char lds_v0[kTile];
-    __shared__ __attribute__((aligned(1024))) char lds_v1[kTile];
-    Place at;
-    if (!find_place<TR>(a, blockIdx.x, at)) return;
-    const RowTile &r = at.rows;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-    const RowAt mine = row_at<TR>(a, r, 32 * wave + (lane & 31));
-    Rows<T, DP> w;
-    w.clear(a);
-
-    const int first = r.begin - r.begin % a.align;
-    const int tiles = r.end > r.begin ? (r.end - first + KT - 1) / KT : 0;
-    const int lo = (int)((int64_t)tiles * at.part / a.splits);
-    const int hi = (int)((int64_t)tiles * (at.part + 1) / a.splits);
-    if (lo < hi) {
-        Stager<T, DP, false, REGS, 4> ks;
-        Stager<T, DP, true, REGS, 4> vs;
-        ks.init(a.K, a.ldk, at.head, a.D, a.Nk, first, wave);
-        vs.init(a.V, a.ldv, at.head, a.D, a.Nk, first, wave);
-        uint8_t byte;
-        // The scores of tile t + 1 are taken while tile t's become weights: matrix
-        // and vector instructions of one wave side by side.
-        typename Rows<T, DP>::Scores s0, s1;
-        typename Rows<T, DP>::Weights p;
-        auto valid_at = [&](int t, uint8_t b) {
-            return valid_keys<T>(a, (int64_t)first + (int64_t)t * KT, r, b);
-        };
-        // K of tile t + 1 and V of tile t are under way
-        auto step = [&](auto more, int t, typename Rows<T, DP>::Scores &cur,
-                        typename Rows<T, DP>::Scores &nxt, lds_char *k_cur, lds_char *k_nxt,
-                        lds_char *v_cur, lds_char *v_nxt) {
-            landed_barrier();  // they have landed; the buffers of K of tile t, V of t - 1 are free
-            const uint64_t valid = valid_at(t, byte);
-            if (more) {
-                byte = mask_at(a, (int64_t)first + (int64_t)(t + 1) * KT);
-                if (t + 2 < hi) ks.ask((t + 2) * KT, k_cur, wave);
-                vs.ask((t + 1) * KT, v_nxt, wave);
-            }
-            if (settle(a, w, cur, r, mine, (int64_t)first + (int64_t)t * KT, valid))
-                clear_values<T, DP>(v_cur, valid);
-            w.raise(cur);
-            // before the other wave of the SIMD while the matrix pipe has work for
-            // this one (4096 x 16384 at 128: 546 -> 515 us)
-            wave_priority<1>();
-            if (more) w.scores(nxt, k_nxt);
-            w.weigh(cur, p);
-            w.values(cur, p, v_cur);
-            if (more) interleave<T, DP>();
-            wave_priority<0>();
-            if (REGS && more) {
-                if (t + 2 < hi) ks.put(k_cur, wave);
-                vs.put(v_nxt, wave);
-            }
-        };
-        lds_char *k0 = (lds_char *)lds_k0, *k1 = (lds_char *)lds_k1;
-        lds_char *v0 = (lds_char *)lds_v0, *v1 = (lds_char *)lds_v1;
-        // K of the first tile and Q on the way together, then the copies that the
-        // first step waits for
-        ks.ask(lo * KT, k0, wave);
-        w.init(a, at.head, mine);
-        byte = mask_at(a, (int64_t)first + (int64_t)lo * KT);
-        ks.put(k0, wave);
-        vs.ask(lo * KT, v0, wave);
-        if (!REGS && lo + 1 < hi) {
-            ks.ask((lo + 1) * KT, k1, wave);
-            landed_barrier<2 * decltype(ks)::kGroups>();
-        } else {
-            landed_barrier<REGS ? 0 : decltype(vs)::kGroups>();
-        }
-        w.scores(s0, k0);
-        if (REGS) {
-            vs.put(v0, wave);
-            if (lo + 1 < hi) ks.ask((lo + 1) * KT, k1, wave);
-            if (lo + 1 < hi) ks.put(k1, wave);
-        }
-        constexpr std::true_type on{};
-        constexpr std::false_type off{};
-        int t = lo;
-        for (; t + 2 < hi; t += 2) {
-            step(on, t, s0, s1, k0, k1, v0, v1);
-            step(on, t + 1, s1, s0, k1, k0, v1, v0);
-        }
-        if (t + 1 < hi) {
-            step(on, t, s0, s1, k0, k1, v0, v1);
-            step(off, t + 1, s1, s0, k1, k0, v1, v0);
-        } else {
-            step(off, t, s0, s1, k0, k1, v0, v1);
-        }
-    }
-
+// The end of a wave of 32 rows: its outputs, or its part of them
+template <typename T, int DP, typename W>
+__device__ __forceinline__ void finish(const AttnArgs &a, const Place &at, const RowAt &mine,
+                                       const W &w, int wave) {
+    constexpr int TR = kAttnSharedRows;
+    const int lane = threadIdx.x & 63;
     const int h = lane >> 5;
     const float total = sum_of_halves(w.l);
     if (a.splits > 1) {
@@ -738,12 +705,114 @@ __global__ __launch_bounds__(256, DP <= (REGS ? 96 : 128) ? 2 : 1) void k_attn_s
         }
 }
 
+template <typename T, int DP, AttnRows HOW>
+__global__ __launch_bounds__(256, DP <= (HOW == kAttnShift ? 96 : 128) ? 2 : 1) void k_attn_shared(AttnArgs a) {
+    constexpr int TR = kAttnSharedRows, KT = Elem<T>::keys, kTile = DP * kRowBytes;
+    constexpr bool SHIFT = HOW == kAttnShift;
+    // variables of their own: the compiler sees that reads of one do not touch
+    // copies into another still in flight
+    __shared__ __attribute__((aligned(1024))) char lds_k0[kTile];
+    __shared__ __attribute__((aligned(1024))) char lds_k1[kTile];
+    __shared__ __attribute__((aligned(1024))) char lds_v0[kTile];
+    __shared__ __attribute__((aligned(1024))) char lds_v1[kTile];
+    Place at;
+    if (!find_place<TR>(a, blockIdx.x, at)) return;
+    const RowTile &r = at.rows;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const RowAt mine = row_at<TR>(a, r, 32 * wave + (lane & 31));
+    Rows<T, DP> w;
+    w.clear(a);
+
+    const int first = r.begin - r.begin % a.align;
+    const int tiles = r.end > r.begin ? (r.end - first + KT - 1) / KT : 0;
+    const int lo = (int)((int64_t)tiles * at.part / a.splits);
+    const int hi = (int)((int64_t)tiles * (at.part + 1) / a.splits);
+    if (lo < hi) {
+        Stager<T, DP, false, HOW, 4> ks;
+        Stager<T, DP, true, HOW, 4> vs;
+        ks.init(a, a.K, a.ldk, at.head, first, wave);
+        vs.init(a, a.V, a.ldv, at.head, first, wave);
+        uint8_t byte;
+        // The scores of tile t + 1 are taken while tile t's become weights: matrix
+        // and vector instructions of one wave side by side.
+        typename Rows<T, DP>::Scores s0, s1;
+        typename Rows<T, DP>::Weights p;
+        auto valid_at = [&](int t, uint8_t b) {
+            return valid_keys<T>(a, (int64_t)first + (int64_t)t * KT, r, b);
+        };
+        // K of tile t + 1 and V of tile t are under way
+        auto step = [&](auto more, int t, typename Rows<T, DP>::Scores &cur,
+                        typename Rows<T, DP>::Scores &nxt, lds_char *k_cur, lds_char *k_nxt,
+                        lds_char *v_cur, lds_char *v_nxt) {
+            landed_barrier();  // they have landed; the buffers of K of tile t, V of t - 1 are free
+            const uint64_t valid = valid_at(t, byte);
+            if (more) {
+                byte = mask_at(a, (int64_t)first + (int64_t)(t + 1) * KT);
+                if (t + 2 < hi) ks.ask((t + 2) * KT, k_cur, wave);
+                vs.ask((t + 1) * KT, v_nxt, wave);
+            }
+            if (settle<T>(a, w, cur, r, mine, (int64_t)first + (int64_t)t * KT, valid))
+                clear_values<T, DP>(v_cur, valid);
+            w.raise(cur, Elem<T>::slack);
+            // before the other wave of the SIMD while the matrix pipe has work for
+            // this one (4096 x 16384 at 128: 546 -> 515 us)
+            wave_priority<1>();
+            if (more) w.scores(nxt, k_nxt);
+            w.weigh(cur, p);
+            w.values(cur, p, v_cur);
+            wave_priority<0>();
+            if (SHIFT && more) {
+                if (t + 2 < hi) ks.put(k_cur, wave);
+                vs.put(v_nxt, wave);
+            }
+        };
+        lds_char *k0 = (lds_char *)lds_k0, *k1 = (lds_char *)lds_k1;
+        lds_char *v0 = (lds_char *)lds_v0, *v1 = (lds_char *)lds_v1;
+        // K of the first tile and Q on the way together, then the copies that the
+        // first step waits for
+        ks.ask(lo * KT, k0, wave);
+        w.init(a, at.head, mine);
+        byte = mask_at(a, (int64_t)first + (int64_t)lo * KT);
+        ks.put(k0, wave);
+        vs.ask(lo * KT, v0, wave);
+        if (!SHIFT && lo + 1 < hi) {
+            ks.ask((lo + 1) * KT, k1, wave);
+            landed_barrier<2 * decltype(ks)::kGroups>();
+        } else {
+            landed_barrier<SHIFT ? 0 : decltype(vs)::kGroups>();
+        }
+        w.scores(s0, k0);
+        if (SHIFT) {
+            vs.put(v0, wave);
+            if (lo + 1 < hi) ks.ask((lo + 1) * KT, k1, wave);
+            if (lo + 1 < hi) ks.put(k1, wave);
+        }
+        constexpr std::true_type on{};
+        constexpr std::false_type off{};
+        int t = lo;
+        lds_char *last = v0;
+        while (t + 1 < hi) {
+            step(on, t++, s0, s1, k0, k1, v0, v1);
+            if (t + 1 == hi) {
+                s0 = s1;
+                last = v1;
+                break;
+            }
+            step(on, t++, s1, s0, k1, k0, v1, v0);
+        }
+        step(off, t, s0, s1, k0, k1, last, v0);
+    }
+
+    finish<T, DP>(a, at, mine, w, wave);
+}
+
 // Waves of a workgroup that splits the keys: as many as 128 KB hold tiles of
 template <int DP> constexpr int split_waves() { return DP <= 64 ? 8 : DP <= 128 ? 4 : 2; }
 
-template <typename T, int DP, bool REGS>
+template <typename T, int DP, AttnRows HOW>
 __global__ __launch_bounds__(64 * split_waves<DP>(), 1) void k_attn_split(AttnArgs a) {
     constexpr int TR = kAttnSplitRows, KT = Elem<T>::keys, kTile = DP * kRowBytes;
+    constexpr bool SHIFT = HOW == kAttnShift;
     constexpr int W = split_waves<DP>();
     __shared__ __attribute__((aligned(1024))) char lds_k[W * kTile];
     __shared__ __attribute__((aligned(1024))) char lds_v[W * kTile];
@@ -762,11 +831,11 @@ __global__ __launch_bounds__(64 * split_waves<DP>(), 1) void k_attn_split(AttnAr
     const int hi = (int)((int64_t)tiles * (at.part + 1) / a.splits);
     lds_char *k = (lds_char *)lds_k + wave * kTile, *v = (lds_char *)lds_v + wave * kTile;
     if (lo < hi) {
-        Stager<T, DP, false, REGS, 1> ks;
-        Stager<T, DP, true, REGS, 1> vs;
+        Stager<T, DP, false, HOW, 1> ks;
+        Stager<T, DP, true, HOW, 1> vs;
         constexpr int kCopies = DP / 8;
-        ks.init(a.K, a.ldk, at.head, a.D, a.Nk, first, 0);
-        vs.init(a.V, a.ldv, at.head, a.D, a.Nk, first, 0);
+        ks.init(a, a.K, a.ldk, at.head, first, 0);
+        vs.init(a, a.V, a.ldv, at.head, first, 0);
         ks.ask(lo * KT, k, 0);
         w.init(a, at.head, mine);
         uint8_t byte = mask_at(a, (int64_t)first + (int64_t)lo * KT);
@@ -776,7 +845,7 @@ __global__ __launch_bounds__(64 * split_waves<DP>(), 1) void k_attn_split(AttnAr
             const int64_t t0 = (int64_t)first + (int64_t)t * KT;
             const bool more = t + W < hi;
             const uint8_t now = byte;
-            if (!REGS) wait_vm<kCopies>();  // K has landed; V may still be in flight
+            if (!SHIFT) wait_vm<kCopies>();  // K has landed; V may still be in flight
             typename Rows<T, DP>::Scores x;
             typename Rows<T, DP>::Weights p;
             w.scores(x, k);
@@ -787,10 +856,10 @@ __global__ __launch_bounds__(64 * split_waves<DP>(), 1) void k_attn_split(AttnAr
                 ks.ask((t + W) * KT, k, 0);
             }
             const uint64_t valid = valid_keys<T>(a, t0, r, now);
-            const bool clear = settle(a, w, x, r, mine, t0, valid);
-            w.raise(x);
+            const bool clear = settle<T>(a, w, x, r, mine, t0, valid);
+            w.raise(x, Elem<T>::slack);
             w.weigh(x, p);
-            if (!REGS) {
+            if (!SHIFT) {
                 if (more)
                     wait_vm<kCopies>();
                 else
@@ -885,21 +954,16 @@ __global__ __launch_bounds__(kBlock) void k_attn_join(AttnArgs a) {
     }
 }
 
+// The launch of a call's main kernel
 template <typename T, int DP>
-nmg_status launch_attn_dim(const AttnArgs &a, bool shared, bool regs, hipStream_t stream) {
-    const dim3 grid((unsigned)(a.tiles * a.splits * a.kv_heads));
-    if (shared && regs)
-        hipLaunchKernelGGL((k_attn_shared<T, DP, true>), grid, dim3(256), 0, stream, a);
-    else if (shared)
-        hipLaunchKernelGGL((k_attn_shared<T, DP, false>), grid, dim3(256), 0, stream, a);
-    else if (regs)
-        hipLaunchKernelGGL((k_attn_split<T, DP, true>), grid, dim3(64 * split_waves<DP>()), 0,
-                           stream, a);
-    else
-        hipLaunchKernelGGL((k_attn_split<T, DP, false>), grid, dim3(64 * split_waves<DP>()), 0,
-                           stream, a);
+void launch_main(const AttnArgs &a, bool shared, AttnRows how, dim3 grid, hipStream_t stream);
+
+template <typename T, int DP>
+nmg_status launch_attn_dim(const AttnArgs &a, bool shared, AttnRows how, hipStream_t stream) {
+    launch_main<T, DP>(a, shared, how, dim3((unsigned)(a.tiles * a.splits * a.kv_heads)), stream);
     if (a.splits > 1) {
-        const dim3 join((unsigned)(a.tiles * a.kv_heads), (unsigned)((a.D + kJoinRows - 1) / kJoinRows));
+        const dim3 join((unsigned)(a.tiles * a.kv_heads),
+                        (unsigned)((a.D + kJoinRows - 1) / kJoinRows));
         if (shared)
             hipLaunchKernelGGL((k_attn_join<T, DP, kAttnSharedRows>), join, dim3(kBlock), 0,
                                stream, a);
@@ -911,13 +975,13 @@ nmg_status launch_attn_dim(const AttnArgs &a, bool shared, bool regs, hipStream_
 }
 
 template <typename T>
-nmg_status launch_attn(const AttnArgs &a, bool shared, bool regs, hipStream_t stream) {
+nmg_status launch_attn(const AttnArgs &a, bool shared, AttnRows how, hipStream_t stream) {
     switch (attn_padded_dim(a.D)) {
-        case 32: return launch_attn_dim<T, 32>(a, shared, regs, stream);
-        case 64: return launch_attn_dim<T, 64>(a, shared, regs, stream);
-        case 96: return launch_attn_dim<T, 96>(a, shared, regs, stream);
-        case 128: return launch_attn_dim<T, 128>(a, shared, regs, stream);
-        default: return launch_attn_dim<T, 256>(a, shared, regs, stream);
+        case 32: return launch_attn_dim<T, 32>(a, shared, how, stream);
+        case 64: return launch_attn_dim<T, 64>(a, shared, how, stream);
+        case 96: return launch_attn_dim<T, 96>(a, shared, how, stream);
+        case 128: return launch_attn_dim<T, 128>(a, shared, how, stream);
+        default: return launch_attn_dim<T, 256>(a, shared, how, stream);
     }
 }
 

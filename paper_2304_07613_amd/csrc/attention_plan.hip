@@ -70,12 +70,15 @@ nmg_status launch_attention(nmg_dtype dtype, const AttnArgs &args, void *workspa
     auto rows_at = [&](int64_t to) {  // rows of K and V start at multiples of `to` bytes
         return aligned(a.K, to) && aligned(a.V, to) && a.ldk * es % to == 0 && a.ldv * es % to == 0;
     };
-    // direct copies: addresses a multiple of 4 bytes, offsets within a head in 31 bits
-    const int64_t head = std::max(a.ldk, a.ldv) * es * attn_padded_dim(a.D);
-    const bool regs = !rows_at(4) || head > INT32_MAX - 4096;
-    a.align = (int32_t)(regs ? 1 : rows_at(16) ? 16 / es : std::max<int64_t>(4 / es, 1));
-    return dtype == NMG_F16 ? launch_attention_f16(a, p.shared, regs, stream)
-                            : launch_attention_f32(a, p.shared, regs, stream);
+    // a lane's offset among 8 rows is 32 bits wide
+    if (std::max(a.ldk, a.ldv) * es > INT32_MAX / 8) return NMG_ERR_UNSUPPORTED;
+    // (a head's padded rows count)
+    const bool wide = std::max(a.ldk, a.ldv) * es * attn_padded_dim(a.D) > INT32_MAX - 4096;
+    const AttnRows how = !rows_at(4) ? kAttnShift : wide ? kAttnWide : kAttnNarrow;
+    // key tiles start at whole 16 bytes of a row where the rows do
+    a.align = (int32_t)(how == kAttnShift ? 1 : rows_at(16) ? 16 / es : 4 / es);
+    return dtype == NMG_F16 ? launch_attention_f16(a, p.shared, how, stream)
+                            : launch_attention_f32(a, p.shared, how, stream);
 }
 
 }  // namespace nmg_internal

@@ -621,20 +621,22 @@ __device__ __forceinline__ void clear_values(lds_char *v, uint64_t valid) {
 // Drafted tokens seen by each row (bit j: key j of the tile, whose key `drafted`
 // is the first drafted token; keys before it: 1): a lane loads its key's byte of
 // every row's line of the tree, a ballot makes the row's bits.
-template <typename T>
+// AT_ONCE rows' loads are in flight together (more take scalar registers that the
+// kernel has no more of).
+template <typename T, int AT_ONCE>
 __device__ __forceinline__ uint64_t seen_keys(const AttnArgs &a, int column, int drafted) {
     const int lane = rarely(threadIdx.x & 63), at = lane - drafted;
     const int from = min(max(at, 0), a.width - 1);
     uint64_t mine = 0;
-    for (int i0 = 0; i0 < 32; i0 += 16) {
-        int seen[16];
+    for (int i0 = 0; i0 < 32; i0 += AT_ONCE) {
+        int seen[AT_ONCE];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
+        for (int i = 0; i < AT_ONCE; ++i) {
             const int64_t c = __builtin_amdgcn_readlane(column, i0 + i);
             seen[i] = a.tree[c * a.ldtree + from] | (at < 0 ? 1 : 0);
         }
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
+        for (int i = 0; i < AT_ONCE; ++i) {
             const uint64_t bits = __ballot((seen[i] != 0) & (at < a.width));
             if ((lane & 31) == i0 + i) mine = bits;
         }
@@ -644,7 +646,7 @@ __device__ __forceinline__ uint64_t seen_keys(const AttnArgs &a, int column, int
 
 // Scores of keys that take no part in a tile at t0 become -inf; true when there
 // are keys whose values have to be cleared
-template <typename T, typename W>
+template <typename T, int AT_ONCE, typename W>
 __device__ __forceinline__ bool settle(const AttnArgs &a, const W &w, typename W::Scores &x,
                                        const RowTile &r, const RowAt &mine, int64_t t0,
                                        uint64_t valid) {
@@ -653,7 +655,7 @@ __device__ __forceinline__ bool settle(const AttnArgs &a, const W &w, typename W
     const bool tree = a.tree && t0 + KT > (int64_t)r.end - r.n;
     if (!full || tree) {
         const int64_t drafted = max((int64_t)r.end - r.n - t0, -(int64_t)INT32_MAX);
-        w.mask(x, tree ? valid & seen_keys<T>(a, mine.column, (int)drafted) : valid);
+        w.mask(x, tree ? valid & seen_keys<T, AT_ONCE>(a, mine.column, (int)drafted) : valid);
     }
     return !full;
 }
@@ -663,6 +665,30 @@ __device__ __forceinline__ uint8_t mask_at(const AttnArgs &a, int64_t t0) {
     if (!a.key_mask) return 1;
     const int64_t c = t0 + (threadIdx.x & 63);
     return c < a.Nk ? a.key_mask[c] : 0;
+}
+
+// The order of a step's instructions: the next scores' matrix instructions
+// between the weights' vector instructions, LDS reads ahead of their use, then
+// the product with V (4096 x 16384 at 64: 340 -> 323 us)
+template <typename T, int DP>
+__device__ __forceinline__ void interleave() {
+#if defined(__HIP_DEVICE_COMPILE__)
+    if constexpr (sizeof(T) == 2) {
+        constexpr int kScores = DP / 16 * 2, kValues = DP / 32 * 4, kVector = 96 / kScores;
+        __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);
+#pragma unroll
+        for (int i = 0; i < kScores; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x002, kVector, 0);
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+        }
+#pragma unroll
+        for (int i = 0; i < kValues; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        }
+    }
+#endif
 }
 
 // Parts in the workspace: sums (padded D x rows), then maxima and totals, of every
@@ -751,7 +777,7 @@ __global__ __launch_bounds__(256, DP <= (HOW == kAttnShift ? 96 : 128) ? 2 : 1) 
                 if (t + 2 < hi) ks.ask((t + 2) * KT, k_cur, wave);
                 vs.ask((t + 1) * KT, v_nxt, wave);
             }
-            if (settle<T>(a, w, cur, r, mine, (int64_t)first + (int64_t)t * KT, valid))
+            if (settle<T, 8>(a, w, cur, r, mine, (int64_t)first + (int64_t)t * KT, valid))
                 clear_values<T, DP>(v_cur, valid);
             w.raise(cur, Elem<T>::slack);
             // before the other wave of the SIMD while the matrix pipe has work for
@@ -760,6 +786,7 @@ __global__ __launch_bounds__(256, DP <= (HOW == kAttnShift ? 96 : 128) ? 2 : 1) 
             if (more) w.scores(nxt, k_nxt);
             w.weigh(cur, p);
             w.values(cur, p, v_cur);
+            if (more) interleave<T, DP>();
             wave_priority<0>();
             if (SHIFT && more) {
                 if (t + 2 < hi) ks.put(k_cur, wave);
@@ -856,7 +883,7 @@ __global__ __launch_bounds__(64 * split_waves<DP>(), 1) void k_attn_split(AttnAr
                 ks.ask((t + W) * KT, k, 0);
             }
             const uint64_t valid = valid_keys<T>(a, t0, r, now);
-            const bool clear = settle<T>(a, w, x, r, mine, t0, valid);
+            const bool clear = settle<T, 16>(a, w, x, r, mine, t0, valid);
             w.raise(x, Elem<T>::slack);
             w.weigh(x, p);
             if (!SHIFT) {

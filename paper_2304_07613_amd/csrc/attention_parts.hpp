@@ -19,8 +19,8 @@
 // while this one's become weights.  Tiles are 32 keys; a staged row is 3 x 64
 // bytes, the parts one after another, which puts 4 consecutive rows on distinct
 // quarters of the LDS banks (the transposing reads of K); V's 16-byte chunks are
-// permuted by (row / 4) % 4 for its reads of 16 rows.  One buffer each for K and
-// V, the next tile in registers meanwhile.
+// permuted by (row / 4) % 4 for its reads of 16 rows.  Two buffers each for K and
+// V; the tiles after them are in registers meanwhile.
 #pragma once
 
 #include "attention_mfma.hpp"
@@ -249,11 +249,12 @@ struct PartRows : RowSums<DP, 1, true> {
 };
 
 template <int DP, bool WIDE>
-__global__ __launch_bounds__(256, DP <= 64 ? 2 : 1) void k_attn_parts(AttnArgs a) {
+__global__ __launch_bounds__(256, DP <= 64 && !WIDE ? 2 : 1) void k_attn_parts(AttnArgs a) {
     constexpr int TR = kAttnSharedRows, KT = kPartKeys;
-    __shared__ __attribute__((aligned(1024))) char lds_k[DP * kPartRow];
-    __shared__ __attribute__((aligned(1024))) char lds_v[DP * kPartRow];
-    __shared__ int odd[2];  // the last tile of K, of V, that holds an infinity or NaN
+    constexpr int kTile = DP * kPartRow;
+    __shared__ __attribute__((aligned(1024))) char lds_k[2 * kTile];
+    __shared__ __attribute__((aligned(1024))) char lds_v[2 * kTile];
+    __shared__ int odd[2][2];  // the last even, odd tile of K, of V, that holds an infinity or NaN
     Place at;
     if (!find_place<TR>(a, blockIdx.x, at)) return;
     const RowTile &r = at.rows;
@@ -271,24 +272,28 @@ __global__ __launch_bounds__(256, DP <= 64 ? 2 : 1) void k_attn_parts(AttnArgs a
         PartStager<DP, true, WIDE> vs;
         ks.init(a, a.K, a.ldk, at.head, first);
         vs.init(a, a.V, a.ldv, at.head, first);
-        lds_char *k = (lds_char *)lds_k, *v = (lds_char *)lds_v;
-        uint8_t byte;
+        auto k_at = [&](int t) { return (lds_char *)lds_k + (t & 1) * kTile; };
+        auto v_at = [&](int t) { return (lds_char *)lds_v + (t & 1) * kTile; };
         auto put_k = [&](int t) {
-            if (ks.put(k, wave)) odd[0] = t;
+            if (ks.put(k_at(t), wave)) odd[0][t & 1] = t;
         };
         auto put_v = [&](int t) {
-            if (vs.put(v, wave)) odd[1] = t;
+            if (vs.put(v_at(t), wave)) odd[1][t & 1] = t;
         };
+        auto k_plain = [&](int t) {
+            return w.plain && __builtin_amdgcn_readfirstlane(odd[0][t & 1]) != t;
+        };
+        auto v_plain = [&](int t) { return __builtin_amdgcn_readfirstlane(odd[1][t & 1]) != t; };
         auto scores_at = [&](int t, typename PartRows<DP>::Scores &x) {
-            if (w.plain && __builtin_amdgcn_readfirstlane(odd[0]) != t)
-                w.scores(x, k);
+            if (k_plain(t))
+                w.scores(x, k_at(t));
             else
                 w.scores_exact(a, x, ks.rows, t * KT, a.Nk - first, at.head, mine);
         };
         ks.ask(lo * KT, wave);
         w.init(a, at.head, mine);
-        byte = mask_at(a, (int64_t)first + (int64_t)lo * KT);
-        if (threadIdx.x < 2) odd[threadIdx.x] = -1;
+        uint8_t byte = mask_at(a, (int64_t)first + (int64_t)lo * KT);
+        if (threadIdx.x < 4) odd[threadIdx.x >> 1][threadIdx.x & 1] = -1;
         __syncthreads();
         put_k(lo);
         vs.ask(lo * KT, wave);
@@ -297,34 +302,35 @@ __global__ __launch_bounds__(256, DP <= 64 ? 2 : 1) void k_attn_parts(AttnArgs a
         typename PartRows<DP>::Scores cur, nxt;
         typename PartRows<DP>::Weights p;
         scores_at(lo, cur);
-        __syncthreads();
-        put_v(lo);
-        if (lo + 1 < hi) put_k(lo + 1);
-        __syncthreads();
-        for (int t = lo; t < hi; ++t) {  // K of tile t + 1 and V of tile t are in LDS
+        for (int t = lo; t < hi; ++t) {
             const int64_t t0 = (int64_t)first + (int64_t)t * KT;
             const uint64_t valid = valid_keys<float>(a, t0, r, byte);
             const bool more = t + 1 < hi;
+            // V of this tile and K of the next, in registers since the last step, into
+            // the buffers that the step before it read; the ones after them asked for
+            put_v(t);
             if (more) {
+                put_k(t + 1);
                 byte = mask_at(a, t0 + KT);
-                if (t + 2 < hi) ks.ask((t + 2) * KT, wave);
                 vs.ask((t + 1) * KT, wave);
+                if (t + 2 < hi) ks.ask((t + 2) * KT, wave);
             }
-            settle<float>(a, w, cur, r, mine, t0, valid);
+            settle<float, 8>(a, w, cur, r, mine, t0, valid);
             w.raise(cur, Elem<float>::slack);
-            if (more) scores_at(t + 1, nxt);
-            w.weigh(cur, p);
-            if (__builtin_amdgcn_readfirstlane(odd[1]) != t)
-                w.values(p, v);  // (a key left out is finite here: 0 times it is 0)
-            else
-                w.values_exact(cur, vs.rows, a.D, t * KT, valid);
-            if (more) {
-                cur = nxt;
-                __syncthreads();
-                if (t + 2 < hi) put_k(t + 2);
-                put_v(t + 1);
-                __syncthreads();
+            __syncthreads();
+            if (more && k_plain(t + 1) && v_plain(t)) {
+                w.scores(nxt, k_at(t + 1));
+                w.weigh(cur, p);
+                w.values(p, v_at(t));  // (a key left out is finite here: 0 times it is 0)
+            } else {
+                w.weigh(cur, p);
+                if (v_plain(t))
+                    w.values(p, v_at(t));
+                else
+                    w.values_exact(cur, vs.rows, a.D, t * KT, valid);
+                if (more) scores_at(t + 1, nxt);
             }
+            cur = nxt;
         }
     }
     finish<float, DP>(a, at, mine, w, wave);

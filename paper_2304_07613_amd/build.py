@@ -3,7 +3,9 @@
 Every translation unit under csrc/ is compiled to an object in parallel, then
 the objects are linked into one shared library; the link is checked for
 undefined kernel launch stubs.  csrc/gen_gelu_table.py writes the binary16
-GELU table into the build folder first.
+GELU table into the build folder first.  csrc/calls.cpp, the marshalling of the
+attention operators' calls, becomes the Python module _calls beside the library
+(host code, g++ against torch's headers).
 """
 from __future__ import annotations
 
@@ -11,6 +13,7 @@ import glob
 import os
 import subprocess
 import sys
+import sysconfig
 import tempfile
 from concurrent.futures import ThreadPoolExecutor
 
@@ -19,6 +22,8 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 HEADER = os.path.join(ROOT, "include", "nmg.h")
 LIB_PATH = os.path.join(HERE, "libnmg.so")
+CALLS_SRC = os.path.join(CSRC, "calls.cpp")
+CALLS_PATH = os.path.join(HERE, "_calls.so")
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall",
@@ -38,7 +43,8 @@ GENERATORS = [os.path.join(CSRC, "gen_gelu_table.py")]
 
 def inputs() -> list:
     """Every file the library is built from."""
-    return sorted(sources() + glob.glob(os.path.join(CSRC, "*.hpp")) + [HEADER] + GENERATORS)
+    return sorted(sources() + glob.glob(os.path.join(CSRC, "*.hpp")) +
+                  [HEADER, CALLS_SRC] + GENERATORS)
 
 
 def _clean(text: str) -> str:
@@ -46,8 +52,28 @@ def _clean(text: str) -> str:
                      if "packed-fp32-ops" not in l and "not a recognized feature" not in l)
 
 
+def build_calls() -> str:
+    """Compile csrc/calls.cpp into the Python module _calls."""
+    import torch
+    from torch.utils import cpp_extension
+
+    inc = cpp_extension.include_paths() + [sysconfig.get_paths()["include"]]
+    tmp = CALLS_PATH + ".tmp"
+    lib = cpp_extension.library_paths()[0]
+    res = subprocess.run(
+        [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall",
+         f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+         *[arg for d in inc for arg in ("-isystem", d)], "-o", tmp, CALLS_SRC, "-L", lib,
+         "-ltorch_python", "-ltorch_cpu", "-lc10"], capture_output=True, text=True)
+    if res.returncode != 0:
+        raise RuntimeError(f"calls.cpp failed:\n{res.stdout}{res.stderr}")
+    os.replace(tmp, CALLS_PATH)
+    return CALLS_PATH
+
+
 def build(verbose: bool = False, jobs: int | None = None) -> str:
-    """Compile csrc/*.hip into libnmg.so next to this file (always rebuilds)."""
+    """Compile csrc/*.hip into libnmg.so, and the module _calls, next to this
+    file (always rebuilds)."""
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     jobs = jobs or min(16, os.cpu_count() or 4)
     inc = ["-I", os.path.join(ROOT, "include")]
@@ -64,7 +90,9 @@ def build(verbose: bool = False, jobs: int | None = None) -> str:
                                  capture_output=True, text=True)
             return src, obj, res
         with ThreadPoolExecutor(max_workers=jobs) as pool:
+            calls = pool.submit(build_calls)
             results = list(pool.map(compile_one, sources()))
+            calls.result()
         errors = [(s, r) for s, _, r in results if r.returncode != 0]
         if errors:
             s, r = errors[0]
@@ -89,9 +117,9 @@ def build(verbose: bool = False, jobs: int | None = None) -> str:
 
 
 def is_stale() -> bool:
-    if not os.path.exists(LIB_PATH):
+    if not (os.path.exists(LIB_PATH) and os.path.exists(CALLS_PATH)):
         return True
-    t = os.path.getmtime(LIB_PATH)
+    t = min(os.path.getmtime(LIB_PATH), os.path.getmtime(CALLS_PATH))
     return any(os.path.getmtime(p) > t for p in inputs())
 
 

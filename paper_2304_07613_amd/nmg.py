@@ -149,6 +149,25 @@ def _load():
     return L
 
 
+_calls = None
+
+
+def _load_calls():
+    """The compiled marshalling of the attention operators, bound to the library."""
+    global _calls
+    L = lib()
+    if not os.path.exists(_build.CALLS_PATH):
+        raise RuntimeError(f"{_build.CALLS_PATH} is not built; run __graft_entry__.build()")
+    from . import _calls as module
+
+    names = ("nmg_rotary", "nmg_qk_norm_rotary", "nmg_attention", "nmg_tree_attention",
+             "nmg_attention_workspace_bytes")
+    module.bind({n: ctypes.cast(getattr(L, n), ctypes.c_void_p).value for n in names}, _check,
+                torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream)
+    _calls = module
+    return module
+
+
 def status_str(status: int) -> str:
     return lib().nmg_status_str(status).decode()
 
@@ -198,13 +217,16 @@ def _stream(t: torch.Tensor) -> int:
 def _need_cuda(*ts):
     """Every tensor on the current GPU: the library launches on the current
     HIP device, on that device's current stream."""
-    cur = torch._C._cuda_getDevice() if ts[0].is_cuda else -1
+    cur = -1
     for t in ts:
-        if t.get_device() != cur or cur < 0:
-            if not t.is_cuda:
-                raise ValueError("libnmg works on GPU tensors only")
-            raise ValueError(f"tensor on {t.device}, but the current device is "
-                             f"cuda:{torch._C._cuda_getDevice()} (select it with torch.cuda.device)")
+        dev = t.get_device()
+        if dev < 0 or not t.is_cuda:
+            raise ValueError("libnmg works on GPU tensors only")
+        if cur < 0:
+            cur = torch._C._cuda_getDevice()
+        if dev != cur:
+            raise ValueError(f"tensor on {t.device}, but the current device is cuda:{cur} "
+                             "(select it with torch.cuda.device)")
 
 
 def _rows(t: torch.Tensor, name: str) -> int:
@@ -566,72 +588,15 @@ def rotary_table(length: int, dim: int, base: float = 10000.0, scaling: str = "n
     return table
 
 
-# These calls are made once a layer and step, for single tokens too, so their
-# checks are few attribute reads each.
-
-def _matrix(t: torch.Tensor, name: str):
-    """(rows, columns, leading dimension) of a 2-D row-major tensor."""
-    shape, st = t.shape, t.stride()
-    if len(st) != 2 or st[1] != 1:
-        raise ValueError(f"{name} must be a 2-D tensor with unit column stride")
-    return shape[0], shape[1], st[0]
-
-
-def _ints(t: torch.Tensor, n: int, name: str) -> int:
-    """Pointer of n contiguous int32 values."""
-    if t.dtype is not torch.int32 or t.dim() != 1 or t.numel() != n or not t.is_contiguous():
-        raise ValueError(f"{name} must be {n} contiguous int32 values")
-    return t.data_ptr()
-
-
-def _rotary_desc(table, positions, pairs: str, N: int) -> _Rotary:
-    code = ROTARY_PAIRS.get(pairs)
-    if code is None:
-        raise ValueError(f"unknown rotary layout {pairs!r}")
-    if table is None:
-        return _Rotary(0, code, 0, None, None)
-    shape = table.shape
-    if len(shape) != 3 or shape[0] != 2 or table.dtype is not torch.float32 or \
-            not table.is_contiguous():
-        raise ValueError("table must be a contiguous float32 (2, dim / 2, length) tensor")
-    return _Rotary(2 * shape[1], code, shape[2], table.data_ptr(), _ints(positions, N, "positions"))
-
-
-def _head_rows(rows: int, heads: int, name: str) -> int:
-    """Rows of one head of a features x tokens matrix."""
-    if heads < 1 or rows < 1 or rows % heads:
-        raise ValueError(f"{name} must have a whole number of rows for each of {heads} heads")
-    return rows // heads
-
-
-def _out_for(t: torch.Tensor, out, name: str) -> torch.Tensor:
-    if out is None:
-        return torch.empty_like(t)
-    if out.dtype != t.dtype or out.shape != t.shape:
-        raise ValueError(f"{name} must have the shape and dtype of its input")
-    return out
-
+# These calls are made for every layer and token, so their marshalling is
+# compiled (csrc/calls.cpp): the same checks, outputs and workspace from torch's
+# allocator, and errors as above.
 
 def rotary(X, heads: int, table, positions, layout: str = "half", out=None):
     """``nmg_rotary``: the first 2 * table.shape[1] rows of each of the `heads`
     heads of X (features x tokens) turned by their tokens' positions, the
     others copied.  out may be X."""
-    code = _DTYPE_CODE.get(X.dtype)
-    if code is None:
-        raise TypeError(f"unsupported dtype {X.dtype}")
-    M, N, ldx = _matrix(X, "X")
-    D = _head_rows(M, heads, "X")
-    desc = _rotary_desc(table, positions, layout, N)
-    if table is None:
-        _need_cuda(X)
-    else:
-        _need_cuda(X, table, positions)
-    out = _out_for(X, out, "out")
-    if out.get_device() != X.get_device():
-        _need_cuda(X, out)
-    _check((_lib or _load()).nmg_rotary(code, heads, D, desc, X.data_ptr(), ldx, N, out.data_ptr(),
-                                        _matrix(out, "out")[2], _stream(X)), "nmg_rotary")
-    return out
+    return (_calls or _load_calls()).rotary(X, heads, table, positions, layout, out)
 
 
 def qk_norm_rotary(Q, K, heads: int, kv_heads: int, q_weight, k_weight, table=None, positions=None,
@@ -639,62 +604,9 @@ def qk_norm_rotary(Q, K, heads: int, kv_heads: int, q_weight, k_weight, table=No
     """``nmg_qk_norm_rotary``: RMS norm of every head's column of Q and K
     (weights float32 of head_dim, or None) and the rotation (none without a
     table).  out: (Q's, K's), which may be Q and K.  Returns both."""
-    code = _DTYPE_CODE.get(Q.dtype)
-    if code is None or K.dtype is not Q.dtype:
-        raise TypeError("Q and K must be float32 or float16, of one dtype")
-    M, N, ldq = _matrix(Q, "Q")
-    Mk, Nk, ldk = _matrix(K, "K")
-    D = _head_rows(M, heads, "Q")
-    if Nk != N or _head_rows(Mk, kv_heads, "K") != D:
-        raise ValueError("Q and K must have heads of one size and the same tokens")
-    desc = _rotary_desc(table, positions, layout, N)
-    used = [Q, K]
-    weights = [None, None]
-    for i, w in enumerate((q_weight, k_weight)):
-        if w is not None:
-            if w.dtype is not torch.float32 or w.dim() != 1 or w.numel() != D or not w.is_contiguous():
-                raise ValueError("norm weights must be head_dim contiguous float32 values")
-            weights[i] = w.data_ptr()
-            used.append(w)
-    if table is not None:
-        used += (table, positions)
-    _need_cuda(*used)
-    if out is None:
-        yq, yk = torch.empty_like(Q), torch.empty_like(K)
-    else:
-        yq, yk = _out_for(Q, out[0], "out[0]"), _out_for(K, out[1], "out[1]")
-        _need_cuda(Q, yq, yk)
-    _check((_lib or _load()).nmg_qk_norm_rotary(
-        code, heads, kv_heads, D, desc, weights[0], weights[1], eps, Q.data_ptr(), ldq, K.data_ptr(),
-        ldk, N, yq.data_ptr(), _matrix(yq, "out[0]")[2], yk.data_ptr(), _matrix(yk, "out[1]")[2],
-        _stream(Q)), "nmg_qk_norm_rotary")
-    return yq, yk
-
-
-def _attend(fn, Q, K, V, heads, kv_heads, q_offsets, kv_begin, kv_end, extra, scale, out):
-    code = _DTYPE_CODE.get(Q.dtype)
-    if code is None or K.dtype is not Q.dtype or V.dtype is not Q.dtype:
-        raise TypeError("Q, K and V must be float32 or float16, of one dtype")
-    M, Nq, ldq = _matrix(Q, "Q")
-    Mk, Nk, ldk = _matrix(K, "K")
-    Mv, Nv, ldv = _matrix(V, "V")
-    D = _head_rows(M, heads, "Q")
-    if Mk != Mv or Nk != Nv or _head_rows(Mk, kv_heads, "K") != D:
-        raise ValueError("K and V must have kv_heads heads of Q's head size, and the same tokens")
-    B = kv_begin.numel()
-    s = _Sequences(B, _ints(q_offsets, B + 1, "q_offsets"), _ints(kv_begin, B, "kv_begin"),
-                   _ints(kv_end, B, "kv_end"))
-    _need_cuda(Q, K, V, q_offsets, kv_begin, kv_end)
-    out = _out_for(Q, out, "out")
-    if out.get_device() != Q.get_device():
-        _need_cuda(Q, out)
-    L = _lib or _load()
-    h = _Heads(heads, kv_heads, D, code)
-    ws, wp, wb = _workspace(L.nmg_attention_workspace_bytes(h, B, Nq, Nk), Q)
-    _check(getattr(L, fn)(h, s, Q.data_ptr(), ldq, Nq, K.data_ptr(), ldk, V.data_ptr(), ldv, Nk, *extra,
-                          D ** -0.5 if scale is None else scale, out.data_ptr(),
-                          _matrix(out, "out")[2], wp, wb, _stream(Q)), fn)
-    return out
+    yq, yk = (None, None) if out is None else out
+    return (_calls or _load_calls()).qk_norm_rotary(Q, K, heads, kv_heads, q_weight, k_weight, table,
+                                                    positions, layout, eps, yq, yk)
 
 
 def attention(Q, K, V, heads: int, kv_heads: int, q_offsets, kv_begin, kv_end, key_mask=None,
@@ -705,15 +617,8 @@ def attention(Q, K, V, heads: int, kv_heads: int, q_offsets, kv_begin, kv_end, k
     the device).  key_mask: uint8 or bool for every key column, 0 leaves it out.
     scale: head_dim ** -0.5 by default.  Scratch memory from torch's
     allocator."""
-    mask = None
-    if key_mask is not None:
-        if key_mask.dtype not in (torch.uint8, torch.bool) or key_mask.shape != (K.shape[1],) or \
-                not key_mask.is_contiguous():
-            raise ValueError("key_mask must be contiguous uint8 or bool, one for every key column")
-        _need_cuda(key_mask)
-        mask = key_mask.data_ptr()
-    return _attend("nmg_attention", Q, K, V, heads, kv_heads, q_offsets, kv_begin, kv_end, (mask,),
-                   scale, out)
+    return (_calls or _load_calls()).attention(Q, K, V, heads, kv_heads, q_offsets, kv_begin, kv_end,
+                                               key_mask, None, scale, out)
 
 
 def tree_attention(Q, K, V, heads: int, kv_heads: int, q_offsets, kv_begin, kv_end, tree,
@@ -722,9 +627,7 @@ def tree_attention(Q, K, V, heads: int, kv_heads: int, q_offsets, kv_begin, kv_e
     values are the last columns of their sequence's key range; tree (uint8 or
     bool, a row per query column) says which drafted tokens of its sequence each
     one attends to, itself included; all earlier columns it attends to."""
-    if tree.dtype not in (torch.uint8, torch.bool) or len(tree.shape) != 2 or \
-            tree.shape[0] != Q.shape[1]:
+    if tree is None:
         raise ValueError("tree must be uint8 or bool with a row for every query column")
-    _need_cuda(tree)
-    return _attend("nmg_tree_attention", Q, K, V, heads, kv_heads, q_offsets, kv_begin, kv_end,
-                   (tree.data_ptr(), _rows(tree, "tree"), tree.shape[1]), scale, out)
+    return (_calls or _load_calls()).attention(Q, K, V, heads, kv_heads, q_offsets, kv_begin, kv_end,
+                                               None, tree, scale, out)

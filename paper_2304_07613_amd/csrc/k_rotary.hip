@@ -18,7 +18,7 @@ namespace {
 
 // N: tokens a thread, U: units a thread
 template <typename T, bool NORM, int N, int U>
-__global__ __launch_bounds__(kBlock, N == 4 && U <= 4 ? 4 : 1) void k_rotary(RotaryArgs a) {
+__global__ __launch_bounds__(kBlock, N == 4 && U <= 4 ? 3 : 1) void k_rotary(RotaryArgs a) {
     __shared__ float sums[2][kBlock / 64][64 * N];
     const int lanes = a.lanes, slices = kBlock / lanes;  // of tokens
     const int x = threadIdx.x % lanes, slice = threadIdx.x / lanes;
@@ -34,44 +34,22 @@ __global__ __launch_bounds__(kBlock, N == 4 && U <= 4 ? 4 : 1) void k_rotary(Rot
 
     const int half = a.R / 2, units = half + (a.D - a.R + 1) / 2;
     int row[U][2];       // of unit i; -1: none
-    float c[U][N], s[U][N], w[U][2];
-    int64_t p[N];
-#pragma unroll
-    for (int n = 0; n < N; ++n) {
-        p[n] = 0;
-        if (a.R && t + n < a.N) p[n] = min(max((int64_t)a.positions[t + n], (int64_t)0), a.length - 1);
-    }
 #pragma unroll
     for (int i = 0; i < U; ++i) {
         const int u = slice + i * slices;
         row[i][0] = row[i][1] = -1;
-#pragma unroll
-        for (int n = 0; n < N; ++n) {
-            c[i][n] = 1.f;
-            s[i][n] = 0.f;
-        }
         if (u < half) {
             row[i][0] = a.interleaved ? 2 * u : u;
             row[i][1] = a.interleaved ? 2 * u + 1 : u + half;
-#pragma unroll
-            for (int n = 0; n < N; ++n) {
-                c[i][n] = a.table[u * a.length + p[n]];
-                s[i][n] = a.table[(half + u) * a.length + p[n]];
-            }
         } else if (u < units) {
             row[i][0] = a.R + 2 * (u - half);
             row[i][1] = row[i][0] + 1 < a.D ? row[i][0] + 1 : -1;
         }
-#pragma unroll
-        for (int e = 0; e < 2; ++e)
-            w[i][e] = NORM && r.weight && row[i][e] >= 0 ? r.weight[row[i][e]] : 1.f;
     }
-
     typedef T TN __attribute__((ext_vector_type(N)));
-    for (int h = h0; h < h1; ++h) {
+    TN in[U][2];         // of the head to come
+    auto load = [&](int h) {
         const T *src = (const T *)r.X + (int64_t)h * a.D * r.ldx + t;
-        T *dst = (T *)r.Y + (int64_t)h * a.D * r.ldy + t;
-        float v[U][2][N];
 #pragma unroll
         for (int i = 0; i < U; ++i)
 #pragma unroll
@@ -87,9 +65,67 @@ __global__ __launch_bounds__(kBlock, N == 4 && U <= 4 ? 4 : 1) void k_rotary(Rot
                             if (t + n < a.N) y[n] = q[n];
                     }
                 }
-#pragma unroll
-                for (int n = 0; n < N; ++n) v[i][e][n] = (float)y[n];
+                in[i][e] = y;
             }
+    };
+    // the first head is on its way while positions, then cosines, sines and weights come
+    load(h0);
+    float c[U][N], s[U][N], w[U][2];
+    int64_t p[N];
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        p[n] = 0;
+        if (a.R && t + n < a.N) p[n] = min(max((int64_t)a.positions[t + n], (int64_t)0), a.length - 1);
+    }
+    // tokens mostly follow one another in their sequence: one load then gives their
+    // cosines, one their sines (16 heads x 128, 16384 tokens binary32: 53.4 -> 51.3 us)
+    bool follow = p[0] + N <= a.length;
+#pragma unroll
+    for (int n = 1; n < N; ++n) follow &= t + n >= a.N || p[n] == p[0] + n;
+    const bool runs = N > 1 && __all(follow || !here);
+    typedef float FN __attribute__((ext_vector_type(N)));
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+        const int u = slice + i * slices;
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            c[i][n] = 1.f;
+            s[i][n] = 0.f;
+        }
+        if (u < half && here) {
+            const float *cs = a.table + u * a.length, *sn = a.table + (half + u) * a.length;
+            if (runs) {
+                FN x, y;
+                __builtin_memcpy(&x, cs + p[0], sizeof x);
+                __builtin_memcpy(&y, sn + p[0], sizeof y);
+#pragma unroll
+                for (int n = 0; n < N; ++n) {
+                    c[i][n] = x[n];
+                    s[i][n] = y[n];
+                }
+            } else {
+#pragma unroll
+                for (int n = 0; n < N; ++n) {
+                    c[i][n] = cs[p[n]];
+                    s[i][n] = sn[p[n]];
+                }
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+            w[i][e] = NORM && r.weight && row[i][e] >= 0 ? r.weight[row[i][e]] : 1.f;
+    }
+
+    for (int h = h0; h < h1; ++h) {
+        T *dst = (T *)r.Y + (int64_t)h * a.D * r.ldy + t;
+        float v[U][2][N];
+#pragma unroll
+        for (int i = 0; i < U; ++i)
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+#pragma unroll
+                for (int n = 0; n < N; ++n) v[i][e][n] = (float)in[i][e][n];
+        if (h + 1 < h1) load(h + 1);
         float scale[N];
         if constexpr (NORM) {
 #pragma unroll
@@ -177,7 +213,14 @@ void launch(const RotaryArgs &a, int tokens, int units, dim3 grid, hipStream_t s
         go(k_rotary<T, NORM, 1, 4>);
     else if (tokens == 1)
         go(k_rotary<T, NORM, 1, 16>);
-    else if (units <= 2)
+    else if (tokens == 2) {
+        if constexpr (sizeof(T) == 2) {
+            if (units <= 4)
+                go(k_rotary<T, NORM, 2, 4>);
+            else
+                go(k_rotary<T, NORM, 2, 8>);
+        }
+    } else if (units <= 2)
         go(k_rotary<T, NORM, 4, 2>);
     else if (units <= 4)
         go(k_rotary<T, NORM, 4, 4>);
@@ -191,8 +234,12 @@ nmg_status launch_rotary(nmg_dtype dtype, const RotaryArgs &args, bool norm, hip
     RotaryArgs a = args;
     const int units = a.R / 2 + (a.D - a.R + 1) / 2;
     auto per_thread = [&] { return (units * a.lanes + kBlock - 1) / kBlock; };
-    // 4 tokens a thread for 128 or more: 256 bytes of a row at a time (at any alignment)
+    const int64_t heads = (int64_t)a.part[0].heads + a.part[1].heads;
+    // 4 tokens a thread for 128 or more: 256 bytes of a row at a time (at any
+    // alignment); 2 where that leaves binary16 fewer than 4 workgroups for every compute
+    // unit (12 + 12 heads x 64 with norms: 4096 tokens 14.9 -> 13.1 us, 32768 52 -> 54)
     int tokens = a.N >= 128 ? 4 : 1;
+    if (tokens == 4 && dtype == NMG_F16 && (a.N + 127) / 128 * heads < 4 * device_cus()) tokens = 2;
     const int most_lanes = tokens == 1 ? 64 : dtype == NMG_F16 ? 32 : 16;
     a.lanes = 1;
     while (a.lanes < most_lanes && (int64_t)a.lanes * tokens < a.N) a.lanes *= 2;
@@ -200,7 +247,6 @@ nmg_status launch_rotary(nmg_dtype dtype, const RotaryArgs &args, bool norm, hip
     if (per_thread() > 8) tokens = 1;
     if (per_thread() > 16) return NMG_ERR_UNSUPPORTED;
     const int64_t width = (int64_t)a.lanes * tokens, blocks = (a.N + width - 1) / width;
-    const int64_t heads = (int64_t)a.part[0].heads + a.part[1].heads;
     a.run = (int)std::max<int64_t>(1, std::min<int64_t>(8, blocks * heads / (4 * device_cus())));
     a.groups0 = (a.part[0].heads + a.run - 1) / a.run;
     const int64_t groups = a.groups0 + (a.part[1].heads + a.run - 1) / a.run;

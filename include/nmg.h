@@ -605,7 +605,8 @@ nmg_status nmg_attention(const nmg_heads *heads, const nmg_sequences *sequences,
  * query columns are drafted tokens, whose keys and values are the last n columns
  * of its key range.  Token t (query column c) attends to every earlier column
  * of the range, and to drafted token i exactly if i < width and tree[c * ldtree +
- * i] != 0 (bytes, Nq x width, ldtree >= width). */
+ * i] != 0 (bytes, Nq x width, ldtree >= width; NMG_ERR_UNSUPPORTED when Nq * ldtree
+ * does not fit 31 bits). */
 nmg_status nmg_tree_attention(const nmg_heads *heads, const nmg_sequences *sequences,
                               const void *Q, int64_t ldq, int64_t Nq, const void *K, int64_t ldk,
                               const void *V, int64_t ldv, int64_t Nk, const uint8_t *tree,

@@ -618,45 +618,48 @@ __device__ __forceinline__ void clear_values(lds_char *v, uint64_t valid) {
     }
 }
 
-// Drafted tokens seen by each row (bit j: key j of the tile, whose key `drafted`
-// is the first drafted token; keys before it: 1): a lane loads its key's byte of
-// every row's line of the tree, a ballot makes the row's bits.
-// AT_ONCE rows' loads are in flight together (more take scalar registers that the
-// kernel has no more of).
+// The keys of the tile at t0 that the lane's row sees of the draft (bit j: key j;
+// keys before the draft: 1).  A lane loads its key's byte of every row's line of
+// the tree, a ballot makes the row's bits; AT_ONCE rows' loads are in flight
+// together.  Called before the tile's copies are waited for: its waits take in
+// what was asked for earlier, and must not take in the next tile's copies.
+struct Draft {
+    bool here;      // the tile holds drafted tokens
+    uint64_t seen;
+};
 template <typename T, int AT_ONCE>
-__device__ __forceinline__ uint64_t seen_keys(const AttnArgs &a, int column, int drafted) {
-    const int lane = rarely(threadIdx.x & 63), at = lane - drafted;
+__device__ __forceinline__ Draft draft_at(const AttnArgs &a, const RowTile &r, const RowAt &mine,
+                                          int64_t t0) {
+    const int64_t drafted = (int64_t)r.end - r.n - t0;  // the draft's first key of the tile
+    Draft x = {a.tree && drafted < Elem<T>::keys, ~0ull};
+    if (!x.here) return x;
+    const int lane = rarely(threadIdx.x & 63);
+    const int at = lane - (int)max(drafted, (int64_t)(64 - INT32_MAX));
     const int from = min(max(at, 0), a.width - 1);
-    uint64_t mine = 0;
+    const int line = mine.column * (int)a.ldtree;  // (a tree of 2^31 bytes or more is refused)
+#pragma unroll 1
     for (int i0 = 0; i0 < 32; i0 += AT_ONCE) {
         int seen[AT_ONCE];
 #pragma unroll
-        for (int i = 0; i < AT_ONCE; ++i) {
-            const int64_t c = __builtin_amdgcn_readlane(column, i0 + i);
-            seen[i] = a.tree[c * a.ldtree + from] | (at < 0 ? 1 : 0);
-        }
+        for (int i = 0; i < AT_ONCE; ++i)
+            seen[i] = a.tree[(uint32_t)(__builtin_amdgcn_readlane(line, i0 + i) + from)] |
+                      (at < 0 ? 1 : 0);
 #pragma unroll
         for (int i = 0; i < AT_ONCE; ++i) {
             const uint64_t bits = __ballot((seen[i] != 0) & (at < a.width));
-            if ((lane & 31) == i0 + i) mine = bits;
+            if ((lane & 31) == i0 + i) x.seen = bits;
         }
     }
-    return mine;
+    return x;
 }
 
-// Scores of keys that take no part in a tile at t0 become -inf; true when there
-// are keys whose values have to be cleared
-template <typename T, int AT_ONCE, typename W>
-__device__ __forceinline__ bool settle(const AttnArgs &a, const W &w, typename W::Scores &x,
-                                       const RowTile &r, const RowAt &mine, int64_t t0,
-                                       uint64_t valid) {
-    constexpr int KT = Elem<T>::keys;
-    const bool full = valid == (KT == 64 ? ~0ull : 0xffffffffull);
-    const bool tree = a.tree && t0 + KT > (int64_t)r.end - r.n;
-    if (!full || tree) {
-        const int64_t drafted = max((int64_t)r.end - r.n - t0, -(int64_t)INT32_MAX);
-        w.mask(x, tree ? valid & seen_keys<T, AT_ONCE>(a, mine.column, (int)drafted) : valid);
-    }
+// Scores of keys that take no part in a tile become -inf; true when there are
+// keys whose values have to be cleared
+template <typename T, typename W>
+__device__ __forceinline__ bool settle(const W &w, typename W::Scores &x, uint64_t valid,
+                                       const Draft &draft) {
+    const bool full = valid == (Elem<T>::keys == 64 ? ~0ull : 0xffffffffull);
+    if (!full || draft.here) w.mask(x, valid & draft.seen);
     return !full;
 }
 
@@ -770,6 +773,8 @@ __global__ __launch_bounds__(256, DP <= (HOW == kAttnShift ? 96 : 128) ? 2 : 1) 
         auto step = [&](auto more, int t, typename Rows<T, DP>::Scores &cur,
                         typename Rows<T, DP>::Scores &nxt, lds_char *k_cur, lds_char *k_nxt,
                         lds_char *v_cur, lds_char *v_nxt) {
+            const Draft draft =
+                draft_at<T, 8>(a, r, mine, (int64_t)first + (int64_t)t * KT);
             landed_barrier();  // they have landed; the buffers of K of tile t, V of t - 1 are free
             const uint64_t valid = valid_at(t, byte);
             if (more) {
@@ -777,7 +782,7 @@ __global__ __launch_bounds__(256, DP <= (HOW == kAttnShift ? 96 : 128) ? 2 : 1) 
                 if (t + 2 < hi) ks.ask((t + 2) * KT, k_cur, wave);
                 vs.ask((t + 1) * KT, v_nxt, wave);
             }
-            if (settle<T, 8>(a, w, cur, r, mine, (int64_t)first + (int64_t)t * KT, valid))
+            if (settle<T>(w, cur, valid, draft))
                 clear_values<T, DP>(v_cur, valid);
             w.raise(cur, Elem<T>::slack);
             // before the other wave of the SIMD while the matrix pipe has work for
@@ -872,6 +877,7 @@ __global__ __launch_bounds__(64 * split_waves<DP>(), 1) void k_attn_split(AttnAr
             const int64_t t0 = (int64_t)first + (int64_t)t * KT;
             const bool more = t + W < hi;
             const uint8_t now = byte;
+            const Draft draft = draft_at<T, 32>(a, r, mine, t0);
             if (!SHIFT) wait_vm<kCopies>();  // K has landed; V may still be in flight
             typename Rows<T, DP>::Scores x;
             typename Rows<T, DP>::Weights p;
@@ -883,7 +889,7 @@ __global__ __launch_bounds__(64 * split_waves<DP>(), 1) void k_attn_split(AttnAr
                 ks.ask((t + W) * KT, k, 0);
             }
             const uint64_t valid = valid_keys<T>(a, t0, r, now);
-            const bool clear = settle<T, 16>(a, w, x, r, mine, t0, valid);
+            const bool clear = settle<T>(w, x, valid, draft);
             w.raise(x, Elem<T>::slack);
             w.weigh(x, p);
             if (!SHIFT) {

@@ -306,6 +306,7 @@ __global__ __launch_bounds__(256, DP <= 64 && !WIDE ? 2 : 1) void k_attn_parts(A
             const int64_t t0 = (int64_t)first + (int64_t)t * KT;
             const uint64_t valid = valid_keys<float>(a, t0, r, byte);
             const bool more = t + 1 < hi;
+            const Draft draft = draft_at<float, 8>(a, r, mine, t0);
             // V of this tile and K of the next, in registers since the last step, into
             // the buffers that the step before it read; the ones after them asked for
             put_v(t);
@@ -315,7 +316,7 @@ __global__ __launch_bounds__(256, DP <= 64 && !WIDE ? 2 : 1) void k_attn_parts(A
                 vs.ask((t + 1) * KT, wave);
                 if (t + 2 < hi) ks.ask((t + 2) * KT, wave);
             }
-            settle<float, 8>(a, w, cur, r, mine, t0, valid);
+            settle<float>(w, cur, valid, draft);
             w.raise(cur, Elem<float>::slack);
             __syncthreads();
             if (more && k_plain(t + 1) && v_plain(t)) {

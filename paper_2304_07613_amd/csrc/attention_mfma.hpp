@@ -958,32 +958,42 @@ __global__ __launch_bounds__(kBlock) void k_attn_join(AttnArgs a) {
     if (!find_place<TR>(one, blockIdx.x, at)) return;
     const RowTile &r = at.rows;
     const int tile = at.tile, head = at.head;
-    __shared__ float weights[kAttnMostSplits][TR], inverse[TR];
+    // of every part and row (as much LDS as there are parts: 2 workgroups fewer a
+    // compute unit cost the join of 8 parts 5 us)
+    extern __shared__ float join_lds[];
+    float(*weights)[TR] = (float(*)[TR])join_lds;
+    float(*totals)[TR] = weights + a.splits;
     const int64_t step = (int64_t)a.kv_heads * a.tiles * ((DP + 2) * TR);
     const float *part = part_at<DP, TR>(a, 0, head, tile);
-    if (threadIdx.x < TR) {
-        const int i = threadIdx.x;
-        float top = -INFINITY, all = 0.f;
-        for (int s = 0; s < a.splits; ++s) top = fmaxf(top, part[s * step + DP * TR + i]);
-        for (int s = 0; s < a.splits; ++s) {
-            const float m = part[s * step + DP * TR + i];
-            const float f = m == -INFINITY ? 0.f : exp2_fast(m - top);
-            weights[s][i] = f;
-            all += f * part[s * step + (DP + 1) * TR + i];
-        }
-        inverse[i] = all == 0.f ? 0.f : 1.f / all;
+    // every part's maxima and totals at once
+    for (int x = threadIdx.x; x < a.splits * TR; x += kBlock) {
+        weights[x / TR][x % TR] = part[(x / TR) * step + DP * TR + x % TR];
+        totals[x / TR][x % TR] = part[(x / TR) * step + (DP + 1) * TR + x % TR];
     }
     __syncthreads();
     const int i = threadIdx.x % TR;
+    if (threadIdx.x < TR) {
+        float top = -INFINITY, all = 0.f;
+        for (int s = 0; s < a.splits; ++s) top = fmaxf(top, weights[s][i]);
+        for (int s = 0; s < a.splits; ++s) {
+            const float m = weights[s][i];
+            const float f = m == -INFINITY ? 0.f : exp2_fast(m - top);
+            weights[s][i] = f;
+            all += f * totals[s][i];
+        }
+        totals[0][i] = all == 0.f ? 0.f : 1.f / all;
+    }
+    __syncthreads();
     const RowAt mine = row_at<TR>(a, r, i);
     if (!mine.valid) return;
+    const float inverse = totals[0][i];
     T *out = (T *)a.O + (int64_t)(head * a.share + mine.g) * a.D * a.ldo + mine.column;
     const int d0 = blockIdx.y * kJoinRows;
     for (int d = d0 + threadIdx.x / TR; d < d0 + kJoinRows && d < a.D; d += kBlock / TR) {
         float x = 0.f;
 #pragma unroll 8
         for (int s = 0; s < a.splits; ++s) x += weights[s][i] * part[s * step + d * TR + i];
-        out[d * a.ldo] = (T)(x * inverse[i]);
+        out[d * a.ldo] = (T)(x * inverse);
     }
 }
 
@@ -997,12 +1007,14 @@ nmg_status launch_attn_dim(const AttnArgs &a, bool shared, AttnRows how, hipStre
     if (a.splits > 1) {
         const dim3 join((unsigned)(a.tiles * a.kv_heads),
                         (unsigned)((a.D + kJoinRows - 1) / kJoinRows));
+        const int tr = shared ? kAttnSharedRows : kAttnSplitRows;
+        const size_t lds = (size_t)a.splits * tr * 2 * sizeof(float);  // 64 KB at most
         if (shared)
-            hipLaunchKernelGGL((k_attn_join<T, DP, kAttnSharedRows>), join, dim3(kBlock), 0,
+            hipLaunchKernelGGL((k_attn_join<T, DP, kAttnSharedRows>), join, dim3(kBlock), lds,
                                stream, a);
         else
-            hipLaunchKernelGGL((k_attn_join<T, DP, kAttnSplitRows>), join, dim3(kBlock), 0, stream,
-                               a);
+            hipLaunchKernelGGL((k_attn_join<T, DP, kAttnSplitRows>), join, dim3(kBlock), lds,
+                               stream, a);
     }
     return launched();
 }

@@ -35,7 +35,7 @@ Plan plan_of(nmg_dtype dtype, const AttnArgs &a) {
     // item's sums written and read: for 512 of 128 rows about 8 steps) and a launch.
     p.splits = 1;
     int64_t best = INT64_MAX;
-    for (int64_t s = 1; s <= kAttnMostSplits && (s == 1 || steps / s >= 4); ++s) {
+    for (int64_t s = 1; s <= kAttnMostSplits && (s == 1 || steps / s >= (p.shared ? 4 : 1)); ++s) {
         const int64_t rounds = (items * s + slots - 1) / slots;
         const int64_t cost = 8 * rounds * ((steps + s - 1) / s + 2) +
                              (s > 1 ? items * s * (p.shared ? 64 : 16) / slots + 40 : 0);

@@ -25,6 +25,7 @@ struct AttnArgs {
     // the plan of the launch
     int32_t tiles;                   // row tiles of one key head, at most
     int32_t splits;                  // parts of every key range
+    int32_t join_rows;               // splits > 1: rows of a head a joining workgroup takes
     int32_t align;                   // key tiles start at a multiple of this column
     float *part;                     // splits > 1: sums, maxima and totals of every part
 };

@@ -948,8 +948,7 @@ __global__ __launch_bounds__(64 * split_waves<DP>(), 1) void k_attn_split(AttnAr
 }
 
 // Parts of every key range, in their order, to outputs: a workgroup per (tile,
-// head, kJoinRows rows of the head)
-constexpr int kJoinRows = 16;
+// head, a.join_rows rows of the head)
 template <typename T, int DP, int TR>
 __global__ __launch_bounds__(kBlock) void k_attn_join(AttnArgs a) {
     AttnArgs one = a;
@@ -988,8 +987,8 @@ __global__ __launch_bounds__(kBlock) void k_attn_join(AttnArgs a) {
     if (!mine.valid) return;
     const float inverse = totals[0][i];
     T *out = (T *)a.O + (int64_t)(head * a.share + mine.g) * a.D * a.ldo + mine.column;
-    const int d0 = blockIdx.y * kJoinRows;
-    for (int d = d0 + threadIdx.x / TR; d < d0 + kJoinRows && d < a.D; d += kBlock / TR) {
+    const int d0 = blockIdx.y * a.join_rows;
+    for (int d = d0 + threadIdx.x / TR; d < d0 + a.join_rows && d < a.D; d += kBlock / TR) {
         float x = 0.f;
 #pragma unroll 8
         for (int s = 0; s < a.splits; ++s) x += weights[s][i] * part[s * step + d * TR + i];
@@ -1006,7 +1005,7 @@ nmg_status launch_attn_dim(const AttnArgs &a, bool shared, AttnRows how, hipStre
     launch_main<T, DP>(a, shared, how, dim3((unsigned)(a.tiles * a.splits * a.kv_heads)), stream);
     if (a.splits > 1) {
         const dim3 join((unsigned)(a.tiles * a.kv_heads),
-                        (unsigned)((a.D + kJoinRows - 1) / kJoinRows));
+                        (unsigned)((a.D + a.join_rows - 1) / a.join_rows));
         const int tr = shared ? kAttnSharedRows : kAttnSplitRows;
         const size_t lds = (size_t)a.splits * tr * 2 * sizeof(float);  // 64 KB at most
         if (shared)

@@ -66,6 +66,11 @@ nmg_status launch_attention(nmg_dtype dtype, const AttnArgs &args, void *workspa
     a.tiles = (int32_t)p.tiles;
     a.splits = (int32_t)splits;
     a.part = (float *)workspace;
+    // a joining thread waits for every row it takes: one each, until that is more than
+    // about 8 workgroups for every compute unit, which read the parts' maxima again
+    a.join_rows = kBlock / (p.shared ? kAttnSharedRows : kAttnSplitRows);
+    while (a.join_rows < 32 && p.tiles * a.kv_heads * a.D / a.join_rows > 8 * device_cus())
+        a.join_rows *= 2;
     const int64_t es = (int64_t)elem_size(dtype);
     auto rows_at = [&](int64_t to) {  // rows of K and V start at multiples of `to` bytes
         return aligned(a.K, to) && aligned(a.V, to) && a.ldk * es % to == 0 && a.ldv * es % to == 0;

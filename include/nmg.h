@@ -589,6 +589,7 @@ typedef struct nmg_sequences {
  * key, or all of whose scores are minus infinity, gives 0.  scale > 0.
  * Statistics and sums are binary32; binary16 weights are rounded to binary16
  * for the product with V.  O overlaps no input.  Nk may be 0 (K, V unused).
+ * NMG_ERR_UNSUPPORTED: head_dim > 256, or rows of K or V of 2^28 bytes or more.
  *
  * workspace (may be NULL; 256-byte aligned): lets few queries over many keys be
  * split over the GPU.  Too little of it: fewer splits, none with 0.  The number

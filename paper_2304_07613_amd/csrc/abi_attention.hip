@@ -193,7 +193,8 @@ nmg_status nmg_tree_attention(const nmg_heads *heads, const nmg_sequences *seque
                               void *workspace, int64_t workspace_bytes, hipStream_t stream) {
     if (!tree) return NMG_ERR_NULL;
     if (width < 1 || ldtree < width) return NMG_ERR_PARAM;
-    if (Nq > 0 && ldtree > INT32_MAX / Nq) return NMG_ERR_UNSUPPORTED;  // offsets of 31 bits
+    if (Nq > 0 && Nq <= INT32_MAX && ldtree > INT32_MAX / Nq)
+        return NMG_ERR_UNSUPPORTED;  // offsets of 31 bits
     return run_attention(heads, sequences, Q, ldq, Nq, K, ldk, V, ldv, Nk, nullptr, tree, ldtree,
                          (int32_t)width, scale, O, ldo, workspace, workspace_bytes, stream);
 }

@@ -564,6 +564,36 @@ def test_operators_in_a_graph_on_another_stream(dev):
         assert torch.equal(y, step())
 
 
+@gpu
+@pytest.mark.parametrize("dtype", ["f32", "f16"])
+@pytest.mark.parametrize("longest", [3, 60])
+def test_attention_many_sequences(dev, dtype, longest):
+    """More sequences than a wave has lanes, some without queries or keys."""
+    rng = np.random.default_rng(longest)
+    q_lens = rng.integers(0, longest + 1, 150).tolist()
+    kv_lens = rng.integers(0, 90, 150).tolist()
+    q_lens[64], q_lens[149], kv_lens[149] = longest, longest, 70
+    run_attention(dev, dtype, 4, 2, 32, q_lens, kv_lens, "dense", seed=2)
+
+
+@gpu
+@pytest.mark.parametrize("dtype,D", [("f16", 64), ("f16", 128), ("f32", 64)])
+def test_attention_repeats(dev, dtype, D):
+    """Every pass over a full GPU gives the same bits, and those of its sequences
+    alone: no result depends on when copies land."""
+    H, n, B = 8, 640, 12
+    q, k, v = (rand(i, H * D, B * n).to(DT[dtype]).to(dev) for i in (1, 2, 3))
+    i32 = lambda t: torch.tensor(t, dtype=torch.int32, device=dev)
+    off = i32([n * b for b in range(B + 1)])
+    first = nmg.attention(q, k, v, H, H, off, off[:-1].contiguous(), off[1:].contiguous())
+    for _ in range(20):
+        assert torch.equal(first, nmg.attention(q, k, v, H, H, off, off[:-1].contiguous(),
+                                                off[1:].contiguous()))
+    one = nmg.attention(q[:, :n].contiguous(), k, v, H, H, i32([0, n]), i32([0]), i32([n]))
+    tol = 2.0 ** -9 if dtype == "f16" else 2.0 ** -17
+    assert (one.float() - first[:, :n].float()).abs().max() <= tol * first.abs().max()
+
+
 # ------------------------------------------------------------------- refusals
 
 def test_rotary_refusals(lib):
@@ -684,3 +714,33 @@ def test_binding_refusals(dev):
     for tree in (torch.ones((5, 6), dtype=torch.bool, device=dev), torch.ones((6, 6), device=dev)):
         with pytest.raises(ValueError):
             nmg.tree_attention(**kw, tree=tree)
+
+
+def test_attention_size_limits(lib):
+    """Rows of K or V of 2^28 bytes, and trees of 2^31, do not fit the kernels'
+    offsets."""
+    p = ctypes.c_void_p(1 << 20)
+
+    def call(ldk, D=64, dtype=nmg.F16, ldt=None):
+        h, s = nmg._Heads(1, 1, D, dtype), nmg._Sequences(1, 1 << 20, 1 << 20, 1 << 20)
+        args = (h, s, p, 4, 4, p, ldk, p, 16, 16)
+        if ldt is None:
+            return lib.nmg_attention(*args, None, 0.125, p, 4, None, 0, None)
+        return lib.nmg_tree_attention(*args, p, ldt, 4, 0.125, p, 4, None, 0, None)
+
+    assert call(1 << 28) == call(1 << 27, dtype=nmg.F32) == nmg.ERR_UNSUPPORTED
+    assert call(16, ldt=1 << 29) == nmg.ERR_UNSUPPORTED
+
+
+@gpu
+def test_binding_counts_arguments(dev):
+    """The compiled marshalling refuses what is not a tensor or a number."""
+    x, table = torch.zeros(64, 4, device=dev), torch.zeros(2, 32, 8, device=dev)
+    pos = torch.zeros(4, dtype=torch.int32, device=dev)
+    for bad in (dict(X=[1, 2]), dict(heads="a"), dict(table=3), dict(positions=None), dict(heads=1.5)):
+        with pytest.raises(TypeError):
+            nmg.rotary(**{**dict(X=x, heads=1, table=table, positions=pos), **bad})
+    with pytest.raises(ValueError):
+        nmg.rotary(x, 1, table, pos, layout=None)
+    with pytest.raises(ValueError):
+        nmg.rotary(x, 1 << 40, table, pos)

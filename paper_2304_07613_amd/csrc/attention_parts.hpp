@@ -12,8 +12,10 @@
 // as fast.
 //
 // Infinities and NaN have no such parts (infinity x 0 among the six products is
-// NaN).  A tile of K or V that holds one anywhere, or a wave whose queries do,
-// takes its product from memory by the binary32 instructions instead.
+// NaN), and the instructions take subnormal parts as 0, which the last part of a
+// number below 2^-103 can be.  A tile of K or V that holds such a number
+// anywhere, or a wave whose queries do, takes its product from memory by the
+// binary32 instructions instead.
 //
 // Otherwise as k_attn_shared: 4 waves of 32 rows, scores of the next tile taken
 // while this one's become weights.  Tiles are 32 keys; a staged row is 3 x 64
@@ -60,9 +62,21 @@ __device__ __forceinline__ void split2(float x, float y, uint32_t (&part)[3]) {
     part[2] = upper_halves(x2, y2);
 }
 
-__device__ __forceinline__ bool not_finite(float x) {
-    return (__float_as_uint(x) & 0x7f800000u) == 0x7f800000u;
-}
+// Whether among some numbers one is infinite, NaN, or not 0 and below 2^-103
+struct Odd {
+    uint32_t least = ~0u;  // of 2 |x| - 1 as the numbers' bits, for 0 the greatest there is
+    bool special = false;
+
+    __device__ __forceinline__ void add(float x) {
+        least = min(least, 2 * __float_as_uint(x) - 1);
+        special |= __builtin_amdgcn_classf(x, 0x207);
+    }
+
+    // for the whole wave
+    __device__ __forceinline__ bool any() const {
+        return __any(special || least < (2u * (127 - 103) << 23) - 1);
+    }
+};
 
 // The 6 of the 9 products of parts that are taken, the smallest first
 constexpr int kPairs[6][2] = {{2, 0}, {0, 2}, {1, 1}, {1, 0}, {0, 1}, {0, 0}};
@@ -88,10 +102,10 @@ struct PartStager {
                 hold[i] = __builtin_bit_cast(v4f, load16_buf(r, off + row));
             });
     }
-    // true if one of this wave's numbers is infinite or NaN
+    // true if one of this wave's numbers has no parts
     __device__ __forceinline__ bool put(lds_char *lds, int wave) {
         const int lane = threadIdx.x & 63;
-        bool bad = false;
+        Odd odd;
 #pragma unroll
         for (int i = 0; i < kGroups; ++i) {
             const int row = 8 * (4 * i + wave) + (lane >> 3);
@@ -104,9 +118,9 @@ struct PartStager {
             for (int p = 0; p < 3; ++p)
                 *(__attribute__((address_space(3))) u2 *)(at + p * kPartBytes) = u2{a[p], b[p]};
 #pragma unroll
-            for (int k = 0; k < 4; ++k) bad |= not_finite(hold[i][k]);
+            for (int k = 0; k < 4; ++k) odd.add(hold[i][k]);
         }
-        return __any(bad);
+        return odd.any();
     }
 };
 
@@ -121,7 +135,7 @@ struct PartRows : RowSums<DP, 1, true> {
         b8 p[3][2];  // part, step of 16 keys
     };
     b8 q[3][QF];
-    bool plain;      // no infinity or NaN among the wave's queries
+    bool plain;      // all of the wave's queries have parts
 
     static __device__ __forceinline__ void parts8(const float (&x)[8], b8 &p0, b8 &p1, b8 &p2) {
         u4 w[3];
@@ -141,7 +155,7 @@ struct PartRows : RowSums<DP, 1, true> {
         const int h = (threadIdx.x & 63) >> 5;
         const float *src =
             (const float *)a.Q + (int64_t)(kv_head * a.share + r.g) * a.D * a.ldq + r.column;
-        bool bad = false;
+        Odd odd;
 #pragma unroll
         for (int c = 0; c < QF; ++c) {
             float x[8];
@@ -150,11 +164,11 @@ struct PartRows : RowSums<DP, 1, true> {
                 const int d = 16 * c + 8 * h + e;
                 const float v = src[min(d, a.D - 1) * a.ldq];
                 x[e] = d < a.D ? v : 0.f;
-                bad |= not_finite(x[e]);
+                odd.add(x[e]);
             }
             parts8(x, q[0][c], q[1][c], q[2][c]);
         }
-        plain = !__any(bad);
+        plain = !odd.any();
     }
 
     __device__ __forceinline__ void scores(Scores &x, lds_char *k) const {
@@ -254,7 +268,8 @@ __global__ __launch_bounds__(256, DP <= 64 && !WIDE ? 2 : 1) void k_attn_parts(A
     constexpr int kTile = DP * kPartRow;
     __shared__ __attribute__((aligned(1024))) char lds_k[2 * kTile];
     __shared__ __attribute__((aligned(1024))) char lds_v[2 * kTile];
-    __shared__ int odd[2][2];  // the last even, odd tile of K, of V, that holds an infinity or NaN
+    // the last even, odd tile of K, of V, that holds a number without parts
+    __shared__ int odd[2][2];
     Place at;
     if (!find_place<TR>(a, blockIdx.x, at)) return;
     const RowTile &r = at.rows;

@@ -565,6 +565,20 @@ def test_operators_in_a_graph_on_another_stream(dev):
 
 
 @gpu
+@pytest.mark.parametrize("q_len", [1, 70])
+@pytest.mark.parametrize("scales", [(1, 1, 1e-30), (1, 1, 1e-33), (1, 1, 1e-36), (1, 1, 1e35), (1e20, 1e-20, 1),
+                                    (1e-33, 1e33, 1), (1e30, 1e-30, 1e-34)])
+def test_attention_magnitudes(dev, q_len, scales):
+    """Binary32 keeps its precision at any magnitude of queries, keys and values."""
+    D, n = 64, 200
+    q, k, v = (rand(i, D, c) * np.float32(f) for i, c, f in zip((1, 2, 3), (q_len, n, n), scales))
+    ints = [torch.tensor(t, dtype=torch.int32, device=dev) for t in ([0, q_len], [0], [n])]
+    got = nmg.attention(q.to(dev), k.to(dev), v.to(dev), 1, 1, *ints)
+    n64 = [t.double().numpy() for t in (q, k, v)]
+    check_attention(got, attend64(*n64, 1, 1, [0, q_len], [0], [n]), n64[2], "f32")
+
+
+@gpu
 @pytest.mark.parametrize("dtype", ["f32", "f16"])
 @pytest.mark.parametrize("longest", [3, 60])
 def test_attention_many_sequences(dev, dtype, longest):

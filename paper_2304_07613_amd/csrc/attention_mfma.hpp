@@ -698,7 +698,7 @@ __device__ __forceinline__ void interleave() {
 // (part, head, tile)
 template <int DP, int TR>
 __device__ __forceinline__ float *part_at(const AttnArgs &a, int part, int head, int tile) {
-    return a.part + ((int64_t)(part * a.kv_heads + head) * a.tiles + tile) * ((DP + 2) * TR);
+    return a.part + (((int64_t)part * a.kv_heads + head) * a.tiles + tile) * ((DP + 2) * TR);
 }
 
 // The end of a wave of 32 rows: its outputs, or its part of them

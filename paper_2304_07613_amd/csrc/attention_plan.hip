@@ -62,7 +62,7 @@ nmg_status launch_attention(nmg_dtype dtype, const AttnArgs &args, void *workspa
     const Plan p = plan_of(dtype, a);
     int64_t splits = std::min<int64_t>(p.splits, workspace_bytes / p.part_bytes);
     if (splits < 2) splits = 1;
-    if (p.tiles * splits * a.kv_heads > INT32_MAX || a.kv_heads > 65535) return NMG_ERR_UNSUPPORTED;
+    if (p.tiles * splits * a.kv_heads > INT32_MAX) return NMG_ERR_UNSUPPORTED;
     a.tiles = (int32_t)p.tiles;
     a.splits = (int32_t)splits;
     a.part = (float *)workspace;

@@ -290,9 +290,10 @@ __device__ __forceinline__ void wait_lds() {
 }
 
 // All but the last n of this wave's copies into LDS have landed and its LDS
-// accesses are done, then the workgroup barrier.  The wait is spelled out: the one the compiler puts before
-// __syncthreads() counts copies into LDS among other memory operations, and at
-// the head of a loop that count can leave copies of the loop's end in flight.
+// accesses are done, then the workgroup barrier.  The wait is spelled out: the one
+// the compiler puts before __syncthreads() counts copies into LDS among other memory
+// operations, and at the head of a loop that count can leave copies of the loop's end
+// in flight.
 template <int n = 0>
 __device__ __forceinline__ void landed_barrier() {
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -734,6 +735,13 @@ __device__ __forceinline__ void finish(const AttnArgs &a, const Place &at, const
         }
 }
 
+// 4 waves of 32 rows over shared key tiles.  128 rows read a key tile once: 128 D
+// multiplications a byte of K or V from L2, so the matrix pipe is the bound where
+// there are workgroups enough: 16 / 4 heads x 128, 4096 columns over 16384 keys, 520 us
+// = 1060 TFLOP/s (a large library product 1330), matrix instructions in 65% of the
+// cycles, the rest the softmax's vector instructions that find no matrix instruction
+// beside them.  2 workgroups on a compute unit: one's barriers and first tiles lie
+// under the other's steps (a third: 515 -> 543 us).
 template <typename T, int DP, AttnRows HOW>
 __global__ __launch_bounds__(256, DP <= (HOW == kAttnShift ? 96 : 128) ? 2 : 1) void k_attn_shared(AttnArgs a) {
     constexpr int TR = kAttnSharedRows, KT = Elem<T>::keys, kTile = DP * kRowBytes;
@@ -838,7 +846,13 @@ __global__ __launch_bounds__(256, DP <= (HOW == kAttnShift ? 96 : 128) ? 2 : 1) 
     finish<T, DP>(a, at, mine, w, wave);
 }
 
-// Waves of a workgroup that splits the keys: as many as 128 KB hold tiles of
+// The waves of a workgroup split the keys of 32 rows, and join over LDS at the end.
+// For few rows: what counts are the bytes of K and V, and before them the chain of
+// loads a workgroup starts with.  32 / 8 heads x 128, 16 sequences of 1 column over 8192
+// keys: 127 us = 4.2 TB/s (a large copy 4.9); 12 heads x 64, 8 of 1 over 512: 7.4 us,
+// most of it the launch, the places and the join.  No barriers before the join: the
+// waves' copies run apart, two tiles a wave on the way.
+// Waves: as many as 128 KB hold tiles of
 template <int DP> constexpr int split_waves() { return DP <= 64 ? 8 : DP <= 128 ? 4 : 2; }
 
 template <typename T, int DP, AttnRows HOW>
@@ -948,7 +962,9 @@ __global__ __launch_bounds__(64 * split_waves<DP>(), 1) void k_attn_split(AttnAr
 }
 
 // Parts of every key range, in their order, to outputs: a workgroup per (tile,
-// head, a.join_rows rows of the head)
+// head, a.join_rows rows of the head).  Reads every part once (32 heads x 128, 252
+// columns in 8 parts: 34 MB, 11 us); few rows wait for two chains of loads, maxima and
+// sums, 3-4 us with the launch.
 template <typename T, int DP, int TR>
 __global__ __launch_bounds__(kBlock) void k_attn_join(AttnArgs a) {
     AttnArgs one = a;

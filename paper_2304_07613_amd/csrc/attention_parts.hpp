@@ -9,7 +9,12 @@
 // |x y| and 2^-24 in the mean, of the product's sign, so that most of it goes
 // with the division by the sum of the weights.  bfloat16 has binary32's range:
 // no scaling.  Six products at 16 times the binary32 matrix rate are 2.7 times
-// as fast.
+// as fast.  12 heads x 64, 8 sequences of 1024 columns over 1024 keys: 153 us = 168
+// TFLOP/s (a large binary32 library product 154).  The splitting of K, V and the
+// weights into parts is vector work beside the matrix instructions, and the bound
+// where there are many workgroups; with one a compute unit (the same heads, 250
+// columns over ranges up to 701 keys: 51 us) it is each workgroup's own chain of
+// tiles, with matrix instructions in 17% of the cycles.
 //
 // Infinities and NaN have no such parts (infinity x 0 among the six products is
 // NaN), and the instructions take subnormal parts as 0, which the last part of a

@@ -16,23 +16,36 @@ struct Plan {
 Plan plan_of(nmg_dtype dtype, const AttnArgs &a) {
     Plan p;
     const int64_t rows = (int64_t)a.Nq * a.share;
-    // one wave's rows cover the average sequence: split the keys over the waves
-    p.shared = rows > (int64_t)kAttnSplitRows * a.sequences;
+    const int64_t each = (rows + a.sequences - 1) / a.sequences;  // of equal sequences
+    const int64_t keys = (a.Nk + a.sequences - 1) / a.sequences;  // that share Nk
+    const int dp = attn_padded_dim(a.D);
+    const int kt = dtype == NMG_F16 ? 64 : 32;
+    // One or two waves' rows cover a sequence: the waves of a workgroup split the keys
+    // rather than the rows, while a compute unit has one such workgroup to run (12 heads
+    // x 64, 512 keys: 8 sequences of 64 columns 11.7 -> 7.4 us, of 128 11.7 -> 13.3; 64 of
+    // 64 23 -> 41).  With more of them one wave's rows, and keys enough that the waves
+    // are worth their start (64 sequences of 1 column: binary16 with 512 keys 22 -> 25 us,
+    // 2048 81 -> 79, binary32 with 128 30 -> 23; 256 of 64 75 -> 92); always for heads
+    // over 128, of which a compute unit holds one workgroup either way (8 x 256, 64
+    // sequences, 256 keys: 51 -> 47).
+    const int64_t few = (each + kAttnSplitRows - 1) / kAttnSplitRows;
+    const bool once = few <= 2 && few * a.sequences <= device_cus() / a.kv_heads;
+    const int64_t enough = dtype == NMG_F16 ? 1024 : 128;
+    p.shared = !once && !(few <= 1 && (dp > 128 || keys >= enough));
     const int tr = p.shared ? kAttnSharedRows : kAttnSplitRows;
     // sum of ceil(rows_b / tr) over sequences that hold `rows` rows together: at most ...
     p.tiles = a.sequences == 1 ? (rows + tr - 1) / tr : std::min(rows / tr + a.sequences, rows);
     // ... and for equal lengths
-    const int64_t each = (rows + a.sequences - 1) / a.sequences;
     const int64_t items = std::min((each + tr - 1) / tr * a.sequences, p.tiles) * a.kv_heads;
-    const int dp = attn_padded_dim(a.D);
-    const int kt = dtype == NMG_F16 ? 64 : 32;
-    const int64_t keys = (a.Nk + a.sequences - 1) / a.sequences;  // of a sequence, if they share Nk
     const int waves = p.shared ? 1 : dp <= 64 ? 8 : dp <= 128 ? 4 : 2;  // that split a part's keys
     const int64_t steps = (keys + (int64_t)kt * waves - 1) / (kt * waves);
     const int64_t slots = (int64_t)device_cus() * (p.shared ? 2 : 1);
     // The split that ends first, in steps of one key tile: rounds of workgroups
     // times (its steps + about 2 to start), and with parts their traffic (an
     // item's sums written and read: for 512 of 128 rows about 8 steps) and a launch.
+    // (One part against the split taken: 12 heads x 64, 1 column over 8192 keys 26 ->
+    // 12.6 us; 32 / 8 x 128, 1 over 32768 243 -> 33, 4 of 63 over 32768 601 -> 188; 16 x
+    // 64, 512 over 16384 218 -> 58; binary32 12 x 64, 256 over 8192 507 -> 61.)
     p.splits = 1;
     int64_t best = INT64_MAX;
     for (int64_t s = 1; s <= kAttnMostSplits && (s == 1 || steps / s >= (p.shared ? 4 : 1)); ++s) {

@@ -608,6 +608,29 @@ def test_attention_repeats(dev, dtype, D):
     assert (one.float() - first[:, :n].float()).abs().max() <= tol * first.abs().max()
 
 
+@gpu
+@pytest.mark.parametrize("dtype", ["f32", "f16"])
+def test_attention_many_rows(dev, dtype):
+    """Rows that several waves share, where the tests above have few a sequence."""
+    for heads, kv_heads, D, q_lens, kv_lens in [
+            (4, 2, 64, [65, 1, 90], [130, 20, 257]), (1, 1, 256, [100], [150]), (3, 1, 80, [40, 33], [77, 45]),
+            (2, 1, 96, [64], [129]), (4, 1, 33, [17], [66]), (2, 2, 1, [70], [9]), (12, 2, 64, [1] * 50, [70] * 50)]:
+        for how, gap in (("dense", 0), ("odd", 1)):
+            print(f"[rows] {heads}/{kv_heads} x {D}, q {q_lens} kv {kv_lens} {dtype} {how}", flush=True)
+            run_attention(dev, dtype, heads, kv_heads, D, q_lens, kv_lens, how, gap=gap, seed=D)
+    for D in (64, 80, 128):
+        test_attention_key_mask(dev, D, [130, 70, 65], dtype)
+    test_attention_past_32_bit_offsets(dev, dtype, 70)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["f32", "f16"])
+@pytest.mark.parametrize("heads,kv_heads,D,drafted,context", [
+    (6, 1, 64, [33, 2, 64], [0, 500, 1]), (8, 2, 80, [63, 17], [300, 5]), (1, 1, 256, [90], [40])])
+def test_tree_attention_many_rows(dev, heads, kv_heads, D, drafted, context, dtype):
+    test_tree_attention(dev, heads, kv_heads, D, drafted, context, dtype)
+
+
 # ------------------------------------------------------------------- refusals
 
 def test_rotary_refusals(lib):

@@ -1,4 +1,5 @@
-"""ctypes binding of ``libnmg.so`` (declared in ``include/nmg.h``).
+"""Binding of ``libnmg.so`` (declared in ``include/nmg.h``): ctypes, and a compiled
+module for the attention operators, whose calls are as short as their marshalling.
 
 Argument marshalling only: torch allocates the outputs on the input's device
 and supplies the current HIP stream; every step of the computation runs in the

@@ -39,7 +39,10 @@ Plan plan_of(nmg_dtype dtype, const AttnArgs &a) {
     const int64_t items = std::min((each + tr - 1) / tr * a.sequences, p.tiles) * a.kv_heads;
     const int waves = p.shared ? 1 : dp <= 64 ? 8 : dp <= 128 ? 4 : 2;  // that split a part's keys
     const int64_t steps = (keys + (int64_t)kt * waves - 1) / (kt * waves);
-    const int64_t slots = (int64_t)device_cus() * (p.shared ? 2 : 1);
+    // workgroups a compute unit holds (binary32 16 heads x 128, 2 sequences of 512
+    // columns over 1024 keys: 87 us in the 4 parts for two of them, 77 in 2 for one)
+    const int held = p.shared && dp <= (dtype == NMG_F16 ? 128 : 64) ? 2 : 1;
+    const int64_t slots = (int64_t)device_cus() * held;
     // The split that ends first, in steps of one key tile: rounds of workgroups
     // times (its steps + about 2 to start), and with parts their traffic (an
     // item's sums written and read: for 512 of 128 rows about 8 steps) and a launch.
@@ -51,7 +54,7 @@ Plan plan_of(nmg_dtype dtype, const AttnArgs &a) {
     for (int64_t s = 1; s <= kAttnMostSplits && (s == 1 || steps / s >= (p.shared ? 4 : 1)); ++s) {
         const int64_t rounds = (items * s + slots - 1) / slots;
         const int64_t cost = 8 * rounds * ((steps + s - 1) / s + 2) +
-                             (s > 1 ? items * s * (p.shared ? 64 : 16) / slots + 40 : 0);
+                             (s > 1 ? items * s * (p.shared ? 32 : 16) / device_cus() + 40 : 0);
         if (cost < best) {
             best = cost;
             p.splits = (int)s;

@@ -50,9 +50,9 @@ Plan plan_of(nmg_dtype dtype, const AttnArgs &a) {
     // 12.6 us; 32 / 8 x 128, 1 over 32768 243 -> 33, 4 of 63 over 32768 601 -> 188; 16 x
     // 64, 512 over 16384 218 -> 58; binary32 12 x 64, 256 over 8192 507 -> 61.)
     // A step is longer in binary32 (16 x 128, 2 of 512 over 600: 75 us with 40, 56), and of
-    // waves that split the keys the fewer they are, so the join (4 us) is fewer of them (32 / 8 x 128, 4 of 1 over
-    // 2000: 25.6 us with 40 and 16 for all, 18.4; binary32 12 x 64, 1 over 1000 22.9 and
-    // 14.6, 8 of 1 24.4 and 20.7).
+    // waves that split the keys the fewer they are, so the join (4 us) is fewer of them
+    // (32 / 8 x 128, 4 of 1 over 2000: 25.6 us with 40 and 16 for all, 18.4; binary32
+    // 12 x 64, 1 over 1000 22.9 and 14.6, 8 of 1 24.4 and 20.7).
     const bool f32 = dtype == NMG_F32;
     const int64_t traffic = p.shared ? 32 : f32 ? 8 : 16;
     const int64_t join = p.shared ? (f32 ? 30 : 40) : f32 ? 7 : dp <= 64 ? 32 : 14;

@@ -197,6 +197,20 @@ __device__ __forceinline__ int rarely(int v) {
     return v;
 }
 
+// The kernel's arguments, read again: what the code after a loop needs of them takes no
+// scalar registers in the loop.  (They are the kernel's only parameter.)
+__device__ __forceinline__ AttnArgs args_again() {
+#if defined(__HIP_DEVICE_COMPILE__)
+    auto p = (const __attribute__((address_space(4))) AttnArgs *)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(p));
+    AttnArgs a;
+    __builtin_memcpy(&a, (const void *)p, sizeof a);
+    return a;
+#else
+    return AttnArgs{};
+#endif
+}
+
 // Over a row's two lanes, lane and lane ^ 32
 __device__ __forceinline__ float larger_of_halves(float v) {
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -448,7 +462,8 @@ struct RowSums {
                 x.s[b][i] = (mine >> key_of(b, i, 0)) & 1 ? x.s[b][i] : -INFINITY;
     }
 
-    // The running maximum moves when a row's grew by more than `slack` powers of 2
+    // The running maximum of a row moves when it grew by more than `slack` powers of 2
+    // (its own alone: what it is rounded by does not depend on the wave's other rows)
     __device__ __forceinline__ void raise(const Scores &x, float slack) {
         float top = x.s[0][0];
 #pragma unroll
@@ -457,7 +472,7 @@ struct RowSums {
             for (int i = 0; i < 16; ++i) top = fmaxf(top, x.s[b][i]);
         top = larger_of_halves(top) * scale2;
         if (__any(top - m > slack)) {  // (nothing seen yet: m is -inf)
-            const float next = fmaxf(m, top);
+            const float next = top - m > slack ? top : m;
             const float keep = m == next ? 1.f : exp2_fast(m - next);
             l *= keep;
 #pragma unroll
@@ -595,12 +610,35 @@ __device__ __forceinline__ uint64_t valid_keys(const AttnArgs &a, int64_t t0, co
     return a.key_mask ? in & __ballot(mask_byte != 0) : in;
 }
 
+// Whether the tile's values in LDS hold an infinity or NaN: an exponent of ones and its
+// least bit carry into the bit above
+template <typename T, int DP>
+__device__ __forceinline__ bool values_not_finite(lds_char *v) {
+    constexpr uint32_t exponent = sizeof(T) == 2 ? 0x7c007c00u : 0x7f800000u;
+    constexpr uint32_t least = sizeof(T) == 2 ? 0x04000400u : 0x00800000u;
+    constexpr uint32_t above = sizeof(T) == 2 ? 0x80008000u : 0x80000000u;
+    lds_char *at = v + 16 * rarely(threadIdx.x & 63);
+    uint32_t any = 0;
+#pragma unroll 4
+    for (int i = 0; i < DP / 8; ++i) {
+        const u4 x = read16(at + 1024 * i);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) any |= (x[e] & exponent) + least;
+    }
+    return __any((any & above) != 0);
+}
+
 // Values of keys left out become 0 in LDS, whatever they hold (their weight is 0,
 // but 0 x NaN is not).  Every wave that reads the tile does it for itself: they
 // write the same bytes.
-template <typename T, int DP>
+// A drafted key is left out by some rows and not by others: where a tile with such keys
+// holds a value that is not finite (SPOILED), it becomes 0 for every row, and goes to
+// the rows that see it at the end (add_not_finite).  All in one go: a wave that finds
+// none any more finds the tile as the others leave it.
+template <typename T, int DP, bool SPOILED>
 __device__ __forceinline__ void clear_values(lds_char *v, uint64_t valid) {
     const int lane = rarely(threadIdx.x & 63);
+#pragma unroll SPOILED ? 1 : DP / 8
     for (int i = 0; i < DP / 8; ++i) {
         const int row = 8 * i + (lane >> 3);
         const int key = Elem<T>::per_chunk * ((lane & 7) ^ chunk_swizzle<T, true>(row));
@@ -609,11 +647,15 @@ __device__ __forceinline__ void clear_values(lds_char *v, uint64_t valid) {
         u4 x = read16(at);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            if constexpr (sizeof(T) == 2)
-                x[e] &= ((bits >> (2 * e)) & 1 ? 0xffffu : 0u) |
-                        ((bits >> (2 * e + 1)) & 1 ? 0xffff0000u : 0u);
-            else
-                x[e] = (bits >> e) & 1 ? x[e] : 0u;
+            if constexpr (sizeof(T) == 2) {
+                const bool lo = SPOILED && (x[e] & 0x7c00u) == 0x7c00u;
+                const bool hi = SPOILED && (x[e] & 0x7c000000u) == 0x7c000000u;
+                x[e] &= ((bits >> (2 * e)) & 1 && !lo ? 0xffffu : 0u) |
+                        ((bits >> (2 * e + 1)) & 1 && !hi ? 0xffff0000u : 0u);
+            } else {
+                const bool odd = SPOILED && (x[e] & 0x7f800000u) == 0x7f800000u;
+                x[e] = (bits >> e) & 1 && !odd ? x[e] : 0u;
+            }
         }
         write16(at, x);
     }
@@ -652,6 +694,57 @@ __device__ __forceinline__ Draft draft_at(const AttnArgs &a, const RowTile &r, c
         }
     }
     return x;
+}
+
+// Infinities and NaN as numbers whose sums over some keys tell which were among them:
+// 1 for infinity, 128 for minus infinity, both for NaN, 0 for what is finite
+__device__ __forceinline__ float code_of(float v) {
+    return v - v == 0.f ? 0.f : v == INFINITY ? 1.f : v == -INFINITY ? 128.f : 129.f;
+}
+
+// What is not finite of the draft's values in the tiles lo, lo + STEP .. below hi
+// (from column `first` on), to the sums of the rows that see its key: a product of 1
+// for a key that is seen and the value's code.  From memory, after the last tile: it
+// is rare, and in the loop its registers cost a workgroup a compute unit (32 sequences
+// of 1024 columns, 12 heads x 64: 135 -> 146 us).
+template <typename T, int DP, int STEP>
+__device__ __forceinline__ void add_not_finite(const AttnArgs &a, const RowTile &r, const RowAt &mine,
+                                               int head, int first, int lo, int hi,
+                                               f16v (&o)[DP / 32]) {
+    constexpr int KT = Elem<T>::keys;
+    const int lane = rarely(threadIdx.x & 63), h = lane >> 5;
+    const int64_t draft = (int64_t)r.end - r.n;  // its first column
+    const uint8_t *line = a.tree + rarely(mine.column) * a.ldtree;
+    const int64_t from = max((int64_t)lo * KT, (max(draft - first, (int64_t)0)) & ~15ll);
+    for (int64_t k = from; k < (int64_t)hi * KT; k += 16) {
+        if (STEP > 1 && ((int)(k / KT) - lo) % STEP) continue;
+        const int64_t key = first + k + 8 * h;
+        const int64_t i0 = key - draft;
+        h8 one;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const int64_t i = i0 + e;
+            one[e] = i >= 0 && i < a.width && key + e >= r.begin && key + e < r.end && line[i]
+                         ? (_Float16)1 : (_Float16)0;
+        }
+#pragma unroll
+        for (int d = 0; d < DP / 32; ++d) {
+            const int row = 32 * d + (lane & 31);
+            const T *src = (const T *)a.V + ((int64_t)head * a.D + row) * a.ldv + key;
+            h8 code;
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                code[e] = (_Float16)(row < a.D && key + e < r.end ? code_of((float)src[e]) : 0.f);
+            const f16v codes = mfma(code, one, f16v{});
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int n = (int)codes[i];
+                if (n & 127) o[d][i] += INFINITY;
+                if (n >> 7) o[d][i] -= INFINITY;
+            }
+            asm volatile("" ::: "memory");  // one block at a time: registers are short here
+        }
+    }
 }
 
 // Scores of keys that take no part in a tile become -inf; true when there are
@@ -741,9 +834,10 @@ __device__ __forceinline__ void finish(const AttnArgs &a, const Place &at, const
 // = 1060 TFLOP/s (a large library product 1330), matrix instructions in 65% of the
 // cycles, the rest the softmax's vector instructions that find no matrix instruction
 // beside them.  2 workgroups on a compute unit: one's barriers and first tiles lie
-// under the other's steps (a third: 515 -> 543 us).
+// under the other's steps (a third: 515 -> 543 us); heads up to 64 have room for a
+// third (32 sequences of 1024 columns, 12 heads x 64: 158 us with two, 143 with three).
 template <typename T, int DP, AttnRows HOW>
-__global__ __launch_bounds__(256, DP <= (HOW == kAttnShift ? 96 : 128) ? 2 : 1) void k_attn_shared(AttnArgs a) {
+__global__ __launch_bounds__(256, DP <= 64 && HOW != kAttnShift ? 3 : DP <= (HOW == kAttnShift ? 96 : 128) ? 2 : 1) void k_attn_shared(AttnArgs a) {
     constexpr int TR = kAttnSharedRows, KT = Elem<T>::keys, kTile = DP * kRowBytes;
     constexpr bool SHIFT = HOW == kAttnShift;
     // variables of their own: the compiler sees that reads of one do not touch
@@ -752,6 +846,7 @@ __global__ __launch_bounds__(256, DP <= (HOW == kAttnShift ? 96 : 128) ? 2 : 1) 
     __shared__ __attribute__((aligned(1024))) char lds_k1[kTile];
     __shared__ __attribute__((aligned(1024))) char lds_v0[kTile];
     __shared__ __attribute__((aligned(1024))) char lds_v1[kTile];
+    __shared__ int odd;  // a wave found a drafted value that is not finite
     Place at;
     if (!find_place<TR>(a, blockIdx.x, at)) return;
     const RowTile &r = at.rows;
@@ -765,6 +860,7 @@ __global__ __launch_bounds__(256, DP <= (HOW == kAttnShift ? 96 : 128) ? 2 : 1) 
     const int lo = (int)((int64_t)tiles * at.part / a.splits);
     const int hi = (int)((int64_t)tiles * (at.part + 1) / a.splits);
     if (lo < hi) {
+        if (threadIdx.x == 0) odd = 0;
         Stager<T, DP, false, HOW, 4> ks;
         Stager<T, DP, true, HOW, 4> vs;
         ks.init(a, a.K, a.ldk, at.head, first, wave);
@@ -790,8 +886,14 @@ __global__ __launch_bounds__(256, DP <= (HOW == kAttnShift ? 96 : 128) ? 2 : 1) 
                 if (t + 2 < hi) ks.ask((t + 2) * KT, k_cur, wave);
                 vs.ask((t + 1) * KT, v_nxt, wave);
             }
-            if (settle<T>(w, cur, valid, draft))
-                clear_values<T, DP>(v_cur, valid);
+            const bool clear = settle<T>(w, cur, valid, draft);
+            const bool spoiled = draft.here && values_not_finite<T, DP>(v_cur);
+            if (spoiled) {
+                odd = 1;
+                clear_values<T, DP, true>(v_cur, valid);
+            } else if (clear) {
+                clear_values<T, DP, false>(v_cur, valid);
+            }
             w.raise(cur, Elem<T>::slack);
             // before the other wave of the SIMD while the matrix pipe has work for
             // this one (4096 x 16384 at 128: 546 -> 515 us)
@@ -841,6 +943,11 @@ __global__ __launch_bounds__(256, DP <= (HOW == kAttnShift ? 96 : 128) ? 2 : 1) 
             step(on, t++, s1, s0, k1, k0, v1, v0);
         }
         step(off, t, s0, s1, k0, k1, last, v0);
+        if (a.tree) {
+            __syncthreads();
+            if (__builtin_amdgcn_readfirstlane(odd))
+                add_not_finite<T, DP, 1>(args_again(), r, mine, at.head, first, lo, hi, w.o);
+        }
     }
 
     finish<T, DP>(a, at, mine, w, wave);
@@ -882,6 +989,7 @@ __global__ __launch_bounds__(64 * split_waves<DP>(), 1) void k_attn_split(AttnAr
         constexpr int kCopies = DP / 8;
         ks.init(a, a.K, a.ldk, at.head, first, 0);
         vs.init(a, a.V, a.ldv, at.head, first, 0);
+        bool odd = false;  // the wave found a drafted value that is not finite
         ks.ask(lo * KT, k, 0);
         w.init(a, at.head, mine);
         uint8_t byte = mask_at(a, (int64_t)first + (int64_t)lo * KT);
@@ -912,7 +1020,13 @@ __global__ __launch_bounds__(64 * split_waves<DP>(), 1) void k_attn_split(AttnAr
                 else
                     wait_vm<0>();
             }
-            if (clear) clear_values<T, DP>(v, valid);
+            const bool spoiled = draft.here && values_not_finite<T, DP>(v);
+            if (spoiled) {
+                odd = true;
+                clear_values<T, DP, true>(v, valid);
+            } else if (clear) {
+                clear_values<T, DP, false>(v, valid);
+            }
             w.values(x, p, v);
             wait_lds();  // V's too
             if (more) {
@@ -920,6 +1034,7 @@ __global__ __launch_bounds__(64 * split_waves<DP>(), 1) void k_attn_split(AttnAr
                 vs.ask((t + W) * KT, v, 0);
             }
         }
+        if (odd) add_not_finite<T, DP, W>(a, r, mine, at.head, first, lo, hi, w.o);
     }
 
     // join the waves: maxima, then sums at the common maximum

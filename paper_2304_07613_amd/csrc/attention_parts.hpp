@@ -247,10 +247,11 @@ struct PartRows : RowSums<DP, 1, true> {
             }
         }
     }
-    // The same from memory, keys outside `valid` left out
+    // The same from memory, keys outside `valid` left out; `finite`: and what is not
+    // finite of the others (see clear_values)
     template <typename Head>
     __device__ __forceinline__ void values_exact(const Scores &x, const Head &v, int D, int at,
-                                                 uint64_t valid) {
+                                                 uint64_t valid, bool finite) {
         const int lane = rarely(threadIdx.x & 63), h = lane >> 5;
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
@@ -259,7 +260,8 @@ struct PartRows : RowSums<DP, 1, true> {
 #pragma unroll
             for (int d = 0; d < DP / 32; ++d) {
                 const int row = 32 * d + (lane & 31);
-                const float y = in && row < D ? ((const float *)(v.base + row * v.ld))[at + key] : 0.f;
+                float y = in && row < D ? ((const float *)(v.base + row * v.ld))[at + key] : 0.f;
+                if (finite && y - y != 0.f) y = 0.f;
                 o[d] = mfma(y, x.s[0][i], o[d]);
             }
             asm volatile("" ::: "memory");  // few loads at once: registers are short here
@@ -275,6 +277,7 @@ __global__ __launch_bounds__(256, DP <= 64 && !WIDE ? 2 : 1) void k_attn_parts(A
     __shared__ __attribute__((aligned(1024))) char lds_v[2 * kTile];
     // the last even, odd tile of K, of V, that holds a number without parts
     __shared__ int odd[2][2];
+    __shared__ int any_odd;  // there was one of V
     Place at;
     if (!find_place<TR>(a, blockIdx.x, at)) return;
     const RowTile &r = at.rows;
@@ -298,7 +301,7 @@ __global__ __launch_bounds__(256, DP <= 64 && !WIDE ? 2 : 1) void k_attn_parts(A
             if (ks.put(k_at(t), wave)) odd[0][t & 1] = t;
         };
         auto put_v = [&](int t) {
-            if (vs.put(v_at(t), wave)) odd[1][t & 1] = t;
+            if (vs.put(v_at(t), wave)) odd[1][t & 1] = t, any_odd = 1;
         };
         auto k_plain = [&](int t) {
             return w.plain && __builtin_amdgcn_readfirstlane(odd[0][t & 1]) != t;
@@ -314,6 +317,7 @@ __global__ __launch_bounds__(256, DP <= 64 && !WIDE ? 2 : 1) void k_attn_parts(A
         w.init(a, at.head, mine);
         uint8_t byte = mask_at(a, (int64_t)first + (int64_t)lo * KT);
         if (threadIdx.x < 4) odd[threadIdx.x >> 1][threadIdx.x & 1] = -1;
+        if (threadIdx.x == 4) any_odd = 0;
         __syncthreads();
         put_k(lo);
         vs.ask(lo * KT, wave);
@@ -348,10 +352,15 @@ __global__ __launch_bounds__(256, DP <= 64 && !WIDE ? 2 : 1) void k_attn_parts(A
                 if (v_plain(t))
                     w.values(p, v_at(t));
                 else
-                    w.values_exact(cur, vs.rows, a.D, t * KT, valid);
+                    w.values_exact(cur, vs.rows, a.D, t * KT, valid, a.tree && r.end - r.n - t0 < KT);
                 if (more) scores_at(t + 1, nxt);
             }
             cur = nxt;
+        }
+        if (a.tree) {
+            __syncthreads();
+            if (__builtin_amdgcn_readfirstlane(any_odd))
+                add_not_finite<float, DP, 1>(args_again(), r, mine, at.head, first, lo, hi, w.o);
         }
     }
     finish<float, DP>(a, at, mine, w, wave);

@@ -587,7 +587,8 @@ typedef struct nmg_sequences {
  * columns attend to its key columns j with key_mask[j] != 0 (Nk bytes; NULL: to
  * all).  What other columns of K and V hold never matters.  A query with no
  * key, or all of whose scores are minus infinity, gives 0.  scale > 0.
- * Statistics and sums are binary32; binary16 weights are rounded to binary16
+ * Statistics and sums are binary32 (a product q . k past its range is infinite;
+ * values may be of any size in it); binary16 weights are rounded to binary16
  * for the product with V.  O overlaps no input.  Nk may be 0 (K, V unused).
  * NMG_ERR_UNSUPPORTED: head_dim > 256, or rows of K or V of 2^28 bytes or more.
  *

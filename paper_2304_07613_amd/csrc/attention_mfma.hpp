@@ -197,8 +197,8 @@ __device__ __forceinline__ int rarely(int v) {
     return v;
 }
 
-// The kernel's arguments, read again: what the code after a loop needs of them takes no
-// scalar registers in the loop.  (They are the kernel's only parameter.)
+// The kernel's arguments, read again: what rarely run code needs of them takes no
+// registers in the loop around it.  (They are the kernel's only parameter.)
 __device__ __forceinline__ AttnArgs args_again() {
 #if defined(__HIP_DEVICE_COMPILE__)
     auto p = (const __attribute__((address_space(4))) AttnArgs *)__builtin_amdgcn_kernarg_segment_ptr();
@@ -226,6 +226,14 @@ __device__ __forceinline__ float sum_of_halves(float v) { return v + __shfl_xor(
 __device__ __forceinline__ float exp2_fast(float v) {
 #if defined(__HIP_DEVICE_COMPILE__)
     return __builtin_amdgcn_exp2f(v);
+#else
+    return v;
+#endif
+}
+
+__device__ __forceinline__ float log2_fast(float v) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    return __builtin_amdgcn_logf(v);
 #else
     return v;
 #endif
@@ -434,6 +442,7 @@ struct RowSums {
     struct Scores {
         f16v s[KB];
     };
+    static constexpr bool wide = WIDE;
     f16v o[DP / 32];
     float m, l;        // running maximum (of scores times log2 e), sum of the lane's weights
     float scale2;      // scale * log2 e
@@ -479,6 +488,37 @@ struct RowSums {
             for (int i = 0; i < DP / 32; ++i) o[i] *= keep;
             m = next;
         }
+    }
+
+    // Sums of binary32 values near the end of the range pass it before they are divided:
+    // they are of weights up to 2^slack, and of as many as there are keys.  The loop over
+    // the keys does not look; where it ends with a sum that is not finite, though the
+    // row's weights are, leveled_rows takes the keys again, with the running maximum
+    // raised before each tile's weights until all so far sum to 1/4: no sum passes the
+    // largest value.
+    __device__ __forceinline__ bool overflowed() const {
+        float sum = 0.f;  // NaN if one of them is not finite
+#pragma unroll
+        for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) sum = fmaf(o[d][i], 0.f, sum);
+        const float total = sum_of_halves(l);
+        return !(sum == 0.f) && total - total == 0.f;
+    }
+    __device__ __forceinline__ void level(const Scores &x) {
+        const float base = m == -INFINITY ? 0.f : m;
+        float sum = l;
+#pragma unroll
+        for (int b = 0; b < KB; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) sum += exp2_fast(fmaf(x.s[b][i], scale2, -base));
+        sum = sum_of_halves(sum);
+        const float next = sum > 0.25f ? m + log2_fast(4.f * sum) : m;
+        const float keep = m == next ? 1.f : exp2_fast(m - next);
+        l *= keep;
+#pragma unroll
+        for (int d = 0; d < DP / 32; ++d) o[d] *= keep;
+        m = next;
     }
 
     // exp2(score - m + lift); 0 for a row that has seen nothing
@@ -764,6 +804,71 @@ __device__ __forceinline__ uint8_t mask_at(const AttnArgs &a, int64_t t0) {
     return c < a.Nk ? a.key_mask[c] : 0;
 }
 
+// Scores of the 32 keys at column c0 from memory, by the binary32 instructions
+template <bool WIDE>
+__device__ __forceinline__ void scores_from_memory(const AttnArgs &a, f16v &x, int head,
+                                                   const RowAt &mine, int64_t c0) {
+    const int lane = rarely(threadIdx.x & 63), h = lane >> 5, row = lane & 31;
+    // the key of S^T's row lane % 32
+    const int key =
+        WIDE ? 16 * (row >> 4) + 8 * ((row >> 2) & 1) + 4 * ((row >> 3) & 1) + (row & 3) : row;
+    const float *k = (const float *)a.K + (int64_t)head * a.D * a.ldk + c0;
+    const float *q = (const float *)a.Q + (int64_t)(head * a.share + mine.g) * a.D * a.ldq + mine.column;
+    x = f16v{};
+    for (int d = h; d < a.D + h; d += 2) {
+        const bool in = d < a.D;
+        const float y = in && key < a.Nk - c0 ? k[d * a.ldk + key] : 0.f;
+        const float z = in ? q[d * a.ldq] : 0.f;
+        x = mfma(y, z, x);
+    }
+}
+
+// Sums of the values of the 32 keys at column c0 (those in `valid`) from memory, by the
+// same instructions; `finite`: infinities and NaN left out (see clear_values)
+template <int DP, typename Sums>
+__device__ __forceinline__ void values_from_memory(const AttnArgs &a, Sums &w,
+                                                   const typename Sums::Scores &x, int head,
+                                                   int64_t c0, uint64_t valid, bool finite) {
+    const int lane = rarely(threadIdx.x & 63), h = lane >> 5;
+    const float *v = (const float *)a.V + (int64_t)head * a.D * a.ldv + c0;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        const int key = Sums::key_of(0, i, h);
+        const bool in = (valid >> key) & 1;
+#pragma unroll
+        for (int d = 0; d < DP / 32; ++d) {
+            const int row = 32 * d + (lane & 31);
+            float y = in && row < a.D ? v[row * a.ldv + key] : 0.f;
+            if (finite && y - y != 0.f) y = 0.f;
+            w.o[d] = mfma(y, x.s[0][i], w.o[d]);
+        }
+        asm volatile("" ::: "memory");  // few loads at once: registers are short here
+    }
+}
+
+// The wave's rows over the tiles lo, lo + step .. below hi once more, from memory, for
+// sums that passed the largest number (RowSums::level)
+template <int DP, typename Sums>
+__device__ __forceinline__ void leveled_rows(const AttnArgs &a, const RowTile &r, const RowAt &mine,
+                                             int head, int first, int lo, int hi, int step, Sums &w) {
+    w.clear(a);
+#pragma unroll 1
+    for (int t = lo; t < hi; t += step) {
+        const int64_t t0 = (int64_t)first + (int64_t)t * Elem<float>::keys;
+        const uint64_t valid = valid_keys<float>(a, t0, r, mask_at(a, t0));
+        const Draft draft = draft_at<float, 8>(a, r, mine, t0);
+        typename Sums::Scores x;
+        scores_from_memory<Sums::wide>(a, x.s[0], head, mine, t0);
+        settle<float>(w, x, valid, draft);
+        w.raise(x, Elem<float>::slack);
+        w.level(x);
+        w.exponentials(x, Elem<float>::lift);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) w.l += x.s[0][i];
+        values_from_memory<DP>(a, w, x, head, t0, valid, draft.here);
+    }
+}
+
 // The order of a step's instructions: the next scores' matrix instructions
 // between the weights' vector instructions, LDS reads ahead of their use, then
 // the product with V (4096 x 16384 at 64: 340 -> 323 us)
@@ -788,8 +893,8 @@ __device__ __forceinline__ void interleave() {
 #endif
 }
 
-// Parts in the workspace: sums (padded D x rows), then maxima and totals, of every
-// (part, head, tile)
+// Parts in the workspace: means (padded D x rows), then maxima and totals, of every
+// (part, head, tile).  (Sums of parts could pass the largest number, means do not.)
 template <int DP, int TR>
 __device__ __forceinline__ float *part_at(const AttnArgs &a, int part, int head, int tile) {
     return a.part + (((int64_t)part * a.kv_heads + head) * a.tiles + tile) * ((DP + 2) * TR);
@@ -803,13 +908,14 @@ __device__ __forceinline__ void finish(const AttnArgs &a, const Place &at, const
     const int lane = threadIdx.x & 63;
     const int h = lane >> 5;
     const float total = sum_of_halves(w.l);
+    const float inv = total == 0.f ? 0.f : 1.f / total;
     if (a.splits > 1) {
         float *part = part_at<DP, TR>(a, at.part, at.head, at.tile) + 32 * wave + (lane & 31);
 #pragma unroll
         for (int d = 0; d < DP / 32; ++d)
 #pragma unroll
             for (int i = 0; i < 16; ++i)
-                part[(32 * d + 8 * (i >> 2) + 4 * h + (i & 3)) * TR] = w.o[d][i];
+                part[(32 * d + 8 * (i >> 2) + 4 * h + (i & 3)) * TR] = w.o[d][i] * inv;
         if (h == 0) {
             part[DP * TR] = w.m;
             part[(DP + 1) * TR] = total;
@@ -817,7 +923,6 @@ __device__ __forceinline__ void finish(const AttnArgs &a, const Place &at, const
         return;
     }
     if (!mine.valid) return;
-    const float inv = total == 0.f ? 0.f : 1.f / total;
     T *out = (T *)a.O + (int64_t)(at.head * a.share + mine.g) * a.D * a.ldo + mine.column;
 #pragma unroll
     for (int d = 0; d < DP / 32; ++d)
@@ -943,6 +1048,8 @@ __global__ __launch_bounds__(256, DP <= 64 && HOW != kAttnShift ? 3 : DP <= (HOW
             step(on, t++, s1, s0, k1, k0, v1, v0);
         }
         step(off, t, s0, s1, k0, k1, last, v0);
+        if constexpr (sizeof(T) == 4)
+            if (__any(w.overflowed())) leveled_rows<DP>(args_again(), r, mine, at.head, first, lo, hi, 1, w);
         if (a.tree) {
             __syncthreads();
             if (__builtin_amdgcn_readfirstlane(odd))
@@ -1034,19 +1141,28 @@ __global__ __launch_bounds__(64 * split_waves<DP>(), 1) void k_attn_split(AttnAr
                 vs.ask((t + W) * KT, v, 0);
             }
         }
+        if constexpr (sizeof(T) == 4)
+            if (__any(w.overflowed())) leveled_rows<DP>(args_again(), r, mine, at.head, first, lo, hi, W, w);
         if (odd) add_not_finite<T, DP, W>(a, r, mine, at.head, first, lo, hi, w.o);
     }
 
-    // join the waves: maxima, then sums at the common maximum
+    // join the waves: maxima and totals, then sums at the common maximum, divided by the
+    // total of all first (sums of finite sums could pass the largest number)
     const int h = lane >> 5, row = lane & 31;
     const float total = sum_of_halves(w.l);
-    if (h == 0) tops[wave][row] = w.m;
+    if (h == 0) {
+        tops[wave][row] = w.m;
+        totals[wave][row] = total;
+    }
     __syncthreads();
     float top = tops[0][row];
 #pragma unroll
     for (int i = 1; i < W; ++i) top = fmaxf(top, tops[i][row]);
-    const float f = w.m == -INFINITY ? 0.f : exp2_fast(w.m - top);
-    if (h == 0) totals[wave][row] = f * total;
+    auto weight_of = [&](float m) { return m == -INFINITY ? 0.f : exp2_fast(m - top); };
+    float all = 0.f;
+#pragma unroll
+    for (int i = 0; i < W; ++i) all += weight_of(tops[i][row]) * totals[i][row];
+    const float f = all == 0.f ? 0.f : weight_of(w.m) / all;
     static_assert(DP * TR * 4 == kTile, "a wave's sums take the place of its keys");
     float *sums = (float *)(lds_k + wave * kTile);
 #pragma unroll
@@ -1055,15 +1171,11 @@ __global__ __launch_bounds__(64 * split_waves<DP>(), 1) void k_attn_split(AttnAr
         for (int i = 0; i < 16; ++i)
             sums[(32 * d + 8 * (i >> 2) + 4 * h + (i & 3)) * TR + row] = f * w.o[d][i];
     __syncthreads();
-    float all = totals[0][row];
-#pragma unroll
-    for (int i = 1; i < W; ++i) all += totals[i][row];
     float *part = part_at<DP, TR>(a, at.part, at.head, at.tile) + row;
     if (a.splits > 1 && threadIdx.x < TR) {
         part[DP * TR] = top;
         part[(DP + 1) * TR] = all;
     }
-    const float inv = all == 0.f ? 0.f : 1.f / all;
     T *out = (T *)a.O + (int64_t)(at.head * a.share + mine.g) * a.D * a.ldo + mine.column;
     for (int d = threadIdx.x / TR; d < DP; d += 2 * W) {
         float x = 0.f;
@@ -1072,7 +1184,7 @@ __global__ __launch_bounds__(64 * split_waves<DP>(), 1) void k_attn_split(AttnAr
         if (a.splits > 1)
             part[d * TR] = x;
         else if (mine.valid && d < a.D)
-            out[d * a.ldo] = (T)(x * inv);
+            out[d * a.ldo] = (T)x;
     }
 }
 
@@ -1107,9 +1219,9 @@ __global__ __launch_bounds__(kBlock) void k_attn_join(AttnArgs a) {
         for (int s = 0; s < a.splits; ++s) top = fmaxf(top, weights[s][i]);
         for (int s = 0; s < a.splits; ++s) {
             const float m = weights[s][i];
-            const float f = m == -INFINITY ? 0.f : exp2_fast(m - top);
+            const float f = (m == -INFINITY ? 0.f : exp2_fast(m - top)) * totals[s][i];
             weights[s][i] = f;
-            all += f * totals[s][i];
+            all += f;
         }
         totals[0][i] = all == 0.f ? 0.f : 1.f / all;
     }
@@ -1122,8 +1234,9 @@ __global__ __launch_bounds__(kBlock) void k_attn_join(AttnArgs a) {
     for (int d = d0 + threadIdx.x / TR; d < d0 + a.join_rows && d < a.D; d += kBlock / TR) {
         float x = 0.f;
 #pragma unroll 8
-        for (int s = 0; s < a.splits; ++s) x += weights[s][i] * part[s * step + d * TR + i];
-        out[d * a.ldo] = (T)(x * inverse);
+        for (int s = 0; s < a.splits; ++s)
+            x += weights[s][i] * inverse * part[s * step + d * TR + i];
+        out[d * a.ldo] = (T)x;
     }
 }
 

@@ -196,25 +196,6 @@ struct PartRows : RowSums<DP, 1, true> {
                 x.s[0] = mfma(f[kPairs[i][0]], q[kPairs[i][1]][c], x.s[0]);
         }
     }
-    // The same from memory, by the binary32 instructions: the tile at column `at`
-    template <typename Head>
-    __device__ __forceinline__ void scores_exact(const AttnArgs &a, Scores &x,
-                                                 const Head &k, int at, int cols, int kv_head,
-                                                 const RowAt &r) const {
-        const int lane = rarely(threadIdx.x & 63), h = lane >> 5;
-        // the key of S^T's row lane % 32
-        const int row = lane & 31;
-        const int c = at + 16 * (row >> 4) + 8 * ((row >> 2) & 1) + 4 * ((row >> 3) & 1) + (row & 3);
-        const float *src =
-            (const float *)a.Q + (int64_t)(kv_head * a.share + r.g) * a.D * a.ldq + r.column;
-        x.s[0] = f16v{};
-        for (int d = h; d < a.D + h; d += 2) {
-            const bool in = d < a.D;
-            const float y = in && c < cols ? ((const float *)(k.base + d * k.ld))[c] : 0.f;
-            const float z = in ? src[d * a.ldq] : 0.f;
-            x.s[0] = mfma(y, z, x.s[0]);
-        }
-    }
 
     // Scores to weights, their parts and sum; x keeps the weights
     __device__ __forceinline__ void weigh(Scores &x, Weights &w) {
@@ -245,26 +226,6 @@ struct PartRows : RowSums<DP, 1, true> {
 #pragma unroll
                 for (int i = 0; i < 6; ++i) o[d] = mfma(f[kPairs[i][0]], w.p[kPairs[i][1]][c], o[d]);
             }
-        }
-    }
-    // The same from memory, keys outside `valid` left out; `finite`: and what is not
-    // finite of the others (see clear_values)
-    template <typename Head>
-    __device__ __forceinline__ void values_exact(const Scores &x, const Head &v, int D, int at,
-                                                 uint64_t valid, bool finite) {
-        const int lane = rarely(threadIdx.x & 63), h = lane >> 5;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const int key = Sums::key_of(0, i, h);
-            const bool in = (valid >> key) & 1;
-#pragma unroll
-            for (int d = 0; d < DP / 32; ++d) {
-                const int row = 32 * d + (lane & 31);
-                float y = in && row < D ? ((const float *)(v.base + row * v.ld))[at + key] : 0.f;
-                if (finite && y - y != 0.f) y = 0.f;
-                o[d] = mfma(y, x.s[0][i], o[d]);
-            }
-            asm volatile("" ::: "memory");  // few loads at once: registers are short here
         }
     }
 };
@@ -311,7 +272,7 @@ __global__ __launch_bounds__(256, DP <= 64 && !WIDE ? 2 : 1) void k_attn_parts(A
             if (k_plain(t))
                 w.scores(x, k_at(t));
             else
-                w.scores_exact(a, x, ks.rows, t * KT, a.Nk - first, at.head, mine);
+                scores_from_memory<true>(args_again(), x.s[0], at.head, mine, (int64_t)first + (int64_t)t * KT);
         };
         ks.ask(lo * KT, wave);
         w.init(a, at.head, mine);
@@ -352,11 +313,13 @@ __global__ __launch_bounds__(256, DP <= 64 && !WIDE ? 2 : 1) void k_attn_parts(A
                 if (v_plain(t))
                     w.values(p, v_at(t));
                 else
-                    w.values_exact(cur, vs.rows, a.D, t * KT, valid, a.tree && r.end - r.n - t0 < KT);
+                    values_from_memory<DP>(args_again(), w, cur, at.head, t0, valid,
+                                           a.tree && r.end - r.n - t0 < KT);
                 if (more) scores_at(t + 1, nxt);
             }
             cur = nxt;
         }
+        if (__any(w.overflowed())) leveled_rows<DP>(args_again(), r, mine, at.head, first, lo, hi, 1, w);
         if (a.tree) {
             __syncthreads();
             if (__builtin_amdgcn_readfirstlane(any_odd))

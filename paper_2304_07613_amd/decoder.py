@@ -81,6 +81,7 @@ class SparseDecoder:
         self.begin = torch.arange(sequences, dtype=torch.int32, device=device) * capacity
         self.lengths = torch.zeros(sequences, dtype=torch.int32, device=device)   # kept tokens
         self.encoder_begin = self.encoder_end = None
+        self.draft = [[] for _ in range(sequences)]     # the parents of the last step
 
     @classmethod
     def random(cls, shape: DecoderShape, n_layers: int, sequences: int, capacity: int, seed: int = 0,
@@ -139,6 +140,7 @@ class SparseDecoder:
         columns = (self.begin + self.lengths - offsets[:-1])[which] + \
             torch.arange(x.shape[1], device=dev)
         positions = (self.lengths[which] + depth).int()
+        self.draft = [[] for _ in parents]
         s = self.shape
         q_rows, kv_rows = s.heads * s.head_dim, s.kv_heads * s.head_dim
         for layer in self.layers:
@@ -160,14 +162,21 @@ class SparseDecoder:
                                   offsets, self.encoder_begin, self.encoder_end)
                 h = layer.fused("cross_o", a, "add", h)
             x = layer.fused("down", layer.fused("up", h, "gelu"), "add", h)
+        self.draft = [list(p) for p in parents]
         return x
 
     def accept(self, kept: list):
         """Keep drafted tokens of the last step: kept[b] are indices of sequence b's
-        draft along one path, ascending; their columns move behind the kept
-        tokens."""
+        draft along one path, the first one's parent -1; their columns move behind
+        the kept tokens.  A draft is accepted from once."""
         if len(kept) != len(self.begin):
             raise ValueError("one list of kept tokens for every sequence")
+        for path, parents in zip(kept, self.draft):
+            last = -1
+            for i in path:
+                if not 0 <= i < len(parents) or parents[i] != last:
+                    raise ValueError("kept tokens are one path through their sequence's last draft")
+                last = i
         start = (self.begin + self.lengths).tolist()
         source = [start[b] + i for b, path in enumerate(kept) for i in path]
         target = [start[b] + i for b, path in enumerate(kept) for i in range(len(path))]
@@ -179,3 +188,4 @@ class SparseDecoder:
                     cache.index_copy_(1, target, cache.index_select(1, source))
         self.lengths += torch.tensor([len(path) for path in kept], dtype=torch.int32,
                                      device=self.begin.device)
+        self.draft = [[] for _ in kept]

@@ -545,7 +545,9 @@ nmg_status nmg_rotary_table(int32_t dim, int64_t length, double base, nmg_rotary
                             double magnitude, float *table, hipStream_t stream);
 
 /* Y = the rotation of X: `heads` heads of `head_dim` rows, N tokens.  Computed in
- * binary32, rounded once.  Y may be X (ldy = ldx); else they do not overlap. */
+ * binary32, rounded once.  Y may be X (ldy = ldx); else they do not overlap.
+ * NMG_ERR_UNSUPPORTED: head_dim > 8192, or more heads and tokens than one launch
+ * holds (2^32 threads: 128 tokens of 8 heads take 256). */
 nmg_status nmg_rotary(nmg_dtype dtype, int32_t heads, int32_t head_dim,
                       const nmg_rotary_desc *rotary, const void *X, int64_t ldx, int64_t N,
                       void *Y, int64_t ldy, hipStream_t stream);
@@ -590,7 +592,9 @@ typedef struct nmg_sequences {
  * Statistics and sums are binary32 (a product q . k past its range is infinite;
  * values may be of any size in it); binary16 weights are rounded to binary16
  * for the product with V.  O overlaps no input.  Nk may be 0 (K, V unused).
- * NMG_ERR_UNSUPPORTED: head_dim > 256, or rows of K or V of 2^28 bytes or more.
+ * NMG_ERR_UNSUPPORTED: head_dim > 256, rows of K or V of 2^28 bytes or more, or
+ * more sequences, heads and columns than one launch holds (2^32 threads; a
+ * sequence takes 256 or 512 of each key head at least).
  *
  * workspace (may be NULL; 256-byte aligned): lets few queries over many keys be
  * split over the GPU.  Too little of it: fewer splits, none with 0.  The number

@@ -51,4 +51,9 @@ inline int attn_padded_dim(int D) {
     return D <= 32 ? 32 : D <= 64 ? 64 : D <= 96 ? 96 : D <= 128 ? 128 : 256;
 }
 
+// Waves of a workgroup that splits the keys: as many as 128 KB hold tiles of
+constexpr int attn_split_waves(int padded_dim) {
+    return padded_dim <= 64 ? 8 : padded_dim <= 128 ? 4 : 2;
+}
+
 }  // namespace nmg_internal

@@ -1066,14 +1066,11 @@ __global__ __launch_bounds__(256, DP <= 64 && HOW != kAttnShift ? 3 : DP <= (HOW
 // keys: 127 us = 4.2 TB/s (a large copy 4.9); 12 heads x 64, 8 of 1 over 512: 7.4 us,
 // most of it the launch, the places and the join.  No barriers before the join: the
 // waves' copies run apart, two tiles a wave on the way.
-// Waves: as many as 128 KB hold tiles of
-template <int DP> constexpr int split_waves() { return DP <= 64 ? 8 : DP <= 128 ? 4 : 2; }
-
 template <typename T, int DP, AttnRows HOW>
-__global__ __launch_bounds__(64 * split_waves<DP>(), 1) void k_attn_split(AttnArgs a) {
+__global__ __launch_bounds__(64 * attn_split_waves(DP), 1) void k_attn_split(AttnArgs a) {
     constexpr int TR = kAttnSplitRows, KT = Elem<T>::keys, kTile = DP * kRowBytes;
     constexpr bool SHIFT = HOW == kAttnShift;
-    constexpr int W = split_waves<DP>();
+    constexpr int W = attn_split_waves(DP);
     __shared__ __attribute__((aligned(1024))) char lds_k[W * kTile];
     __shared__ __attribute__((aligned(1024))) char lds_v[W * kTile];
     __shared__ float tops[W][TR], totals[W][TR];

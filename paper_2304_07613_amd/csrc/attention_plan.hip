@@ -37,7 +37,7 @@ Plan plan_of(nmg_dtype dtype, const AttnArgs &a) {
     p.tiles = a.sequences == 1 ? (rows + tr - 1) / tr : std::min(rows / tr + a.sequences, rows);
     // ... and for equal lengths
     const int64_t items = std::min((each + tr - 1) / tr * a.sequences, p.tiles) * a.kv_heads;
-    const int waves = p.shared ? 1 : dp <= 64 ? 8 : dp <= 128 ? 4 : 2;  // that split a part's keys
+    const int waves = p.shared ? 1 : attn_split_waves(dp);  // that split a part's keys
     const int64_t steps = (keys + (int64_t)kt * waves - 1) / (kt * waves);
     // workgroups a compute unit holds (binary32 16 heads x 128, 2 sequences of 512
     // columns over 1024 keys: 87 us in the 4 parts for two of them, 77 in 2 for one)
@@ -85,7 +85,9 @@ nmg_status launch_attention(nmg_dtype dtype, const AttnArgs &args, void *workspa
     const Plan p = plan_of(dtype, a);
     int64_t splits = std::min<int64_t>(p.splits, workspace_bytes / p.part_bytes);
     if (splits < 2) splits = 1;
-    if (p.tiles * splits * a.kv_heads > INT32_MAX) return NMG_ERR_UNSUPPORTED;
+    const int threads = p.shared ? 4 * 64 : attn_split_waves(attn_padded_dim(a.D)) * 64;
+    if (!launchable(p.tiles * splits * a.kv_heads, std::max(threads, kBlock)))
+        return NMG_ERR_UNSUPPORTED;
     a.tiles = (int32_t)p.tiles;
     a.splits = (int32_t)splits;
     a.part = (float *)workspace;

@@ -49,6 +49,11 @@ inline nmg_status launched() {
     return hipGetLastError() == hipSuccess ? NMG_OK : NMG_ERR_LAUNCH;
 }
 
+// A launch holds fewer than 2^32 threads along x
+inline bool launchable(int64_t blocks, int threads) {
+    return blocks <= UINT32_MAX / (uint32_t)threads;
+}
+
 // Rows per group unit of the matrix-core kernels: the largest of 32, 16, 8,
 // 4 that divides g; 0 if g % 4 != 0.
 inline int mfma_unit(const nmg_layout *L) {

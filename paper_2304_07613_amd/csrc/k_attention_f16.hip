@@ -8,7 +8,7 @@ void launch_how(const AttnArgs &a, bool shared, dim3 grid, hipStream_t stream) {
     if (shared)
         hipLaunchKernelGGL((k_attn_shared<_Float16, DP, HOW>), grid, dim3(256), 0, stream, a);
     else
-        hipLaunchKernelGGL((k_attn_split<_Float16, DP, HOW>), grid, dim3(64 * split_waves<DP>()), 0,
+        hipLaunchKernelGGL((k_attn_split<_Float16, DP, HOW>), grid, dim3(64 * attn_split_waves(DP)), 0,
                            stream, a);
 }
 

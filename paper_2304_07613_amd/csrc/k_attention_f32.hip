@@ -9,7 +9,7 @@ template <int DP, bool WIDE>
 void launch_how(const AttnArgs &a, bool shared, dim3 grid, hipStream_t stream) {
     constexpr AttnRows how = WIDE ? kAttnWide : kAttnNarrow;
     if (!shared) {
-        hipLaunchKernelGGL((k_attn_split<float, DP, how>), grid, dim3(64 * split_waves<DP>()), 0,
+        hipLaunchKernelGGL((k_attn_split<float, DP, how>), grid, dim3(64 * attn_split_waves(DP)), 0,
                            stream, a);
     } else {
         if constexpr (DP <= 128)

@@ -252,7 +252,7 @@ nmg_status launch_rotary(nmg_dtype dtype, const RotaryArgs &args, bool norm, hip
     a.run = (int)std::max<int64_t>(1, std::min<int64_t>(8, blocks * heads / (4 * device_cus())));
     a.groups0 = (a.part[0].heads + a.run - 1) / a.run;
     const int64_t groups = a.groups0 + (a.part[1].heads + a.run - 1) / a.run;
-    if (blocks * groups > INT32_MAX) return NMG_ERR_UNSUPPORTED;
+    if (!launchable(blocks * groups, kBlock)) return NMG_ERR_UNSUPPORTED;
     a.blocks = (int)blocks;
     const dim3 grid((unsigned)(blocks * groups));
     const int u = per_thread();

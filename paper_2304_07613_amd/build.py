@@ -4,17 +4,19 @@ Every translation unit under csrc/ is compiled to an object in parallel, then
 the objects are linked into one shared library; the link is checked for
 undefined kernel launch stubs.  csrc/gen_gelu_table.py writes the binary16
 GELU table into the build folder first.  csrc/calls.cpp, the marshalling of the
-attention operators' calls, becomes the Python module _calls beside the library
-(host code, g++ against torch's headers).
+attention operators' calls, becomes a Python module beside the library (host code,
+g++ against torch's headers); the library does not need it.
 """
 from __future__ import annotations
 
 import glob
+import importlib.metadata
 import os
 import subprocess
 import sys
 import sysconfig
 import tempfile
+import warnings
 from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
@@ -23,7 +25,16 @@ CSRC = os.path.join(HERE, "csrc")
 HEADER = os.path.join(ROOT, "include", "nmg.h")
 LIB_PATH = os.path.join(HERE, "libnmg.so")
 CALLS_SRC = os.path.join(CSRC, "calls.cpp")
-CALLS_PATH = os.path.join(HERE, "_calls.so")
+
+
+def calls_path() -> str:
+    """The module _calls for this Python and this torch: it is built against both."""
+    try:
+        torch = importlib.metadata.version("torch")
+    except importlib.metadata.PackageNotFoundError:
+        torch = "none"
+    return os.path.join(HERE, f"_calls.torch-{torch}{sysconfig.get_config_var('EXT_SUFFIX')}")
+
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall",
@@ -58,7 +69,8 @@ def build_calls() -> str:
     from torch.utils import cpp_extension
 
     inc = cpp_extension.include_paths() + [sysconfig.get_paths()["include"]]
-    tmp = CALLS_PATH + ".tmp"
+    path = calls_path()
+    tmp = path + ".tmp"
     lib = cpp_extension.library_paths()[0]
     res = subprocess.run(
         [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall",
@@ -67,13 +79,29 @@ def build_calls() -> str:
          "-ltorch_python", "-ltorch_cpu", "-lc10"], capture_output=True, text=True)
     if res.returncode != 0:
         raise RuntimeError(f"calls.cpp failed:\n{res.stdout}{res.stderr}")
-    os.replace(tmp, CALLS_PATH)
-    return CALLS_PATH
+    os.replace(tmp, path)
+    return path
 
 
 def build(verbose: bool = False, jobs: int | None = None) -> str:
     """Compile csrc/*.hip into libnmg.so, and the module _calls, next to this
-    file (always rebuilds)."""
+    file (always rebuilds).  A module that does not compile is a warning, and gone:
+    the library is there without it, and the binding's attention operators say so
+    when they are called."""
+    with ThreadPoolExecutor(max_workers=1) as pool:
+        calls = pool.submit(build_calls)
+        library = build_library(verbose, jobs)
+    try:
+        calls.result()
+    except Exception as e:
+        if os.path.exists(calls_path()):    # of other sources
+            os.remove(calls_path())
+        warnings.warn(f"the attention operators' Python module is not built: {e}", RuntimeWarning)
+    return library
+
+
+def build_library(verbose: bool = False, jobs: int | None = None) -> str:
+    """Compile csrc/*.hip into libnmg.so."""
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     jobs = jobs or min(16, os.cpu_count() or 4)
     inc = ["-I", os.path.join(ROOT, "include")]
@@ -90,9 +118,7 @@ def build(verbose: bool = False, jobs: int | None = None) -> str:
                                  capture_output=True, text=True)
             return src, obj, res
         with ThreadPoolExecutor(max_workers=jobs) as pool:
-            calls = pool.submit(build_calls)
             results = list(pool.map(compile_one, sources()))
-            calls.result()
         errors = [(s, r) for s, _, r in results if r.returncode != 0]
         if errors:
             s, r = errors[0]
@@ -117,9 +143,11 @@ def build(verbose: bool = False, jobs: int | None = None) -> str:
 
 
 def is_stale() -> bool:
-    if not (os.path.exists(LIB_PATH) and os.path.exists(CALLS_PATH)):
+    """Whether the library, or the module for this Python and torch, is missing or
+    older than what it is built from."""
+    if not (os.path.exists(LIB_PATH) and os.path.exists(calls_path())):
         return True
-    t = min(os.path.getmtime(LIB_PATH), os.path.getmtime(CALLS_PATH))
+    t = min(os.path.getmtime(LIB_PATH), os.path.getmtime(calls_path()))
     return any(os.path.getmtime(p) > t for p in inputs())
 
 

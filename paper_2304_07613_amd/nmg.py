@@ -12,6 +12,7 @@ product), 5.2 (magnitude converter and conversion back to dense).
 from __future__ import annotations
 
 import ctypes
+import importlib.util
 import os
 import re
 
@@ -157,9 +158,13 @@ def _load_calls():
     """The compiled marshalling of the attention operators, bound to the library."""
     global _calls
     L = lib()
-    if not os.path.exists(_build.CALLS_PATH):
-        raise RuntimeError(f"{_build.CALLS_PATH} is not built; run __graft_entry__.build()")
-    from . import _calls as module
+    path = _build.calls_path()
+    if not os.path.exists(path):
+        raise RuntimeError(f"{path} is not built; run __graft_entry__.build()")
+    name = __package__ + "._calls"
+    spec = importlib.util.spec_from_file_location(name, path)
+    module = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(module)
 
     names = ("nmg_rotary", "nmg_qk_norm_rotary", "nmg_attention", "nmg_tree_attention",
              "nmg_attention_workspace_bytes")

@@ -78,6 +78,8 @@ void arguments(Py_ssize_t got, Py_ssize_t want) {
 int dtype_code(const at::Tensor &t) {
     return t.scalar_type() == at::kFloat ? 0 : t.scalar_type() == at::kHalf ? 1 : -1;
 }
+const char *const kMatrix = "a matrix must be a 2-D tensor with unit column stride";
+
 // Leading dimension of a 2-D row-major tensor
 int64_t rows(const at::Tensor &t, const char *what) {
     if (t.dim() != 2 || t.stride(1) != 1) refuse_value(what);
@@ -124,11 +126,27 @@ struct Gpu {
     }
 };
 
-at::Tensor output(const at::Tensor &like, const at::Tensor *given) {
-    if (!given) return at::empty_like(like);
+// Without the interpreter lock: memory is allocated and kernels are launched then, and
+// nothing of Python's is touched.  (A launch may wait, and so may the allocator.)
+struct Unlocked {
+    PyThreadState *state = PyEval_SaveThread();
+    Unlocked() = default;
+    Unlocked(const Unlocked &) = delete;
+    ~Unlocked() { PyEval_RestoreThread(state); }
+};
+
+// The output that was given, checked; undefined if none was
+at::Tensor output(Gpu &gpu, const at::Tensor &like, const at::Tensor *given) {
+    if (!given) return at::Tensor();
     if (given->scalar_type() != like.scalar_type() || given->sizes() != like.sizes())
         refuse_value("an output must have the shape and dtype of its input");
+    gpu(*given);
+    (void)rows(*given, kMatrix);
     return *given;
+}
+// (called Unlocked)
+void allocate(at::Tensor &y, const at::Tensor &like) {
+    if (!y.defined()) y = at::empty_like(like, at::MemoryFormat::Contiguous);
 }
 
 void checked(int status, const char *what) {
@@ -160,8 +178,6 @@ Rotary rotary_desc(Gpu &gpu, PyObject *table, PyObject *positions, PyObject *pai
     return r;
 }
 
-const char *const kMatrix = "a matrix must be a 2-D tensor with unit column stride";
-
 at::Tensor rotary(PyObject *const *a) {
     const at::Tensor &x = tensor(a[0], "X must be a tensor");
     const int code = dtype_code(x);
@@ -172,11 +188,16 @@ at::Tensor rotary(PyObject *const *a) {
     Gpu gpu;
     const Rotary r = rotary_desc(gpu, a[2], a[3], a[4], N);
     gpu(x);
-    at::Tensor y = output(x, maybe(a[5], "out must be a tensor"));
-    gpu(y);
-    checked(nmg_rotary(code, heads, (int32_t)D, &r, x.data_ptr(), ldx, N, y.data_ptr(),
-                       rows(y, kMatrix), gpu.stream()),
-            "nmg_rotary");
+    at::Tensor y = output(gpu, x, maybe(a[5], "out must be a tensor"));
+    void *const stream = gpu.stream();
+    int status;
+    {
+        Unlocked now;
+        allocate(y, x);
+        status = nmg_rotary(code, heads, (int32_t)D, &r, x.data_ptr(), ldx, N, y.data_ptr(),
+                            y.stride(0), stream);
+    }
+    checked(status, "nmg_rotary");
     return y;
 }
 
@@ -205,14 +226,19 @@ std::pair<at::Tensor, at::Tensor> qk_norm_rotary(PyObject *const *a) {
     const double eps = real(a[9]);
     gpu(q);
     gpu(k);
-    at::Tensor yq = output(q, maybe(a[10], "out[0] must be a tensor"));
-    at::Tensor yk = output(k, maybe(a[11], "out[1] must be a tensor"));
-    gpu(yq);
-    gpu(yk);
-    checked(nmg_qk_norm_rotary(code, heads, kv_heads, (int32_t)D, &r, weights[0], weights[1],
-                               (float)eps, q.data_ptr(), ldq, k.data_ptr(), ldk, N, yq.data_ptr(),
-                               rows(yq, kMatrix), yk.data_ptr(), rows(yk, kMatrix), gpu.stream()),
-            "nmg_qk_norm_rotary");
+    at::Tensor yq = output(gpu, q, maybe(a[10], "out[0] must be a tensor"));
+    at::Tensor yk = output(gpu, k, maybe(a[11], "out[1] must be a tensor"));
+    void *const stream = gpu.stream();
+    int status;
+    {
+        Unlocked now;
+        allocate(yq, q);
+        allocate(yk, k);
+        status = nmg_qk_norm_rotary(code, heads, kv_heads, (int32_t)D, &r, weights[0], weights[1],
+                                    (float)eps, q.data_ptr(), ldq, k.data_ptr(), ldk, N,
+                                    yq.data_ptr(), yq.stride(0), yk.data_ptr(), yk.stride(0), stream);
+    }
+    checked(status, "nmg_qk_norm_rotary");
     return {yq, yk};
 }
 
@@ -262,31 +288,34 @@ at::Tensor attention(PyObject *const *a) {
         gpu(*tree);
     }
     const float scale = a[10] == Py_None ? (float)(1.0 / std::sqrt((double)D)) : (float)real(a[10]);
-    at::Tensor o = output(q, maybe(a[11], "out must be a tensor"));
-    gpu(o);
-    const int64_t ldo = rows(o, kMatrix);
-    // freed after the call returns: the allocator hands it out again in stream order
-    at::Tensor space;
-    int64_t room = nmg_attention_workspace_bytes(&h, s.count, Nq, Nk);
-    if (room > 0) {
-        try {
-            space = at::empty({room}, q.options().dtype(at::kByte));
-        } catch (const c10::OutOfMemoryError &) {
-            room = 0;
+    at::Tensor o = output(gpu, q, maybe(a[11], "out must be a tensor"));
+    void *const stream = gpu.stream();
+    int status;
+    {
+        Unlocked now;
+        allocate(o, q);
+        // freed after the call returns: the allocator hands it out again in stream order
+        at::Tensor space;
+        int64_t room = nmg_attention_workspace_bytes(&h, s.count, Nq, Nk);
+        if (room > 0) {
+            try {
+                space = at::empty({room}, q.options().dtype(at::kByte));
+            } catch (const c10::OutOfMemoryError &) {
+                room = 0;
+            }
         }
+        void *ws = room > 0 ? space.data_ptr() : nullptr;
+        room = std::max<int64_t>(room, 0);
+        if (tree)
+            status = nmg_tree_attention(&h, &s, q.data_ptr(), ldq, Nq, k.data_ptr(), ldk, v.data_ptr(),
+                                        ldv, Nk, tree->data_ptr(), ldtree, tree->size(1), scale,
+                                        o.data_ptr(), o.stride(0), ws, room, stream);
+        else
+            status = nmg_attention(&h, &s, q.data_ptr(), ldq, Nq, k.data_ptr(), ldk, v.data_ptr(), ldv,
+                                   Nk, mask ? mask->data_ptr() : nullptr, scale, o.data_ptr(),
+                                   o.stride(0), ws, room, stream);
     }
-    void *ws = room > 0 ? space.data_ptr() : nullptr;
-    room = std::max<int64_t>(room, 0);
-    if (tree)
-        checked(nmg_tree_attention(&h, &s, q.data_ptr(), ldq, Nq, k.data_ptr(), ldk, v.data_ptr(), ldv,
-                                   Nk, tree->data_ptr(), ldtree, tree->size(1), scale, o.data_ptr(),
-                                   ldo, ws, room, gpu.stream()),
-                "nmg_tree_attention");
-    else
-        checked(nmg_attention(&h, &s, q.data_ptr(), ldq, Nq, k.data_ptr(), ldk, v.data_ptr(), ldv, Nk,
-                              mask ? mask->data_ptr() : nullptr, scale, o.data_ptr(), ldo, ws, room,
-                              gpu.stream()),
-                "nmg_attention");
+    checked(status, tree ? "nmg_tree_attention" : "nmg_attention");
     return o;
 }
 

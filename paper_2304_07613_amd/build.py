@@ -68,12 +68,14 @@ def build_calls() -> str:
     import torch
     from torch.utils import cpp_extension
 
-    inc = cpp_extension.include_paths() + [sysconfig.get_paths()["include"]]
+    inc = [os.path.dirname(HEADER), os.path.join(os.environ.get("ROCM_PATH", "/opt/rocm"), "include"),
+           sysconfig.get_paths()["include"], *cpp_extension.include_paths()]
     path = calls_path()
     tmp = path + ".tmp"
     lib = cpp_extension.library_paths()[0]
     res = subprocess.run(
         [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall",
+         "-D__HIP_PLATFORM_AMD__",   # what HIP's headers (nmg.h's stream type) ask of a host compiler
          f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
          *[arg for d in inc for arg in ("-isystem", d)], "-o", tmp, CALLS_SRC, "-L", lib,
          "-ltorch_python", "-ltorch_cpu", "-lc10"], capture_output=True, text=True)

@@ -13,35 +13,18 @@
 
 #include <cmath>
 
+#include "nmg.h"
+
 namespace {
 
-// include/nmg.h's types and functions, by the C ABI
-struct Rotary {
-    int32_t dim;
-    int pairs;
-    int64_t length;
-    const void *table, *positions;
-};
-struct Heads {
-    int32_t heads, kv_heads, head_dim;
-    int dtype;
-};
-struct Sequences {
-    int32_t count;
-    const void *q_offsets, *kv_begin, *kv_end;
-};
-int (*nmg_rotary)(int, int32_t, int32_t, const Rotary *, const void *, int64_t, int64_t, void *,
-                  int64_t, void *);
-int (*nmg_qk_norm_rotary)(int, int32_t, int32_t, int32_t, const Rotary *, const void *, const void *,
-                          float, const void *, int64_t, const void *, int64_t, int64_t, void *,
-                          int64_t, void *, int64_t, void *);
-int (*nmg_attention)(const Heads *, const Sequences *, const void *, int64_t, int64_t, const void *,
-                     int64_t, const void *, int64_t, int64_t, const void *, float, void *, int64_t,
-                     void *, int64_t, void *);
-int (*nmg_tree_attention)(const Heads *, const Sequences *, const void *, int64_t, int64_t,
-                          const void *, int64_t, const void *, int64_t, int64_t, const void *,
-                          int64_t, int64_t, float, void *, int64_t, void *, int64_t, void *);
-int64_t (*nmg_attention_workspace_bytes)(const Heads *, int32_t, int64_t, int64_t);
+// The library's functions, bound when it is loaded
+struct Library {
+    decltype(&::nmg_rotary) rotary;
+    decltype(&::nmg_qk_norm_rotary) qk_norm_rotary;
+    decltype(&::nmg_attention) attention;
+    decltype(&::nmg_tree_attention) tree_attention;
+    decltype(&::nmg_attention_workspace_bytes) attention_workspace_bytes;
+} library;
 PyObject *check;          // nmg._check(status, what): raises NmgError
 PyObject *current_device, *current_stream;  // torch._C's
 
@@ -75,9 +58,10 @@ void arguments(Py_ssize_t got, Py_ssize_t want) {
     if (got != want) refuse(PyExc_TypeError, "wrong number of arguments");
 }
 
-int dtype_code(const at::Tensor &t) {
-    return t.scalar_type() == at::kFloat ? 0 : t.scalar_type() == at::kHalf ? 1 : -1;
+bool dtype_ok(const at::Tensor &t) {
+    return t.scalar_type() == at::kFloat || t.scalar_type() == at::kHalf;
 }
+nmg_dtype dtype_of(const at::Tensor &t) { return t.scalar_type() == at::kFloat ? NMG_F32 : NMG_F16; }
 const char *const kMatrix = "a matrix must be a 2-D tensor with unit column stride";
 
 // Leading dimension of a 2-D row-major tensor
@@ -85,10 +69,10 @@ int64_t rows(const at::Tensor &t, const char *what) {
     if (t.dim() != 2 || t.stride(1) != 1) refuse_value(what);
     return t.stride(0);
 }
-const void *ints(const at::Tensor &t, int64_t n, const char *what) {
+const int32_t *ints(const at::Tensor &t, int64_t n, const char *what) {
     if (t.scalar_type() != at::kInt || t.dim() != 1 || t.numel() != n || !t.is_contiguous())
         refuse_value(what);
-    return t.data_ptr();
+    return t.data_ptr<int32_t>();
 }
 int64_t head_rows(int64_t all, int64_t heads) {
     if (heads < 1 || all < 1 || all % heads)
@@ -113,7 +97,7 @@ struct Gpu {
         if (d != device)
             refuse_value("a tensor is not on the current device (select it with torch.cuda.device)");
     }
-    void *stream() const {
+    hipStream_t stream() const {
         PyObject *index = PyLong_FromLong(device);
         if (!index) throw Refused{};
         PyObject *raw = PyObject_CallOneArg(current_stream, index);
@@ -122,7 +106,7 @@ struct Gpu {
         void *s = PyLong_AsVoidPtr(raw);
         Py_DECREF(raw);
         if (!s && PyErr_Occurred()) throw Refused{};
-        return s;
+        return (hipStream_t)s;
     }
 };
 
@@ -149,19 +133,19 @@ void allocate(at::Tensor &y, const at::Tensor &like) {
     if (!y.defined()) y = at::empty_like(like, at::MemoryFormat::Contiguous);
 }
 
-void checked(int status, const char *what) {
-    if (status == 0) return;
-    PyObject *r = PyObject_CallFunction(check, "is", status, what);
+void checked(nmg_status status, const char *what) {
+    if (status == NMG_OK) return;
+    PyObject *r = PyObject_CallFunction(check, "is", (int)status, what);
     Py_XDECREF(r);
     if (r) PyErr_SetString(PyExc_RuntimeError, what);
     throw Refused{};
 }
 
-Rotary rotary_desc(Gpu &gpu, PyObject *table, PyObject *positions, PyObject *pairs, int64_t N) {
-    Rotary r = {0, 0, 0, nullptr, nullptr};
+nmg_rotary_desc rotary_desc(Gpu &gpu, PyObject *table, PyObject *positions, PyObject *pairs, int64_t N) {
+    nmg_rotary_desc r = {0, NMG_ROTARY_HALF, 0, nullptr, nullptr};
     if (!PyUnicode_Check(pairs)) refuse_value("unknown rotary layout");
     if (PyUnicode_CompareWithASCIIString(pairs, "interleaved") == 0)
-        r.pairs = 1;
+        r.pairs = NMG_ROTARY_INTERLEAVED;
     else if (PyUnicode_CompareWithASCIIString(pairs, "half") != 0)
         refuse_value("unknown rotary layout");
     const at::Tensor *t = maybe(table, "table must be a tensor or None");
@@ -171,7 +155,7 @@ Rotary rotary_desc(Gpu &gpu, PyObject *table, PyObject *positions, PyObject *pai
     const at::Tensor &p = tensor(positions, "positions must be a tensor");
     r.dim = (int32_t)(2 * t->size(1));
     r.length = t->size(2);
-    r.table = t->data_ptr();
+    r.table = t->data_ptr<float>();
     r.positions = ints(p, N, "positions must be N contiguous int32 values");
     gpu(*t);
     gpu(p);
@@ -180,21 +164,20 @@ Rotary rotary_desc(Gpu &gpu, PyObject *table, PyObject *positions, PyObject *pai
 
 at::Tensor rotary(PyObject *const *a) {
     const at::Tensor &x = tensor(a[0], "X must be a tensor");
-    const int code = dtype_code(x);
-    if (code < 0) refuse(PyExc_TypeError, "X must be float32 or float16");
+    if (!dtype_ok(x)) refuse(PyExc_TypeError, "X must be float32 or float16");
     const int64_t ldx = rows(x, kMatrix), N = x.size(1);
     const int32_t heads = int32(a[1]);
     const int64_t D = head_rows(x.size(0), heads);
     Gpu gpu;
-    const Rotary r = rotary_desc(gpu, a[2], a[3], a[4], N);
+    const nmg_rotary_desc r = rotary_desc(gpu, a[2], a[3], a[4], N);
     gpu(x);
     at::Tensor y = output(gpu, x, maybe(a[5], "out must be a tensor"));
-    void *const stream = gpu.stream();
-    int status;
+    const hipStream_t stream = gpu.stream();
+    nmg_status status;
     {
         Unlocked now;
         allocate(y, x);
-        status = nmg_rotary(code, heads, (int32_t)D, &r, x.data_ptr(), ldx, N, y.data_ptr(),
+        status = library.rotary(dtype_of(x), heads, (int32_t)D, &r, x.data_ptr(), ldx, N, y.data_ptr(),
                             y.stride(0), stream);
     }
     checked(status, "nmg_rotary");
@@ -203,8 +186,7 @@ at::Tensor rotary(PyObject *const *a) {
 
 std::pair<at::Tensor, at::Tensor> qk_norm_rotary(PyObject *const *a) {
     const at::Tensor &q = tensor(a[0], "Q must be a tensor"), &k = tensor(a[1], "K must be a tensor");
-    const int code = dtype_code(q);
-    if (code < 0 || k.scalar_type() != q.scalar_type())
+    if (!dtype_ok(q) || k.scalar_type() != q.scalar_type())
         refuse(PyExc_TypeError, "Q and K must be float32 or float16, of one dtype");
     const int64_t ldq = rows(q, kMatrix), ldk = rows(k, kMatrix), N = q.size(1);
     const int32_t heads = int32(a[2]), kv_heads = int32(a[3]);
@@ -212,7 +194,7 @@ std::pair<at::Tensor, at::Tensor> qk_norm_rotary(PyObject *const *a) {
     if (k.size(1) != N || head_rows(k.size(0), kv_heads) != D)
         refuse_value("Q and K must have heads of one size and the same tokens");
     Gpu gpu;
-    const void *weights[2];
+    const float *weights[2];
     for (int i = 0; i < 2; ++i) {
         const at::Tensor *w = maybe(a[4 + i], "norm weights must be tensors or None");
         weights[i] = nullptr;
@@ -220,21 +202,21 @@ std::pair<at::Tensor, at::Tensor> qk_norm_rotary(PyObject *const *a) {
         if (w->scalar_type() != at::kFloat || w->dim() != 1 || w->numel() != D || !w->is_contiguous())
             refuse_value("norm weights must be head_dim contiguous float32 values");
         gpu(*w);
-        weights[i] = w->data_ptr();
+        weights[i] = w->data_ptr<float>();
     }
-    const Rotary r = rotary_desc(gpu, a[6], a[7], a[8], N);
+    const nmg_rotary_desc r = rotary_desc(gpu, a[6], a[7], a[8], N);
     const double eps = real(a[9]);
     gpu(q);
     gpu(k);
     at::Tensor yq = output(gpu, q, maybe(a[10], "out[0] must be a tensor"));
     at::Tensor yk = output(gpu, k, maybe(a[11], "out[1] must be a tensor"));
-    void *const stream = gpu.stream();
-    int status;
+    const hipStream_t stream = gpu.stream();
+    nmg_status status;
     {
         Unlocked now;
         allocate(yq, q);
         allocate(yk, k);
-        status = nmg_qk_norm_rotary(code, heads, kv_heads, (int32_t)D, &r, weights[0], weights[1],
+        status = library.qk_norm_rotary(dtype_of(q), heads, kv_heads, (int32_t)D, &r, weights[0], weights[1],
                                     (float)eps, q.data_ptr(), ldq, k.data_ptr(), ldk, N,
                                     yq.data_ptr(), yq.stride(0), yk.data_ptr(), yk.stride(0), stream);
     }
@@ -249,8 +231,8 @@ bool bytes(const at::Tensor &t) {
 at::Tensor attention(PyObject *const *a) {
     const at::Tensor &q = tensor(a[0], "Q must be a tensor"), &k = tensor(a[1], "K must be a tensor"),
                      &v = tensor(a[2], "V must be a tensor");
-    Heads h = {int32(a[3]), int32(a[4]), 0, dtype_code(q)};
-    if (h.dtype < 0 || k.scalar_type() != q.scalar_type() || v.scalar_type() != q.scalar_type())
+    nmg_heads h = {int32(a[3]), int32(a[4]), 0, dtype_of(q)};
+    if (!dtype_ok(q) || k.scalar_type() != q.scalar_type() || v.scalar_type() != q.scalar_type())
         refuse(PyExc_TypeError, "Q, K and V must be float32 or float16, of one dtype");
     const int64_t ldq = rows(q, kMatrix), ldk = rows(k, kMatrix), ldv = rows(v, kMatrix);
     const int64_t Nq = q.size(1), Nk = k.size(1), D = head_rows(q.size(0), h.heads);
@@ -262,7 +244,7 @@ at::Tensor attention(PyObject *const *a) {
                      &end = tensor(a[7], "kv_end must be a tensor");
     const int64_t B = begin.numel();
     if (B > INT32_MAX) refuse_value("too many sequences");
-    const Sequences s = {(int32_t)B,
+    const nmg_sequences s = {(int32_t)B,
                          ints(offsets, B + 1, "q_offsets must be one more contiguous int32 value than kv_begin has"),
                          ints(begin, B, "kv_begin must be contiguous int32 values"),
                          ints(end, B, "kv_end must be as many contiguous int32 values as kv_begin")};
@@ -289,14 +271,14 @@ at::Tensor attention(PyObject *const *a) {
     }
     const float scale = a[10] == Py_None ? (float)(1.0 / std::sqrt((double)D)) : (float)real(a[10]);
     at::Tensor o = output(gpu, q, maybe(a[11], "out must be a tensor"));
-    void *const stream = gpu.stream();
-    int status;
+    const hipStream_t stream = gpu.stream();
+    nmg_status status;
     {
         Unlocked now;
         allocate(o, q);
         // freed after the call returns: the allocator hands it out again in stream order
         at::Tensor space;
-        int64_t room = nmg_attention_workspace_bytes(&h, s.count, Nq, Nk);
+        int64_t room = library.attention_workspace_bytes(&h, s.count, Nq, Nk);
         if (room > 0) {
             try {
                 space = at::empty({room}, q.options().dtype(at::kByte));
@@ -307,12 +289,12 @@ at::Tensor attention(PyObject *const *a) {
         void *ws = room > 0 ? space.data_ptr() : nullptr;
         room = std::max<int64_t>(room, 0);
         if (tree)
-            status = nmg_tree_attention(&h, &s, q.data_ptr(), ldq, Nq, k.data_ptr(), ldk, v.data_ptr(),
-                                        ldv, Nk, tree->data_ptr(), ldtree, tree->size(1), scale,
+            status = library.tree_attention(&h, &s, q.data_ptr(), ldq, Nq, k.data_ptr(), ldk, v.data_ptr(),
+                                        ldv, Nk, (const uint8_t *)tree->data_ptr(), ldtree, tree->size(1), scale,
                                         o.data_ptr(), o.stride(0), ws, room, stream);
         else
-            status = nmg_attention(&h, &s, q.data_ptr(), ldq, Nq, k.data_ptr(), ldk, v.data_ptr(), ldv,
-                                   Nk, mask ? mask->data_ptr() : nullptr, scale, o.data_ptr(),
+            status = library.attention(&h, &s, q.data_ptr(), ldq, Nq, k.data_ptr(), ldk, v.data_ptr(), ldv,
+                                   Nk, mask ? (const uint8_t *)mask->data_ptr() : nullptr, scale, o.data_ptr(),
                                    o.stride(0), ws, room, stream);
     }
     checked(status, tree ? "nmg_tree_attention" : "nmg_attention");
@@ -372,12 +354,12 @@ PyObject *py_bind(PyObject *, PyObject *const *a, Py_ssize_t n) {
             if (!p) refuse_value(name);
             return p;
         };
-        nmg_rotary = (decltype(nmg_rotary))at("nmg_rotary");
-        nmg_qk_norm_rotary = (decltype(nmg_qk_norm_rotary))at("nmg_qk_norm_rotary");
-        nmg_attention = (decltype(nmg_attention))at("nmg_attention");
-        nmg_tree_attention = (decltype(nmg_tree_attention))at("nmg_tree_attention");
-        nmg_attention_workspace_bytes =
-            (decltype(nmg_attention_workspace_bytes))at("nmg_attention_workspace_bytes");
+        auto bound = [&](auto &f, const char *name) { f = (std::decay_t<decltype(f)>)at(name); };
+        bound(library.rotary, "nmg_rotary");
+        bound(library.qk_norm_rotary, "nmg_qk_norm_rotary");
+        bound(library.attention, "nmg_attention");
+        bound(library.tree_attention, "nmg_tree_attention");
+        bound(library.attention_workspace_bytes, "nmg_attention_workspace_bytes");
         PyObject **kept[3] = {&check, &current_device, &current_stream};
         for (int i = 0; i < 3; ++i) {
             Py_INCREF(a[1 + i]);

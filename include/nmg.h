@@ -556,7 +556,8 @@ nmg_status nmg_rotary(nmg_dtype dtype, int32_t heads, int32_t head_dim,
  * values of one token) becomes the rotation of
  *     x[d] * w[d] / sqrt(sum_d x[d]^2 / head_dim + eps)
  * with w = q_weight for the q_heads heads of Q, k_weight for the k_heads of K
- * (binary32, head_dim values; NULL: ones).  binary32 throughout, rounded once.
+ * (binary32, head_dim values; NULL: ones).  binary32 throughout, rounded once;
+ * the x may be of any size, also where their squares are past the range.
  * k_heads may be 0 (K, YK unused).  YQ may be Q and YK may be K. */
 nmg_status nmg_qk_norm_rotary(nmg_dtype dtype, int32_t q_heads, int32_t k_heads, int32_t head_dim,
                               const nmg_rotary_desc *rotary, const float *q_weight,

@@ -18,6 +18,68 @@
 
 namespace {
 
+// Whether squares passed an end of binary32's range (below it only where eps is too)
+__device__ __forceinline__ bool squares_far(float sum, float eps) {
+    return sum == INFINITY || (sum < 0x1p-90f && eps < 0x1p-90f);
+}
+
+// One head of a workgroup's tokens with such squares: summed once more, of the values
+// times a power of two.  From memory and token by token, in few registers: it is rare.
+template <int N>
+__device__ __forceinline__ void norm_far(const RotaryArgs &a, const RotaryRows &r, int h, int64_t t,
+                                         int x, int slice, int slices, float *sums) {
+    const int lanes = a.lanes, half = a.R / 2, units = half + (a.D - a.R + 1) / 2;
+    const float *src = (const float *)r.X + (int64_t)h * a.D * r.ldx;
+    float *dst = (float *)r.Y + (int64_t)h * a.D * r.ldy;
+#pragma unroll 1
+    for (int n = 0; n < N; ++n) {
+        const int64_t c = t + n;
+        const bool here = c < a.N;
+        auto rows_of = [&](int u, int &f, int &g) {  // of unit u; g may be none: -1
+            f = u >= half ? a.R + 2 * (u - half) : a.interleaved ? 2 * u : u;
+            g = u < half ? (a.interleaved ? f + 1 : f + half) : f + 1 < a.D ? f + 1 : -1;
+        };
+        float scale = 1.f, sum = 0.f;
+#pragma unroll 1
+        for (int pass = 0; pass < 2; ++pass) {
+            float part = 0.f;
+            for (int u = slice; u < units && here; u += slices) {
+                int f, g;
+                rows_of(u, f, g);
+                const float p = scale * src[f * r.ldx + c], q = g < 0 ? 0.f : scale * src[g * r.ldx + c];
+                part = fmaf(p, p, fmaf(q, q, part));
+            }
+            for (int d = lanes; d < 64; d *= 2) part += __shfl_xor(part, d);
+            __syncthreads();  // the sums before have been read
+            if ((threadIdx.x & 63) < lanes) sums[threadIdx.x / 64 * 64 + x] = part;
+            __syncthreads();
+            sum = 0.f;
+            for (int i = 0; i < kBlock / 64; ++i) sum += sums[i * 64 + x];
+            if (pass == 0 && squares_far(sum, a.eps)) scale = sum == INFINITY ? 0x1p-100f : 0x1p100f;
+        }
+        if (!here) continue;
+        // scale / rms may pass the range, where the values are below it
+        const float first = fmaxf(scale, 1.f);
+        const float second = fminf(scale, 1.f) / sqrtf(sum / (float)a.D + a.eps * scale * scale);
+        for (int u = slice; u < units; u += slices) {
+            int f, g;
+            rows_of(u, f, g);
+            float p = first * src[f * r.ldx + c], q = g < 0 ? 0.f : first * src[g * r.ldx + c];
+            p = p * second * (r.weight ? r.weight[f] : 1.f);
+            q = q * second * (r.weight && g >= 0 ? r.weight[g] : 1.f);
+            if (u < half) {
+                const int64_t at = min(max((int64_t)a.positions[c], (int64_t)0), a.length - 1);
+                const float cs = a.table[u * a.length + at], sn = a.table[(half + u) * a.length + at];
+                const float y = p * cs - q * sn;
+                q = p * sn + q * cs;
+                p = y;
+            }
+            dst[f * r.ldy + c] = p;
+            if (g >= 0) dst[g * r.ldy + c] = q;
+        }
+    }
+}
+
 // N: tokens a thread, U: units a thread
 template <typename T, bool NORM, int N, int U>
 __global__ __launch_bounds__(kBlock, N == 4 && U <= 4 ? 3 : 1) void k_rotary(RotaryArgs a) {
@@ -118,6 +180,7 @@ __global__ __launch_bounds__(kBlock, N == 4 && U <= 4 ? 3 : 1) void k_rotary(Rot
             w[i][e] = NORM && r.weight && row[i][e] >= 0 ? r.weight[row[i][e]] : 1.f;
     }
 
+    int far = 0;             // bit h - h0: head h's squares passed the range
     for (int h = h0; h < h1; ++h) {
         T *dst = (T *)r.Y + (int64_t)h * a.D * r.ldy + t;
         float v[U][2][N];
@@ -145,12 +208,20 @@ __global__ __launch_bounds__(kBlock, N == 4 && U <= 4 ? 3 : 1) void k_rotary(Rot
 #pragma unroll
                 for (int n = 0; n < N; ++n) mine[threadIdx.x / 64][x * N + n] = scale[n];
             __syncthreads();
+            bool out = false;
 #pragma unroll
             for (int n = 0; n < N; ++n) {
                 float sum = 0.f;
 #pragma unroll
                 for (int i = 0; i < kBlock / 64; ++i) sum += mine[i][x * N + n];
                 scale[n] = 1.f / sqrtf(sum / (float)a.D + a.eps);
+                out |= squares_far(sum, a.eps);
+            }
+            // binary32: a wave holds lanes of every token of the workgroup and all have the
+            // same sums, so all of them leave such a head for the end
+            if (sizeof(T) == 4 && __any(out)) {
+                far |= 1 << (h - h0);
+                continue;
             }
         }
 #pragma unroll
@@ -181,6 +252,9 @@ __global__ __launch_bounds__(kBlock, N == 4 && U <= 4 ? 3 : 1) void k_rotary(Rot
             }
         }
     }
+    if constexpr (NORM && sizeof(T) == 4)
+        for (; far; far &= far - 1)
+            norm_far<N>(a, r, h0 + __builtin_ctz(far), t, x, slice, slices, &sums[0][0][0]);
 }
 
 __global__ __launch_bounds__(kBlock) void k_rotary_table(RotaryTableArgs a) {

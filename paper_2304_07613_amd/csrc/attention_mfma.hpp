@@ -54,7 +54,10 @@ constexpr float kLog2e = 1.4426950408889634f;
 // What differs between the element types.  kLift: weights are 2^kLift times
 // exp(s - m), and m may lag kSlack (in powers of 2) behind the true maximum: the
 // largest binary16 weight is 2^15, and weights stay normal numbers down to
-// 2^-21 of the largest.
+// 2^-21 of the largest.  Binary16 weights are rounded to binary16, the type of the
+// other operand of their product; the total that divides it is of the rounded ones.
+// With the output's own rounding that is 2.3 to 2.9e-4 off (2-norm) where binary32
+// weights are 2.1e-4; a second part for the lost bits would double that product.
 template <typename T> struct Elem;
 template <> struct Elem<_Float16> {
     static constexpr int keys = 64, per_chunk = 8;
@@ -933,12 +936,13 @@ __device__ __forceinline__ void finish(const AttnArgs &a, const Place &at, const
         }
 }
 
-// 4 waves of 32 rows over shared key tiles.  128 rows read a key tile once: 128 D
-// multiplications a byte of K or V from L2, so the matrix pipe is the bound where
-// there are workgroups enough: 16 / 4 heads x 128, 4096 columns over 16384 keys, 520 us
-// = 1060 TFLOP/s (a large library product 1330), matrix instructions in 65% of the
-// cycles, the rest the softmax's vector instructions that find no matrix instruction
-// beside them.  2 workgroups on a compute unit: one's barriers and first tiles lie
+// 4 waves of 32 rows over shared key tiles.  128 rows read a key tile once: 64
+// multiplications a byte of K and V in binary16 (8 TB/s from the L2s at the rate below,
+// where the workgroups of a head on one XCD find each other's tiles), so the matrix
+// pipe is the bound where there are workgroups enough: 16 / 4 heads x 128, 4096 columns
+// over 16384 keys, 520 us = 1060 TFLOP/s (a large library product 1330), matrix
+// instructions in 64% of the cycles, the rest the softmax's vector instructions that
+// find no matrix instruction beside them.  2 workgroups on a compute unit: one's barriers and first tiles lie
 // under the other's steps (a third: 515 -> 543 us); heads up to 64 have room for a
 // third (32 sequences of 1024 columns, 12 heads x 64: 158 us with two, 143 with three).
 template <typename T, int DP, AttnRows HOW>

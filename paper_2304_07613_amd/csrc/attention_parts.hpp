@@ -12,9 +12,10 @@
 // as fast.  12 heads x 64, 8 sequences of 1024 columns over 1024 keys: 153 us = 168
 // TFLOP/s (a large binary32 library product 154).  The splitting of K, V and the
 // weights into parts is vector work beside the matrix instructions, and the bound
-// where there are many workgroups; with one a compute unit (the same heads, 250
-// columns over ranges up to 701 keys: 51 us) it is each workgroup's own chain of
-// tiles, with matrix instructions in 17% of the cycles.
+// where there are many workgroups; with fewer than compute units (the same heads, 8
+// sequences of up to 250 columns over up to 701 keys: 192 workgroups with a row tile,
+// 51 us) it is each one's own chain of tiles, with matrix instructions in 18% of the
+// cycles.
 //
 // Infinities and NaN have no such parts (infinity x 0 among the six products is
 // NaN), and the instructions take subnormal parts as 0, which the last part of a

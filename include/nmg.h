@@ -622,6 +622,166 @@ nmg_status nmg_tree_attention(const nmg_heads *heads, const nmg_sequences *seque
 int64_t nmg_attention_workspace_bytes(const nmg_heads *heads, int32_t sequences, int64_t Nq,
                                       int64_t Nk);
 
+/* ------------------------------------------------------------------------
+ * A CACHE IN 8 BITS.  Keys and values of many sequences and layers: whole blocks
+ * of `block` tokens as pages of 8-bit codes, with one scale for each page and key
+ * head; the tokens behind a sequence's last whole block, drafted ones among them,
+ * in the activations' type (its open tokens).  So every token is rounded once,
+ * with its block, and the newest ones not at all.
+ *
+ * A sequence with n kept tokens (lengths, int32 on the device, count `sequences`,
+ * read when the kernels run) has n / block pages, whose numbers stand in its row of
+ * the table; token p behind them lies in slot p % room of its open tokens, kept ones
+ * first, then the drafted ones.  Pages may be shared by rows; `references` counts
+ * the rows that hold each.  A row's pages come first, -1 behind them.
+ *
+ * A step of a decoder: nmg_cache_append and nmg_cache_attention in every layer,
+ * nmg_cache_reserve when sequences may pass the end of a block, nmg_cache_commit of
+ * the tokens that stay.
+ *
+ * Lengths outside what a row holds are cut to it and page numbers outside the pool
+ * are taken as the nearest inside by reads and left out by writes: other contents
+ * than described give unspecified values, but no access leaves the buffers.
+ * ---------------------------------------------------------------------- */
+
+typedef enum nmg_cache_format {
+    NMG_CACHE_E4M3 = 0,      /* 8-bit floating point: 4 exponent, 3 fraction bits, up to 448 */
+    NMG_CACHE_INT8 = 1       /* integers -127 .. 127                                         */
+} nmg_cache_format;
+
+/* Every buffer is the caller's, on the device, contiguous, the large ones 16-byte
+ * aligned.  dim16 is head_dim rounded up to 16 (a key's row; the values behind
+ * head_dim are zeros, written by the library).  NMG_ERR_UNSUPPORTED: head_dim > 256, another
+ * block than 64 or 128, layers * kv_heads > 32767, (row + 1) block + room past 31
+ * bits, or 2^24 sequences or more. */
+typedef struct nmg_cache {
+    int32_t layers, kv_heads, head_dim;
+    nmg_dtype dtype;         /* of open tokens, and of the matrices that meet the cache */
+    nmg_cache_format format;
+    int32_t block;           /* tokens of a page: 64 or 128                             */
+    int32_t pages;           /* pages of a layer                                        */
+    int32_t sequences;
+    int32_t row;             /* entries of the table for each sequence                  */
+    int32_t room;            /* open tokens of a sequence, a multiple of block: the most
+                                drafted tokens and block - 1 kept ones                  */
+    void *k_pages;           /* layers x pages x kv_heads x block x dim16 codes         */
+    void *v_pages;           /* layers x pages x kv_heads x head_dim x block codes      */
+    float *k_scales;         /* layers x pages x kv_heads, powers of two                */
+    float *v_scales;
+    void *k_open;            /* layers x sequences x kv_heads x room x dim16            */
+    void *v_open;            /* layers x sequences x kv_heads x head_dim x room         */
+    int32_t *table;          /* sequences x row                                         */
+    int32_t *references;     /* pages                                                   */
+} nmg_cache;
+
+/* Drafted tokens come in: K and V are kv_heads * head_dim x N, sequence b's columns
+ * q_offsets[b] .. q_offsets[b+1] - 1 (int32, count + 1, ascending, on the device)
+ * its drafted tokens 0, 1, ..., which follow its kept ones.  Columns of no sequence,
+ * and those past the room, are left out.  May be repeated: a draft takes the place of
+ * the last one. */
+nmg_status nmg_cache_append(const nmg_cache *cache, int32_t layer, const int32_t *q_offsets,
+                            const int32_t *lengths, const void *K, int64_t ldk, const void *V,
+                            int64_t ldv, int64_t N, hipStream_t stream);
+
+/* O = softmax(scale Q^T K) V^T of every drafted token (Q, O: heads * head_dim x Nq,
+ * columns as in nmg_cache_append) over its sequence's kept tokens, and the drafted
+ * tokens that it sees: i of its sequence exactly if i < width and tree[c * ldtree +
+ * i] != 0 for query column c (bytes, Nq x width); without a tree (NULL) itself and
+ * those before it.  Query head h reads key head h / (heads / kv_heads).  Keys and values of
+ * pages are code * scale; a page whose scale is NaN makes what attends to it NaN. What other
+ * slots, pages and codes hold never matters.  A token that sees nothing, or all of whose scores are minus
+ * infinity, gives 0; drafted tokens past the room are seen by none.  Infinities and
+ * NaN of open tokens and queries reach the outputs that the formula makes them reach, and no
+ * others.  Statistics and sums are binary32; binary16 weights are rounded
+ * to binary16 for the product with V.  scale > 0.  O overlaps no input; columns
+ * of no sequence are not written.  NMG_ERR_UNSUPPORTED: Nq * heads / kv_heads past 31
+ * bits, or more row tiles and heads than one launch holds.
+ *
+ * longest: the most kept tokens that any sequence has, or 0 for all that its row
+ * holds.  It only guides how many parts the keys are split into: a smaller or larger
+ * value changes times, not what is computed.  workspace (may be NULL; 256-byte
+ * aligned): lets few queries over many keys be split over the GPU.  Too little of
+ * it: fewer parts, one with 0.  The parts, and with them the order of sums, depend
+ * on the sizes, `longest` and workspace_bytes alone.  nmg_cache_attention_workspace_bytes: the most a
+ * call uses (pure host code; -1 for invalid arguments). */
+nmg_status nmg_cache_attention(const nmg_cache *cache, int32_t layer, int32_t heads,
+                               const int32_t *q_offsets, const int32_t *lengths, const void *Q,
+                               int64_t ldq, int64_t Nq, const uint8_t *tree, int64_t ldtree,
+                               int64_t width, int64_t longest, float scale, void *O, int64_t ldo,
+                               void *workspace, int64_t workspace_bytes, hipStream_t stream);
+int64_t nmg_cache_attention_workspace_bytes(const nmg_cache *cache, int32_t heads, int64_t Nq,
+                                            int64_t longest);
+
+/* Drafted tokens that stay, in every layer: of sequence b those with the numbers
+ * kept[kept_offsets[b]] .. kept[kept_offsets[b+1] - 1] (ascending; n_kept int32 values
+ * on the device), or without a list (NULL; n_kept unused) its first kept_offsets[b+1] -
+ * kept_offsets[b].  They move behind the kept ones; every whole block among the open
+ * tokens becomes the page that the table names for it.  new_lengths[b] (int32, not
+ * lengths itself) is the new number of kept tokens: as many as the room holds, and
+ * none from the last token of a block on for which the table has no page.
+ *
+ * A block x of one layer and key head becomes codes c = x / scale, rounded to the
+ * nearest code, ties to even; scale is the smallest power of two from 2^-126 on with
+ * max |x| <= scale * (largest code).  No code stands for more than the largest value of the
+ * type: what would is the next smaller code.  A block with an infinity or NaN has
+ * the scale NaN and codes 0. */
+nmg_status nmg_cache_commit(const nmg_cache *cache, const int32_t *lengths, const int32_t *kept_offsets,
+                            const int32_t *kept, int64_t n_kept, int32_t *new_lengths,
+                            hipStream_t stream);
+
+/* Pages for coming tokens: every sequence, one after the other, gets the lowest
+ * pages with no reference until its row has (lengths[b] + tokens[b]) / block pages
+ * (tokens: int32 on the device, one a sequence).  *missing (int32 on the device): pages that the pool
+ * or the row did not have. */
+nmg_status nmg_cache_reserve(const nmg_cache *cache, const int32_t *lengths, const int32_t *tokens,
+                             int32_t *missing, hipStream_t stream);
+
+/* Sequence to[i] becomes a copy of from[i] (lists on the HOST, read before the call
+ * returns): its own pages are given back, it shares the other's whole blocks and gets a copy of the kept open
+ * tokens in every layer.  Drafted tokens are not copied.  NMG_ERR_PARAM: a number outside the
+ * sequences, one twice in `to`, or one in both lists. */
+nmg_status nmg_cache_fork(const nmg_cache *cache, int32_t *lengths, int32_t count, const int32_t *from,
+                          const int32_t *to, hipStream_t stream);
+
+/* The sequences of a list (on the HOST, each once, else NMG_ERR_PARAM) give their
+ * pages back and have no tokens. */
+nmg_status nmg_cache_free(const nmg_cache *cache, int32_t *lengths, int32_t count, const int32_t *which,
+                          hipStream_t stream);
+
+/* The pages in use (references > 0), L of them, move to the front of the pool: the k-th free page
+ * below L gets the contents of the k-th used page from L on.  table and references
+ * (outputs; may be the cache's own) follow, *live is L.  Pages from L on keep their
+ * contents.  workspace: nmg_cache_compact_workspace_bytes (-1 for an invalid cache), 256-byte
+ * aligned (NMG_ERR_CAPACITY: too small). */
+nmg_status nmg_cache_compact(const nmg_cache *cache, int32_t *table, int32_t *references, int32_t *live,
+                             void *workspace, int64_t workspace_bytes, hipStream_t stream);
+int64_t nmg_cache_compact_workspace_bytes(const nmg_cache *cache);
+
+/* Norm of a token's M features x: x w + b with
+ *   RMS    x / sqrt(mean(x^2) + eps)
+ *   LAYER  (x - mean(x)) / sqrt(mean((x - mean(x))^2) + eps)
+ *   NONE   x itself
+ * in the place of x; weight and bias binary32, M values on the device, NULL: ones and zeros. */
+typedef enum nmg_norm_kind { NMG_NORM_NONE = 0, NMG_NORM_RMS = 1, NMG_NORM_LAYER = 2 } nmg_norm_kind;
+typedef struct nmg_norm {
+    nmg_norm_kind kind;
+    const float *weight, *bias;
+    float eps;               /* >= 0 */
+} nmg_norm;
+
+/* What stands between a block of a layer and the next one, on features x tokens:
+ *     H = R + scale * G * after(A)      Y = before(H)
+ * A (M x N) is the block's output, G a gate for every element (NULL: ones), R the residual
+ * (NULL: zeros); after and before may be NULL (NONE).  H or Y may be NULL.  Computed in binary32,
+ * Y from the H that is not yet rounded, both rounded once; binary32 inputs may be of any
+ * size, also where their squares are past the range.  H and Y may each be A, G or R
+ * (with its leading dimension), not both the same.  NMG_ERR_UNSUPPORTED: M >
+ * 32768, or more tokens than one launch holds (2^32 threads, 512 for 64 tokens or fewer). */
+nmg_status nmg_residual_norm(nmg_dtype dtype, int64_t M, int64_t N, const void *A, int64_t lda,
+                             const nmg_norm *after, const void *G, int64_t ldg, float scale,
+                             const void *R, int64_t ldr, const nmg_norm *before, void *H, int64_t ldh,
+                             void *Y, int64_t ldy, hipStream_t stream);
+
 /* Static description of a status code; never NULL. */
 const char *nmg_status_str(nmg_status status);
 

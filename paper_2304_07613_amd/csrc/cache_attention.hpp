@@ -1,0 +1,791 @@
+// cache_attention.hpp -- attention over an 8-bit cache on the matrix cores: one
+// pass over pages and open tokens, online softmax, nothing staged in LDS.
+//
+// The rows of a (sequence, key head) are its drafted tokens in every query head that
+// shares the key head: row r = g T + t is token t of query head head * share + g.
+// A workgroup of four waves has NT tiles of 16 rows; its waves take key tiles of 64
+// tokens in turn, each with a running maximum, total and sum of its own, and join
+// them at the end through LDS.
+//
+// One layout serves both products without moving a value between lanes.  Lane l
+// is (x, c) = (l % 16, l / 16).
+//   scores  S^T = K Q^T: matrix instruction s of the key tile (s = 0 .. 3) takes as its row x
+//           the key 16 (x / 4) + 4 s + x % 4, so that lane (x, c) ends up with the
+//           scores of keys 16 c + 4 s + i (i = 0 .. 3) of query row x: over all
+//           s the 16 keys 16 c .. 16 c + 15.  A lane's part of a key's row is 16
+//           values from feature 64 k + 16 c on (one 16-byte load of codes); the order in
+//           which features are summed is the same for Q, which is loaded so once.
+//   sums    O^T = V P^T: the lane's weights are those of keys 16 c .. 16 c + 15, its part of
+//           V 16 values of feature 16 d + x from key 16 c on (one 16-byte load of
+//           codes).
+//
+// A page's scales are powers of two: the key scale goes into the scores.
+#pragma once
+
+#include "cache.hpp"
+
+namespace {
+
+typedef _Float16 h8 __attribute__((ext_vector_type(8)));
+typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+typedef float v2f __attribute__((ext_vector_type(2)));
+typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+
+constexpr float kLog2e = 1.44269504088896340736f;
+constexpr float kMinusInf = -__builtin_inff();
+
+// ---------------------------------------------------------------- codes
+
+// Two codes of a word (kHigh: its upper two) as binary16, exact
+template <bool kInt8, bool kHigh>
+__device__ __forceinline__ h2 decode2(uint32_t w) {
+    if constexpr (kInt8) {
+        // w holds code + 128; 0x6400 + u is 1024 + u in binary16
+        const uint32_t u = __builtin_amdgcn_perm(0x64646464u, w, kHigh ? 0x07030702u : 0x07010700u);
+        h2 v;
+        __builtin_memcpy(&v, &u, 4);
+        return v - h2{(_Float16)1152.f, (_Float16)1152.f};
+    } else {
+#if defined(__HIP_DEVICE_COMPILE__)
+        return __builtin_bit_cast(h2, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.f, kHigh));
+#else
+        return h2{};
+#endif
+    }
+}
+template <bool kInt8>
+__device__ __forceinline__ h8 decode8(uint32_t a, uint32_t b) {
+    if constexpr (kInt8) {
+        a ^= 0x80808080u;
+        b ^= 0x80808080u;
+    }
+    const h2 p = decode2<kInt8, false>(a), q = decode2<kInt8, true>(a);
+    const h2 r = decode2<kInt8, false>(b), s = decode2<kInt8, true>(b);
+    return h8{p[0], p[1], q[0], q[1], r[0], r[1], s[0], s[1]};
+}
+// Four codes as binary32, exact
+template <bool kInt8>
+__device__ __forceinline__ v4f decode4f(uint32_t w) {
+    if constexpr (kInt8) {
+        return v4f{(float)(int8_t)w, (float)(int8_t)(w >> 8), (float)(int8_t)(w >> 16),
+                   (float)((int32_t)w >> 24)};
+    } else {
+#if defined(__HIP_DEVICE_COMPILE__)
+        const v2f a = __builtin_bit_cast(v2f, __builtin_amdgcn_cvt_pk_f32_fp8(w, false));
+        const v2f b = __builtin_bit_cast(v2f, __builtin_amdgcn_cvt_pk_f32_fp8(w, true));
+        return v4f{a[0], a[1], b[0], b[1]};
+#else
+        return v4f{};
+#endif
+    }
+}
+
+__device__ __forceinline__ v4f mfma_f16(h8 a, h8 b, v4f c) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+#else
+    return c;
+#endif
+}
+__device__ __forceinline__ v4f mfma_f32(float a, float b, v4f c) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0);
+#else
+    return c;
+#endif
+}
+__device__ __forceinline__ float exp2_fast(float x) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    return __builtin_amdgcn_exp2f(x);
+#else
+    return x;
+#endif
+}
+
+// ------------------------------------------------------- what a workgroup has
+
+// Row tiles: sequence b has the slots [first(b), first(b + 1)), first(b) =
+// floor(offset(b) share / rows) + b, at least as many as its rows fill: the launch needs no
+// lengths.
+struct RowTile {
+    int b, T, q0, n;        // sequence, its query columns and their first; kept tokens
+    int first, rows;        // first row of the tile, rows of the sequence
+};
+
+template <int kRows>
+__device__ __forceinline__ bool row_tile(const CacheAttnArgs &a, int slot, RowTile &t) {
+    auto offset = [&](int b) {
+        const int v = a.q_offsets[b];
+        return v < 0 ? 0 : v > a.Nq ? a.Nq : v;
+    };
+    auto first = [&](int b) { return (int)((int64_t)offset(b) * a.share / kRows) + b; };
+    int lo = 0, hi = a.c.sequences - 1;   // the last b with first(b) <= slot
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) / 2;
+        if (first(mid) <= slot)
+            lo = mid;
+        else
+            hi = mid - 1;
+    }
+    t.b = __builtin_amdgcn_readfirstlane(lo);
+    t.q0 = offset(t.b);
+    t.T = offset(t.b + 1) - t.q0;
+    const int at = slot - first(t.b);
+    if (at < 0 || t.T <= 0 || (int64_t)at * kRows >= (int64_t)t.T * a.share) return false;
+    t.first = at * kRows;
+    t.rows = t.T * a.share;
+    t.n = cache_length(a.c, a.lengths, t.b);
+    return true;
+}
+
+// Key tiles of a row tile: whole pages' first, then those of the open tokens that
+// its rows may see
+struct KeyTiles {
+    int paged, all;         // tiles of pages, and of both
+    int open, kept;         // open tokens, and how many of them are kept ones
+};
+template <int kRows>
+__device__ __forceinline__ KeyTiles key_tiles(const CacheAttnArgs &a, const RowTile &t) {
+    KeyTiles k;
+    const int blocks = t.n / a.c.block;
+    k.kept = t.n - blocks * a.c.block;
+    k.paged = blocks * (a.c.block / 64);
+    k.open = (int)min((int64_t)k.kept + t.T, (int64_t)a.c.room);
+    int seen = k.open;
+    if (!a.tree && t.first / t.T == (min(t.first + kRows, t.rows) - 1) / t.T)  // one head's rows
+        seen = min(seen, k.kept + (min(t.first + kRows, t.rows) - 1) % t.T + 1);
+    k.all = k.paged + (seen + 63) / 64;
+    return k;
+}
+
+// ------------------------------------------------------------------ results
+
+// A wave's result of 16 NT rows: sums o (features x rows as the matrix instructions
+// leave them), divided by the totals; maxima m and totals l per row
+template <int VT, int NT>
+struct Result {
+    v4f o[VT][NT];
+    float m[NT], l[NT];
+
+    // With another's result of the same rows, which `get(d, n)` and (m2, l2) give
+    template <typename F>
+    __device__ __forceinline__ void join(int n, float m2, float l2, F &&get) {
+        const float top = fmaxf(m[n], m2), base = top == kMinusInf ? 0.f : top;
+        const float w1 = l[n] * exp2_fast(m[n] - base), w2 = l2 * exp2_fast(m2 - base);
+        const float all = w1 + w2, inv = all == 0.f ? 0.f : 1.f / all;
+        const float f1 = w1 * inv, f2 = w2 * inv;
+        // (a side without weight adds nothing, whatever it holds)
+#pragma unroll
+        for (int d = 0; d < VT; ++d) {
+            const v4f other = get(d, n);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                o[d][n][i] = (f1 == 0.f ? 0.f : o[d][n][i] * f1) + (f2 == 0.f ? 0.f : other[i] * f2);
+        }
+        m[n] = top;
+        l[n] = all;
+    }
+};
+
+// The four waves' results joined in wave 0, through LDS: two at a time
+template <int VT, int NT>
+__device__ __forceinline__ void join_waves(Result<VT, NT> &r, float *lds) {
+    constexpr int kO = VT * NT * 256, kWave = kO + NT * 128;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    auto put = [&](float *to) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+#pragma unroll
+            for (int d = 0; d < VT; ++d)
+                *reinterpret_cast<v4f *>(to + (d * NT + n) * 256 + lane * 4) = r.o[d][n];
+            to[kO + n * 128 + lane] = r.m[n];
+            to[kO + n * 128 + 64 + lane] = r.l[n];
+        }
+    };
+    auto take = [&](const float *from) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+            r.join(n, from[kO + n * 128 + lane], from[kO + n * 128 + 64 + lane], [&](int d, int m) {
+                return *reinterpret_cast<const v4f *>(from + (d * NT + m) * 256 + lane * 4);
+            });
+    };
+    if (wave >= 2) put(lds + (wave - 2) * kWave);
+    __syncthreads();
+    if (wave < 2) take(lds + wave * kWave);
+    __syncthreads();
+    if (wave == 1) put(lds);
+    __syncthreads();
+    if (wave == 0) take(lds);
+}
+template <int VT, int NT>
+constexpr int join_floats() { return std::max(2 * (VT * NT * 256 + NT * 128), 4 * 1024); }
+
+// Floats of one part's result: a row of sums for every feature, then maxima, then totals
+__host__ __device__ inline int64_t part_floats(int D, int rows) { return (int64_t)(D + 2) * rows; }
+
+template <typename T, int VT, int NT>
+__device__ __forceinline__ void store_result(const CacheAttnArgs &a, const RowTile &t, int head,
+                                             int slot, int part, const Result<VT, NT> &r) {
+    constexpr int kRows = 16 * NT;
+    const int lane = threadIdx.x & 63, x = lane % 16, c = lane / 16, D = a.c.D;
+    if (a.parts > 1) {
+        float *to = a.part + (((int64_t)head * a.slots + slot) * a.parts + part) * part_floats(D, kRows);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+#pragma unroll
+            for (int d = 0; d < VT; ++d)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (16 * d + 4 * c + i < D)
+                        to[(16 * d + 4 * c + i) * kRows + 16 * n + x] = r.o[d][n][i];
+            if (c == 0) {
+                to[D * kRows + 16 * n + x] = r.m[n];
+                to[(D + 1) * kRows + 16 * n + x] = r.l[n];
+            }
+        }
+        return;
+    }
+    T *O = static_cast<T *>(a.O);
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        const int row = t.first + 16 * n + x;
+        if (row >= t.rows) continue;
+        const int64_t h = head * a.share + row / t.T;
+        T *to = O + h * D * a.ldo + t.q0 + row % t.T;
+#pragma unroll
+        for (int d = 0; d < VT; ++d)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (16 * d + 4 * c + i < D) to[(16 * d + 4 * c + i) * a.ldo] = (T)r.o[d][n][i];
+    }
+}
+
+// ------------------------------------------------------------------ the pass
+
+// The largest of v over the four lanes (x, 0 .. 3)
+__device__ __forceinline__ float max_over_c(float v) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    const uint32_t u = __float_as_uint(v);
+    auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    v = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    const uint32_t w = __float_as_uint(v);
+    auto q = __builtin_amdgcn_permlane16_swap(w, w, false, false);
+    return fmaxf(__uint_as_float(q[0]), __uint_as_float(q[1]));
+#else
+    return v;
+#endif
+}
+__device__ __forceinline__ float sum_over_c(float v) {
+    v += __shfl_xor(v, 32);
+    return v + __shfl_xor(v, 16);
+}
+// e of v = m 2^e, 1 <= |m| < 2; 0 for 0
+__device__ __forceinline__ int exponent_of(float v) {
+    return v == 0.f ? 0 : __builtin_amdgcn_frexp_expf(v) - 1;
+}
+// What was loaded before is loaded again, rather than kept in registers
+__device__ __forceinline__ void reload() { asm volatile("" ::: "memory"); }
+// LDS that the wave's lanes wrote is read by its other lanes
+__device__ __forceinline__ void wave_sync() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
+template <typename T, int VT, int NT, bool kInt8>
+__global__ __launch_bounds__(256, NT == 1 ? 2 : 1) void k_cache_attention(CacheAttnArgs a, int total) {
+    constexpr bool kF32 = std::is_same<T, float>::value;
+    constexpr int KC = (VT + 3) / 4, W = 16 * NT;
+    constexpr int kWords = kF32 ? 4 : 2;          // 16-byte words of 16 open values
+    __shared__ __align__(16) float lds[join_floats<VT, NT>()];
+    const int lane = threadIdx.x & 63, x = lane % 16, c = lane / 16;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const CacheView &v = a.c;
+    const int D = v.D, D16 = v.D16, room = v.room;
+
+    const int at = xcd_tile(blockIdx.x, total);
+    const int slot = at % a.slots, part = at / a.slots % a.parts, head = at / a.slots / a.parts;
+    RowTile t;
+    if (!row_tile<W>(a, slot, t)) return;
+    const KeyTiles kt = key_tiles<W>(a, t);
+    const int per = (kt.all + a.parts - 1) / a.parts;
+    const int begin = part * per, end = min(kt.all, begin + per);
+    if (begin >= end) return;
+
+    // queries: the lane's features 64 k + 16 c + j of row x of every row tile
+    std::conditional_t<kF32, float[NT][KC][16], h8[NT][KC][2]> q;
+    int qe[NT];
+    int token[NT];
+    {
+        const T *Q = static_cast<const T *>(a.Q);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const int row = min(t.first + 16 * n + x, t.rows - 1);
+            token[n] = row % t.T;
+            const T *from = Q + (int64_t)(head * a.share + row / t.T) * D * a.ldq + t.q0 + token[n];
+            float top = 0.f;
+#pragma unroll
+            for (int k = 0; k < KC; ++k)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {
+                    const int d = 64 * k + 16 * c + j;
+                    const T value = d < D ? from[d * a.ldq] : (T)0.f;
+                    if constexpr (kF32) {
+                        q[n][k][j] = value;
+                        top = fmaxf(top, fabsf(value));
+                    } else {
+                        q[n][k][j / 8][j % 8] = value;
+                    }
+                }
+            qe[n] = 0;
+            if constexpr (kF32) {
+                // scaled by a power of two to below 2, so that no product with codes
+                // passes the range where the score itself does not
+                top = max_over_c(top);
+                if (top < __builtin_inff()) qe[n] = exponent_of(top);
+#pragma unroll
+                for (int k = 0; k < KC; ++k)
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) q[n][k][j] = __builtin_ldexpf(q[n][k][j], -qe[n]);
+            }
+        }
+    }
+
+    Result<VT, NT> r;
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        r.m[n] = kMinusInf;
+        r.l[n] = 0.f;
+#pragma unroll
+        for (int d = 0; d < VT; ++d) r.o[d][n] = v4f{0.f, 0.f, 0.f, 0.f};
+    }
+    // The sums are kept in units of a power of two.  binary16: of the tile at hand's
+    // values, since its weights leave no room for another factor.  binary32: of the
+    // largest scale so far, the weights take the rest.
+    float unit = kF32 ? 0x1p-126f : 1.f;
+    const float factor = a.scale * kLog2e;
+
+    auto new_unit = [&](float vs) {
+        if (kF32 ? !(vs <= unit) : vs != unit) {
+            const float f = unit / vs;
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int d = 0; d < VT; ++d) r.o[d][n] *= f;
+            unit = vs;
+        }
+    };
+    // scores s (in units of log 2) to weights, in place
+    auto softmax = [&](v4f (&s)[4][NT]) {
+        float top[NT];
+        bool up = false;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            float m = fmaxf(fmaxf(s[0][n][0], s[0][n][1]), fmaxf(s[0][n][2], s[0][n][3]));
+#pragma unroll
+            for (int i = 1; i < 4; ++i)
+                m = fmaxf(fmaxf(m, fmaxf(s[i][n][0], s[i][n][1])), fmaxf(s[i][n][2], s[i][n][3]));
+            top[n] = fmaxf(r.m[n], max_over_c(m));
+            up |= top[n] > r.m[n];
+        }
+        if (__any(up)) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                const float f = top[n] > r.m[n] ? exp2_fast(r.m[n] - top[n]) : 1.f;
+                r.m[n] = top[n];
+                r.l[n] *= f;
+#pragma unroll
+                for (int d = 0; d < VT; ++d) r.o[d][n] *= f;
+            }
+        }
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            // binary16 weights are 2^15 at most, so that the small ones stay normal down to
+            // 2^-29 of the largest (totals have the same factor)
+            const float base = (r.m[n] == kMinusInf ? 0.f : r.m[n]) - (kF32 ? 0.f : 15.f);
+            float sum = 0.f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    s[i][n][j] = exp2_fast(s[i][n][j] - base);
+                    sum += s[i][n][j];
+                }
+            r.l[n] += sum;
+        }
+    };
+    // the lane's 16 weights of a row tile as the matrix instructions take them
+    auto weights = [&](const v4f (&s)[4][NT], int n, h8 (&p)[2]) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) p[i / 8][i % 8] = (_Float16)s[i / 4][n][i % 4];
+    };
+
+    // ---- whole pages
+    const int per_block = v.block / 64, paged_end = min(end, kt.paged);
+    const int64_t heads = v.heads;
+    const int32_t *table = v.table + (int64_t)t.b * v.row;
+    auto page_of = [&](int tile) {
+        const int p = table[min(tile / per_block, v.row - 1)];
+        return __builtin_amdgcn_readfirstlane(p < 0 ? 0 : p >= v.pages ? v.pages - 1 : p);
+    };
+    u4 kk[4][KC];
+    float ks = 1.f, vs = 1.f;
+    auto load_keys = [&](int tile, int page) {
+        const int64_t of = ((int64_t)a.layer * v.pages + page) * heads + head;
+        const uint8_t *from = v.k_pages + of * v.block * D16 + (int64_t)(tile % per_block) * 64 * D16 + 16 * c;
+        ks = v.k_scales[of];
+        vs = v.v_scales[of];
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+            const uint8_t *row = from + (16 * (x / 4) + 4 * s + x % 4) * D16;
+#pragma unroll
+            for (int k = 0; k < KC; ++k)
+                kk[s][k] = 64 * k + 16 * c < D16 ? *reinterpret_cast<const u4 *>(row + 64 * k) : u4{0, 0, 0, 0};
+        }
+    };
+    int tile = begin + wave;
+    int page = 0, next_page = 0;
+    if (tile < paged_end) {
+        page = page_of(tile);
+        next_page = page_of(tile + 4);
+        load_keys(tile, page);
+    }
+    for (; tile < paged_end; tile += 4) {
+        u4 vv[VT];
+        const int64_t of = ((int64_t)a.layer * v.pages + page) * heads + head;
+        const uint8_t *from = v.v_pages + of * D * v.block + (tile % per_block) * 64 + 16 * c;
+#pragma unroll
+        for (int d = 0; d < VT; ++d)
+            vv[d] = 16 * d + x < D ? *reinterpret_cast<const u4 *>(from + (16 * d + x) * v.block)
+                                   : u4{0, 0, 0, 0};
+        const int after = page_of(tile + 8);
+        const float tile_ks = ks, tile_vs = vs < 0x1p-32f && !kF32 ? 0x1p-32f : vs;
+        v4f s[4][NT];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n) s[i][n] = v4f{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int k = 0; k < KC; ++k) {
+                if constexpr (kF32) {
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) {
+                        const v4f f = decode4f<kInt8>(kk[i][k][w]);
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+#pragma unroll
+                            for (int n = 0; n < NT; ++n) s[i][n] = mfma_f32(f[j], q[n][k][4 * w + j], s[i][n]);
+                    }
+                } else {
+                    const h8 f0 = decode8<kInt8>(kk[i][k][0], kk[i][k][1]);
+                    const h8 f1 = decode8<kInt8>(kk[i][k][2], kk[i][k][3]);
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        s[i][n] = mfma_f16(f0, q[n][k][0], s[i][n]);
+                        s[i][n] = mfma_f16(f1, q[n][k][1], s[i][n]);
+                    }
+                }
+            }
+        }
+        if (tile + 4 < paged_end) load_keys(tile + 4, next_page);
+        page = next_page;
+        next_page = after;
+        if constexpr (kF32) {
+            const int ke = exponent_of(tile_ks);
+            const float nan = tile_ks - tile_ks;       // of a block that is not finite
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        s[i][n][j] = __builtin_ldexpf(s[i][n][j] * factor, qe[n] + ke) + nan;
+        } else {
+            const float f = factor * tile_ks;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int n = 0; n < NT; ++n) s[i][n] *= f;
+        }
+        softmax(s);
+        new_unit(tile_vs);
+        if constexpr (kF32) {
+            const float f = tile_vs / unit;
+#pragma unroll
+            for (int d = 0; d < VT; ++d)
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    const v4f g = decode4f<kInt8>(vv[d][w]);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) r.o[d][n] = mfma_f32(g[j], s[w][n][j] * f, r.o[d][n]);
+                }
+        } else {
+            h8 p[NT][2];
+#pragma unroll
+            for (int n = 0; n < NT; ++n) weights(s, n, p[n]);
+#pragma unroll
+            for (int d = 0; d < VT; ++d) {
+                const h8 g0 = decode8<kInt8>(vv[d][0], vv[d][1]), g1 = decode8<kInt8>(vv[d][2], vv[d][3]);
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    r.o[d][n] = mfma_f16(g0, p[n][0], r.o[d][n]);
+                    r.o[d][n] = mfma_f16(g1, p[n][1], r.o[d][n]);
+                }
+            }
+        }
+    }
+
+    // ---- open tokens
+    for (; tile < end; tile += 4) {
+        const int first = 64 * (tile - kt.paged);          // of the open tokens
+        const int at_slot = (int)((uint32_t)(t.n - kt.kept + first) % (uint32_t)room);
+        const int64_t ring = ((int64_t)a.layer * v.sequences + t.b) * heads + head;
+        const T *kf = static_cast<const T *>(v.k_open) + (ring * room + at_slot) * D16 + 16 * c;
+        const T *vf = static_cast<const T *>(v.v_open) + ring * D * room + at_slot;
+        // which of the lane's keys each of its rows sees
+        uint32_t seen[NT];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            seen[n] = 0;
+            const uint8_t *line = a.tree ? a.tree + (int64_t)(t.q0 + token[n]) * a.ldtree : nullptr;
+            for (int j = 0; j < 16; ++j) {
+                const int u = first + 16 * c + j, e = u - kt.kept;
+                bool see = u < kt.open;
+                if (see && e >= 0) see = line ? e < a.width && line[e] != 0 : e <= token[n];
+                seen[n] |= (uint32_t)see << j;
+            }
+        }
+        v4f s[4][NT];
+        auto key_row = [&](int m) { return kf + (16 * (x / 4) + 4 * m + x % 4) * D16; };
+        auto key_word = [&](const T *row, int k, int w) {
+            return 64 * k + 16 * c < D16 ? *reinterpret_cast<const u4 *>(row + 64 * k + w * (16 / kWords))
+                                         : u4{0, 0, 0, 0};
+        };
+        int ke = 0;
+        if constexpr (kF32) {
+            // the tile's keys are scaled like codes, by its largest finite value
+            uint32_t top = 0;
+#pragma unroll 1
+            for (int m = 0; m < 4; ++m)
+#pragma unroll
+                for (int k = 0; k < KC; ++k)
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) {
+                        const u4 y = key_word(key_row(m), k, w);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const uint32_t b = y[e] & 0x7fffffffu;
+                            top = b < 0x7f800000u && b > top ? b : top;
+                        }
+                    }
+            for (int d = 1; d < 64; d *= 2) top = max(top, (uint32_t)__shfl_xor((int)top, d));
+            ke = exponent_of(__uint_as_float(top));
+            reload();
+        }
+#pragma unroll
+        for (int m = 0; m < 4; ++m) {
+            const T *row = key_row(m);
+#pragma unroll
+            for (int n = 0; n < NT; ++n) s[m][n] = v4f{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int k = 0; k < KC; ++k) {
+                if constexpr (kF32) {
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) {
+                        const u4 y = key_word(row, k, w);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const float f = __builtin_ldexpf(__uint_as_float(y[e]), -ke);
+#pragma unroll
+                            for (int n = 0; n < NT; ++n) s[m][n] = mfma_f32(f, q[n][k][4 * w + e], s[m][n]);
+                        }
+                    }
+                } else {
+                    const h8 f0 = __builtin_bit_cast(h8, key_word(row, k, 0));
+                    const h8 f1 = __builtin_bit_cast(h8, key_word(row, k, 1));
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        s[m][n] = mfma_f16(f0, q[n][k][0], s[m][n]);
+                        s[m][n] = mfma_f16(f1, q[n][k][1], s[m][n]);
+                    }
+                }
+            }
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    float y = s[m][n][e] * factor;
+                    if constexpr (kF32) y = __builtin_ldexpf(y, qe[n] + ke);
+                    s[m][n][e] = seen[n] >> (4 * m + e) & 1 ? y : kMinusInf;
+                }
+        }
+        softmax(s);
+        // values: those behind the open tokens are whatever the ring held, so none are taken
+        const int valid = kt.open - first - 16 * c;       // of the lane's 16
+        auto value_word = [&](int d, int w) {
+            u4 y = 16 * d + x < D && valid > w * (16 / kWords)
+                       ? *reinterpret_cast<const u4 *>(vf + (int64_t)(16 * d + x) * room + 16 * c +
+                                                       w * (16 / kWords))
+                       : u4{0, 0, 0, 0};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                if constexpr (kF32) {
+                    if (4 * w + e >= valid) y[e] = 0;
+                } else {
+                    if (8 * w + 2 * e >= valid) y[e] = 0;
+                    if (8 * w + 2 * e + 1 >= valid) y[e] &= 0xffffu;
+                }
+            }
+            return y;
+        };
+        float tile_vs = 1.f;
+        bool odd = false;          // a value that is not finite
+        u4 vo[kF32 ? 1 : VT][kWords];
+        if constexpr (kF32) {
+            uint32_t top = 0;
+#pragma unroll 2
+            for (int d = 0; d < VT; ++d)
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    const u4 y = value_word(d, w);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const uint32_t b = y[e] & 0x7fffffffu;
+                        odd |= b >= 0x7f800000u;
+                        top = b < 0x7f800000u && b > top ? b : top;
+                    }
+                }
+            for (int d = 1; d < 64; d *= 2) top = max(top, (uint32_t)__shfl_xor((int)top, d));
+            tile_vs = __builtin_ldexpf(1.f, max(exponent_of(__uint_as_float(top)), -126));
+            reload();
+        } else {
+            // 0 times a value that is not finite is NaN
+            v4f z = {0.f, 0.f, 0.f, 0.f};
+            const h8 none = {};
+#pragma unroll
+            for (int d = 0; d < VT; ++d)
+#pragma unroll
+                for (int w = 0; w < 2; ++w) {
+                    vo[d][w] = value_word(d, w);
+                    z = mfma_f16(__builtin_bit_cast(h8, vo[d][w]), none, z);
+                }
+            odd = z[0] != z[0] || z[1] != z[1] || z[2] != z[2] || z[3] != z[3];
+        }
+        new_unit(tile_vs);
+        if (__any(odd)) {
+            // every row takes the values that it sees and no others, one by one: weights
+            // (-1: not seen) through the wave's part of LDS
+            float *shared = lds + wave * 1024;
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                wave_sync();
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    shared[(16 * c + e) * 16 + x] = seen[n] >> e & 1 ? s[e / 4][n][e % 4] : -1.f;
+                wave_sync();
+#pragma unroll
+                for (int d = 0; d < VT; ++d)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int f = 16 * d + 4 * c + e;
+                        float o = r.o[d][n][e];
+#pragma unroll 1
+                        for (int key = 0; key < 64 && first + key < kt.open; ++key) {
+                            const float p = shared[key * 16 + x];
+                            if (f < D && p != -1.f) o += p * ((float)vf[(int64_t)f * room + key] / unit);
+                        }
+                        r.o[d][n][e] = o;
+                    }
+            }
+        } else if constexpr (kF32) {
+            const float f = 1.f / unit;
+#pragma unroll
+            for (int d = 0; d < VT; ++d)
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    const u4 y = value_word(d, w);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+#pragma unroll
+                        for (int n = 0; n < NT; ++n)
+                            r.o[d][n] = mfma_f32(__uint_as_float(y[e]) * f, s[w][n][e], r.o[d][n]);
+                }
+        } else {
+            h8 p[NT][2];
+#pragma unroll
+            for (int n = 0; n < NT; ++n) weights(s, n, p[n]);
+#pragma unroll
+            for (int d = 0; d < VT; ++d)
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    r.o[d][n] = mfma_f16(__builtin_bit_cast(h8, vo[d][0]), p[n][0], r.o[d][n]);
+                    r.o[d][n] = mfma_f16(__builtin_bit_cast(h8, vo[d][1]), p[n][1], r.o[d][n]);
+                }
+        }
+    }
+    if (end > kt.paged) __syncthreads();     // (the waves' parts of LDS are free again)
+
+    // ---- the wave's sums over its totals, then the four waves'
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        r.l[n] = sum_over_c(r.l[n]);
+        const float inv = r.l[n] == 0.f ? 0.f : 1.f / r.l[n];
+#pragma unroll
+        for (int d = 0; d < VT; ++d)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) r.o[d][n][i] = r.o[d][n][i] * inv * unit;
+    }
+    if (end - begin > 1) join_waves(r, lds);
+    if (wave == 0) store_result<T>(a, t, head, slot, part, r);
+}
+
+// Parts of a row tile's keys joined: a thread takes a row of the tile and every
+// 256 / W-th feature
+template <typename T, int W>
+__global__ __launch_bounds__(256) void k_cache_join(CacheAttnArgs a) {
+    const int slot = blockIdx.x % a.slots, head = blockIdx.x / a.slots;
+    RowTile t;
+    if (!row_tile<W>(a, slot, t)) return;
+    const KeyTiles kt = key_tiles<W>(a, t);
+    const int per = (kt.all + a.parts - 1) / a.parts, used = (kt.all + per - 1) / per;
+    const int row = threadIdx.x % W, D = a.c.D;
+    if (t.first + row >= t.rows) return;
+    const int64_t size = part_floats(D, W);
+    const float *from = a.part + ((int64_t)head * a.slots + slot) * a.parts * size + row;
+    float top = kMinusInf;
+    for (int p = 0; p < used; ++p) top = fmaxf(top, from[p * size + D * W]);
+    const float base = top == kMinusInf ? 0.f : top;
+    float all = 0.f;
+    for (int p = 0; p < used; ++p)
+        all += from[p * size + (D + 1) * W] * exp2_fast(from[p * size + D * W] - base);
+    const float inv = all == 0.f ? 0.f : 1.f / all;
+    const int64_t h = head * a.share + (t.first + row) / t.T;
+    T *to = static_cast<T *>(a.O) + h * D * a.ldo + t.q0 + (t.first + row) % t.T;
+    for (int d = threadIdx.x / W; d < D; d += 256 / W) {
+        float o = 0.f;
+        for (int p = 0; p < used; ++p) {
+            const float w = from[p * size + (D + 1) * W] * exp2_fast(from[p * size + D * W] - base) * inv;
+            o += w == 0.f ? 0.f : w * from[p * size + d * W];
+        }
+        to[d * a.ldo] = (T)o;
+    }
+}
+
+template <typename T, int VT, int NT>
+nmg_status run_cache_attention(nmg_cache_format format, const CacheAttnArgs &a, hipStream_t stream) {
+    const int64_t total = (int64_t)a.slots * a.parts * a.c.heads;
+    if (total > INT32_MAX / 256) return NMG_ERR_UNSUPPORTED;
+    if (format == NMG_CACHE_INT8)
+        k_cache_attention<T, VT, NT, true><<<(int)total, 256, 0, stream>>>(a, (int)total);
+    else
+        k_cache_attention<T, VT, NT, false><<<(int)total, 256, 0, stream>>>(a, (int)total);
+    nmg_status st = launched();
+    if (st == NMG_OK && a.parts > 1) {
+        k_cache_join<T, 16 * NT><<<a.slots * a.c.heads, 256, 0, stream>>>(a);
+        st = launched();
+    }
+    return st;
+}
+
+}  // namespace

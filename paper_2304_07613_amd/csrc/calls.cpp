@@ -1,5 +1,5 @@
-// calls.cpp -- the Python side of the attention operators' C ABI: checks of
-// tensors, outputs and workspace from torch's allocator, torch's current stream.
+// calls.cpp -- the Python side of the C ABI of the attention operators, the 8-bit
+// cache's calls of every layer or step and the residual norm: checks of tensors, outputs and workspace from torch's allocator, torch's current stream.
 // They are called for every layer and token, where the time of a call is the
 // host's: as a module the marshalling takes about 1 us, through ctypes 5 to 7.
 //
@@ -25,6 +25,13 @@ struct Library {
     decltype(&::nmg_tree_attention) tree_attention;
     decltype(&::nmg_attention_workspace_bytes) attention_workspace_bytes;
 } library;
+struct CacheLibrary {
+    decltype(&::nmg_cache_append) append;
+    decltype(&::nmg_cache_attention) attention;
+    decltype(&::nmg_cache_attention_workspace_bytes) workspace_bytes;
+    decltype(&::nmg_cache_commit) commit;
+    decltype(&::nmg_residual_norm) residual_norm;
+} more;
 PyObject *check;          // nmg._check(status, what): raises NmgError
 PyObject *current_device, *current_stream;  // torch._C's
 
@@ -301,6 +308,181 @@ at::Tensor attention(PyObject *const *a) {
     return o;
 }
 
+// The cache of nmg.Cache: the address of its nmg_cache and the device of its buffers
+const nmg_cache *cache_of(PyObject *address, PyObject *device, Gpu &gpu, const at::Tensor &t) {
+    const nmg_cache *c = static_cast<const nmg_cache *>(PyLong_AsVoidPtr(address));
+    if (!c) {
+        if (PyErr_Occurred()) throw Refused{};
+        refuse_value("a cache is expected");
+    }
+    gpu(t);
+    if (int32(device) != gpu.device) refuse_value("the cache is not on the current device");
+    return c;
+}
+
+const char *const kLengths = "lengths must be contiguous int32 values, one for every sequence";
+const char *const kOffsets = "q_offsets must be one more contiguous int32 value than there are sequences";
+
+void cache_append(PyObject *const *a) {
+    const at::Tensor &k = tensor(a[3], "K must be a tensor"), &v = tensor(a[4], "V must be a tensor"),
+                     &offsets = tensor(a[5], "q_offsets must be a tensor"),
+                     &lengths = tensor(a[6], "lengths must be a tensor");
+    Gpu gpu;
+    const nmg_cache *c = cache_of(a[0], a[1], gpu, k);
+    const int32_t layer = int32(a[2]);
+    gpu(v);
+    gpu(offsets);
+    gpu(lengths);
+    if (!dtype_ok(k) || !dtype_ok(v) || dtype_of(k) != c->dtype || dtype_of(v) != c->dtype)
+        refuse(PyExc_TypeError, "K and V must be of the cache's dtype");
+    const int64_t ldk = rows(k, kMatrix), ldv = rows(v, kMatrix), N = k.size(1);
+    if (k.size(0) != (int64_t)c->kv_heads * c->head_dim || v.sizes() != k.sizes())
+        refuse_value("K and V must have kv_heads * head_dim rows and the same tokens");
+    const int32_t *q = ints(offsets, (int64_t)c->sequences + 1, kOffsets), *n = ints(lengths, c->sequences, kLengths);
+    const hipStream_t stream = gpu.stream();
+    nmg_status status;
+    {
+        Unlocked now;
+        status = more.append(c, layer, q, n, k.data_ptr(), ldk, v.data_ptr(), ldv, N, stream);
+    }
+    checked(status, "nmg_cache_append");
+}
+
+at::Tensor cache_attention(PyObject *const *a) {
+    const at::Tensor &q = tensor(a[3], "Q must be a tensor"),
+                     &offsets = tensor(a[5], "q_offsets must be a tensor"),
+                     &lengths = tensor(a[6], "lengths must be a tensor");
+    Gpu gpu;
+    const nmg_cache *c = cache_of(a[0], a[1], gpu, q);
+    const int32_t layer = int32(a[2]), heads = int32(a[4]);
+    gpu(offsets);
+    gpu(lengths);
+    if (!dtype_ok(q) || dtype_of(q) != c->dtype) refuse(PyExc_TypeError, "Q must be of the cache's dtype");
+    const int64_t ldq = rows(q, kMatrix), N = q.size(1), D = head_rows(q.size(0), heads);
+    if (D != c->head_dim) refuse_value("Q must have heads of the cache's head size");
+    const int32_t *qo = ints(offsets, (int64_t)c->sequences + 1, kOffsets), *n = ints(lengths, c->sequences, kLengths);
+    const at::Tensor *tree = maybe(a[7], "tree must be a tensor or None");
+    int64_t ldtree = 0;
+    if (tree) {
+        if (!bytes(*tree) || tree->dim() != 2 || tree->size(0) != N)
+            refuse_value("tree must be uint8 or bool with a row for every query column");
+        ldtree = rows(*tree, kMatrix);
+        gpu(*tree);
+    }
+    const int32_t longest = a[8] == Py_None ? 0 : int32(a[8]);
+    const float scale = a[9] == Py_None ? (float)(1.0 / std::sqrt((double)D)) : (float)real(a[9]);
+    at::Tensor o = output(gpu, q, maybe(a[10], "out must be a tensor"));
+    const hipStream_t stream = gpu.stream();
+    nmg_status status;
+    {
+        Unlocked now;
+        allocate(o, q);
+        at::Tensor space;
+        int64_t room = more.workspace_bytes(c, heads, N, longest);
+        if (room > 0) {
+            try {
+                space = at::empty({room}, q.options().dtype(at::kByte));
+            } catch (const c10::OutOfMemoryError &) {
+                room = 0;
+            }
+        }
+        void *ws = room > 0 ? space.data_ptr() : nullptr;
+        room = std::max<int64_t>(room, 0);
+        status = more.attention(c, layer, heads, qo, n, q.data_ptr(), ldq, N,
+                                tree ? (const uint8_t *)tree->data_ptr() : nullptr, ldtree,
+                                tree ? tree->size(1) : 0, longest, scale, o.data_ptr(), o.stride(0), ws, room,
+                                stream);
+    }
+    checked(status, "nmg_cache_attention");
+    return o;
+}
+
+at::Tensor cache_commit(PyObject *const *a) {
+    const at::Tensor &lengths = tensor(a[2], "lengths must be a tensor"),
+                     &offsets = tensor(a[3], "kept_offsets must be a tensor");
+    Gpu gpu;
+    const nmg_cache *c = cache_of(a[0], a[1], gpu, lengths);
+    gpu(offsets);
+    const int32_t *n = ints(lengths, c->sequences, kLengths);
+    const int32_t *ko = ints(offsets, (int64_t)c->sequences + 1,
+                         "kept_offsets must be one more contiguous int32 value than there are sequences");
+    const at::Tensor *list = maybe(a[4], "kept must be a tensor or None");
+    const int32_t *kept = nullptr;
+    int64_t n_kept = 0;
+    bool none = false;             // a list of no tokens: nothing is kept
+    if (list) {
+        kept = ints(*list, list->numel(), "kept must be contiguous int32 values");
+        gpu(*list);
+        n_kept = list->numel();
+        none = n_kept == 0;
+    }
+    at::Tensor out;
+    if (const at::Tensor *given = maybe(a[5], "out must be a tensor or None")) {
+        (void)ints(*given, c->sequences, "out must be contiguous int32 values, one for every sequence");
+        gpu(*given);
+        out = *given;
+    }
+    const hipStream_t stream = gpu.stream();
+    nmg_status status;
+    {
+        Unlocked now;
+        allocate(out, lengths);
+        if (none) kept = n;        // (never read: an empty tensor has no address, NULL means no list)
+        status = more.commit(c, n, ko, kept, n_kept, out.data_ptr<int32_t>(), stream);
+    }
+    checked(status, "nmg_cache_commit");
+    return out;
+}
+
+// nmg.Norm: (address of its nmg_norm, features or -1, device or -1), or None
+const nmg_norm *norm_of(PyObject *o, int64_t M, const Gpu &gpu) {
+    if (o == Py_None) return nullptr;
+    if (!PyTuple_Check(o) || PyTuple_GET_SIZE(o) != 3) refuse(PyExc_TypeError, "a norm must be an nmg.Norm or None");
+    const nmg_norm *n = static_cast<const nmg_norm *>(PyLong_AsVoidPtr(PyTuple_GET_ITEM(o, 0)));
+    if (!n && PyErr_Occurred()) throw Refused{};
+    const int32_t m = int32(PyTuple_GET_ITEM(o, 1)), device = int32(PyTuple_GET_ITEM(o, 2));
+    if (m >= 0 && m != M) refuse_value("a norm's weight and bias must have a value for every row");
+    if (device >= 0 && device != gpu.device) refuse_value("a norm is not on the current device");
+    return n;
+}
+
+std::pair<at::Tensor, at::Tensor> residual_norm(PyObject *const *a) {
+    const at::Tensor &x = tensor(a[0], "A must be a tensor");
+    if (!dtype_ok(x)) refuse(PyExc_TypeError, "A must be float32 or float16");
+    const int64_t ldx = rows(x, kMatrix), M = x.size(0), N = x.size(1);
+    Gpu gpu;
+    gpu(x);
+    const at::Tensor *other[2] = {maybe(a[1], "R must be a tensor or None"), maybe(a[2], "gate must be a tensor or None")};
+    int64_t ld[2] = {0, 0};
+    for (int i = 0; i < 2; ++i) {
+        if (!other[i]) continue;
+        if (other[i]->scalar_type() != x.scalar_type() || other[i]->sizes() != x.sizes())
+            refuse_value("R and gate must have the shape and dtype of A");
+        ld[i] = rows(*other[i], kMatrix);
+        gpu(*other[i]);
+    }
+    const float scale = (float)real(a[3]);
+    const nmg_norm *after = norm_of(a[4], M, gpu), *before = norm_of(a[5], M, gpu);
+    at::Tensor h = output(gpu, x, maybe(a[6], "out[0] must be a tensor"));
+    at::Tensor y = output(gpu, x, maybe(a[7], "out[1] must be a tensor"));
+    const int keep = PyObject_IsTrue(a[8]);
+    if (keep < 0) throw Refused{};
+    const hipStream_t stream = gpu.stream();
+    nmg_status status;
+    {
+        Unlocked now;
+        if (keep) allocate(h, x);
+        if (before) allocate(y, x);
+        status = more.residual_norm(
+            dtype_of(x), M, N, x.data_ptr(), ldx, after, other[1] ? other[1]->data_ptr() : nullptr, ld[1], scale,
+            other[0] ? other[0]->data_ptr() : nullptr, ld[0], before, h.defined() ? h.data_ptr() : nullptr,
+            h.defined() ? h.stride(0) : 0, y.defined() ? y.data_ptr() : nullptr, y.defined() ? y.stride(0) : 0,
+            stream);
+    }
+    checked(status, "nmg_residual_norm");
+    return {h, y};
+}
+
 // No C++ exception leaves a call
 template <typename F>
 PyObject *guarded(F f) {
@@ -343,6 +525,59 @@ PyObject *py_attention(PyObject *, PyObject *const *a, Py_ssize_t n) {
     });
 }
 
+PyObject *py_cache_append(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return guarded([&]() -> PyObject * {
+        arguments(n, 7);
+        cache_append(a);
+        Py_RETURN_NONE;
+    });
+}
+PyObject *py_cache_attention(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return guarded([&] {
+        arguments(n, 11);
+        return THPVariable_Wrap(cache_attention(a));
+    });
+}
+PyObject *py_cache_commit(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return guarded([&] {
+        arguments(n, 6);
+        return THPVariable_Wrap(cache_commit(a));
+    });
+}
+PyObject *py_residual_norm(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return guarded([&]() -> PyObject * {
+        arguments(n, 9);
+        auto r = residual_norm(a);
+        auto wrap = [](const at::Tensor &t) {      // (an undefined tensor wraps to None)
+            return THPVariable_Wrap(t);
+        };
+        PyObject *h = wrap(r.first), *y = h ? wrap(r.second) : nullptr;
+        PyObject *both = y ? PyTuple_Pack(2, h, y) : nullptr;
+        Py_XDECREF(h);
+        Py_XDECREF(y);
+        return both;
+    });
+}
+
+// bind_more(functions): addresses of the cache's and the norm's functions by name
+PyObject *py_bind_more(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return guarded([&]() -> PyObject * {
+        arguments(n, 1);
+        auto bound = [&](auto &f, const char *name) {
+            PyObject *v = PyDict_Check(a[0]) ? PyDict_GetItemString(a[0], name) : nullptr;
+            void *p = v ? PyLong_AsVoidPtr(v) : nullptr;
+            if (!p) refuse_value(name);
+            f = (std::decay_t<decltype(f)>)p;
+        };
+        bound(more.append, "nmg_cache_append");
+        bound(more.attention, "nmg_cache_attention");
+        bound(more.workspace_bytes, "nmg_cache_attention_workspace_bytes");
+        bound(more.commit, "nmg_cache_commit");
+        bound(more.residual_norm, "nmg_residual_norm");
+        Py_RETURN_NONE;
+    });
+}
+
 // bind(functions, check, current_device, current_stream): addresses of the
 // library's functions by name, nmg._check, and torch._C's two
 PyObject *py_bind(PyObject *, PyObject *const *a, Py_ssize_t n) {
@@ -372,6 +607,11 @@ PyObject *py_bind(PyObject *, PyObject *const *a, Py_ssize_t n) {
 
 PyMethodDef methods[] = {
     {"bind", (PyCFunction)(void (*)())py_bind, METH_FASTCALL, nullptr},
+    {"bind_more", (PyCFunction)(void (*)())py_bind_more, METH_FASTCALL, nullptr},
+    {"cache_append", (PyCFunction)(void (*)())py_cache_append, METH_FASTCALL, nullptr},
+    {"cache_attention", (PyCFunction)(void (*)())py_cache_attention, METH_FASTCALL, nullptr},
+    {"cache_commit", (PyCFunction)(void (*)())py_cache_commit, METH_FASTCALL, nullptr},
+    {"residual_norm", (PyCFunction)(void (*)())py_residual_norm, METH_FASTCALL, nullptr},
     {"rotary", (PyCFunction)(void (*)())py_rotary, METH_FASTCALL, nullptr},
     {"qk_norm_rotary", (PyCFunction)(void (*)())py_qk_norm_rotary, METH_FASTCALL, nullptr},
     {"attention", (PyCFunction)(void (*)())py_attention, METH_FASTCALL, nullptr},

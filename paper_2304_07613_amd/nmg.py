@@ -1,5 +1,6 @@
 """Binding of ``libnmg.so`` (declared in ``include/nmg.h``): ctypes, and a compiled
-module for the attention operators, whose calls are as short as their marshalling.
+module for the calls of every layer and token (the attention operators, the 8-bit
+cache's, the residual norm), which are as short as their marshalling.
 
 Argument marshalling only: torch allocates the outputs on the input's device
 and supplies the current HIP stream; every step of the computation runs in the
@@ -30,6 +31,8 @@ KERNELS = {"auto": 0, "valu": 1, "mfma": 2, "mfma_general": 3, "mfma_scalar": 4,
 _KERNEL_NAME = {v: k for k, v in KERNELS.items()}
 EPILOGUES = {"none": 0, "gelu": 1, "add": 2}
 ROTARY_PAIRS = {"half": 0, "interleaved": 1}
+CACHE_FORMATS = {"e4m3": (0, torch.float8_e4m3fn), "int8": (1, torch.int8)}
+NORMS = {"none": 0, "rms": 1, "layer": 2}
 ROTARY_SCALING = {"none": 0, "linear": 1, "ntk": 2, "parts": 3}
 
 OK, ERR_NULL, ERR_PARAM, ERR_SHAPE, ERR_DTYPE, ERR_ALIGN, ERR_LAUNCH, ERR_UNSUPPORTED, ERR_CAPACITY = \
@@ -65,6 +68,22 @@ class _Sequences(ctypes.Structure):
                 ("kv_begin", ctypes.c_void_p), ("kv_end", ctypes.c_void_p)]
 
 
+class _Cache(ctypes.Structure):
+    _fields_ = [("layers", ctypes.c_int32), ("kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int), ("format", ctypes.c_int),
+                ("block", ctypes.c_int32), ("pages", ctypes.c_int32),
+                ("sequences", ctypes.c_int32), ("row", ctypes.c_int32), ("room", ctypes.c_int32),
+                ("k_pages", ctypes.c_void_p), ("v_pages", ctypes.c_void_p),
+                ("k_scales", ctypes.c_void_p), ("v_scales", ctypes.c_void_p),
+                ("k_open", ctypes.c_void_p), ("v_open", ctypes.c_void_p),
+                ("table", ctypes.c_void_p), ("references", ctypes.c_void_p)]
+
+
+class _Norm(ctypes.Structure):
+    _fields_ = [("kind", ctypes.c_int), ("weight", ctypes.c_void_p), ("bias", ctypes.c_void_p),
+                ("eps", ctypes.c_float)]
+
+
 class _PLayout(ctypes.Structure):
     _fields_ = [("M", ctypes.c_int32), ("K", ctypes.c_int32), ("n", ctypes.c_int32),
                 ("m", ctypes.c_int32), ("g", ctypes.c_int32), ("P", ctypes.c_int32),
@@ -94,6 +113,8 @@ def _load():
     vp, i64, i32, lp = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32, ctypes.POINTER(_Layout)
     pp = ctypes.POINTER(_PLayout)
     rp, hp, sp = (ctypes.POINTER(t) for t in (_Rotary, _Heads, _Sequences))
+    cp, np = ctypes.POINTER(_Cache), ctypes.POINTER(_Norm)
+    ip = ctypes.POINTER(i32)
     f32, f64 = ctypes.c_float, ctypes.c_double
     sig = {
         "nmg_layout_init": ([lp, i32, i32, i32, i32, i32, ctypes.c_int], ctypes.c_int),
@@ -140,6 +161,18 @@ def _load():
         "nmg_tree_attention": ([hp, sp, vp, i64, i64, vp, i64, vp, i64, i64, vp, i64, i64, f32, vp,
                                 i64, vp, i64, vp], ctypes.c_int),
         "nmg_attention_workspace_bytes": ([hp, i32, i64, i64], i64),
+        "nmg_cache_append": ([cp, i32, vp, vp, vp, i64, vp, i64, i64, vp], ctypes.c_int),
+        "nmg_cache_attention": ([cp, i32, i32, vp, vp, vp, i64, i64, vp, i64, i64, i64, f32, vp, i64,
+                                 vp, i64, vp], ctypes.c_int),
+        "nmg_cache_attention_workspace_bytes": ([cp, i32, i64, i64], i64),
+        "nmg_cache_commit": ([cp, vp, vp, vp, i64, vp, vp], ctypes.c_int),
+        "nmg_cache_reserve": ([cp, vp, vp, vp, vp], ctypes.c_int),
+        "nmg_cache_fork": ([cp, vp, i32, ip, ip, vp], ctypes.c_int),
+        "nmg_cache_free": ([cp, vp, i32, ip, vp], ctypes.c_int),
+        "nmg_cache_compact": ([cp, vp, vp, vp, vp, i64, vp], ctypes.c_int),
+        "nmg_cache_compact_workspace_bytes": ([cp], i64),
+        "nmg_residual_norm": ([ctypes.c_int, i64, i64, vp, i64, np, vp, i64, f32, vp, i64, np, vp, i64,
+                               vp, i64, vp], ctypes.c_int),
         "nmg_status_str": ([ctypes.c_int], ctypes.c_char_p),
         "nmg_version": ([], ctypes.c_char_p),
     }
@@ -155,7 +188,7 @@ _calls = None
 
 
 def _load_calls():
-    """The compiled marshalling of the attention operators, bound to the library."""
+    """The compiled marshalling of the calls of every layer, bound to the library."""
     global _calls
     L = lib()
     path = _build.calls_path()
@@ -170,6 +203,9 @@ def _load_calls():
              "nmg_attention_workspace_bytes")
     module.bind({n: ctypes.cast(getattr(L, n), ctypes.c_void_p).value for n in names}, _check,
                 torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream)
+    more = ("nmg_cache_append", "nmg_cache_attention", "nmg_cache_attention_workspace_bytes",
+            "nmg_cache_commit", "nmg_residual_norm")
+    module.bind_more({n: ctypes.cast(getattr(L, n), ctypes.c_void_p).value for n in more})
     _calls = module
     return module
 
@@ -637,3 +673,200 @@ def tree_attention(Q, K, V, heads: int, kv_heads: int, q_offsets, kv_begin, kv_e
         raise ValueError("tree must be uint8 or bool with a row for every query column")
     return (_calls or _load_calls()).attention(Q, K, V, heads, kv_heads, q_offsets, kv_begin, kv_end,
                                                None, tree, scale, out)
+
+
+# ------------------------------------------------------------ a cache in 8 bits
+
+class Cache:
+    """Buffers of a cache in 8 bits for several sequences and layers (``nmg_cache``);
+    they are read by the attribute names below and not exchanged afterwards.
+
+        k_pages     layers x pages x kv_heads x block x dim16   float8_e4m3fn or int8
+        v_pages     layers x pages x kv_heads x head_dim x block
+        k_scales    layers x pages x kv_heads                   float32
+        v_scales
+        k_open      layers x sequences x kv_heads x room x dim16  float32 or float16
+        v_open      layers x sequences x kv_heads x head_dim x room
+        table       sequences x row                             int32, -1: no page
+        references  pages                                       int32, rows that hold a page
+
+    dim16 is head_dim rounded up to 16."""
+
+    def __init__(self, k_pages, v_pages, k_scales, v_scales, k_open, v_open, table, references):
+        if v_pages.dim() != 5 or v_open.dim() != 5 or table.dim() != 2:
+            raise ValueError("pages and open tokens must have 5 dimensions and the table 2")
+        layers, pages, heads, dim, block = v_pages.shape
+        sequences, row, room, wide = *table.shape, v_open.shape[4], (dim + 15) // 16 * 16
+        by_code = {t: (name, code) for name, (code, t) in CACHE_FORMATS.items()}
+        if v_pages.dtype not in by_code or v_open.dtype not in _DTYPE_CODE:
+            raise TypeError("pages must be float8_e4m3fn or int8, open tokens float32 or float16")
+        want = {"k_pages": ((layers, pages, heads, block, wide), v_pages.dtype),
+                "v_pages": ((layers, pages, heads, dim, block), v_pages.dtype),
+                "k_scales": ((layers, pages, heads), torch.float32),
+                "v_scales": ((layers, pages, heads), torch.float32),
+                "k_open": ((layers, sequences, heads, room, wide), v_open.dtype),
+                "v_open": ((layers, sequences, heads, dim, room), v_open.dtype),
+                "table": ((sequences, row), torch.int32), "references": ((pages,), torch.int32)}
+        given = locals()
+        for name, (shape, dtype) in want.items():
+            t = given[name]
+            if t.dtype != dtype:
+                raise TypeError(f"{name} must be {dtype}")
+            if tuple(t.shape) != shape or not t.is_contiguous():
+                raise ValueError(f"{name} must be contiguous {shape}")
+            if not t.is_cuda or t.device != v_pages.device:
+                raise ValueError("a cache's tensors must be on one GPU")
+        self.buffers = {name: given[name] for name in want}
+        self.format, code = by_code[v_pages.dtype]
+        self.layers, self.pages, self.kv_heads, self.head_dim, self.block = v_pages.shape
+        self.sequences, self.row, self.room, self.dtype = sequences, row, room, v_open.dtype
+        self.device, self.index = v_pages.device, v_pages.get_device()
+        self.c = _Cache(layers, heads, dim, _DTYPE_CODE[v_open.dtype], code, block, pages, sequences,
+                        row, room, *(t.data_ptr() for t in self.buffers.values()))
+        self.address = ctypes.addressof(self.c)
+        if lib().nmg_cache_compact_workspace_bytes(self.c) < 0:
+            raise NmgError(ERR_UNSUPPORTED, "nmg_cache")
+
+    def __getattr__(self, name):
+        try:
+            return self.__dict__["buffers"][name]
+        except KeyError:
+            raise AttributeError(name) from None
+
+    @classmethod
+    def empty(cls, layers: int, kv_heads: int, head_dim: int, sequences: int, pages: int, row: int,
+              room: int, block: int = 64, format: str = "e4m3", dtype=torch.float16, device="cuda"):
+        """A cache without tokens: every page free, every row of the table empty."""
+        if format not in CACHE_FORMATS:
+            raise ValueError(f"unknown cache format {format!r}")
+        code, wide = CACHE_FORMATS[format][1], (head_dim + 15) // 16 * 16
+        make = lambda shape, t, v=0: torch.full(shape, v, dtype=t, device=device)   # noqa: E731
+        page = lambda *shape: make(shape, torch.uint8).view(code)                   # noqa: E731
+        return cls(page(layers, pages, kv_heads, block, wide), page(layers, pages, kv_heads, head_dim, block),
+                   make((layers, pages, kv_heads), torch.float32), make((layers, pages, kv_heads), torch.float32),
+                   make((layers, sequences, kv_heads, room, wide), dtype),
+                   make((layers, sequences, kv_heads, head_dim, room), dtype),
+                   make((sequences, row), torch.int32, -1), make((pages,), torch.int32))
+
+
+def _lengths(cache, t, name="lengths"):
+    """Checks an int32 value for every sequence, on the cache's device, which is current."""
+    _need_cuda(t, cache.table)
+    if t.dtype != torch.int32 or tuple(t.shape) != (cache.sequences,) or not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous int32 values, one for every sequence")
+    return t.data_ptr()
+
+
+def cache_append(cache: Cache, layer: int, K, V, q_offsets, lengths):
+    """``nmg_cache_append``: the drafted tokens' keys and values of one layer
+    (features x tokens), sequence b's in columns q_offsets[b] .. q_offsets[b + 1] -
+    1, behind its lengths[b] kept ones (int32 tensors on the device)."""
+    (_calls or _load_calls()).cache_append(cache.address, cache.index, layer, K, V, q_offsets, lengths)
+
+
+def cache_attention(cache: Cache, layer: int, Q, heads: int, q_offsets, lengths, tree=None,
+                    longest: int | None = None, scale: float | None = None, out=None):
+    """``nmg_cache_attention``: every drafted token (a column of Q) attends to its
+    sequence's kept tokens and to the drafted ones that its row of `tree` (uint8 or
+    bool) names, or without a tree to itself and those before it.  longest: the
+    most kept tokens of a sequence, where the program knows it (it guides the
+    split over the GPU).  scale: head_dim ** -0.5 by default.  Scratch memory from
+    torch's allocator."""
+    return (_calls or _load_calls()).cache_attention(cache.address, cache.index, layer, Q, heads, q_offsets,
+                                                     lengths, tree, longest, scale, out)
+
+
+def cache_commit(cache: Cache, lengths, kept_offsets, kept=None, out=None):
+    """``nmg_cache_commit``: of sequence b's drafted tokens those numbered
+    kept[kept_offsets[b]] .. kept[kept_offsets[b + 1] - 1] stay (int32, ascending), without
+    `kept` the first kept_offsets[b + 1] - kept_offsets[b]; whole blocks become
+    pages.  Returns the new lengths (out, which is not lengths)."""
+    return (_calls or _load_calls()).cache_commit(cache.address, cache.index, lengths, kept_offsets, kept, out)
+
+
+def cache_reserve(cache: Cache, lengths, tokens) -> torch.Tensor:
+    """``nmg_cache_reserve``: pages for tokens[b] more tokens of every sequence.
+    Returns the number of pages that were not there (int32, on the device)."""
+    n, t = _lengths(cache, lengths), _lengths(cache, tokens, "tokens")
+    missing = torch.empty(1, dtype=torch.int32, device=lengths.device)
+    _check(lib().nmg_cache_reserve(cache.c, n, t, missing.data_ptr(), _stream(lengths)), "nmg_cache_reserve")
+    return missing
+
+
+def _list(values):
+    values = [int(v) for v in values]
+    if any(not 0 <= v < 1 << 31 for v in values):
+        raise NmgError(ERR_PARAM, "a sequence's number")
+    return (ctypes.c_int32 * len(values))(*values), len(values)
+
+
+def cache_fork(cache: Cache, lengths, sources, targets):
+    """``nmg_cache_fork``: sequences `targets` become copies of `sources` (lists of
+    numbers), which share their pages.  Changes lengths."""
+    n, (a, count), (b, other) = _lengths(cache, lengths), _list(sources), _list(targets)
+    if count != other:
+        raise ValueError("one target for every source")
+    _check(lib().nmg_cache_fork(cache.c, n, count, a, b, _stream(lengths)), "nmg_cache_fork")
+
+
+def cache_free(cache: Cache, lengths, sequences):
+    """``nmg_cache_free``: the sequences of a list give their pages back and have no
+    tokens.  Changes lengths."""
+    n, (a, count) = _lengths(cache, lengths), _list(sequences)
+    _check(lib().nmg_cache_free(cache.c, n, count, a, _stream(lengths)), "nmg_cache_free")
+
+
+def cache_compact(cache: Cache, table=None, references=None) -> torch.Tensor:
+    """``nmg_cache_compact``: the pages in use move to the front of the pool; the
+    table and the references follow, into the cache's own or those given.  Returns
+    the number of pages in use (int32, on the device)."""
+    table = cache.table if table is None else table
+    references = cache.references if references is None else references
+    _need_cuda(table, references, cache.table)
+    for t, like in ((table, cache.table), (references, cache.references)):
+        if t.dtype != torch.int32 or t.shape != like.shape or not t.is_contiguous():
+            raise ValueError("table and references must be contiguous int32 of the cache's shapes")
+    live = torch.empty(1, dtype=torch.int32, device=table.device)
+    nbytes = lib().nmg_cache_compact_workspace_bytes(cache.c)
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=table.device)
+    _check(lib().nmg_cache_compact(cache.c, table.data_ptr(), references.data_ptr(), live.data_ptr(),
+                                   ws.data_ptr(), nbytes, _stream(table)), "nmg_cache_compact")
+    return live
+
+
+# ------------------------------------------------------- norms around a block
+
+class Norm:
+    """A norm over features (``nmg_norm``): kind "rms", "layer" or "none", weight and
+    bias float32 with a value for every feature, or None."""
+
+    def __init__(self, kind: str = "rms", weight=None, bias=None, eps: float = 1e-6):
+        if kind not in NORMS:
+            raise ValueError(f"unknown norm {kind!r}")
+        rows, device = -1, -1
+        for t in (weight, bias):
+            if t is None:
+                continue
+            if t.dtype != torch.float32 or t.dim() != 1 or not t.is_contiguous():
+                raise ValueError("a norm's weight and bias must be contiguous float32 vectors")
+            if not t.is_cuda:
+                raise ValueError("libnmg works on GPU tensors only")
+            if rows >= 0 and (t.numel() != rows or t.get_device() != device):
+                raise ValueError("a norm's weight and bias must be of one size, on one GPU")
+            rows, device = t.numel(), t.get_device()
+        self.kind, self.weight, self.bias, self.eps = kind, weight, bias, eps
+        self.c = _Norm(NORMS[kind], None if weight is None else weight.data_ptr(),
+                       None if bias is None else bias.data_ptr(), eps)
+        self.args = (ctypes.addressof(self.c), rows, device)
+
+
+def residual_norm(A, R=None, gate=None, scale: float = 1.0, after: Norm | None = None,
+                  before: Norm | None = None, out=None, keep: bool = True):
+    """``nmg_residual_norm``: H = R + scale * gate * after(A) and Y = before(H) of
+    matrices features x tokens, one pass.  Returns (H, Y); Y is None without `before`, H
+    with keep=False, where only Y is wanted.  out: (H, Y), each None or a tensor, which may be A, gate or R."""
+    h, y = (None, None) if out is None else out
+    if (before is None and y is not None) or (not keep and h is not None):
+        raise ValueError("an output is given that the call does not have")
+    return (_calls or _load_calls()).residual_norm(A, R, gate, scale, None if after is None else after.args,
+                                                   None if before is None else before.args, h, y, keep)

@@ -10,12 +10,20 @@ tokens.  A layer (residual sums as in ``stack.py``, no LayerNorm):
     h       = h + CO(attention of CQ h to the encoder's keys and values)
     y       = h + Down(GELU(Up(h)))
 
+Layers may have norms before and after each of the three blocks (``block_norms``): a
+block reads before(x) and the sum becomes x + branch_scale * after(block), one pass
+between two blocks.
+
 Several tokens are drafted at once as a tree (``step``); those that turn out
 right are kept (``accept``), the others' columns of the cache are overwritten by
 the next draft.  One token a sequence is a tree of one node.
 
 The cache of a layer holds keys and values of `capacity` columns for every
-sequence side by side; ``torch`` holds the buffers and moves cache columns.
+sequence side by side; ``torch`` holds the buffers and moves cache columns.  With
+cache="e4m3" or "int8" it is one ``nmg.Cache`` of all layers instead: pages of 8-bit
+codes, handed out as sequences grow, and the tokens of their last block as they are;
+sequences can then be copied (``fork``), dropped (``free``) and their pages moved
+together (``compact``).
 """
 from __future__ import annotations
 
@@ -25,6 +33,7 @@ import torch
 
 from . import nmg, synth
 
+BLOCKS = ("attention", "cross", "ffn")
 NAMES = ("qkv", "ao", "cross_q", "cross_kv", "cross_o", "up", "down")
 
 
@@ -58,6 +67,8 @@ class DecoderLayer:
     keys: torch.Tensor | None = None             # the cache: kv_heads * head_dim x columns
     values: torch.Tensor | None = None
     cross: tuple = field(default_factory=tuple)  # the encoder's keys and values
+    before: dict = field(default_factory=dict)   # block -> nmg.Norm of its input, for every
+    after: dict = field(default_factory=dict)    # one of BLOCKS or none; -> of its output
 
     def linear(self, name, x):
         v, idx, layout = self.packed[name]
@@ -70,23 +81,38 @@ class DecoderLayer:
 
 class SparseDecoder:
     def __init__(self, shape: DecoderShape, layers, sequences: int, capacity: int,
-                 base: float = 10000.0, pairs: str = "half", **scaling):
+                 base: float = 10000.0, pairs: str = "half", cache: str | None = None, block: int = 64,
+                 pages: int | None = None, max_draft: int = 64, branch_scale: float = 1.0, **scaling):
+        """cache: the format of an 8-bit cache, with blocks of `block` tokens, `pages`
+        pages (by default as many as all sequences fill) and drafts of up to `max_draft`
+        tokens a sequence.  branch_scale: the blocks' factor in the sums of layers with
+        norms around them."""
         self.shape, self.layers, self.capacity, self.pairs = shape, layers, capacity, pairs
+        self.branch_scale, self.max_draft, self.cache = branch_scale, max_draft, None
+        if any(layer.before for layer in layers) != all(layer.before for layer in layers):
+            raise ValueError("norms around the blocks of every layer or of none")
         device = layers[0].packed["qkv"][0].device
         self.table = nmg.rotary_table(capacity, shape.head_dim, base, device=device, **scaling)
         rows = shape.kv_heads * shape.head_dim
-        for layer in layers:
+        if cache is not None:
+            row = -(-capacity // block)
+            self.cache = nmg.Cache.empty(len(layers), shape.kv_heads, shape.head_dim, sequences,
+                                         sequences * row if pages is None else pages, row,
+                                         block * (1 + -(-max_draft // block)), block, cache, shape.dtype, device)
+        for layer in layers if cache is None else ():
             layer.keys = torch.zeros((rows, sequences * capacity), dtype=shape.dtype, device=device)
             layer.values = torch.zeros_like(layer.keys)
         self.begin = torch.arange(sequences, dtype=torch.int32, device=device) * capacity
         self.lengths = torch.zeros(sequences, dtype=torch.int32, device=device)   # kept tokens
         self.encoder_begin = self.encoder_end = None
         self.draft = [[] for _ in range(sequences)]     # the parents of the last step
+        self.kept = [0] * sequences                     # lengths, as the host knows them
 
     @classmethod
     def random(cls, shape: DecoderShape, n_layers: int, sequences: int, capacity: int, seed: int = 0,
-               norms: bool = True, device="cuda:0", **kw):
-        """A decoder of seeded normal weights."""
+               norms: bool = True, device="cuda:0", block_norms: str | None = None, **kw):
+        """A decoder of seeded normal weights.  norms: of queries and keys; block_norms: "rms"
+        or "layer", before and after every block."""
         layers = []
         for i in range(n_layers):
             packed = {}
@@ -97,6 +123,12 @@ class SparseDecoder:
             if norms:
                 layer.q_norm = (1 + 0.1 * synth.normal((shape.head_dim,), 7 + i)).to(device)
                 layer.k_norm = (1 + 0.1 * synth.normal((shape.head_dim,), 57 + i)).to(device)
+            if block_norms:
+                for j, name in enumerate(BLOCKS):
+                    for norms_of, at in ((layer.before, 200 + 10 * i + j), (layer.after, 400 + 10 * i + j)):
+                        weight = (1 + 0.1 * synth.normal((shape.hidden,), at)).to(device)
+                        bias = (0.1 * synth.normal((shape.hidden,), 1000 + at)).to(device)
+                        norms_of[name] = nmg.Norm(block_norms, weight, bias if block_norms == "layer" else None)
             layers.append(layer)
         return cls(shape, layers, sequences, capacity, **kw)
 
@@ -129,6 +161,8 @@ class SparseDecoder:
                 depth.append(int(tree[row + i].sum()) - 1)
             row += len(p)
         dev = x.device
+        if self.cache is not None and max(counts) > self.max_draft:
+            raise ValueError("a draft is longer than max_draft")
         tree, depth = tree.to(dev), torch.tensor(depth, dtype=torch.int32, device=dev)
         counts = torch.tensor(counts, dtype=torch.int32, device=dev)
         if int((self.lengths + counts).max()) > self.capacity:
@@ -141,29 +175,58 @@ class SparseDecoder:
             torch.arange(x.shape[1], device=dev)
         positions = (self.lengths[which] + depth).int()
         self.draft = [[] for _ in parents]
-        s = self.shape
-        q_rows, kv_rows = s.heads * s.head_dim, s.kv_heads * s.head_dim
-        for layer in self.layers:
-            qkv = layer.linear("qkv", x)
-            q, k, v = qkv[:q_rows], qkv[q_rows:q_rows + kv_rows], qkv[q_rows + kv_rows:]
-            if layer.q_norm is not None:
-                nmg.qk_norm_rotary(q, k, s.heads, s.kv_heads, layer.q_norm, layer.k_norm, self.table,
-                                   positions, self.pairs, out=(q, k))
-            else:   # queries and keys are rows of one matrix: heads of one call
-                qk = qkv[:q_rows + kv_rows]
-                nmg.rotary(qk, s.heads + s.kv_heads, self.table, positions, self.pairs, out=qk)
-            layer.keys.index_copy_(1, columns, k)
-            layer.values.index_copy_(1, columns, v)
-            a = nmg.tree_attention(q, layer.keys, layer.values, s.heads, s.kv_heads, offsets,
-                                   self.begin, ends, tree)
-            h = layer.fused("ao", a, "add", x)
-            if layer.cross:
-                a = nmg.attention(layer.linear("cross_q", h), *layer.cross, s.heads, s.kv_heads,
-                                  offsets, self.encoder_begin, self.encoder_end)
-                h = layer.fused("cross_o", a, "add", h)
-            x = layer.fused("down", layer.fused("up", h, "gelu"), "add", h)
+        if self.layers[0].before:
+            x = self._normed_layers(x, offsets, columns, ends, positions, tree)
+        else:
+            for i, layer in enumerate(self.layers):
+                h = layer.fused("ao", self._attend(i, layer, x, offsets, columns, ends, positions, tree), "add", x)
+                if layer.cross:
+                    h = layer.fused("cross_o", self._attend_encoder(layer, h, offsets), "add", h)
+                x = layer.fused("down", layer.fused("up", h, "gelu"), "add", h)
         self.draft = [list(p) for p in parents]
         return x
+
+    def _normed_layers(self, x, offsets, columns, ends, positions, tree):
+        """The layers with norms around their blocks: x the sum so far, y the next block's input."""
+        _, y = nmg.residual_norm(x, before=self.layers[0].before["attention"], keep=False)
+        for i, layer in enumerate(self.layers):
+            after, before, scale = layer.after, layer.before, self.branch_scale
+            a = layer.linear("ao", self._attend(i, layer, y, offsets, columns, ends, positions, tree))
+            x, y = nmg.residual_norm(a, x, None, scale, after.get("attention"),
+                                     before["cross" if layer.cross else "ffn"])
+            if layer.cross:
+                a = layer.linear("cross_o", self._attend_encoder(layer, y, offsets))
+                x, y = nmg.residual_norm(a, x, None, scale, after.get("cross"), before["ffn"])
+            a = layer.linear("down", layer.fused("up", y, "gelu"))
+            last = i + 1 == len(self.layers)
+            x, y = nmg.residual_norm(a, x, None, scale, after.get("ffn"),
+                                     None if last else self.layers[i + 1].before["attention"])
+        return x
+
+    def _attend(self, i, layer, x, offsets, columns, ends, positions, tree):
+        """Drafted tokens' attention to the cache and their ancestors."""
+        s = self.shape
+        q_rows, kv_rows = s.heads * s.head_dim, s.kv_heads * s.head_dim
+        qkv = layer.linear("qkv", x)
+        q, k, v = qkv[:q_rows], qkv[q_rows:q_rows + kv_rows], qkv[q_rows + kv_rows:]
+        if layer.q_norm is not None:
+            nmg.qk_norm_rotary(q, k, s.heads, s.kv_heads, layer.q_norm, layer.k_norm, self.table,
+                               positions, self.pairs, out=(q, k))
+        else:   # queries and keys are rows of one matrix: heads of one call
+            qk = qkv[:q_rows + kv_rows]
+            nmg.rotary(qk, s.heads + s.kv_heads, self.table, positions, self.pairs, out=qk)
+        if self.cache is not None:
+            nmg.cache_append(self.cache, i, k, v, offsets, self.lengths)
+            return nmg.cache_attention(self.cache, i, q, s.heads, offsets, self.lengths, tree, max(self.kept) or 1)
+        layer.keys.index_copy_(1, columns, k)
+        layer.values.index_copy_(1, columns, v)
+        return nmg.tree_attention(q, layer.keys, layer.values, s.heads, s.kv_heads, offsets,
+                                  self.begin, ends, tree)
+
+    def _attend_encoder(self, layer, x, offsets):
+        s = self.shape
+        return nmg.attention(layer.linear("cross_q", x), *layer.cross, s.heads, s.kv_heads,
+                             offsets, self.encoder_begin, self.encoder_end)
 
     def accept(self, kept: list):
         """Keep drafted tokens of the last step: kept[b] are indices of sequence b's
@@ -177,6 +240,9 @@ class SparseDecoder:
                 if not 0 <= i < len(parents) or parents[i] != last:
                     raise ValueError("kept tokens are one path through their sequence's last draft")
                 last = i
+        if self.cache is not None:
+            self._commit(kept)
+            return
         start = (self.begin + self.lengths).tolist()
         source = [start[b] + i for b, path in enumerate(kept) for i in path]
         target = [start[b] + i for b, path in enumerate(kept) for i in range(len(path))]
@@ -188,4 +254,44 @@ class SparseDecoder:
                     cache.index_copy_(1, target, cache.index_select(1, source))
         self.lengths += torch.tensor([len(path) for path in kept], dtype=torch.int32,
                                      device=self.begin.device)
+        self._count(kept)
+
+    def _count(self, kept):
+        self.kept = [n + len(path) for n, path in zip(self.kept, kept)]
         self.draft = [[] for _ in kept]
+
+    def _commit(self, kept):
+        counts, dev = [len(path) for path in kept], self.begin.device
+        i32 = lambda v: torch.tensor(v, dtype=torch.int32, device=dev)   # noqa: E731
+        missing = nmg.cache_reserve(self.cache, self.lengths, i32(counts))
+        # (without a page for every block of every sequence the pool may run out)
+        if self.cache.pages < self.cache.sequences * self.cache.row and missing.item():
+            raise RuntimeError("no page is free for the kept tokens: free sequences, then accept again")
+        offsets = i32([0] + counts).cumsum(0).int()
+        first = all(path == list(range(len(path))) for path in kept)
+        self.lengths = nmg.cache_commit(self.cache, self.lengths, offsets,
+                                        None if first else i32([i for path in kept for i in path]))
+        self._count(kept)
+
+    def _paged(self):
+        if self.cache is None:
+            raise ValueError("sequences share pages of an 8-bit cache only")
+        return self.cache
+
+    def fork(self, sources: list, targets: list):
+        """Sequences `targets` go on as copies of `sources`; the last draft is gone."""
+        nmg.cache_fork(self._paged(), self.lengths, sources, targets)
+        for a, b in zip(sources, targets):
+            self.kept[b] = self.kept[a]
+        self.draft = [[] for _ in self.draft]
+
+    def free(self, sequences: list):
+        """These sequences have no tokens any more, their pages are free; the last draft is gone."""
+        nmg.cache_free(self._paged(), self.lengths, sequences)
+        for b in sequences:
+            self.kept[b] = 0
+        self.draft = [[] for _ in self.draft]
+
+    def compact(self) -> int:
+        """The pages in use move to the front of the pool: their number."""
+        return int(nmg.cache_compact(self._paged()).item())

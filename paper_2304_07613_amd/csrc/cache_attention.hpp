@@ -94,6 +94,14 @@ __device__ __forceinline__ v4f mfma_f32(float a, float b, v4f c) {
     return c;
 #endif
 }
+// 16 bytes of a buffer at offset `at` of the lane and `first` of the wave
+__device__ __forceinline__ u4 buf_load16(buf_rsrc_t r, uint32_t at, uint32_t first) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    return __builtin_bit_cast(u4, __builtin_amdgcn_raw_buffer_load_b128(r, at, first, 0));
+#else
+    return u4{};
+#endif
+}
 __device__ __forceinline__ float exp2_fast(float x) {
 #if defined(__HIP_DEVICE_COMPILE__)
     return __builtin_amdgcn_exp2f(x);
@@ -114,27 +122,29 @@ struct RowTile {
 
 template <int kRows>
 __device__ __forceinline__ bool row_tile(const CacheAttnArgs &a, int slot, RowTile &t) {
-    auto offset = [&](int b) {
-        const int v = a.q_offsets[b];
-        return v < 0 ? 0 : v > a.Nq ? a.Nq : v;
-    };
-    auto first = [&](int b) { return (int)((int64_t)offset(b) * a.share / kRows) + b; };
-    int lo = 0, hi = a.c.sequences - 1;   // the last b with first(b) <= slot
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) / 2;
-        if (first(mid) <= slot)
-            lo = mid;
-        else
-            hi = mid - 1;
-    }
-    t.b = __builtin_amdgcn_readfirstlane(lo);
-    t.q0 = offset(t.b);
-    t.T = offset(t.b + 1) - t.q0;
-    const int at = slot - first(t.b);
+    auto inside = [&](int v) { return v < 0 ? 0 : v > a.Nq ? a.Nq : v; };
+    const int lane = threadIdx.x & 63;
+    // the last b with first(b) <= slot, 64 at a time; a step of the last kind has its
+    // offsets and length too
+    int lo = 0, n = a.c.sequences, stride, at;
+    do {
+        stride = (n + 63) / 64;
+        const int b = lo + min(lane * stride, n - 1);
+        const int from = inside(a.q_offsets[b]), to = inside(a.q_offsets[b + 1]);
+        const int kept = cache_length(a.c, a.lengths, b), first = (int)((int64_t)from * a.share / kRows) + b;
+        const int found = __popcll(__ballot(lane * stride < n && first <= slot)) - 1;
+        if (found < 0) return false;
+        t.b = lo + found * stride;
+        t.q0 = __builtin_amdgcn_readlane(from, found);
+        t.T = __builtin_amdgcn_readlane(to, found) - t.q0;
+        t.n = __builtin_amdgcn_readlane(kept, found);
+        at = slot - __builtin_amdgcn_readlane(first, found);
+        lo = t.b;
+        n = min(stride, n - found * stride);
+    } while (stride > 1);
     if (at < 0 || t.T <= 0 || (int64_t)at * kRows >= (int64_t)t.T * a.share) return false;
     t.first = at * kRows;
     t.rows = t.T * a.share;
-    t.n = cache_length(a.c, a.lengths, t.b);
     return true;
 }
 
@@ -220,6 +230,8 @@ __device__ __forceinline__ void join_waves(Result<VT, NT> &r, float *lds) {
 template <int VT, int NT>
 constexpr int join_floats() { return std::max(2 * (VT * NT * 256 + NT * 128), 4 * 1024); }
 
+constexpr int kMaxParts = 64;
+
 // Floats of one part's result: a row of sums for every feature, then maxima, then totals
 __host__ __device__ inline int64_t part_floats(int D, int rows) { return (int64_t)(D + 2) * rows; }
 
@@ -291,8 +303,14 @@ __device__ __forceinline__ void wave_sync() {
     __builtin_amdgcn_wave_barrier();
 }
 
+// Waves of a SIMD that the registers are to leave room for
+template <typename T, int VT, int NT>
+constexpr int attention_waves() {
+    return VT == 16 || NT == 4 || (std::is_same<T, float>::value && VT * NT == 16) ? 1 : 2;
+}
+
 template <typename T, int VT, int NT, bool kInt8>
-__global__ __launch_bounds__(256, NT == 1 ? 2 : 1) void k_cache_attention(CacheAttnArgs a, int total) {
+__global__ __launch_bounds__(256, (attention_waves<T, VT, NT>())) void k_cache_attention(CacheAttnArgs a, int total) {
     constexpr bool kF32 = std::is_same<T, float>::value;
     constexpr int KC = (VT + 3) / 4, W = 16 * NT;
     constexpr int kWords = kF32 ? 4 : 2;          // 16-byte words of 16 open values
@@ -311,6 +329,41 @@ __global__ __launch_bounds__(256, NT == 1 ? 2 : 1) void k_cache_attention(CacheA
     const int begin = part * per, end = min(kt.all, begin + per);
     if (begin >= end) return;
 
+    // ---- pages: the first ones are asked for before the queries
+    const int per_block = v.block / 64, paged_end = min(end, kt.paged);
+    const int64_t heads = v.heads;
+    const int32_t *table = v.table + (int64_t)t.b * v.row;
+    auto page_of = [&](int tile) {
+        const int p = table[min(tile / per_block, v.row - 1)];
+        return __builtin_amdgcn_readfirstlane(p < 0 ? 0 : p >= v.pages ? v.pages - 1 : p);
+    };
+    // A page's part of a head is one buffer: a load takes its base from scalar registers and
+    // one offset per lane, what lies behind the head reads as zeros.
+    const uint32_t k_bytes = v.block * D16, v_bytes = D * v.block, past = 0x7fffffffu;
+    const uint32_t k_at = (16 * (x / 4) + x % 4) * D16 + 16 * c, v_at = x * v.block + 16 * c;
+    uint32_t k_off[KC];
+#pragma unroll
+    for (int k = 0; k < KC; ++k) k_off[k] = 64 * k + 16 * c < D16 ? k_at + 64 * k : past;
+    u4 kk[4][KC];
+    float ks = 1.f, vs = 1.f;
+    auto load_keys = [&](int tile, int page) {
+        const int64_t of = ((int64_t)a.layer * v.pages + page) * heads + head;
+        const buf_rsrc_t from = buf_rsrc(v.k_pages + of * k_bytes, k_bytes);
+        const uint32_t first = (tile % per_block) * 64 * D16;
+        ks = v.k_scales[of];
+        vs = v.v_scales[of];
+#pragma unroll
+        for (int s = 0; s < 4; ++s)
+#pragma unroll
+            for (int k = 0; k < KC; ++k) kk[s][k] = buf_load16(from, k_off[k], first + 4 * s * D16);
+    };
+    int tile = begin + wave;
+    int page = 0, next_page = 0;
+    if (tile < paged_end) {
+        page = page_of(tile);
+        next_page = page_of(tile + 4);
+        load_keys(tile, page);
+    }
     // queries: the lane's features 64 k + 16 c + j of row x of every row tile
     std::conditional_t<kF32, float[NT][KC][16], h8[NT][KC][2]> q;
     int qe[NT];
@@ -321,14 +374,15 @@ __global__ __launch_bounds__(256, NT == 1 ? 2 : 1) void k_cache_attention(CacheA
         for (int n = 0; n < NT; ++n) {
             const int row = min(t.first + 16 * n + x, t.rows - 1);
             token[n] = row % t.T;
-            const T *from = Q + (int64_t)(head * a.share + row / t.T) * D * a.ldq + t.q0 + token[n];
+            const T *from = Q + ((int64_t)(head * a.share + row / t.T) * D + 16 * c) * a.ldq + t.q0 + token[n];
             float top = 0.f;
 #pragma unroll
             for (int k = 0; k < KC; ++k)
 #pragma unroll
                 for (int j = 0; j < 16; ++j) {
                     const int d = 64 * k + 16 * c + j;
-                    const T value = d < D ? from[d * a.ldq] : (T)0.f;
+                    const T value = d < D ? *from : (T)0.f;
+                    from += j < 15 ? a.ldq : 49 * a.ldq;
                     if constexpr (kF32) {
                         q[n][k][j] = value;
                         top = fmaxf(top, fabsf(value));
@@ -420,43 +474,13 @@ __global__ __launch_bounds__(256, NT == 1 ? 2 : 1) void k_cache_attention(CacheA
     };
 
     // ---- whole pages
-    const int per_block = v.block / 64, paged_end = min(end, kt.paged);
-    const int64_t heads = v.heads;
-    const int32_t *table = v.table + (int64_t)t.b * v.row;
-    auto page_of = [&](int tile) {
-        const int p = table[min(tile / per_block, v.row - 1)];
-        return __builtin_amdgcn_readfirstlane(p < 0 ? 0 : p >= v.pages ? v.pages - 1 : p);
-    };
-    u4 kk[4][KC];
-    float ks = 1.f, vs = 1.f;
-    auto load_keys = [&](int tile, int page) {
-        const int64_t of = ((int64_t)a.layer * v.pages + page) * heads + head;
-        const uint8_t *from = v.k_pages + of * v.block * D16 + (int64_t)(tile % per_block) * 64 * D16 + 16 * c;
-        ks = v.k_scales[of];
-        vs = v.v_scales[of];
-#pragma unroll
-        for (int s = 0; s < 4; ++s) {
-            const uint8_t *row = from + (16 * (x / 4) + 4 * s + x % 4) * D16;
-#pragma unroll
-            for (int k = 0; k < KC; ++k)
-                kk[s][k] = 64 * k + 16 * c < D16 ? *reinterpret_cast<const u4 *>(row + 64 * k) : u4{0, 0, 0, 0};
-        }
-    };
-    int tile = begin + wave;
-    int page = 0, next_page = 0;
-    if (tile < paged_end) {
-        page = page_of(tile);
-        next_page = page_of(tile + 4);
-        load_keys(tile, page);
-    }
     for (; tile < paged_end; tile += 4) {
         u4 vv[VT];
         const int64_t of = ((int64_t)a.layer * v.pages + page) * heads + head;
-        const uint8_t *from = v.v_pages + of * D * v.block + (tile % per_block) * 64 + 16 * c;
+        const buf_rsrc_t from = buf_rsrc(v.v_pages + of * v_bytes, v_bytes);
+        const uint32_t first = (tile % per_block) * 64;
 #pragma unroll
-        for (int d = 0; d < VT; ++d)
-            vv[d] = 16 * d + x < D ? *reinterpret_cast<const u4 *>(from + (16 * d + x) * v.block)
-                                   : u4{0, 0, 0, 0};
+        for (int d = 0; d < VT; ++d) vv[d] = buf_load16(from, v_at + first + 16 * d * v.block, 0);
         const int after = page_of(tile + 8);
         const float tile_ks = ks, tile_vs = vs < 0x1p-32f && !kF32 ? 0x1p-32f : vs;
         v4f s[4][NT];
@@ -541,7 +565,7 @@ __global__ __launch_bounds__(256, NT == 1 ? 2 : 1) void k_cache_attention(CacheA
         const int first = 64 * (tile - kt.paged);          // of the open tokens
         const int at_slot = (int)((uint32_t)(t.n - kt.kept + first) % (uint32_t)room);
         const int64_t ring = ((int64_t)a.layer * v.sequences + t.b) * heads + head;
-        const T *kf = static_cast<const T *>(v.k_open) + (ring * room + at_slot) * D16 + 16 * c;
+        const T *kf = static_cast<const T *>(v.k_open) + (ring * room + at_slot) * D16;
         const T *vf = static_cast<const T *>(v.v_open) + ring * D * room + at_slot;
         // which of the lane's keys each of its rows sees
         uint32_t seen[NT];
@@ -557,10 +581,10 @@ __global__ __launch_bounds__(256, NT == 1 ? 2 : 1) void k_cache_attention(CacheA
             }
         }
         v4f s[4][NT];
-        auto key_row = [&](int m) { return kf + (16 * (x / 4) + 4 * m + x % 4) * D16; };
-        auto key_word = [&](const T *row, int k, int w) {
-            return 64 * k + 16 * c < D16 ? *reinterpret_cast<const u4 *>(row + 64 * k + w * (16 / kWords))
-                                         : u4{0, 0, 0, 0};
+        const buf_rsrc_t key_tile = buf_rsrc(kf, 64 * D16 * sizeof(T));
+        auto key_word = [&](int m, int k, int w) {
+            const uint32_t at = k_off[k] == past ? past : k_off[k] * (uint32_t)sizeof(T);
+            return buf_load16(key_tile, at, (4 * m * D16 + w * (16 / kWords)) * sizeof(T));
         };
         int ke = 0;
         if constexpr (kF32) {
@@ -572,7 +596,7 @@ __global__ __launch_bounds__(256, NT == 1 ? 2 : 1) void k_cache_attention(CacheA
                 for (int k = 0; k < KC; ++k)
 #pragma unroll
                     for (int w = 0; w < 4; ++w) {
-                        const u4 y = key_word(key_row(m), k, w);
+                        const u4 y = key_word(m, k, w);
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
                             const uint32_t b = y[e] & 0x7fffffffu;
@@ -585,7 +609,6 @@ __global__ __launch_bounds__(256, NT == 1 ? 2 : 1) void k_cache_attention(CacheA
         }
 #pragma unroll
         for (int m = 0; m < 4; ++m) {
-            const T *row = key_row(m);
 #pragma unroll
             for (int n = 0; n < NT; ++n) s[m][n] = v4f{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -593,7 +616,7 @@ __global__ __launch_bounds__(256, NT == 1 ? 2 : 1) void k_cache_attention(CacheA
                 if constexpr (kF32) {
 #pragma unroll
                     for (int w = 0; w < 4; ++w) {
-                        const u4 y = key_word(row, k, w);
+                        const u4 y = key_word(m, k, w);
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
                             const float f = __builtin_ldexpf(__uint_as_float(y[e]), -ke);
@@ -602,8 +625,8 @@ __global__ __launch_bounds__(256, NT == 1 ? 2 : 1) void k_cache_attention(CacheA
                         }
                     }
                 } else {
-                    const h8 f0 = __builtin_bit_cast(h8, key_word(row, k, 0));
-                    const h8 f1 = __builtin_bit_cast(h8, key_word(row, k, 1));
+                    const h8 f0 = __builtin_bit_cast(h8, key_word(m, k, 0));
+                    const h8 f1 = __builtin_bit_cast(h8, key_word(m, k, 1));
 #pragma unroll
                     for (int n = 0; n < NT; ++n) {
                         s[m][n] = mfma_f16(f0, q[n][k][0], s[m][n]);
@@ -641,7 +664,6 @@ __global__ __launch_bounds__(256, NT == 1 ? 2 : 1) void k_cache_attention(CacheA
         };
         float tile_vs = 1.f;
         bool odd = false;          // a value that is not finite
-        u4 vo[kF32 ? 1 : VT][kWords];
         if constexpr (kF32) {
             uint32_t top = 0;
 #pragma unroll 2
@@ -666,10 +688,8 @@ __global__ __launch_bounds__(256, NT == 1 ? 2 : 1) void k_cache_attention(CacheA
 #pragma unroll
             for (int d = 0; d < VT; ++d)
 #pragma unroll
-                for (int w = 0; w < 2; ++w) {
-                    vo[d][w] = value_word(d, w);
-                    z = mfma_f16(__builtin_bit_cast(h8, vo[d][w]), none, z);
-                }
+                for (int w = 0; w < 2; ++w) z = mfma_f16(__builtin_bit_cast(h8, value_word(d, w)), none, z);
+            reload();
             odd = z[0] != z[0] || z[1] != z[1] || z[2] != z[2] || z[3] != z[3];
         }
         new_unit(tile_vs);
@@ -688,7 +708,8 @@ __global__ __launch_bounds__(256, NT == 1 ? 2 : 1) void k_cache_attention(CacheA
                 for (int d = 0; d < VT; ++d)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        const int f = 16 * d + 4 * c + e;
+                        int f = 16 * d + 4 * c + e;
+                        asm volatile("" : "+v"(f));      // (its address is not kept for the next n)
                         float o = r.o[d][n][e];
 #pragma unroll 1
                         for (int key = 0; key < 64 && first + key < kt.open; ++key) {
@@ -716,12 +737,14 @@ __global__ __launch_bounds__(256, NT == 1 ? 2 : 1) void k_cache_attention(CacheA
 #pragma unroll
             for (int n = 0; n < NT; ++n) weights(s, n, p[n]);
 #pragma unroll
-            for (int d = 0; d < VT; ++d)
+            for (int d = 0; d < VT; ++d) {
+                const h8 g0 = __builtin_bit_cast(h8, value_word(d, 0)), g1 = __builtin_bit_cast(h8, value_word(d, 1));
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
-                    r.o[d][n] = mfma_f16(__builtin_bit_cast(h8, vo[d][0]), p[n][0], r.o[d][n]);
-                    r.o[d][n] = mfma_f16(__builtin_bit_cast(h8, vo[d][1]), p[n][1], r.o[d][n]);
+                    r.o[d][n] = mfma_f16(g0, p[n][0], r.o[d][n]);
+                    r.o[d][n] = mfma_f16(g1, p[n][1], r.o[d][n]);
                 }
+            }
         }
     }
     if (end > kt.paged) __syncthreads();     // (the waves' parts of LDS are free again)
@@ -740,33 +763,43 @@ __global__ __launch_bounds__(256, NT == 1 ? 2 : 1) void k_cache_attention(CacheA
     if (wave == 0) store_result<T>(a, t, head, slot, part, r);
 }
 
-// Parts of a row tile's keys joined: a thread takes a row of the tile and every
-// 256 / W-th feature
+// Parts of a row tile's keys joined.  A thread takes a row of the tile and every 256 / W-th
+// feature of its workgroup's; the parts' weights are made once, in LDS.
 template <typename T, int W>
 __global__ __launch_bounds__(256) void k_cache_join(CacheAttnArgs a) {
+    __shared__ float top_of[kMaxParts][W], weight[kMaxParts][W];
     const int slot = blockIdx.x % a.slots, head = blockIdx.x / a.slots;
     RowTile t;
     if (!row_tile<W>(a, slot, t)) return;
     const KeyTiles kt = key_tiles<W>(a, t);
     const int per = (kt.all + a.parts - 1) / a.parts, used = (kt.all + per - 1) / per;
-    const int row = threadIdx.x % W, D = a.c.D;
-    if (t.first + row >= t.rows) return;
+    constexpr int kGroups = 256 / W;
+    const int row = threadIdx.x % W, g = threadIdx.x / W, D = a.c.D;
     const int64_t size = part_floats(D, W);
     const float *from = a.part + ((int64_t)head * a.slots + slot) * a.parts * size + row;
-    float top = kMinusInf;
-    for (int p = 0; p < used; ++p) top = fmaxf(top, from[p * size + D * W]);
+    for (int p = g; p < used; p += kGroups) {
+        top_of[p][row] = from[p * size + D * W];
+        weight[p][row] = from[p * size + (D + 1) * W];
+    }
+    __syncthreads();
+    float top = kMinusInf, all = 0.f;
+    for (int p = 0; p < used; ++p) top = fmaxf(top, top_of[p][row]);
     const float base = top == kMinusInf ? 0.f : top;
-    float all = 0.f;
-    for (int p = 0; p < used; ++p)
-        all += from[p * size + (D + 1) * W] * exp2_fast(from[p * size + D * W] - base);
+    for (int p = 0; p < used; ++p) all += weight[p][row] * exp2_fast(top_of[p][row] - base);
     const float inv = all == 0.f ? 0.f : 1.f / all;
+    __syncthreads();
+    for (int p = g; p < used; p += kGroups) weight[p][row] *= exp2_fast(top_of[p][row] - base) * inv;
+    __syncthreads();
+    if (t.first + row >= t.rows) return;
     const int64_t h = head * a.share + (t.first + row) / t.T;
     T *to = static_cast<T *>(a.O) + h * D * a.ldo + t.q0 + (t.first + row) % t.T;
-    for (int d = threadIdx.x / W; d < D; d += 256 / W) {
+    const int each = (D + gridDim.y - 1) / gridDim.y, end = min(D, ((int)blockIdx.y + 1) * each);
+    for (int d = blockIdx.y * each + g; d < end; d += kGroups) {
         float o = 0.f;
+#pragma unroll 8
         for (int p = 0; p < used; ++p) {
-            const float w = from[p * size + (D + 1) * W] * exp2_fast(from[p * size + D * W] - base) * inv;
-            o += w == 0.f ? 0.f : w * from[p * size + d * W];
+            const float w = weight[p][row], v = from[p * size + d * W];
+            o += w == 0.f ? 0.f : w * v;
         }
         to[d * a.ldo] = (T)o;
     }
@@ -782,7 +815,10 @@ nmg_status run_cache_attention(nmg_cache_format format, const CacheAttnArgs &a, 
         k_cache_attention<T, VT, NT, false><<<(int)total, 256, 0, stream>>>(a, (int)total);
     nmg_status st = launched();
     if (st == NMG_OK && a.parts > 1) {
-        k_cache_join<T, 16 * NT><<<a.slots * a.c.heads, 256, 0, stream>>>(a);
+        // workgroups for every compute unit, as far as a feature for every thread goes
+        const int64_t tiles = (int64_t)a.slots * a.c.heads, most = std::max(1, a.c.D * 16 * NT / 256);
+        const int y = (int)std::min<int64_t>(most, std::max<int64_t>(1, 1024 / tiles));
+        k_cache_join<T, 16 * NT><<<dim3((int)tiles, y), 256, 0, stream>>>(a);
         st = launched();
     }
     return st;

@@ -21,13 +21,13 @@ int64_t part_bytes(const CacheAttnArgs &a, const Plan &p, int64_t parts) {
 Plan plan(nmg_dtype dtype, const CacheAttnArgs &a, int64_t longest) {
     Plan p;
     const int64_t rows = ((int64_t)a.Nq + a.c.sequences - 1) / a.c.sequences * a.share;
-    const int most = dtype == NMG_F32 ? (a.c.D > 128 ? 1 : 2) : a.c.D > 128 ? 2 : 4;
+    const int most = dtype == NMG_F32 ? (a.c.D > 128 ? 1 : 2) : 2;
     p.nt = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
     if (p.nt > most) p.nt = most;
     p.slots = (int64_t)a.Nq * a.share / (16 * p.nt) + a.c.sequences;
     const int64_t full = (rows + 16 * p.nt - 1) / (16 * p.nt) * a.c.sequences * a.c.heads;
     const int64_t tiles = longest / 64 + 1;
-    p.parts = std::max<int64_t>(1, std::min((int64_t)2 * device_cus() / full, tiles / 8));
+    p.parts = std::max<int64_t>(1, std::min((int64_t)2 * device_cus() / full, std::min<int64_t>(64, tiles / 8)));
     return p;
 }
 

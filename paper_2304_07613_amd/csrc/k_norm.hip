@@ -3,62 +3,103 @@
 //
 // A workgroup takes a tile of tokens with all their features and holds it in registers
 // from the first read to the last store: every matrix is read or written once.  A
-// thread has kVec neighbouring tokens of every (512 / lanes)-th row, so that the
+// thread has kVec neighbouring tokens of every (threads / lanes)-th row, so that the
 // tile's part of a row is one run; the sums of a token go over lanes, then over
-// waves through LDS.
+// waves through LDS.  Rows may start on any element: the loads of kVec tokens do not
+// ask for more.
 #include "norm.hpp"
 
 namespace {
 
-constexpr int kThreads = 512;
+constexpr int kThreads = 512;    // of a workgroup; 1024 were slower at every size (128 registers each)
 constexpr int kHold = 64;        // values a thread holds, at most
 
 template <typename T, int kVec>
-struct __align__(sizeof(T) * kVec) Pack {
+struct Pack {
     T v[kVec];
+    // kWhole: all kVec are inside, else the first `valid`
+    template <bool kWhole>
+    __device__ __forceinline__ static Pack load(const T *from, int valid) {
+        Pack p = {};
+        if constexpr (kWhole)
+            __builtin_memcpy(&p, from, sizeof p);
+        else
+#pragma unroll
+            for (int e = 0; e < kVec; ++e)
+                if (e < valid) p.v[e] = from[e];
+        return p;
+    }
+    template <bool kWhole>
+    __device__ __forceinline__ void store(T *to, int valid) const {
+        if constexpr (kWhole)
+            __builtin_memcpy(to, this, sizeof *this);
+        else
+#pragma unroll
+            for (int e = 0; e < kVec; ++e)
+                if (e < valid) to[e] = v[e];
+    }
 };
 
-// Sums (kMax: largest) of v over the threads of the same tokens
-template <int kVec, bool kMax>
-__device__ __forceinline__ void over_rows(float (&v)[kVec], int lanes, float *lds) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, tokens = lanes * kVec;
-#pragma unroll
-    for (int e = 0; e < kVec; ++e)
-        for (int d = 32; d >= lanes; d /= 2) {
-            const float o = __shfl_xor(v[e], d);
-            v[e] = kMax ? fmaxf(v[e], o) : v[e] + o;
-        }
-    float *total = lds + kThreads / 64 * 64 * kVec;
-    __syncthreads();                             // (the last call's totals have been read)
-    if (lane < lanes)
-#pragma unroll
-        for (int e = 0; e < kVec; ++e) lds[wave * tokens + lane * kVec + e] = v[e];
-    __syncthreads();
-    if ((int)threadIdx.x < tokens) {
-        float s = lds[threadIdx.x];
-        for (int w = 1; w < kThreads / 64; ++w) {
-            const float o = lds[w * tokens + threadIdx.x];
-            s = kMax ? fmaxf(s, o) : s + o;
-        }
-        total[threadIdx.x] = s;
-    }
-    __syncthreads();
-    const int first = threadIdx.x % lanes * kVec;
-#pragma unroll
-    for (int e = 0; e < kVec; ++e) v[e] = total[first + e];
-}
+// Sums (kMax: largest) of v over the threads of the same tokens.  Two buffers in turn, so that
+// one barrier a call is enough.
 template <int kVec>
-constexpr int over_rows_floats() { return (kThreads / 64 + 1) * 64 * kVec; }
+struct Reducer {
+    static constexpr int kWaves = kThreads / 64;
+    float *lds;
+    int lanes, turn = 0;
+
+    template <bool kMax>
+    __device__ __forceinline__ void operator()(float (&v)[kVec]) {
+        auto both = [](float a, float b) { return kMax ? fmaxf(a, b) : a + b; };
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, tokens = lanes * kVec;
+        float *here = lds + turn * kWaves * tokens;
+        turn ^= 1;
+        if (kVec > 1 && lanes * kVec <= 64) {
+            // halves are exchanged first: a lane ends up with one of its tokens, after 10
+            // moves in place of 6 kVec
+            int token = 0;
+#pragma unroll
+            for (int c = kVec / 2, d = 32; c >= 1; c /= 2, d /= 2) {
+                const bool up = lane & d;
+#pragma unroll
+                for (int e = 0; e < c; ++e) {
+                    const float send = up ? v[e] : v[e + c], keep = up ? v[e + c] : v[e];
+                    v[e] = both(keep, __shfl_xor(send, d));
+                }
+                token += up ? c : 0;
+            }
+            for (int d = 32 / kVec; d >= lanes; d /= 2) v[0] = both(v[0], __shfl_xor(v[0], d));
+            if (lane % (64 / kVec) < lanes) here[wave * tokens + lane % lanes * kVec + token] = v[0];
+        } else {
+#pragma unroll
+            for (int e = 0; e < kVec; ++e)
+                for (int d = 32; d >= lanes; d /= 2) v[e] = both(v[e], __shfl_xor(v[e], d));
+            if (lane < lanes)
+#pragma unroll
+                for (int e = 0; e < kVec; ++e) here[wave * tokens + lane * kVec + e] = v[e];
+        }
+        __syncthreads();
+        const float *mine = here + threadIdx.x % lanes * kVec;
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) v[e] = mine[e];
+        for (int w = 1; w < kWaves; ++w)
+#pragma unroll
+            for (int e = 0; e < kVec; ++e) v[e] = both(v[e], mine[w * tokens + e]);
+    }
+};
 
 // x becomes its norm, without weight and bias
 template <typename T, int kVec, int kPer>
-__device__ __forceinline__ void normed(float (&x)[kPer][kVec], const nmg_norm &norm, int M, int lanes,
-                                       float *lds) {
+__device__ __forceinline__ void normed(float (&x)[kPer][kVec], const nmg_norm &norm, int M,
+                                       Reducer<kVec> &reduce) {
     if (norm.kind == NMG_NORM_NONE) return;
-    const int step = kThreads / lanes, r0 = threadIdx.x / lanes;
+    const int step = kThreads / reduce.lanes, r0 = threadIdx.x / reduce.lanes;
     const float inv_m = 1.f / (float)M;
     float mean[kVec], ss[kVec];
-    auto statistics = [&]() {
+    int ex[kVec] = {};
+    bool scaled = false;
+#pragma unroll 1
+    for (;;) {
 #pragma unroll
         for (int e = 0; e < kVec; ++e) mean[e] = 0.f;
         if (norm.kind == NMG_NORM_LAYER) {
@@ -66,7 +107,7 @@ __device__ __forceinline__ void normed(float (&x)[kPer][kVec], const nmg_norm &n
             for (int i = 0; i < kPer; ++i)
 #pragma unroll
                 for (int e = 0; e < kVec; ++e) mean[e] += x[i][e];   // (rows past M hold 0)
-            over_rows<kVec, false>(mean, lanes, lds);
+            reduce.template operator()<false>(mean);
 #pragma unroll
             for (int e = 0; e < kVec; ++e) mean[e] *= inv_m;
         }
@@ -79,112 +120,146 @@ __device__ __forceinline__ void normed(float (&x)[kPer][kVec], const nmg_norm &n
                 const float d = r0 + i * step < M ? x[i][e] - mean[e] : 0.f;
                 ss[e] += d * d;
             }
-        over_rows<kVec, false>(ss, lanes, lds);
-    };
-    statistics();
-    if constexpr (std::is_same<T, float>::value) {
+        reduce.template operator()<false>(ss);
+        if constexpr (!std::is_same<T, float>::value) break;
         // Squares or sums past the range, or below it where eps does not cover what is
         // lost: the tokens are scaled by a power of two each to below 2 and summed again.
         bool again = false;
 #pragma unroll
         for (int e = 0; e < kVec; ++e)
             again |= !(ss[e] < __builtin_inff()) || (ss[e] < 0x1p-80f && norm.eps < 0x1p-60f);
-        if (__syncthreads_or(again)) {
-            float top[kVec];
+        if (scaled || !__syncthreads_or(again)) break;
+        scaled = true;
+        float top[kVec];
 #pragma unroll
-            for (int e = 0; e < kVec; ++e) {
-                top[e] = 0.f;
+        for (int e = 0; e < kVec; ++e) {
+            top[e] = 0.f;
 #pragma unroll
-                for (int i = 0; i < kPer; ++i) {
-                    const float v = fabsf(x[i][e]);
-                    if (v < __builtin_inff()) top[e] = fmaxf(top[e], v);
-                }
+            for (int i = 0; i < kPer; ++i) {
+                const float v = fabsf(x[i][e]);
+                if (v < __builtin_inff()) top[e] = fmaxf(top[e], v);
             }
-            over_rows<kVec, true>(top, lanes, lds);
-            int ex[kVec];
+        }
+        reduce.template operator()<true>(top);
 #pragma unroll
-            for (int e = 0; e < kVec; ++e) {
-                ex[e] = top[e] == 0.f ? 0 : __builtin_amdgcn_frexp_expf(top[e]) - 1;
+        for (int e = 0; e < kVec; ++e) {
+            ex[e] = top[e] == 0.f ? 0 : __builtin_amdgcn_frexp_expf(top[e]) - 1;
 #pragma unroll
-                for (int i = 0; i < kPer; ++i) x[i][e] = __builtin_ldexpf(x[i][e], -ex[e]);
-            }
-            statistics();
-#pragma unroll
-            for (int e = 0; e < kVec; ++e) {
-                // x / sqrt(mean square + eps) with both over 2^ex
-                const double var = (double)ss[e] / M + __builtin_ldexp((double)norm.eps, -2 * ex[e]);
-                const float inv = (float)(1.0 / sqrt(var));
-#pragma unroll
-                for (int i = 0; i < kPer; ++i) x[i][e] = (x[i][e] - mean[e]) * inv;
-            }
-            return;
+            for (int i = 0; i < kPer; ++i) x[i][e] = __builtin_ldexpf(x[i][e], -ex[e]);
         }
     }
 #pragma unroll
     for (int e = 0; e < kVec; ++e) {
-        const float inv = 1.f / sqrtf(ss[e] * inv_m + norm.eps);
+        float inv;
+        if (std::is_same<T, float>::value && scaled)    // x / sqrt(mean square + eps), both over 2^ex
+            inv = (float)(1.0 / sqrt((double)ss[e] / M + __builtin_ldexp((double)norm.eps, -2 * ex[e])));
+        else
+            inv = 1.f / sqrtf(ss[e] * inv_m + norm.eps);
 #pragma unroll
         for (int i = 0; i < kPer; ++i) x[i][e] = (x[i][e] - mean[e]) * inv;
     }
 }
 
-template <typename T, int kVec, int kPer>
-__global__ __launch_bounds__(kThreads) void k_residual_norm(NormArgs a, int tiles) {
-    __shared__ float lds[over_rows_floats<kVec>()];
+// kWhole: every token of the tile is inside
+template <typename T, int kVec, int kPer, bool kWhole>
+__device__ __forceinline__ void residual_norm(const NormArgs &a, int tile, float *lds) {
     using P = Pack<T, kVec>;
+    // the gate, the residual and the weights are asked for with A where the registers
+    // hold them beside it
+    constexpr bool kEarly = kPer * kVec * (int)sizeof(T) <= 128, kWeights = kPer <= 4;
+    constexpr int kE = kEarly ? kPer : 1, kW = kWeights ? kPer : 1;
     const int lanes = a.lanes, step = kThreads / lanes, r0 = threadIdx.x / lanes;
-    const int64_t n = (int64_t)xcd_tile(blockIdx.x, tiles) * lanes * kVec + threadIdx.x % lanes * kVec;
-    const bool in = n < a.N;     // (kVec tokens are inside together: N and the tiles are multiples)
+    const int64_t n = (int64_t)tile * lanes * kVec + threadIdx.x % lanes * kVec;
+    const int valid = kWhole ? kVec : (int)max((int64_t)0, min((int64_t)kVec, a.N - n));
     float x[kPer][kVec];
-    auto load = [&](const void *from, int64_t ld, int r) {
-        return *reinterpret_cast<const P *>(static_cast<const T *>(from) + (int64_t)r * ld + n);
+    // row r of a matrix at the thread's tokens: what a thread's rows differ by is the same for all
+    auto at_row = [&](const void *from, int64_t ld, int i) {
+        return static_cast<const T *>(from) + ((int64_t)r0 * ld + n) + (int64_t)(i * step) * ld;
     };
+    auto load = [&](const void *from, int64_t ld, int i) {
+        return P::template load<kWhole>(at_row(from, ld, i), valid);
+    };
+    P gate[kE], residual[kE];
+    float w1[kW], b1[kW], w2[kW], b2[kW];
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
         const int r = r0 + i * step;
         P p = {};
-        if (in && r < a.M) p = load(a.A, a.lda, r);
+        if (valid && r < a.M) p = load(a.A, a.lda, i);
 #pragma unroll
         for (int e = 0; e < kVec; ++e) x[i][e] = (float)p.v[e];
     }
-    normed<T, kVec, kPer>(x, a.after, a.M, lanes, lds);
+    auto others = [&](int i, int to) {
+        if (a.G) gate[to] = load(a.G, a.ldg, i);
+        if (a.R) residual[to] = load(a.R, a.ldr, i);
+    };
+    auto firsts = [&](int r, int i) {
+        w1[i] = a.after.weight ? a.after.weight[r] : 1.f;
+        b1[i] = a.after.bias ? a.after.bias[r] : 0.f;
+    };
+    auto lasts = [&](int r, int i) {
+        w2[i] = a.before.weight ? a.before.weight[r] : 1.f;
+        b2[i] = a.before.bias ? a.before.bias[r] : 0.f;
+    };
+    if constexpr (kEarly)
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            const int r = r0 + i * step;
+            if (!valid || r >= a.M) continue;
+            others(i, i);
+            if constexpr (kWeights) {
+                firsts(r, i);
+                lasts(r, i);
+            }
+        }
+    Reducer<kVec> reduce{lds, lanes};
+    normed<T, kVec, kPer>(x, a.after, a.M, reduce);
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
         const int r = r0 + i * step;
-        if (!in || r >= a.M) {
+        if (!valid || r >= a.M) {
 #pragma unroll
             for (int e = 0; e < kVec; ++e) x[i][e] = 0.f;
             continue;
         }
-        const float w = a.after.weight ? a.after.weight[r] : 1.f, b = a.after.bias ? a.after.bias[r] : 0.f;
-        P g, res;
-        if (a.G) g = load(a.G, a.ldg, r);
-        if (a.R) res = load(a.R, a.ldr, r);
+        const int at = kEarly ? i : 0, w = kWeights ? i : 0;
+        if constexpr (!kEarly) others(i, at);
+        if constexpr (!kWeights) firsts(r, w);
         P h;
 #pragma unroll
         for (int e = 0; e < kVec; ++e) {
-            float y = x[i][e] * w + b;
-            if (a.G) y *= (float)g.v[e];
+            float y = x[i][e] * w1[w] + b1[w];
+            if (a.G) y *= (float)gate[at].v[e];
             y *= a.scale;
-            if (a.R) y += (float)res.v[e];
+            if (a.R) y += (float)residual[at].v[e];
             x[i][e] = y;
             h.v[e] = (T)y;
         }
-        if (a.H) *reinterpret_cast<P *>(static_cast<T *>(a.H) + (int64_t)r * a.ldh + n) = h;
+        if (a.H) h.template store<kWhole>(const_cast<T *>(at_row(a.H, a.ldh, i)), valid);
     }
     if (!a.Y) return;
-    normed<T, kVec, kPer>(x, a.before, a.M, lanes, lds);
+    normed<T, kVec, kPer>(x, a.before, a.M, reduce);
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
         const int r = r0 + i * step;
-        if (!in || r >= a.M) continue;
-        const float w = a.before.weight ? a.before.weight[r] : 1.f,
-                    b = a.before.bias ? a.before.bias[r] : 0.f;
+        if (!valid || r >= a.M) continue;
+        const int at = kWeights ? i : 0;
+        if constexpr (!kWeights) lasts(r, at);
         P y;
 #pragma unroll
-        for (int e = 0; e < kVec; ++e) y.v[e] = (T)(x[i][e] * w + b);
-        *reinterpret_cast<P *>(static_cast<T *>(a.Y) + (int64_t)r * a.ldy + n) = y;
+        for (int e = 0; e < kVec; ++e) y.v[e] = (T)(x[i][e] * w2[at] + b2[at]);
+        y.template store<kWhole>(const_cast<T *>(at_row(a.Y, a.ldy, i)), valid);
     }
+}
+
+template <typename T, int kVec, int kPer>
+__global__ __launch_bounds__(kThreads, 2) void k_residual_norm(NormArgs a, int tiles) {
+    extern __shared__ float lds[];
+    const int tile = xcd_tile(blockIdx.x, tiles);
+    if (((int64_t)tile + 1) * a.lanes * kVec <= a.N)
+        residual_norm<T, kVec, kPer, true>(a, tile, lds);
+    else
+        residual_norm<T, kVec, kPer, false>(a, tile, lds);
 }
 
 template <typename T, int kVec>
@@ -193,9 +268,10 @@ nmg_status run(NormArgs a, int tokens, hipStream_t stream) {
     const int tiles = (int)(((int64_t)a.N + tokens - 1) / tokens);
     if ((int64_t)tiles * kThreads >= ((int64_t)1 << 32)) return NMG_ERR_UNSUPPORTED;
     const int step = kThreads / a.lanes, per = (a.M + step - 1) / step;
+    const size_t room = 2 * (kThreads / 64) * tokens * sizeof(float);
     auto go = [&](auto k) {
         constexpr int kPer = decltype(k)::value;
-        k_residual_norm<T, kVec, kPer><<<tiles, kThreads, 0, stream>>>(a, tiles);
+        k_residual_norm<T, kVec, kPer><<<tiles, kThreads, room, stream>>>(a, tiles);
         return launched();
     };
     if (per <= kHold / kVec / 8) return go(std::integral_constant<int, kHold / kVec / 8>{});
@@ -207,23 +283,12 @@ nmg_status run(NormArgs a, int tokens, hipStream_t stream) {
 template <typename T>
 nmg_status plan(const NormArgs &a, hipStream_t stream) {
     constexpr int kVec = 16 / sizeof(T);
-    bool vec = a.N % kVec == 0;
-    auto fits = [&](const void *p, int64_t ld) {
-        if (p) vec = vec && aligned(p, 16) && ld % kVec == 0;
-    };
-    fits(a.A, a.lda);
-    fits(a.G, a.ldg);
-    fits(a.R, a.ldr);
-    fits(a.H, a.ldh);
-    fits(a.Y, a.ldy);
-    // the most tokens whose features the workgroup can hold
-    int most = 64 * (vec ? kVec : 1);
-    while (most > 1 && (int64_t)most * a.M > (int64_t)kThreads * kHold) most /= 2;
-    // fewer while compute units stand idle
-    int tokens = most;
+    // The most tokens whose features a workgroup can hold, fewer while compute units stand
+    // idle.
+    int tokens = 64;
+    while (tokens > 1 && (int64_t)tokens * a.M > (int64_t)kThreads * kHold) tokens /= 2;
     while (tokens > kVec && ((int64_t)a.N + tokens - 1) / tokens < device_cus()) tokens /= 2;
-    if (vec && tokens >= kVec) return run<T, kVec>(a, tokens, stream);
-    return run<T, 1>(a, std::min(tokens, 64), stream);
+    return tokens < kVec ? run<T, 1>(a, tokens, stream) : run<T, kVec>(a, tokens, stream);
 }
 
 }  // namespace

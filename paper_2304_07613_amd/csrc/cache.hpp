@@ -50,6 +50,10 @@ struct CacheAttnArgs {
     float *part;                     // parts > 1: their results
 };
 
+// Rows of a workgroup: 16 or 32 that its four waves split the keys of; 64 (head_dim > 128) or
+// 128, a quarter for each wave (binary16)
+enum CacheAttnRows { kRows16 = 16, kRows32 = 32, kRows64 = 64, kRows128 = 128 };
+
 nmg_status launch_cache_append(nmg_dtype dtype, const CacheView &c, int32_t layer,
                                const int32_t *q_offsets, const int32_t *lengths, const void *K,
                                int64_t ldk, const void *V, int64_t ldv, int32_t N, hipStream_t stream);

@@ -1,5 +1,6 @@
 // cache_attention.hpp -- attention over an 8-bit cache on the matrix cores: one
-// pass over pages and open tokens, online softmax, nothing staged in LDS.
+// pass over pages and open tokens, online softmax; few rows with nothing staged in LDS,
+// many with the decoded tiles there.
 //
 // The rows of a (sequence, key head) are its drafted tokens in every query head that
 // shares the key head: row r = g T + t is token t of query head head * share + g.
@@ -112,36 +113,70 @@ __device__ __forceinline__ float exp2_fast(float x) {
 
 // ------------------------------------------------------- what a workgroup has
 
-// Row tiles: sequence b has the slots [first(b), first(b + 1)), first(b) =
-// floor(offset(b) share / rows) + b, at least as many as its rows fill: the launch needs no
-// lengths.
+// A workgroup's row tile, key head and part of the keys.  The lengths are on the device and the
+// launch has room for any; the workgroups that there are come first, so that the
+// idle ones do not fall on some compute units more than on others.
 struct RowTile {
     int b, T, q0, n;        // sequence, its query columns and their first; kept tokens
     int first, rows;        // first row of the tile, rows of the sequence
+    int slot, part, head;
 };
 
 template <int kRows>
-__device__ __forceinline__ bool row_tile(const CacheAttnArgs &a, int slot, RowTile &t) {
+__device__ __forceinline__ bool row_tile(const CacheAttnArgs &a, int index, int parts, RowTile &t) {
     auto inside = [&](int v) { return v < 0 ? 0 : v > a.Nq ? a.Nq : v; };
     const int lane = threadIdx.x & 63;
-    // the last b with first(b) <= slot, 64 at a time; a step of the last kind has its
-    // offsets and length too
-    int lo = 0, n = a.c.sequences, stride, at;
-    do {
-        stride = (n + 63) / 64;
-        const int b = lo + min(lane * stride, n - 1);
-        const int from = inside(a.q_offsets[b]), to = inside(a.q_offsets[b + 1]);
-        const int kept = cache_length(a.c, a.lengths, b), first = (int)((int64_t)from * a.share / kRows) + b;
-        const int found = __popcll(__ballot(lane * stride < n && first <= slot)) - 1;
-        if (found < 0) return false;
-        t.b = lo + found * stride;
-        t.q0 = __builtin_amdgcn_readlane(from, found);
-        t.T = __builtin_amdgcn_readlane(to, found) - t.q0;
-        t.n = __builtin_amdgcn_readlane(kept, found);
-        at = slot - __builtin_amdgcn_readlane(first, found);
-        lo = t.b;
-        n = min(stride, n - found * stride);
-    } while (stride > 1);
+    auto place = [&](int slots) {
+        const int total = slots * parts * a.c.heads;
+        if (index >= total) return false;
+        const int at = xcd_tile(index, total);
+        t.slot = at % slots;
+        t.part = at / slots % parts;
+        t.head = at / slots / parts;
+        return true;
+    };
+    int at;
+    if (a.c.sequences <= 64) {
+        // every sequence's row tiles counted, one lane each
+        const int b = min(lane, a.c.sequences - 1);
+        const int from = inside(a.q_offsets[b]), columns = inside(a.q_offsets[b + 1]) - from;
+        const int kept = cache_length(a.c, a.lengths, b);
+        const int tiles = lane < a.c.sequences && columns > 0
+                              ? (int)(((int64_t)columns * a.share + kRows - 1) / kRows) : 0;
+        int upto = tiles;
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) {
+            const int up = __shfl_up(upto, d);
+            upto += lane >= d ? up : 0;
+        }
+        if (!place(min(__builtin_amdgcn_readlane(upto, 63), a.slots))) return false;
+        t.b = min(__popcll(__ballot(upto <= t.slot)), a.c.sequences - 1);
+        t.q0 = __builtin_amdgcn_readlane(from, t.b);
+        t.T = __builtin_amdgcn_readlane(columns, t.b);
+        t.n = __builtin_amdgcn_readlane(kept, t.b);
+        at = t.slot - __builtin_amdgcn_readlane(upto - tiles, t.b);
+    } else {
+        // sequence b has the slots [first(b), first(b + 1)), first(b) = floor(offset(b) share /
+        // rows) + b, at least as many as its rows fill: the last b with first(b) <=
+        // slot, 64 at a time; the last step has its offsets and length too
+        if (!place(a.slots)) return false;
+        int lo = 0, n = a.c.sequences, stride;
+        do {
+            stride = (n + 63) / 64;
+            const int b = lo + min(lane * stride, n - 1);
+            const int from = inside(a.q_offsets[b]), to = inside(a.q_offsets[b + 1]);
+            const int kept = cache_length(a.c, a.lengths, b), first = (int)((int64_t)from * a.share / kRows) + b;
+            const int found = __popcll(__ballot(lane * stride < n && first <= t.slot)) - 1;
+            if (found < 0) return false;
+            t.b = lo + found * stride;
+            t.q0 = __builtin_amdgcn_readlane(from, found);
+            t.T = __builtin_amdgcn_readlane(to, found) - t.q0;
+            t.n = __builtin_amdgcn_readlane(kept, found);
+            at = t.slot - __builtin_amdgcn_readlane(first, found);
+            lo = t.b;
+            n = min(stride, n - found * stride);
+        } while (stride > 1);
+    }
     if (at < 0 || t.T <= 0 || (int64_t)at * kRows >= (int64_t)t.T * a.share) return false;
     t.first = at * kRows;
     t.rows = t.T * a.share;
@@ -166,6 +201,29 @@ __device__ __forceinline__ KeyTiles key_tiles(const CacheAttnArgs &a, const RowT
         seen = min(seen, k.kept + (min(t.first + kRows, t.rows) - 1) % t.T + 1);
     k.all = k.paged + (seen + 63) / 64;
     return k;
+}
+
+// Which of the 16 open tokens from `first` on a drafted token sees, a bit each
+__device__ __forceinline__ uint32_t seen_of(const CacheAttnArgs &a, const RowTile &t, const KeyTiles &k,
+                                            int token, int first) {
+    uint32_t seen = 0;
+    if (a.tree) {
+        // (all 16 bytes are on their way at once: places past the ends are read inside)
+        const uint8_t *line = a.tree + (int64_t)(t.q0 + token) * a.ldtree;
+        uint8_t b[16];
+#pragma unroll
+        for (int j = 0; j < 16; ++j) b[j] = line[min(max(first + j - k.kept, 0), a.width - 1)];
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+            const int e = first + j - k.kept;
+            seen |= (uint32_t)(e < 0 || (e < a.width && b[j] != 0)) << j;
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 16; ++j) seen |= (uint32_t)(first + j - k.kept <= token) << j;
+    }
+    const int left = k.open - first;                 // the others are no tokens
+    return left >= 16 ? seen : left <= 0 ? 0 : seen & ((1u << left) - 1);
 }
 
 // ------------------------------------------------------------------ results
@@ -230,15 +288,15 @@ __device__ __forceinline__ void join_waves(Result<VT, NT> &r, float *lds) {
 template <int VT, int NT>
 constexpr int join_floats() { return std::max(2 * (VT * NT * 256 + NT * 128), 4 * 1024); }
 
-constexpr int kMaxParts = 64;
+constexpr int kMaxParts = 32;
 
 // Floats of one part's result: a row of sums for every feature, then maxima, then totals
 __host__ __device__ inline int64_t part_floats(int D, int rows) { return (int64_t)(D + 2) * rows; }
 
-template <typename T, int VT, int NT>
-__device__ __forceinline__ void store_result(const CacheAttnArgs &a, const RowTile &t, int head,
+// kRows: of the row tile, of which `at` and what follows are the wave's
+template <typename T, int kRows, int VT, int NT>
+__device__ __forceinline__ void store_result(const CacheAttnArgs &a, const RowTile &t, int at, int head,
                                              int slot, int part, const Result<VT, NT> &r) {
-    constexpr int kRows = 16 * NT;
     const int lane = threadIdx.x & 63, x = lane % 16, c = lane / 16, D = a.c.D;
     if (a.parts > 1) {
         float *to = a.part + (((int64_t)head * a.slots + slot) * a.parts + part) * part_floats(D, kRows);
@@ -249,10 +307,10 @@ __device__ __forceinline__ void store_result(const CacheAttnArgs &a, const RowTi
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
                     if (16 * d + 4 * c + i < D)
-                        to[(16 * d + 4 * c + i) * kRows + 16 * n + x] = r.o[d][n][i];
+                        to[(16 * d + 4 * c + i) * kRows + at + 16 * n + x] = r.o[d][n][i];
             if (c == 0) {
-                to[D * kRows + 16 * n + x] = r.m[n];
-                to[(D + 1) * kRows + 16 * n + x] = r.l[n];
+                to[D * kRows + at + 16 * n + x] = r.m[n];
+                to[(D + 1) * kRows + at + 16 * n + x] = r.l[n];
             }
         }
         return;
@@ -260,7 +318,7 @@ __device__ __forceinline__ void store_result(const CacheAttnArgs &a, const RowTi
     T *O = static_cast<T *>(a.O);
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-        const int row = t.first + 16 * n + x;
+        const int row = t.first + at + 16 * n + x;
         if (row >= t.rows) continue;
         const int64_t h = head * a.share + row / t.T;
         T *to = O + h * D * a.ldo + t.q0 + row % t.T;
@@ -291,16 +349,151 @@ __device__ __forceinline__ float sum_over_c(float v) {
     v += __shfl_xor(v, 32);
     return v + __shfl_xor(v, 16);
 }
+// A value that is the same for the wave, through the scalar cache: loads of registers in
+// flight are not waited for
+template <typename T>
+__device__ __forceinline__ T scalar_load(const T *p) {
+    return *(const __attribute__((address_space(4))) T *)(uintptr_t)p;
+}
 // e of v = m 2^e, 1 <= |m| < 2; 0 for 0
 __device__ __forceinline__ int exponent_of(float v) {
     return v == 0.f ? 0 : __builtin_amdgcn_frexp_expf(v) - 1;
 }
 // What was loaded before is loaded again, rather than kept in registers
 __device__ __forceinline__ void reload() { asm volatile("" ::: "memory"); }
+// No instruction is moved across
+__device__ __forceinline__ void issued() { __builtin_amdgcn_sched_barrier(0); }
 // LDS that the wave's lanes wrote is read by its other lanes
 __device__ __forceinline__ void wave_sync() {
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
+}
+
+// What a wave carries from key tile to key tile, for 16 NT rows (lane (x, c): row x of
+// every 16, features 16 d + 4 c + i)
+template <bool kF32, int VT, int NT>
+struct Pass {
+    v4f o[VT][NT];          // sums of weights times values
+    v4f total[NT];          // of the weights: binary16 by a matrix instruction with ones (four
+                            // equal values), binary32 the lane's part
+    float m[NT];            // largest score so far
+    // The sums are in units of a power of two.  binary16: of the tile at hand's values,
+    // since its weights leave no room for another factor.  binary32: of the largest
+    // scale so far, the weights take the rest.
+    float unit;
+
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            m[n] = kMinusInf;
+            total[n] = v4f{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int d = 0; d < VT; ++d) o[d][n] = v4f{0.f, 0.f, 0.f, 0.f};
+        }
+        unit = kF32 ? 0x1p-126f : 1.f;
+    }
+    __device__ __forceinline__ void new_unit(float vs) {
+        if (kF32 ? !(vs <= unit) : vs != unit) {
+            const float f = unit / vs;
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int d = 0; d < VT; ++d) o[d][n] *= f;
+            unit = vs;
+        }
+    }
+    // Scores s * f (in units of log 2, f > 0) to weights, in place
+    __device__ __forceinline__ void softmax(v4f (&s)[4][NT], float f) {
+        float top[NT];
+        bool up = false;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            float t = fmaxf(fmaxf(s[0][n][0], s[0][n][1]), fmaxf(s[0][n][2], s[0][n][3]));
+#pragma unroll
+            for (int i = 1; i < 4; ++i)
+                t = fmaxf(fmaxf(t, fmaxf(s[i][n][0], s[i][n][1])), fmaxf(s[i][n][2], s[i][n][3]));
+            top[n] = fmaxf(m[n], max_over_c(t) * f);
+            up |= top[n] > m[n];
+        }
+        if (__any(up)) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                const float g = top[n] > m[n] ? exp2_fast(m[n] - top[n]) : 1.f;
+                m[n] = top[n];
+                total[n] *= g;
+#pragma unroll
+                for (int d = 0; d < VT; ++d) o[d][n] *= g;
+            }
+        }
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            // binary16 weights are 2^15 at most, so that the small ones stay normal down to
+            // 2^-29 of the largest (totals have the same factor)
+            const float base = (m[n] == kMinusInf ? 0.f : m[n]) - (kF32 ? 0.f : 15.f);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    s[i][n][j] = exp2_fast(__builtin_fmaf(s[i][n][j], f, -base));
+                    if constexpr (kF32) total[n][0] += s[i][n][j];
+                }
+        }
+    }
+    // binary16: the lane's 16 weights as the matrix instructions take them, and their total
+    __device__ __forceinline__ void weights(const v4f (&s)[4][NT], h8 (&p)[NT][2]) {
+        const h8 ones = {1, 1, 1, 1, 1, 1, 1, 1};
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) p[n][i / 8][i % 8] = (_Float16)s[i / 4][n][i % 4];
+            total[n] = mfma_f16(ones, p[n][0], total[n]);
+            total[n] = mfma_f16(ones, p[n][1], total[n]);
+        }
+    }
+    // the sums over their totals
+    __device__ __forceinline__ void finish(Result<VT, NT> &r) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            r.m[n] = m[n];
+            r.l[n] = kF32 ? sum_over_c(total[n][0]) : total[n][0];
+            const float inv = r.l[n] == 0.f ? 0.f : 1.f / r.l[n];
+#pragma unroll
+            for (int d = 0; d < VT; ++d)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) r.o[d][n][i] = o[d][n][i] * inv * unit;
+        }
+    }
+};
+
+// Sums over a tile of open tokens some of whose values are not finite: every row takes the
+// values that it sees and no others, one by one: weights (-1: not seen) through the wave's
+// 4 KB of LDS.  `count`: the tile's tokens.
+template <typename T, bool kF32, int VT, int NT>
+__device__ __forceinline__ void odd_sums(Pass<kF32, VT, NT> &r, const v4f (&s)[4][NT], const uint32_t (&seen)[NT],
+                                         float *lds, const T *values, int D, int room, int count) {
+    const int lane = threadIdx.x & 63, x = lane % 16, c = lane / 16;
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        wave_sync();
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+            lds[(16 * c + e) * 16 + x] = seen[n] >> e & 1 ? s[e / 4][n][e % 4] : -1.f;
+        wave_sync();
+#pragma unroll
+        for (int d = 0; d < VT; ++d)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                int f = 16 * d + 4 * c + e;
+                asm volatile("" : "+v"(f));      // (its address is not kept for the next n)
+                float o = r.o[d][n][e];
+#pragma unroll 1
+                for (int key = 0; key < 64 && key < count; ++key) {
+                    const float p = lds[key * 16 + x];
+                    if (f < D && p != -1.f) o += p * ((float)values[(int64_t)f * room + key] / r.unit);
+                }
+                r.o[d][n][e] = o;
+            }
+    }
 }
 
 // Waves of a SIMD that the registers are to leave room for
@@ -310,7 +503,7 @@ constexpr int attention_waves() {
 }
 
 template <typename T, int VT, int NT, bool kInt8>
-__global__ __launch_bounds__(256, (attention_waves<T, VT, NT>())) void k_cache_attention(CacheAttnArgs a, int total) {
+__global__ __launch_bounds__(256, (attention_waves<T, VT, NT>())) void k_cache_attention(CacheAttnArgs a) {
     constexpr bool kF32 = std::is_same<T, float>::value;
     constexpr int KC = (VT + 3) / 4, W = 16 * NT;
     constexpr int kWords = kF32 ? 4 : 2;          // 16-byte words of 16 open values
@@ -320,22 +513,21 @@ __global__ __launch_bounds__(256, (attention_waves<T, VT, NT>())) void k_cache_a
     const CacheView &v = a.c;
     const int D = v.D, D16 = v.D16, room = v.room;
 
-    const int at = xcd_tile(blockIdx.x, total);
-    const int slot = at % a.slots, part = at / a.slots % a.parts, head = at / a.slots / a.parts;
     RowTile t;
-    if (!row_tile<W>(a, slot, t)) return;
+    if (!row_tile<W>(a, blockIdx.x, a.parts, t)) return;
+    const int slot = t.slot, part = t.part, head = t.head;
     const KeyTiles kt = key_tiles<W>(a, t);
     const int per = (kt.all + a.parts - 1) / a.parts;
     const int begin = part * per, end = min(kt.all, begin + per);
     if (begin >= end) return;
 
     // ---- pages: the first ones are asked for before the queries
-    const int per_block = v.block / 64, paged_end = min(end, kt.paged);
+    const int two = v.block == 128, paged_end = min(end, kt.paged);   // key tiles of a page: 1 << two
     const int64_t heads = v.heads;
     const int32_t *table = v.table + (int64_t)t.b * v.row;
     auto page_of = [&](int tile) {
-        const int p = table[min(tile / per_block, v.row - 1)];
-        return __builtin_amdgcn_readfirstlane(p < 0 ? 0 : p >= v.pages ? v.pages - 1 : p);
+        const int p = scalar_load(table + min(tile >> two, v.row - 1));
+        return p < 0 ? 0 : p >= v.pages ? v.pages - 1 : p;
     };
     // A page's part of a head is one buffer: a load takes its base from scalar registers and
     // one offset per lane, what lies behind the head reads as zeros.
@@ -349,9 +541,9 @@ __global__ __launch_bounds__(256, (attention_waves<T, VT, NT>())) void k_cache_a
     auto load_keys = [&](int tile, int page) {
         const int64_t of = ((int64_t)a.layer * v.pages + page) * heads + head;
         const buf_rsrc_t from = buf_rsrc(v.k_pages + of * k_bytes, k_bytes);
-        const uint32_t first = (tile % per_block) * 64 * D16;
-        ks = v.k_scales[of];
-        vs = v.v_scales[of];
+        const uint32_t first = (tile & two) * 64 * D16;
+        ks = scalar_load(v.k_scales + of);
+        vs = scalar_load(v.v_scales + of);
 #pragma unroll
         for (int s = 0; s < 4; ++s)
 #pragma unroll
@@ -404,83 +596,19 @@ __global__ __launch_bounds__(256, (attention_waves<T, VT, NT>())) void k_cache_a
         }
     }
 
-    Result<VT, NT> r;
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        r.m[n] = kMinusInf;
-        r.l[n] = 0.f;
-#pragma unroll
-        for (int d = 0; d < VT; ++d) r.o[d][n] = v4f{0.f, 0.f, 0.f, 0.f};
-    }
-    // The sums are kept in units of a power of two.  binary16: of the tile at hand's
-    // values, since its weights leave no room for another factor.  binary32: of the
-    // largest scale so far, the weights take the rest.
-    float unit = kF32 ? 0x1p-126f : 1.f;
+    Pass<kF32, VT, NT> r;
+    r.clear();
     const float factor = a.scale * kLog2e;
-
-    auto new_unit = [&](float vs) {
-        if (kF32 ? !(vs <= unit) : vs != unit) {
-            const float f = unit / vs;
-#pragma unroll
-            for (int n = 0; n < NT; ++n)
-#pragma unroll
-                for (int d = 0; d < VT; ++d) r.o[d][n] *= f;
-            unit = vs;
-        }
-    };
-    // scores s (in units of log 2) to weights, in place
-    auto softmax = [&](v4f (&s)[4][NT]) {
-        float top[NT];
-        bool up = false;
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            float m = fmaxf(fmaxf(s[0][n][0], s[0][n][1]), fmaxf(s[0][n][2], s[0][n][3]));
-#pragma unroll
-            for (int i = 1; i < 4; ++i)
-                m = fmaxf(fmaxf(m, fmaxf(s[i][n][0], s[i][n][1])), fmaxf(s[i][n][2], s[i][n][3]));
-            top[n] = fmaxf(r.m[n], max_over_c(m));
-            up |= top[n] > r.m[n];
-        }
-        if (__any(up)) {
-#pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                const float f = top[n] > r.m[n] ? exp2_fast(r.m[n] - top[n]) : 1.f;
-                r.m[n] = top[n];
-                r.l[n] *= f;
-#pragma unroll
-                for (int d = 0; d < VT; ++d) r.o[d][n] *= f;
-            }
-        }
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            // binary16 weights are 2^15 at most, so that the small ones stay normal down to
-            // 2^-29 of the largest (totals have the same factor)
-            const float base = (r.m[n] == kMinusInf ? 0.f : r.m[n]) - (kF32 ? 0.f : 15.f);
-            float sum = 0.f;
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    s[i][n][j] = exp2_fast(s[i][n][j] - base);
-                    sum += s[i][n][j];
-                }
-            r.l[n] += sum;
-        }
-    };
-    // the lane's 16 weights of a row tile as the matrix instructions take them
-    auto weights = [&](const v4f (&s)[4][NT], int n, h8 (&p)[2]) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) p[i / 8][i % 8] = (_Float16)s[i / 4][n][i % 4];
-    };
 
     // ---- whole pages
     for (; tile < paged_end; tile += 4) {
         u4 vv[VT];
         const int64_t of = ((int64_t)a.layer * v.pages + page) * heads + head;
         const buf_rsrc_t from = buf_rsrc(v.v_pages + of * v_bytes, v_bytes);
-        const uint32_t first = (tile % per_block) * 64;
+        const uint32_t first = (tile & two) * 64;
 #pragma unroll
         for (int d = 0; d < VT; ++d) vv[d] = buf_load16(from, v_at + first + 16 * d * v.block, 0);
+        issued();        // before the scores: they are the time that the values have to come
         const int after = page_of(tile + 8);
         const float tile_ks = ks, tile_vs = vs < 0x1p-32f && !kF32 ? 0x1p-32f : vs;
         v4f s[4][NT];
@@ -511,6 +639,7 @@ __global__ __launch_bounds__(256, (attention_waves<T, VT, NT>())) void k_cache_a
             }
         }
         if (tile + 4 < paged_end) load_keys(tile + 4, next_page);
+        issued();
         page = next_page;
         next_page = after;
         if constexpr (kF32) {
@@ -523,17 +652,11 @@ __global__ __launch_bounds__(256, (attention_waves<T, VT, NT>())) void k_cache_a
 #pragma unroll
                     for (int j = 0; j < 4; ++j)
                         s[i][n][j] = __builtin_ldexpf(s[i][n][j] * factor, qe[n] + ke) + nan;
-        } else {
-            const float f = factor * tile_ks;
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int n = 0; n < NT; ++n) s[i][n] *= f;
         }
-        softmax(s);
-        new_unit(tile_vs);
+        r.softmax(s, kF32 ? 1.f : factor * tile_ks);
+        r.new_unit(tile_vs);
         if constexpr (kF32) {
-            const float f = tile_vs / unit;
+            const float f = tile_vs / r.unit;
 #pragma unroll
             for (int d = 0; d < VT; ++d)
 #pragma unroll
@@ -546,8 +669,7 @@ __global__ __launch_bounds__(256, (attention_waves<T, VT, NT>())) void k_cache_a
                 }
         } else {
             h8 p[NT][2];
-#pragma unroll
-            for (int n = 0; n < NT; ++n) weights(s, n, p[n]);
+            r.weights(s, p);
 #pragma unroll
             for (int d = 0; d < VT; ++d) {
                 const h8 g0 = decode8<kInt8>(vv[d][0], vv[d][1]), g1 = decode8<kInt8>(vv[d][2], vv[d][3]);
@@ -570,16 +692,7 @@ __global__ __launch_bounds__(256, (attention_waves<T, VT, NT>())) void k_cache_a
         // which of the lane's keys each of its rows sees
         uint32_t seen[NT];
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            seen[n] = 0;
-            const uint8_t *line = a.tree ? a.tree + (int64_t)(t.q0 + token[n]) * a.ldtree : nullptr;
-            for (int j = 0; j < 16; ++j) {
-                const int u = first + 16 * c + j, e = u - kt.kept;
-                bool see = u < kt.open;
-                if (see && e >= 0) see = line ? e < a.width && line[e] != 0 : e <= token[n];
-                seen[n] |= (uint32_t)see << j;
-            }
-        }
+        for (int n = 0; n < NT; ++n) seen[n] = seen_of(a, t, kt, token[n], first + 16 * c);
         v4f s[4][NT];
         const buf_rsrc_t key_tile = buf_rsrc(kf, 64 * D16 * sizeof(T));
         auto key_word = [&](int m, int k, int w) {
@@ -590,7 +703,7 @@ __global__ __launch_bounds__(256, (attention_waves<T, VT, NT>())) void k_cache_a
         if constexpr (kF32) {
             // the tile's keys are scaled like codes, by its largest finite value
             uint32_t top = 0;
-#pragma unroll 1
+#pragma unroll(KC == 1 ? 4 : KC == 2 ? 2 : 1)
             for (int m = 0; m < 4; ++m)
 #pragma unroll
                 for (int k = 0; k < KC; ++k)
@@ -638,12 +751,12 @@ __global__ __launch_bounds__(256, (attention_waves<T, VT, NT>())) void k_cache_a
             for (int n = 0; n < NT; ++n)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    float y = s[m][n][e] * factor;
-                    if constexpr (kF32) y = __builtin_ldexpf(y, qe[n] + ke);
+                    float y = s[m][n][e];
+                    if constexpr (kF32) y = __builtin_ldexpf(y * factor, qe[n] + ke);
                     s[m][n][e] = seen[n] >> (4 * m + e) & 1 ? y : kMinusInf;
                 }
         }
-        softmax(s);
+        r.softmax(s, kF32 ? 1.f : factor);
         // values: those behind the open tokens are whatever the ring held, so none are taken
         const int valid = kt.open - first - 16 * c;       // of the lane's 16
         auto value_word = [&](int d, int w) {
@@ -666,7 +779,7 @@ __global__ __launch_bounds__(256, (attention_waves<T, VT, NT>())) void k_cache_a
         bool odd = false;          // a value that is not finite
         if constexpr (kF32) {
             uint32_t top = 0;
-#pragma unroll 2
+#pragma unroll 4
             for (int d = 0; d < VT; ++d)
 #pragma unroll
                 for (int w = 0; w < 4; ++w) {
@@ -692,35 +805,15 @@ __global__ __launch_bounds__(256, (attention_waves<T, VT, NT>())) void k_cache_a
             reload();
             odd = z[0] != z[0] || z[1] != z[1] || z[2] != z[2] || z[3] != z[3];
         }
-        new_unit(tile_vs);
+        r.new_unit(tile_vs);
         if (__any(odd)) {
-            // every row takes the values that it sees and no others, one by one: weights
-            // (-1: not seen) through the wave's part of LDS
-            float *shared = lds + wave * 1024;
-#pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                wave_sync();
-#pragma unroll
-                for (int e = 0; e < 16; ++e)
-                    shared[(16 * c + e) * 16 + x] = seen[n] >> e & 1 ? s[e / 4][n][e % 4] : -1.f;
-                wave_sync();
-#pragma unroll
-                for (int d = 0; d < VT; ++d)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        int f = 16 * d + 4 * c + e;
-                        asm volatile("" : "+v"(f));      // (its address is not kept for the next n)
-                        float o = r.o[d][n][e];
-#pragma unroll 1
-                        for (int key = 0; key < 64 && first + key < kt.open; ++key) {
-                            const float p = shared[key * 16 + x];
-                            if (f < D && p != -1.f) o += p * ((float)vf[(int64_t)f * room + key] / unit);
-                        }
-                        r.o[d][n][e] = o;
-                    }
+            if constexpr (!kF32) {      // (their total too)
+                h8 p[NT][2];
+                r.weights(s, p);
             }
+            odd_sums<T>(r, s, seen, lds + wave * 1024, vf, D, room, kt.open - first);
         } else if constexpr (kF32) {
-            const float f = 1.f / unit;
+            const float f = 1.f / r.unit;
 #pragma unroll
             for (int d = 0; d < VT; ++d)
 #pragma unroll
@@ -734,8 +827,7 @@ __global__ __launch_bounds__(256, (attention_waves<T, VT, NT>())) void k_cache_a
                 }
         } else {
             h8 p[NT][2];
-#pragma unroll
-            for (int n = 0; n < NT; ++n) weights(s, n, p[n]);
+            r.weights(s, p);
 #pragma unroll
             for (int d = 0; d < VT; ++d) {
                 const h8 g0 = __builtin_bit_cast(h8, value_word(d, 0)), g1 = __builtin_bit_cast(h8, value_word(d, 1));
@@ -750,17 +842,260 @@ __global__ __launch_bounds__(256, (attention_waves<T, VT, NT>())) void k_cache_a
     if (end > kt.paged) __syncthreads();     // (the waves' parts of LDS are free again)
 
     // ---- the wave's sums over its totals, then the four waves'
+    Result<VT, NT> mine;
+    r.finish(mine);
+    if (end - begin > 1) join_waves(mine, lds);
+    if (wave == 0) store_result<T, 16 * NT>(a, t, 0, head, slot, part, mine);
+}
+
+// ------------------------------------------------- many rows (binary16)
+
+// Barrier of a workgroup whose waves share LDS; loads from memory go on
+__device__ __forceinline__ void lds_barrier() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
+// The same pass where a (sequence, key head) has many rows: a wave has rows of its own, all four
+// go through the same key tiles.  Each decodes a quarter of a tile -- the decoding is most of a
+// tile's vector work -- and leaves it in LDS as the matrix instructions take it, 16 bytes a
+// lane, so that neither side has a bank conflict.  Two buffers: while tile i is multiplied,
+// tile i + 1 is decoded and tile i + 2 on its way.
+template <int VT, int NT, bool kInt8>
+__global__ __launch_bounds__(256, VT == 16 ? 1 : 2) void k_cache_attention_shared(CacheAttnArgs a) {
+    using T = _Float16;
+    constexpr int KC = (VT + 3) / 4, W = 64 * NT, kFragments = 8 * KC + 2 * VT, VQ = (VT + 3) / 4;
+    __shared__ __align__(16) h8 frag[2][kFragments][64];
+    __shared__ int odd_of[4];
+    const int lane = threadIdx.x & 63, x = lane % 16, c = lane / 16;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const CacheView &v = a.c;
+    const int D = v.D, D16 = v.D16, room = v.room;
+
+    RowTile t;
+    if (!row_tile<W>(a, blockIdx.x, a.parts, t)) return;
+    const int slot = t.slot, part = t.part, head = t.head;
+    const KeyTiles kt = key_tiles<W>(a, t);
+    const int per = (kt.all + a.parts - 1) / a.parts;
+    const int begin = part * per, end = min(kt.all, begin + per);
+    if (begin >= end) return;
+    const int first_row = t.first + 16 * NT * wave;
+    const bool rows = first_row < t.rows;            // the wave has some
+
+    const int two = v.block == 128, paged_end = min(end, kt.paged);
+    const int64_t heads = v.heads;
+    const int32_t *table = v.table + (int64_t)t.b * v.row;
+    auto head_of_page = [&](int tile) {              // of the pool's pages and scales
+        const int p = scalar_load(table + min(tile >> two, v.row - 1));
+        return ((int64_t)a.layer * v.pages + (p < 0 ? 0 : p >= v.pages ? v.pages - 1 : p)) * heads + head;
+    };
+    const uint32_t k_bytes = v.block * D16, v_bytes = D * v.block, past = 0x7fffffffu;
+    const uint32_t k_at = (16 * (x / 4) + x % 4) * D16 + 16 * c, v_at = x * v.block + 16 * c;
+    uint32_t k_off[KC];
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        r.l[n] = sum_over_c(r.l[n]);
-        const float inv = r.l[n] == 0.f ? 0.f : 1.f / r.l[n];
+    for (int k = 0; k < KC; ++k) k_off[k] = 64 * k + 16 * c < D16 ? k_at + 64 * k : past;
+    // the wave's quarter of a tile: keys 16 (.) + 4 wave + (.), features of 16 d, d % 4 == wave
+    u4 kk[KC], vv[VQ];
+    float ks = 1.f, vs = 1.f;
+    auto load = [&](int tile) {
+        const int64_t of = head_of_page(tile);
+        const buf_rsrc_t from_k = buf_rsrc(v.k_pages + of * k_bytes, k_bytes);
+        const buf_rsrc_t from_v = buf_rsrc(v.v_pages + of * v_bytes, v_bytes);
+#pragma unroll
+        for (int k = 0; k < KC; ++k) kk[k] = buf_load16(from_k, k_off[k], ((tile & two) * 64 + 4 * wave) * D16);
+#pragma unroll
+        for (int i = 0; i < VQ; ++i)
+            vv[i] = buf_load16(from_v, v_at + (tile & two) * 64 + 16 * (wave + 4 * i) * v.block, 0);
+    };
+    auto scales = [&](int tile) {
+        const int64_t of = head_of_page(tile);
+        ks = scalar_load(v.k_scales + of);
+        vs = scalar_load(v.v_scales + of);
+    };
+    auto decode = [&](int to) {
+#pragma unroll
+        for (int k = 0; k < KC; ++k) {
+            frag[to][(wave * KC + k) * 2][lane] = decode8<kInt8>(kk[k][0], kk[k][1]);
+            frag[to][(wave * KC + k) * 2 + 1][lane] = decode8<kInt8>(kk[k][2], kk[k][3]);
+        }
+#pragma unroll
+        for (int i = 0; i < VQ; ++i) {
+            const int d = wave + 4 * i;
+            if (VT % 4 && d >= VT) continue;
+            frag[to][8 * KC + 2 * d][lane] = decode8<kInt8>(vv[i][0], vv[i][1]);
+            frag[to][8 * KC + 2 * d + 1][lane] = decode8<kInt8>(vv[i][2], vv[i][3]);
+        }
+    };
+    if (begin < paged_end) load(begin);
+
+    h8 q[NT][KC][2];
+    int token[NT];
+    {
+        const T *Q = static_cast<const T *>(a.Q);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const int row = min(first_row + 16 * n + x, t.rows - 1);
+            token[n] = row % t.T;
+            const T *from = Q + ((int64_t)(head * a.share + row / t.T) * D + 16 * c) * a.ldq + t.q0 + token[n];
+#pragma unroll
+            for (int k = 0; k < KC; ++k)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {
+                    q[n][k][j / 8][j % 8] = 64 * k + 16 * c + j < D ? *from : (T)0.f;
+                    from += j < 15 ? a.ldq : 49 * a.ldq;
+                }
+        }
+    }
+    Pass<false, VT, NT> r;
+    r.clear();
+    const float factor = a.scale * kLog2e;
+
+    auto scores = [&](int from, v4f (&s)[4][NT]) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n) s[i][n] = v4f{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int k = 0; k < KC; ++k)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const h8 f = frag[from][(i * KC + k) * 2 + h][lane];
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) s[i][n] = mfma_f16(f, q[n][k][h], s[i][n]);
+                }
+        }
+    };
+    auto sums = [&](int from, const v4f (&s)[4][NT]) {
+        h8 p[NT][2];
+        r.weights(s, p);
 #pragma unroll
         for (int d = 0; d < VT; ++d)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) r.o[d][n][i] = r.o[d][n][i] * inv * unit;
+            for (int h = 0; h < 2; ++h) {
+                const h8 g = frag[from][8 * KC + 2 * d + h][lane];
+#pragma unroll
+                for (int n = 0; n < NT; ++n) r.o[d][n] = mfma_f16(g, p[n][h], r.o[d][n]);
+            }
+    };
+
+    // ---- whole pages
+    if (begin < paged_end) {
+        decode(0);
+        if (begin + 1 < paged_end) load(begin + 1);
+        scales(begin);
+        lds_barrier();
     }
-    if (end - begin > 1) join_waves(r, lds);
-    if (wave == 0) store_result<T>(a, t, head, slot, part, r);
+    for (int tile = begin, buffer = 0; tile < paged_end; ++tile, buffer ^= 1) {
+        const float tile_ks = ks, tile_vs = vs < 0x1p-32f ? 0x1p-32f : vs;
+        if (tile + 1 < paged_end) {
+            decode(buffer ^ 1);
+            scales(tile + 1);
+        }
+        if (tile + 2 < paged_end) load(tile + 2);
+        if (rows) {
+            v4f s[4][NT];
+            scores(buffer, s);
+            r.softmax(s, factor * tile_ks);
+            r.new_unit(tile_vs);
+            sums(buffer, s);
+        }
+        lds_barrier();
+    }
+
+    // ---- open tokens: the next tile is on its way while one is multiplied
+    const int64_t ring = ((int64_t)a.layer * v.sequences + t.b) * heads + head;
+    auto first_slot = [&](int tile) {
+        return (int)((uint32_t)(t.n - kt.kept + 64 * (tile - kt.paged)) % (uint32_t)room);
+    };
+    u4 ko[KC][2], vo[VQ][2];
+    uint32_t seen[NT];
+    auto load_open = [&](int tile) {
+        const int first = 64 * (tile - kt.paged), at_slot = first_slot(tile);
+        const buf_rsrc_t key_tile = buf_rsrc(static_cast<const T *>(v.k_open) + (ring * room + at_slot) * D16,
+                                             64 * D16 * sizeof(T));
+        const T *vf = static_cast<const T *>(v.v_open) + ring * D * room + at_slot;
+        const int valid = kt.open - first - 16 * c;
+#pragma unroll
+        for (int k = 0; k < KC; ++k)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const uint32_t from = k_off[k] == past ? past : k_off[k] * (uint32_t)sizeof(T);
+                ko[k][h] = buf_load16(key_tile, from, (4 * wave * D16 + 8 * h) * sizeof(T));
+            }
+#pragma unroll
+        for (int i = 0; i < VQ; ++i)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int d = 16 * (wave + 4 * i) + x;
+                vo[i][h] = d < D && valid > 8 * h
+                               ? *reinterpret_cast<const u4 *>(vf + (int64_t)d * room + 16 * c + 8 * h)
+                               : u4{0, 0, 0, 0};
+            }
+    };
+    int tile = max(begin, kt.paged);
+    if (tile < end) load_open(tile);
+    for (; tile < end; ++tile) {
+        const int first = 64 * (tile - kt.paged);
+        const T *vf = static_cast<const T *>(v.v_open) + ring * D * room + first_slot(tile);
+#pragma unroll
+        for (int k = 0; k < KC; ++k)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                frag[0][(wave * KC + k) * 2 + h][lane] = __builtin_bit_cast(h8, ko[k][h]);
+        const int valid = kt.open - first - 16 * c;
+        v4f z = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < VQ; ++i) {
+            const int d = wave + 4 * i;
+            if (VT % 4 && d >= VT) continue;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                u4 y = vo[i][h];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    if (8 * h + 2 * e >= valid) y[e] = 0;
+                    if (8 * h + 2 * e + 1 >= valid) y[e] &= 0xffffu;
+                }
+                const h8 g = __builtin_bit_cast(h8, y), none = {};
+                frag[0][8 * KC + 2 * d + h][lane] = g;
+                z = mfma_f16(g, none, z);            // NaN where a value is not finite
+            }
+        }
+        if (rows)
+#pragma unroll
+            for (int n = 0; n < NT; ++n) seen[n] = seen_of(a, t, kt, token[n], first + 16 * c);
+        if (tile + 1 < end) load_open(tile + 1);
+        const bool mine = __any(z[0] != z[0] || z[1] != z[1] || z[2] != z[2] || z[3] != z[3]);
+        if (lane == 0) odd_of[wave] = mine;
+        lds_barrier();
+        if (rows) {
+            v4f s[4][NT];
+            scores(0, s);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (!(seen[n] >> (4 * i + e) & 1)) s[i][n][e] = kMinusInf;
+            r.softmax(s, factor);
+            r.new_unit(1.f);
+            if (odd_of[0] | odd_of[1] | odd_of[2] | odd_of[3]) {
+                h8 p[NT][2];
+                r.weights(s, p);                     // (the total)
+                odd_sums<T>(r, s, seen, reinterpret_cast<float *>(frag[1]) + wave * 1024, vf, D, room,
+                            kt.open - first);
+            } else {
+                sums(0, s);
+            }
+        }
+        lds_barrier();
+    }
+    if (!rows) return;
+    Result<VT, NT> mine;
+    r.finish(mine);
+    store_result<T, W>(a, t, 16 * NT * wave, head, slot, part, mine);
 }
 
 // Parts of a row tile's keys joined.  A thread takes a row of the tile and every 256 / W-th
@@ -768,9 +1103,9 @@ __global__ __launch_bounds__(256, (attention_waves<T, VT, NT>())) void k_cache_a
 template <typename T, int W>
 __global__ __launch_bounds__(256) void k_cache_join(CacheAttnArgs a) {
     __shared__ float top_of[kMaxParts][W], weight[kMaxParts][W];
-    const int slot = blockIdx.x % a.slots, head = blockIdx.x / a.slots;
     RowTile t;
-    if (!row_tile<W>(a, slot, t)) return;
+    if (!row_tile<W>(a, blockIdx.x, 1, t)) return;
+    const int slot = t.slot, head = t.head;
     const KeyTiles kt = key_tiles<W>(a, t);
     const int per = (kt.all + a.parts - 1) / a.parts, used = (kt.all + per - 1) / per;
     constexpr int kGroups = 256 / W;
@@ -805,20 +1140,29 @@ __global__ __launch_bounds__(256) void k_cache_join(CacheAttnArgs a) {
     }
 }
 
-template <typename T, int VT, int NT>
+// kShared: the waves of a workgroup have rows of their own
+template <typename T, int VT, int NT, bool kShared = false>
 nmg_status run_cache_attention(nmg_cache_format format, const CacheAttnArgs &a, hipStream_t stream) {
     const int64_t total = (int64_t)a.slots * a.parts * a.c.heads;
     if (total > INT32_MAX / 256) return NMG_ERR_UNSUPPORTED;
-    if (format == NMG_CACHE_INT8)
-        k_cache_attention<T, VT, NT, true><<<(int)total, 256, 0, stream>>>(a, (int)total);
-    else
-        k_cache_attention<T, VT, NT, false><<<(int)total, 256, 0, stream>>>(a, (int)total);
+    if constexpr (kShared) {
+        if (format == NMG_CACHE_INT8)
+            k_cache_attention_shared<VT, NT, true><<<(int)total, 256, 0, stream>>>(a);
+        else
+            k_cache_attention_shared<VT, NT, false><<<(int)total, 256, 0, stream>>>(a);
+    } else {
+        if (format == NMG_CACHE_INT8)
+            k_cache_attention<T, VT, NT, true><<<(int)total, 256, 0, stream>>>(a);
+        else
+            k_cache_attention<T, VT, NT, false><<<(int)total, 256, 0, stream>>>(a);
+    }
     nmg_status st = launched();
     if (st == NMG_OK && a.parts > 1) {
+        constexpr int W = (kShared ? 64 : 16) * NT;
         // workgroups for every compute unit, as far as a feature for every thread goes
-        const int64_t tiles = (int64_t)a.slots * a.c.heads, most = std::max(1, a.c.D * 16 * NT / 256);
+        const int64_t tiles = (int64_t)a.slots * a.c.heads, most = std::max(1, a.c.D * W / 256);
         const int y = (int)std::min<int64_t>(most, std::max<int64_t>(1, 1024 / tiles));
-        k_cache_join<T, 16 * NT><<<dim3((int)tiles, y), 256, 0, stream>>>(a);
+        k_cache_join<T, W><<<dim3((int)tiles, y), 256, 0, stream>>>(a);
         st = launched();
     }
     return st;

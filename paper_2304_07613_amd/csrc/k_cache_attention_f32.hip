@@ -3,16 +3,17 @@
 
 namespace nmg_internal {
 
-nmg_status cache_attention_f32(nmg_cache_format format, const CacheAttnArgs &a, int nt,
+nmg_status cache_attention_f32(nmg_cache_format format, const CacheAttnArgs &a, CacheAttnRows rows,
                                hipStream_t stream) {
     const int tiles = (a.c.D + 15) / 16;
-    if (tiles > 8) return run_cache_attention<float, 16, 1>(format, a, stream);
-    if (tiles > 6) return nt == 1 ? run_cache_attention<float, 8, 1>(format, a, stream)
-                                  : run_cache_attention<float, 8, 2>(format, a, stream);
-    if (tiles > 4) return nt == 1 ? run_cache_attention<float, 6, 1>(format, a, stream)
-                                  : run_cache_attention<float, 6, 2>(format, a, stream);
-    return nt == 1 ? run_cache_attention<float, 4, 1>(format, a, stream)
-                   : run_cache_attention<float, 4, 2>(format, a, stream);
+    if (rows == kRows16)
+        return tiles > 8   ? run_cache_attention<float, 16, 1>(format, a, stream)
+               : tiles > 6 ? run_cache_attention<float, 8, 1>(format, a, stream)
+               : tiles > 4 ? run_cache_attention<float, 6, 1>(format, a, stream)
+                           : run_cache_attention<float, 4, 1>(format, a, stream);
+    return tiles > 6   ? run_cache_attention<float, 8, 2>(format, a, stream)
+           : tiles > 4 ? run_cache_attention<float, 6, 2>(format, a, stream)
+                       : run_cache_attention<float, 4, 2>(format, a, stream);
 }
 
 }  // namespace nmg_internal

@@ -682,6 +682,39 @@ def test_values_of_any_size_in_binary32(dev, k_size, v_size, q_size):
 
 @gpu
 @pytest.mark.parametrize("dtype", ["f16", "f32"])
+@pytest.mark.parametrize("heads,kv_heads,dim", [(4, 2, 64), (3, 1, 80), (6, 1, 96), (4, 1, 128), (2, 1, 200),
+                                                (2, 2, 256), (8, 1, 16)])
+def test_many_rows(dev, heads, kv_heads, dim, dtype):
+    """Drafts long enough for every kernel: sequences of unequal length, a wave or a
+    workgroup without rows, the last key tile partly filled, values that are not finite."""
+    for block, fmt in ((64, "int8"), (128, "e4m3")):
+        b = Both(dev, 1, kv_heads, dim, 4, 40, 8, 384, block, fmt, dtype)
+        b.grow([200, 0, 129, 64])
+        for counts in ([130, 255, 1, 70], [64, 64, 64, 64], [0, 257, 0, 0]):
+            print(f"{heads}/{kv_heads} x {dim} {dtype} {fmt} {counts}", flush=True)
+            tree = random_tree(dim, counts)
+            q = b.draft(counts)
+            b.attend(heads, q)
+            b.attend(heads, q, tree)
+            b.attend(heads, q, tree, longest=4000)
+            q = b.draft(counts, lambda K, V, q: V.__setitem__((dim // 2, slice(None, None, 50)), math.nan))
+            b.attend(heads, q, tree)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
+def test_many_rows_over_parts(dev, dtype):
+    for dim, fmt in ((64, "e4m3"), (128, "int8"), (256, "e4m3")):
+        b = Both(dev, 1, 1, dim, 2, 60, 50, 512, 64, fmt, dtype)
+        b.grow([2000, 300])
+        q = b.draft([100, 37])
+        for longest in (None, 2000, 100):
+            print(dim, fmt, dtype, longest, flush=True)
+            b.attend(3, q, random_tree(dim, [100, 37]), longest=longest)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
 def test_pages_of_very_different_sizes(dev, dtype):
     """Attention that looks at one page whose values are tiny beside the others'."""
     b = Both(dev, 1, 1, 64, 1, 20, 8, 128, 64, "e4m3", dtype)

@@ -46,8 +46,9 @@ struct CacheAttnArgs {
     float scale;
     // the plan of the launch
     int32_t slots;                   // row tiles of all sequences, at most
-    int32_t parts;                   // of every sequence's keys
-    float *part;                     // parts > 1: their results
+    int32_t target;                  // workgroups that splitting the keys aims at, 0: no splitting
+    int64_t part_count;              // parts whose results there is room for
+    float *part;
 };
 
 // Rows of a workgroup: 16 or 32 that its four waves split the keys of; 64 (head_dim > 128) or

@@ -32,6 +32,13 @@ typedef _Float16 h2 __attribute__((ext_vector_type(2)));
 typedef float v2f __attribute__((ext_vector_type(2)));
 typedef uint32_t u4 __attribute__((ext_vector_type(4)));
 
+// Parts of a sequence's keys, at most; what the join's LDS holds of many rows
+constexpr int max_parts(int rows) { return rows > 32 ? 16 : 64; }
+constexpr int kPartUnits = 8;      // key tiles of a part, at least: two a wave
+// A larger score moves the reference of a row's weights, and scales its sums, once it is 2^6 times
+// larger: for most inputs that happens in the first tile alone, where every new maximum of one
+// of 32 rows would do it nearly every time
+constexpr float kSlack = 6.f;
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kMinusInf = -__builtin_inff();
 
@@ -114,65 +121,124 @@ __device__ __forceinline__ float exp2_fast(float x) {
 // ------------------------------------------------------- what a workgroup has
 
 // A workgroup's row tile, key head and part of the keys.  The lengths are on the device and the
-// launch has room for any; the workgroups that there are come first, so that the
-// idle ones do not fall on some compute units more than on others.
+// launch has room for any.  Up to 64 sequences: every wave counts the row tiles and key
+// tiles of all, so that all parts are about equal whatever the lengths, and the
+// workgroups that there are come first (else the idle ones fall on some compute
+// units more than on others).
 struct RowTile {
     int b, T, q0, n;        // sequence, its query columns and their first; kept tokens
     int first, rows;        // first row of the tile, rows of the sequence
-    int slot, part, head;
+    int head, part, parts;  // parts of the sequence's keys
+    int64_t place;          // of the tile's first part among all parts' results
 };
 
-template <int kRows>
-__device__ __forceinline__ bool row_tile(const CacheAttnArgs &a, int index, int parts, RowTile &t) {
-    auto inside = [&](int v) { return v < 0 ? 0 : v > a.Nq ? a.Nq : v; };
+// Key tiles of a sequence: whole pages' first, then those of the open tokens
+struct KeyTiles {
+    int paged, all;         // tiles of pages, and of both
+    int open, kept;         // open tokens, and how many of them are kept ones
+    // In units of a page's tile, a tile of open tokens is three.  (It takes 7 us beside 2.5
+    // where many rows meet it.)
+    __device__ __forceinline__ int units() const { return paged + 3 * (all - paged); }
+    __device__ __forceinline__ int tile_at(int unit) const {
+        return unit <= paged ? unit : paged + (unit - paged + 1) / 3;
+    }
+    // the tiles of a part
+    __device__ __forceinline__ void range(int part, int parts, int *begin, int *end) const {
+        const int per = (units() + parts - 1) / parts;
+        *begin = min(all, tile_at(min(part * per, units())));
+        *end = min(all, tile_at(min((part + 1) * per, units())));
+    }
+};
+__device__ __forceinline__ KeyTiles key_tiles(const CacheAttnArgs &a, int n, int T) {
+    KeyTiles k;
+    const int blocks = n / a.c.block;
+    k.kept = n - blocks * a.c.block;
+    k.paged = blocks * (a.c.block / 64);
+    k.open = (int)min((int64_t)k.kept + T, (int64_t)a.c.room);
+    k.all = k.paged + (k.open + 63) / 64;
+    return k;
+}
+
+__device__ __forceinline__ int wave_sum_upto(int v) {      // over this lane and those before it
     const int lane = threadIdx.x & 63;
-    auto place = [&](int slots) {
-        const int total = slots * parts * a.c.heads;
-        if (index >= total) return false;
-        const int at = xcd_tile(index, total);
-        t.slot = at % slots;
-        t.part = at / slots % parts;
-        t.head = at / slots / parts;
-        return true;
-    };
-    int at;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        const int up = __shfl_up(v, d);
+        v += lane >= d ? up : 0;
+    }
+    return v;
+}
+
+// kJoin: index runs over row tiles and heads, else over their parts too
+template <int kRows, bool kJoin>
+__device__ __forceinline__ bool row_tile(const CacheAttnArgs &a, int index, RowTile &t) {
+    auto inside = [&](int v) { return v < 0 ? 0 : v > a.Nq ? a.Nq : v; };
+    const int lane = threadIdx.x & 63, heads = a.c.heads;
+    int at;                                         // of the sequence's row tiles
     if (a.c.sequences <= 64) {
-        // every sequence's row tiles counted, one lane each
         const int b = min(lane, a.c.sequences - 1);
         const int from = inside(a.q_offsets[b]), columns = inside(a.q_offsets[b + 1]) - from;
         const int kept = cache_length(a.c, a.lengths, b);
         const int tiles = lane < a.c.sequences && columns > 0
                               ? (int)(((int64_t)columns * a.share + kRows - 1) / kRows) : 0;
-        int upto = tiles;
-#pragma unroll
-        for (int d = 1; d < 64; d *= 2) {
-            const int up = __shfl_up(upto, d);
-            upto += lane >= d ? up : 0;
+        int parts = 1;
+        const int tiles_upto = wave_sum_upto(tiles), all_tiles = __builtin_amdgcn_readlane(tiles_upto, 63);
+        if (all_tiles > a.slots) return false;      // (offsets that are not as described)
+        if (a.target > 0) {
+            // parts of `per` units: about half a part more each than the units make
+            const int units = key_tiles(a, kept, max(columns, 0)).units();
+            float work = (float)tiles * units;
+            for (int d = 32; d; d /= 2) work += __shfl_xor(work, d);
+            const float aim = fmaxf((float)a.target - 0.5f * all_tiles * heads, 1.f);
+            const int per = max(kPartUnits, (int)fminf(ceilf(work * heads / aim), 1e9f));
+            parts = min(max_parts(kRows), (units + per - 1) / per);
+            if (parts < 1) parts = 1;
         }
-        if (!place(min(__builtin_amdgcn_readlane(upto, 63), a.slots))) return false;
-        t.b = min(__popcll(__ballot(upto <= t.slot)), a.c.sequences - 1);
+        const int each = kJoin ? tiles : tiles * parts;
+        const int upto = kJoin ? tiles_upto : wave_sum_upto(each);
+        const int total = __builtin_amdgcn_readlane(upto, 63);
+        if (index >= total * heads) return false;
+        const int place = kJoin ? index : xcd_tile(index, total * heads), unit = place % total;
+        t.head = place / total;
+        t.b = min(__popcll(__ballot(upto <= unit)), a.c.sequences - 1);
         t.q0 = __builtin_amdgcn_readlane(from, t.b);
         t.T = __builtin_amdgcn_readlane(columns, t.b);
         t.n = __builtin_amdgcn_readlane(kept, t.b);
-        at = t.slot - __builtin_amdgcn_readlane(upto - tiles, t.b);
+        t.parts = __builtin_amdgcn_readlane(parts, t.b);
+        const int before = unit - __builtin_amdgcn_readlane(upto - each, t.b);
+        at = kJoin ? before : before % max(1, __builtin_amdgcn_readlane(tiles, t.b));
+        t.part = kJoin ? 0 : before / max(1, __builtin_amdgcn_readlane(tiles, t.b));
+        if (a.target > 0) {
+            const int parts_upto = kJoin ? wave_sum_upto(tiles * parts) : upto;
+            const int64_t all = __builtin_amdgcn_readlane(parts_upto, 63);
+            t.place = t.head * all + __builtin_amdgcn_readlane(parts_upto - tiles * parts, t.b) +
+                      (int64_t)at * t.parts;
+            if ((t.head + 1) * all > a.part_count) return false;      // (never, of lengths that stay)
+        }
     } else {
         // sequence b has the slots [first(b), first(b + 1)), first(b) = floor(offset(b) share /
         // rows) + b, at least as many as its rows fill: the last b with first(b) <=
         // slot, 64 at a time; the last step has its offsets and length too
-        if (!place(a.slots)) return false;
+        t.parts = max(1, min(a.target / max(1, a.slots * heads), max_parts(kRows)));
+        const int slots = a.slots, parts = kJoin ? 1 : t.parts;
+        if (index >= slots * parts * heads) return false;
+        const int place = kJoin ? index : xcd_tile(index, slots * parts * heads), slot = place % slots;
+        t.part = place / slots % parts;
+        t.head = place / slots / parts;
+        t.place = ((int64_t)t.head * slots + slot) * t.parts;
         int lo = 0, n = a.c.sequences, stride;
         do {
             stride = (n + 63) / 64;
             const int b = lo + min(lane * stride, n - 1);
             const int from = inside(a.q_offsets[b]), to = inside(a.q_offsets[b + 1]);
             const int kept = cache_length(a.c, a.lengths, b), first = (int)((int64_t)from * a.share / kRows) + b;
-            const int found = __popcll(__ballot(lane * stride < n && first <= t.slot)) - 1;
+            const int found = __popcll(__ballot(lane * stride < n && first <= slot)) - 1;
             if (found < 0) return false;
             t.b = lo + found * stride;
             t.q0 = __builtin_amdgcn_readlane(from, found);
             t.T = __builtin_amdgcn_readlane(to, found) - t.q0;
             t.n = __builtin_amdgcn_readlane(kept, found);
-            at = t.slot - __builtin_amdgcn_readlane(first, found);
+            at = slot - __builtin_amdgcn_readlane(first, found);
             lo = t.b;
             n = min(stride, n - found * stride);
         } while (stride > 1);
@@ -183,24 +249,13 @@ __device__ __forceinline__ bool row_tile(const CacheAttnArgs &a, int index, int 
     return true;
 }
 
-// Key tiles of a row tile: whole pages' first, then those of the open tokens that
-// its rows may see
-struct KeyTiles {
-    int paged, all;         // tiles of pages, and of both
-    int open, kept;         // open tokens, and how many of them are kept ones
-};
+// Tiles past `end` that no row of the tile sees are left out: without a tree a row of one
+// head's tokens sees none behind its own
 template <int kRows>
-__device__ __forceinline__ KeyTiles key_tiles(const CacheAttnArgs &a, const RowTile &t) {
-    KeyTiles k;
-    const int blocks = t.n / a.c.block;
-    k.kept = t.n - blocks * a.c.block;
-    k.paged = blocks * (a.c.block / 64);
-    k.open = (int)min((int64_t)k.kept + t.T, (int64_t)a.c.room);
-    int seen = k.open;
-    if (!a.tree && t.first / t.T == (min(t.first + kRows, t.rows) - 1) / t.T)  // one head's rows
-        seen = min(seen, k.kept + (min(t.first + kRows, t.rows) - 1) % t.T + 1);
-    k.all = k.paged + (seen + 63) / 64;
-    return k;
+__device__ __forceinline__ int seen_end(const CacheAttnArgs &a, const RowTile &t, const KeyTiles &k, int end) {
+    const int last = min(t.first + kRows, t.rows) - 1;
+    if (a.tree || t.first / t.T != last / t.T) return end;
+    return min(end, k.paged + (min(k.open, k.kept + last % t.T + 1) + 63) / 64);
 }
 
 // Which of the 16 open tokens from `first` on a drafted token sees, a bit each
@@ -288,18 +343,16 @@ __device__ __forceinline__ void join_waves(Result<VT, NT> &r, float *lds) {
 template <int VT, int NT>
 constexpr int join_floats() { return std::max(2 * (VT * NT * 256 + NT * 128), 4 * 1024); }
 
-constexpr int kMaxParts = 32;
-
 // Floats of one part's result: a row of sums for every feature, then maxima, then totals
 __host__ __device__ inline int64_t part_floats(int D, int rows) { return (int64_t)(D + 2) * rows; }
 
 // kRows: of the row tile, of which `at` and what follows are the wave's
 template <typename T, int kRows, int VT, int NT>
-__device__ __forceinline__ void store_result(const CacheAttnArgs &a, const RowTile &t, int at, int head,
-                                             int slot, int part, const Result<VT, NT> &r) {
+__device__ __forceinline__ void store_result(const CacheAttnArgs &a, const RowTile &t, int at,
+                                             const Result<VT, NT> &r) {
     const int lane = threadIdx.x & 63, x = lane % 16, c = lane / 16, D = a.c.D;
-    if (a.parts > 1) {
-        float *to = a.part + (((int64_t)head * a.slots + slot) * a.parts + part) * part_floats(D, kRows);
+    if (t.parts > 1) {
+        float *to = a.part + (t.place + t.part) * part_floats(D, kRows);
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
 #pragma unroll
@@ -320,7 +373,7 @@ __device__ __forceinline__ void store_result(const CacheAttnArgs &a, const RowTi
     for (int n = 0; n < NT; ++n) {
         const int row = t.first + at + 16 * n + x;
         if (row >= t.rows) continue;
-        const int64_t h = head * a.share + row / t.T;
+        const int64_t h = t.head * a.share + row / t.T;
         T *to = O + h * D * a.ldo + t.q0 + row % t.T;
 #pragma unroll
         for (int d = 0; d < VT; ++d)
@@ -332,6 +385,15 @@ __device__ __forceinline__ void store_result(const CacheAttnArgs &a, const RowTi
 
 // ------------------------------------------------------------------ the pass
 
+// The larger of two; of NaN and a number either (a NaN score makes its weight NaN).  fmaxf
+// would first quieten both.
+__device__ __forceinline__ float larger(float a, float b) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    return __builtin_amdgcn_fmed3f(a, b, __builtin_inff());
+#else
+    return a;
+#endif
+}
 // The largest of v over the four lanes (x, 0 .. 3)
 __device__ __forceinline__ float max_over_c(float v) {
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -348,12 +410,6 @@ __device__ __forceinline__ float max_over_c(float v) {
 __device__ __forceinline__ float sum_over_c(float v) {
     v += __shfl_xor(v, 32);
     return v + __shfl_xor(v, 16);
-}
-// A value that is the same for the wave, through the scalar cache: loads of registers in
-// flight are not waited for
-template <typename T>
-__device__ __forceinline__ T scalar_load(const T *p) {
-    return *(const __attribute__((address_space(4))) T *)(uintptr_t)p;
 }
 // e of v = m 2^e, 1 <= |m| < 2; 0 for 0
 __device__ __forceinline__ int exponent_of(float v) {
@@ -376,7 +432,7 @@ struct Pass {
     v4f o[VT][NT];          // sums of weights times values
     v4f total[NT];          // of the weights: binary16 by a matrix instruction with ones (four
                             // equal values), binary32 the lane's part
-    float m[NT];            // largest score so far
+    float m[NT];            // the reference of the weights: no score so far is more than kSlack larger
     // The sums are in units of a power of two.  binary16: of the tile at hand's values,
     // since its weights leave no room for another factor.  binary32: of the largest
     // scale so far, the weights take the rest.
@@ -408,18 +464,18 @@ struct Pass {
         bool up = false;
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-            float t = fmaxf(fmaxf(s[0][n][0], s[0][n][1]), fmaxf(s[0][n][2], s[0][n][3]));
+            float t = larger(larger(s[0][n][0], s[0][n][1]), larger(s[0][n][2], s[0][n][3]));
 #pragma unroll
             for (int i = 1; i < 4; ++i)
-                t = fmaxf(fmaxf(t, fmaxf(s[i][n][0], s[i][n][1])), fmaxf(s[i][n][2], s[i][n][3]));
-            top[n] = fmaxf(m[n], max_over_c(t) * f);
-            up |= top[n] > m[n];
+                t = larger(t, larger(larger(s[i][n][0], s[i][n][1]), larger(s[i][n][2], s[i][n][3])));
+            top[n] = max_over_c(t) * f;
+            up |= top[n] > m[n] + kSlack;
         }
         if (__any(up)) {
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
                 const float g = top[n] > m[n] ? exp2_fast(m[n] - top[n]) : 1.f;
-                m[n] = top[n];
+                m[n] = fmaxf(m[n], top[n]);
                 total[n] *= g;
 #pragma unroll
                 for (int d = 0; d < VT; ++d) o[d][n] *= g;
@@ -428,8 +484,8 @@ struct Pass {
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
             // binary16 weights are 2^15 at most, so that the small ones stay normal down to
-            // 2^-29 of the largest (totals have the same factor)
-            const float base = (m[n] == kMinusInf ? 0.f : m[n]) - (kF32 ? 0.f : 15.f);
+            // 2^-23 of the reference (totals have the same factor)
+            const float base = (m[n] == kMinusInf ? 0.f : m[n]) - (kF32 ? 0.f : 15.f - kSlack);
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -496,6 +552,33 @@ __device__ __forceinline__ void odd_sums(Pass<kF32, VT, NT> &r, const v4f (&s)[4
     }
 }
 
+// The pages of a wave's next 64 key tiles (first, first + step, ...) and their scales, a lane
+// each: no load of a tile waits for a look at the table
+struct Ahead {
+    int64_t of;             // where the page's head lies among the heads of all pages
+    float ks, vs;
+
+    __device__ __forceinline__ void look(const CacheAttnArgs &a, const RowTile &t, int first, int step, int end) {
+        const CacheView &v = a.c;
+        const int tile = first + step * (int)(threadIdx.x & 63);
+        of = 0;
+        ks = vs = 1.f;
+        if (tile < end) {
+            const int p = v.table[(int64_t)t.b * v.row + min(tile / (v.block / 64), v.row - 1)];
+            of = ((int64_t)a.layer * v.pages + min(max(p, 0), v.pages - 1)) * v.heads + t.head;
+            ks = v.k_scales[of];
+            vs = v.v_scales[of];
+        }
+    }
+    __device__ __forceinline__ int64_t place(int i) const {
+        const uint32_t lo = __builtin_amdgcn_readlane((int)of, i), hi = __builtin_amdgcn_readlane((int)(of >> 32), i);
+        return (int64_t)((uint64_t)hi << 32 | lo);
+    }
+    __device__ __forceinline__ float scale(float of_lane, int i) const {
+        return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(of_lane), i));
+    }
+};
+
 // Waves of a SIMD that the registers are to leave room for
 template <typename T, int VT, int NT>
 constexpr int attention_waves() {
@@ -514,21 +597,18 @@ __global__ __launch_bounds__(256, (attention_waves<T, VT, NT>())) void k_cache_a
     const int D = v.D, D16 = v.D16, room = v.room;
 
     RowTile t;
-    if (!row_tile<W>(a, blockIdx.x, a.parts, t)) return;
-    const int slot = t.slot, part = t.part, head = t.head;
-    const KeyTiles kt = key_tiles<W>(a, t);
-    const int per = (kt.all + a.parts - 1) / a.parts;
-    const int begin = part * per, end = min(kt.all, begin + per);
+    if (!row_tile<W, false>(a, blockIdx.x, t)) return;
+    const int head = t.head;
+    const KeyTiles kt = key_tiles(a, t.n, t.T);
+    int begin, end;
+    kt.range(t.part, t.parts, &begin, &end);
     if (begin >= end) return;
+    end = seen_end<W>(a, t, kt, end);               // (then the part's result is that of no keys)
 
     // ---- pages: the first ones are asked for before the queries
     const int two = v.block == 128, paged_end = min(end, kt.paged);   // key tiles of a page: 1 << two
     const int64_t heads = v.heads;
-    const int32_t *table = v.table + (int64_t)t.b * v.row;
-    auto page_of = [&](int tile) {
-        const int p = scalar_load(table + min(tile >> two, v.row - 1));
-        return p < 0 ? 0 : p >= v.pages ? v.pages - 1 : p;
-    };
+    Ahead pages;
     // A page's part of a head is one buffer: a load takes its base from scalar registers and
     // one offset per lane, what lies behind the head reads as zeros.
     const uint32_t k_bytes = v.block * D16, v_bytes = D * v.block, past = 0x7fffffffu;
@@ -537,24 +617,18 @@ __global__ __launch_bounds__(256, (attention_waves<T, VT, NT>())) void k_cache_a
 #pragma unroll
     for (int k = 0; k < KC; ++k) k_off[k] = 64 * k + 16 * c < D16 ? k_at + 64 * k : past;
     u4 kk[4][KC];
-    float ks = 1.f, vs = 1.f;
-    auto load_keys = [&](int tile, int page) {
-        const int64_t of = ((int64_t)a.layer * v.pages + page) * heads + head;
-        const buf_rsrc_t from = buf_rsrc(v.k_pages + of * k_bytes, k_bytes);
+    auto load_keys = [&](int tile, int i) {
+        const buf_rsrc_t from = buf_rsrc(v.k_pages + pages.place(i) * k_bytes, k_bytes);
         const uint32_t first = (tile & two) * 64 * D16;
-        ks = scalar_load(v.k_scales + of);
-        vs = scalar_load(v.v_scales + of);
 #pragma unroll
         for (int s = 0; s < 4; ++s)
 #pragma unroll
             for (int k = 0; k < KC; ++k) kk[s][k] = buf_load16(from, k_off[k], first + 4 * s * D16);
     };
     int tile = begin + wave;
-    int page = 0, next_page = 0;
     if (tile < paged_end) {
-        page = page_of(tile);
-        next_page = page_of(tile + 4);
-        load_keys(tile, page);
+        pages.look(a, t, tile, 4, paged_end);
+        load_keys(tile, 0);
     }
     // queries: the lane's features 64 k + 16 c + j of row x of every row tile
     std::conditional_t<kF32, float[NT][KC][16], h8[NT][KC][2]> q;
@@ -601,16 +675,16 @@ __global__ __launch_bounds__(256, (attention_waves<T, VT, NT>())) void k_cache_a
     const float factor = a.scale * kLog2e;
 
     // ---- whole pages
-    for (; tile < paged_end; tile += 4) {
+    for (int at = 0; tile < paged_end; tile += 4, ++at) {
         u4 vv[VT];
-        const int64_t of = ((int64_t)a.layer * v.pages + page) * heads + head;
-        const buf_rsrc_t from = buf_rsrc(v.v_pages + of * v_bytes, v_bytes);
+        const int i64 = at & 63;
+        const buf_rsrc_t from = buf_rsrc(v.v_pages + pages.place(i64) * v_bytes, v_bytes);
         const uint32_t first = (tile & two) * 64;
 #pragma unroll
         for (int d = 0; d < VT; ++d) vv[d] = buf_load16(from, v_at + first + 16 * d * v.block, 0);
         issued();        // before the scores: they are the time that the values have to come
-        const int after = page_of(tile + 8);
-        const float tile_ks = ks, tile_vs = vs < 0x1p-32f && !kF32 ? 0x1p-32f : vs;
+        const float tile_ks = pages.scale(pages.ks, i64), vs = pages.scale(pages.vs, i64);
+        const float tile_vs = vs < 0x1p-32f && !kF32 ? 0x1p-32f : vs;
         v4f s[4][NT];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -638,10 +712,11 @@ __global__ __launch_bounds__(256, (attention_waves<T, VT, NT>())) void k_cache_a
                 }
             }
         }
-        if (tile + 4 < paged_end) load_keys(tile + 4, next_page);
+        if (tile + 4 < paged_end) {
+            if (i64 == 63) pages.look(a, t, tile + 4, 4, paged_end);
+            load_keys(tile + 4, (at + 1) & 63);
+        }
         issued();
-        page = next_page;
-        next_page = after;
         if constexpr (kF32) {
             const int ke = exponent_of(tile_ks);
             const float nan = tile_ks - tile_ks;       // of a block that is not finite
@@ -703,7 +778,7 @@ __global__ __launch_bounds__(256, (attention_waves<T, VT, NT>())) void k_cache_a
         if constexpr (kF32) {
             // the tile's keys are scaled like codes, by its largest finite value
             uint32_t top = 0;
-#pragma unroll(KC == 1 ? 4 : KC == 2 ? 2 : 1)
+#pragma unroll KC == 1 ? 4 : KC == 2 ? 2 : 1
             for (int m = 0; m < 4; ++m)
 #pragma unroll
                 for (int k = 0; k < KC; ++k)
@@ -845,7 +920,7 @@ __global__ __launch_bounds__(256, (attention_waves<T, VT, NT>())) void k_cache_a
     Result<VT, NT> mine;
     r.finish(mine);
     if (end - begin > 1) join_waves(mine, lds);
-    if (wave == 0) store_result<T, 16 * NT>(a, t, 0, head, slot, part, mine);
+    if (wave == 0) store_result<T, 16 * NT>(a, t, 0, mine);
 }
 
 // ------------------------------------------------- many rows (binary16)
@@ -874,22 +949,19 @@ __global__ __launch_bounds__(256, VT == 16 ? 1 : 2) void k_cache_attention_share
     const int D = v.D, D16 = v.D16, room = v.room;
 
     RowTile t;
-    if (!row_tile<W>(a, blockIdx.x, a.parts, t)) return;
-    const int slot = t.slot, part = t.part, head = t.head;
-    const KeyTiles kt = key_tiles<W>(a, t);
-    const int per = (kt.all + a.parts - 1) / a.parts;
-    const int begin = part * per, end = min(kt.all, begin + per);
+    if (!row_tile<W, false>(a, blockIdx.x, t)) return;
+    const int head = t.head;
+    const KeyTiles kt = key_tiles(a, t.n, t.T);
+    int begin, end;
+    kt.range(t.part, t.parts, &begin, &end);
     if (begin >= end) return;
+    end = seen_end<W>(a, t, kt, end);               // (then the part's result is that of no keys)
     const int first_row = t.first + 16 * NT * wave;
     const bool rows = first_row < t.rows;            // the wave has some
 
     const int two = v.block == 128, paged_end = min(end, kt.paged);
     const int64_t heads = v.heads;
-    const int32_t *table = v.table + (int64_t)t.b * v.row;
-    auto head_of_page = [&](int tile) {              // of the pool's pages and scales
-        const int p = scalar_load(table + min(tile >> two, v.row - 1));
-        return ((int64_t)a.layer * v.pages + (p < 0 ? 0 : p >= v.pages ? v.pages - 1 : p)) * heads + head;
-    };
+    Ahead pages;                                     // of the tile that is loaded next
     const uint32_t k_bytes = v.block * D16, v_bytes = D * v.block, past = 0x7fffffffu;
     const uint32_t k_at = (16 * (x / 4) + x % 4) * D16 + 16 * c, v_at = x * v.block + 16 * c;
     uint32_t k_off[KC];
@@ -897,9 +969,13 @@ __global__ __launch_bounds__(256, VT == 16 ? 1 : 2) void k_cache_attention_share
     for (int k = 0; k < KC; ++k) k_off[k] = 64 * k + 16 * c < D16 ? k_at + 64 * k : past;
     // the wave's quarter of a tile: keys 16 (.) + 4 wave + (.), features of 16 d, d % 4 == wave
     u4 kk[KC], vv[VQ];
-    float ks = 1.f, vs = 1.f;
-    auto load = [&](int tile) {
-        const int64_t of = head_of_page(tile);
+    float ks[3], vs[3];                              // of the tile at hand and the next two
+    auto load = [&](int tile, int to) {
+        const int i = (tile - begin) & 63;
+        if (i == 0) pages.look(a, t, tile, 1, paged_end);
+        const int64_t of = pages.place(i);
+        ks[to] = pages.scale(pages.ks, i);
+        vs[to] = pages.scale(pages.vs, i);
         const buf_rsrc_t from_k = buf_rsrc(v.k_pages + of * k_bytes, k_bytes);
         const buf_rsrc_t from_v = buf_rsrc(v.v_pages + of * v_bytes, v_bytes);
 #pragma unroll
@@ -907,11 +983,6 @@ __global__ __launch_bounds__(256, VT == 16 ? 1 : 2) void k_cache_attention_share
 #pragma unroll
         for (int i = 0; i < VQ; ++i)
             vv[i] = buf_load16(from_v, v_at + (tile & two) * 64 + 16 * (wave + 4 * i) * v.block, 0);
-    };
-    auto scales = [&](int tile) {
-        const int64_t of = head_of_page(tile);
-        ks = scalar_load(v.k_scales + of);
-        vs = scalar_load(v.v_scales + of);
     };
     auto decode = [&](int to) {
 #pragma unroll
@@ -927,7 +998,7 @@ __global__ __launch_bounds__(256, VT == 16 ? 1 : 2) void k_cache_attention_share
             frag[to][8 * KC + 2 * d + 1][lane] = decode8<kInt8>(vv[i][2], vv[i][3]);
         }
     };
-    if (begin < paged_end) load(begin);
+    if (begin < paged_end) load(begin, 0);
 
     h8 q[NT][KC][2];
     int token[NT];
@@ -951,28 +1022,30 @@ __global__ __launch_bounds__(256, VT == 16 ? 1 : 2) void k_cache_attention_share
     r.clear();
     const float factor = a.scale * kLog2e;
 
+    // (products that follow one another are of different sums: none waits for the last)
     auto scores = [&](int from, v4f (&s)[4][NT]) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < 4; ++i)
 #pragma unroll
             for (int n = 0; n < NT; ++n) s[i][n] = v4f{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int k = 0; k < KC; ++k)
+        for (int k = 0; k < KC; ++k)
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
                     const h8 f = frag[from][(i * KC + k) * 2 + h][lane];
 #pragma unroll
                     for (int n = 0; n < NT; ++n) s[i][n] = mfma_f16(f, q[n][k][h], s[i][n]);
                 }
-        }
     };
     auto sums = [&](int from, const v4f (&s)[4][NT]) {
         h8 p[NT][2];
         r.weights(s, p);
 #pragma unroll
-        for (int d = 0; d < VT; ++d)
+        for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
+            for (int d = 0; d < VT; ++d) {
                 const h8 g = frag[from][8 * KC + 2 * d + h][lane];
 #pragma unroll
                 for (int n = 0; n < NT; ++n) r.o[d][n] = mfma_f16(g, p[n][h], r.o[d][n]);
@@ -982,17 +1055,17 @@ __global__ __launch_bounds__(256, VT == 16 ? 1 : 2) void k_cache_attention_share
     // ---- whole pages
     if (begin < paged_end) {
         decode(0);
-        if (begin + 1 < paged_end) load(begin + 1);
-        scales(begin);
+        if (begin + 1 < paged_end) load(begin + 1, 1);
         lds_barrier();
     }
     for (int tile = begin, buffer = 0; tile < paged_end; ++tile, buffer ^= 1) {
-        const float tile_ks = ks, tile_vs = vs < 0x1p-32f ? 0x1p-32f : vs;
-        if (tile + 1 < paged_end) {
-            decode(buffer ^ 1);
-            scales(tile + 1);
-        }
-        if (tile + 2 < paged_end) load(tile + 2);
+        const float tile_ks = ks[0], tile_vs = vs[0] < 0x1p-32f ? 0x1p-32f : vs[0];
+        if (tile + 1 < paged_end) decode(buffer ^ 1);
+        if (tile + 2 < paged_end) load(tile + 2, 2);
+        ks[0] = ks[1];
+        vs[0] = vs[1];
+        ks[1] = ks[2];
+        vs[1] = vs[2];
         if (rows) {
             v4f s[4][NT];
             scores(buffer, s);
@@ -1095,26 +1168,27 @@ __global__ __launch_bounds__(256, VT == 16 ? 1 : 2) void k_cache_attention_share
     if (!rows) return;
     Result<VT, NT> mine;
     r.finish(mine);
-    store_result<T, W>(a, t, 16 * NT * wave, head, slot, part, mine);
+    store_result<T, W>(a, t, 16 * NT * wave, mine);
 }
 
 // Parts of a row tile's keys joined.  A thread takes a row of the tile and every 256 / W-th
 // feature of its workgroup's; the parts' weights are made once, in LDS.
 template <typename T, int W>
 __global__ __launch_bounds__(256) void k_cache_join(CacheAttnArgs a) {
-    __shared__ float top_of[kMaxParts][W], weight[kMaxParts][W];
+    __shared__ float top_of[max_parts(W)][W], weight[max_parts(W)][W];
     RowTile t;
-    if (!row_tile<W>(a, blockIdx.x, 1, t)) return;
-    const int slot = t.slot, head = t.head;
-    const KeyTiles kt = key_tiles<W>(a, t);
-    const int per = (kt.all + a.parts - 1) / a.parts, used = (kt.all + per - 1) / per;
+    if (!row_tile<W, true>(a, blockIdx.x, t) || t.parts == 1) return;
+    const int used = t.parts;
+    const KeyTiles kt = key_tiles(a, t.n, t.T);
     constexpr int kGroups = 256 / W;
     const int row = threadIdx.x % W, g = threadIdx.x / W, D = a.c.D;
     const int64_t size = part_floats(D, W);
-    const float *from = a.part + ((int64_t)head * a.slots + slot) * a.parts * size + row;
+    const float *from = a.part + t.place * size + row;
     for (int p = g; p < used; p += kGroups) {
-        top_of[p][row] = from[p * size + D * W];
-        weight[p][row] = from[p * size + (D + 1) * W];
+        int begin, end;
+        kt.range(p, used, &begin, &end);             // (a part without tiles has left nothing)
+        top_of[p][row] = begin < end ? from[p * size + D * W] : kMinusInf;
+        weight[p][row] = begin < end ? from[p * size + (D + 1) * W] : 0.f;
     }
     __syncthreads();
     float top = kMinusInf, all = 0.f;
@@ -1126,24 +1200,41 @@ __global__ __launch_bounds__(256) void k_cache_join(CacheAttnArgs a) {
     for (int p = g; p < used; p += kGroups) weight[p][row] *= exp2_fast(top_of[p][row] - base) * inv;
     __syncthreads();
     if (t.first + row >= t.rows) return;
-    const int64_t h = head * a.share + (t.first + row) / t.T;
+    const int64_t h = t.head * a.share + (t.first + row) / t.T;
     T *to = static_cast<T *>(a.O) + h * D * a.ldo + t.q0 + (t.first + row) % t.T;
+    // two features of eight parts at a time, so that many loads are on their way whatever the number of parts
     const int each = (D + gridDim.y - 1) / gridDim.y, end = min(D, ((int)blockIdx.y + 1) * each);
-    for (int d = blockIdx.y * each + g; d < end; d += kGroups) {
-        float o = 0.f;
-#pragma unroll 8
-        for (int p = 0; p < used; ++p) {
-            const float w = weight[p][row], v = from[p * size + d * W];
-            o += w == 0.f ? 0.f : w * v;
+    for (int d = blockIdx.y * each + g; d < end; d += 2 * kGroups) {
+        float o[2] = {};
+        for (int p0 = 0; p0 < used; p0 += 8) {
+            float v[8][2];
+#pragma unroll
+            for (int p = 0; p < 8; ++p)
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+                    v[p][i] = from[min(p0 + p, used - 1) * size + min(d + i * kGroups, D - 1) * W];
+#pragma unroll
+            for (int p = 0; p < 8; ++p)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) asm volatile("" : "+v"(v[p][i]));   // (loaded, whatever the weight)
+#pragma unroll
+            for (int p = 0; p < 8; ++p) {
+                const float w = p0 + p < used ? weight[p0 + p][row] : 0.f;
+#pragma unroll
+                for (int i = 0; i < 2; ++i) o[i] += w == 0.f ? 0.f : w * v[p][i];   // (what has no weight may be anything)
+            }
         }
-        to[d * a.ldo] = (T)o;
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            if (d + i * kGroups < end) to[(d + i * kGroups) * a.ldo] = (T)o[i];
     }
 }
 
 // kShared: the waves of a workgroup have rows of their own
 template <typename T, int VT, int NT, bool kShared = false>
 nmg_status run_cache_attention(nmg_cache_format format, const CacheAttnArgs &a, hipStream_t stream) {
-    const int64_t total = (int64_t)a.slots * a.parts * a.c.heads;
+    // as many as there may be: row tiles, and what they are split into
+    const int64_t total = (int64_t)a.slots * a.c.heads + a.target;
     if (total > INT32_MAX / 256) return NMG_ERR_UNSUPPORTED;
     if constexpr (kShared) {
         if (format == NMG_CACHE_INT8)
@@ -1157,7 +1248,7 @@ nmg_status run_cache_attention(nmg_cache_format format, const CacheAttnArgs &a, 
             k_cache_attention<T, VT, NT, false><<<(int)total, 256, 0, stream>>>(a);
     }
     nmg_status st = launched();
-    if (st == NMG_OK && a.parts > 1) {
+    if (st == NMG_OK && a.target > 0) {
         constexpr int W = (kShared ? 64 : 16) * NT;
         // workgroups for every compute unit, as far as a feature for every thread goes
         const int64_t tiles = (int64_t)a.slots * a.c.heads, most = std::max(1, a.c.D * W / 256);

@@ -13,12 +13,12 @@ namespace {
 struct Plan {
     CacheAttnRows rows;
     int64_t slots;       // row tiles of all sequences, at most
-    int64_t parts;
+    int64_t target;      // workgroups that splitting the keys aims at, 0: no splitting
 };
 
-int64_t part_bytes(const CacheAttnArgs &a, const Plan &p, int64_t parts) {
-    return parts > 1 ? 4 * parts * p.slots * a.c.heads * (a.c.D + 2) * p.rows : 0;
-}
+int64_t part_bytes(const CacheAttnArgs &a, const Plan &p) { return 4 * (int64_t)(a.c.D + 2) * p.rows; }
+// Parts' results: a sequence has up to one part more than its share of the target
+int64_t part_count(const CacheAttnArgs &a, const Plan &p) { return p.target + p.slots * a.c.heads; }
 
 Plan plan(nmg_dtype dtype, const CacheAttnArgs &a, int64_t longest) {
     Plan p;
@@ -33,8 +33,9 @@ Plan plan(nmg_dtype dtype, const CacheAttnArgs &a, int64_t longest) {
         p.rows = rows <= 16 || wide ? kRows16 : kRows32;
     p.slots = (int64_t)a.Nq * a.share / p.rows + a.c.sequences;
     const int64_t full = (rows + p.rows - 1) / p.rows * a.c.sequences * a.c.heads;
-    const int64_t tiles = longest / 64 + 1;
-    p.parts = std::max<int64_t>(1, std::min((int64_t)2 * device_cus() / full, std::min<int64_t>(32, tiles / 8)));
+    // two workgroups a compute unit, where the keys give each 8 tiles
+    const int64_t tiles = longest / 64 + 1, most = 2 * device_cus();
+    p.target = 2 * full <= most && tiles >= 16 ? most : 0;
     return p;
 }
 
@@ -42,7 +43,7 @@ Plan plan(nmg_dtype dtype, const CacheAttnArgs &a, int64_t longest) {
 
 int64_t cache_attention_workspace(nmg_dtype dtype, const CacheAttnArgs &a, int64_t longest) {
     const Plan p = plan(dtype, a, longest);
-    return part_bytes(a, p, p.parts);
+    return p.target ? part_bytes(a, p) * part_count(a, p) : 0;
 }
 
 nmg_status launch_cache_attention(nmg_dtype dtype, nmg_cache_format format, CacheAttnArgs a,
@@ -50,10 +51,12 @@ nmg_status launch_cache_attention(nmg_dtype dtype, nmg_cache_format format, Cach
                                   hipStream_t stream) {
     Plan p = plan(dtype, a, longest);
     if (!workspace) workspace_bytes = 0;
-    while (p.parts > 1 && part_bytes(a, p, p.parts) > workspace_bytes) --p.parts;
     if (p.slots * a.c.heads > INT32_MAX / 256) return NMG_ERR_UNSUPPORTED;
+    // less room: fewer parts, none where not every row tile has two
+    a.part_count = std::min(part_count(a, p), workspace_bytes / part_bytes(a, p));
+    p.target = std::min(p.target, a.part_count - p.slots * a.c.heads);
     a.slots = (int32_t)p.slots;
-    a.parts = (int32_t)p.parts;
+    a.target = (int32_t)(p.target >= p.slots * a.c.heads ? p.target : 0);
     a.part = static_cast<float *>(workspace);
     return dtype == NMG_F32 ? cache_attention_f32(format, a, p.rows, stream)
                             : cache_attention_f16(format, a, p.rows, stream);

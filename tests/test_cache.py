@@ -12,8 +12,8 @@ with u = 2^-24 and n keys:
   weights    off by a factor 1 + 2 e_s; sums add n + 32 roundings:
              (4 e_s + (n + 32) u) sum_j p_j |v_j|
   binary16   weights are rounded once for the sums and not for the total: 2^-11
-             sum_j p_j |v_j|, and 2^-40 n max |v| where they are subnormal (the
-             largest is 2^15, a subnormal's half step 2^-25); outputs 2^-11 |y| + 2^-24
+             sum_j p_j |v_j|, and 2^-34 n max |v| where they are subnormal (the
+             largest is 2^9 to 2^15, a subnormal's half step 2^-25); outputs 2^-11 |y| + 2^-24
 """
 import ctypes
 import math
@@ -218,7 +218,7 @@ def attend64(model, layer, Q, heads, q, tree=None, scale=None):
                 out[at, q[b] + t] = p @ vv
                 w = np.where(np.isfinite(vv), np.abs(vv), 0)
                 bound[at, q[b] + t] = (4 * e + (m + 32) * U + half * 2.0 ** -11) * (p @ w) + \
-                    half * 2.0 ** -40 * m * w.max()
+                    half * 2.0 ** -34 * m * w.max()
     return out, bound
 
 

@@ -8,8 +8,9 @@ namespace {
 // ---------------------------------------------------------------- append
 
 // Columns of K and V (features x tokens) to the rings: a workgroup takes 64 columns
-// of 64 features of one key head.  Values stay as they lie, feature after feature; keys are turned
-// through LDS, so that both sides are read and written along their rows.
+// of 64 features of one key head.  Values stay as they lie, feature after feature, four
+// tokens at a time where their slots follow one another; keys are turned through LDS, so that both sides are
+// read and written along their rows.
 template <typename T>
 __global__ __launch_bounds__(kBlock) void k_cache_append(CacheView v, int layer, const int32_t *q_offsets,
                                                          const int32_t *lengths, const T *K, int64_t ldk,
@@ -19,49 +20,92 @@ __global__ __launch_bounds__(kBlock) void k_cache_append(CacheView v, int layer,
     const int n0 = blockIdx.x * 64, d0 = blockIdx.y % ((v.D16 + 63) / 64) * 64,
               head = blockIdx.y / ((v.D16 + 63) / 64);
     const int tid = threadIdx.x;
+    // what is read goes on its way before the places are known
+    constexpr int kRows = kBlock / 16;
+    const int j4 = tid % 16 * 4, left = N - n0 - j4;      // the thread's four columns
+    struct alignas(sizeof(T)) Four { T e[4]; };
+    Four k[64 / kRows], val[64 / kRows];
+#pragma unroll
+    for (int i = 0; i < 64 / kRows; ++i) {
+        const int d = d0 + tid / 16 + i * kRows;
+        const int64_t row = (int64_t)head * v.D + d;
+        k[i] = val[i] = Four{};
+        if (d >= v.D) continue;
+        const T *from_k = K + row * ldk + n0 + j4, *from_v = V + row * ldv + n0 + j4;
+        if (left >= 4) {
+            __builtin_memcpy(&k[i], from_k, sizeof(Four));
+            __builtin_memcpy(&val[i], from_v, sizeof(Four));
+        } else {
+#pragma unroll
+            for (int e = 0; e < 3; ++e)
+                if (e < left) {
+                    k[i].e[e] = from_k[e];
+                    val[i].e[e] = from_v[e];
+                }
+        }
+    }
     if (tid < 64) {
         const int col = n0 + tid;
-        int lo = -1, slot = 0;
-        if (col < N && col >= q_offsets[0] && col < q_offsets[v.sequences]) {
-            lo = 0;
-            int hi = v.sequences - 1;                 // the last b with q_offsets[b] <= col
-            while (lo < hi) {
-                const int mid = (lo + hi + 1) / 2;
+        int b = -1, first = 0, n = 0;
+        if (v.sequences <= 64) {           // a lane looks up a sequence, then all compare
+            const int s = min(tid, v.sequences - 1);
+            const int from = q_offsets[s], to = q_offsets[s + 1], length = cache_length(v, lengths, s);
+            for (int q = 0; q < v.sequences; ++q) {
+                const int lo = __builtin_amdgcn_readlane(from, q), hi = __builtin_amdgcn_readlane(to, q);
+                if (col >= lo && col < hi) {
+                    b = q;
+                    first = lo;
+                    n = __builtin_amdgcn_readlane(length, q);
+                }
+            }
+        } else if (col >= q_offsets[0] && col < q_offsets[v.sequences]) {
+            b = 0;
+            int hi = v.sequences - 1;      // the last b with q_offsets[b] <= col
+            while (b < hi) {
+                const int mid = (b + hi + 1) / 2;
                 if (q_offsets[mid] <= col)
-                    lo = mid;
+                    b = mid;
                 else
                     hi = mid - 1;
             }
-            const int n = cache_length(v, lengths, lo), i = col - q_offsets[lo];
-            if (i < 0 || n % v.block + i >= v.room)
-                lo = -1;                              // past the room
-            else
-                slot = (int)((uint32_t)(n + i) % (uint32_t)v.room);
+            first = q_offsets[b];
+            n = cache_length(v, lengths, b);
         }
-        ring[tid] = lo;
-        at[tid] = slot;
+        const int i = (int)((uint32_t)col - (uint32_t)first);
+        const bool in = b >= 0 && col < N && i >= 0 && i < v.room - n % v.block;   // not past the room
+        ring[tid] = in ? b : -1;
+        at[tid] = in ? (int)((uint32_t)(n + i) % (uint32_t)v.room) : 0;
     }
     __syncthreads();
     const int64_t head_of = (int64_t)layer * v.sequences;
     T *ko = static_cast<T *>(v.k_open), *vo = static_cast<T *>(v.v_open);
-    {
-        const int j = tid % 64;
-        const bool in = ring[j] >= 0;
-        const int64_t r = ((head_of + ring[j]) * v.heads + head);
-        for (int i = tid / 64; i < 64; i += kBlock / 64) {
-            const int d = d0 + i;
-            const int64_t row = (int64_t)head * v.D + d;
-            tile[i][j] = d < v.D && in ? K[row * ldk + n0 + j] : (T)0.f;
-            if (d < v.D && in) vo[(r * v.D + d) * v.room + at[j]] = V[row * ldv + n0 + j];
-        }
+    auto head_ring = [&](int j) { return (head_of + ring[j]) * v.heads + head; };
+    const bool run = ring[j4] >= 0 && ring[j4] == ring[j4 + 3] && at[j4 + 3] == at[j4] + 3;
+#pragma unroll
+    for (int i = 0; i < 64 / kRows; ++i) {
+        const int r = tid / 16 + i * kRows, d = d0 + r;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) tile[r][j4 + e] = k[i].e[e];
+        if (d >= v.D) continue;
+        if (run)
+            __builtin_memcpy(vo + (head_ring(j4) * v.D + d) * v.room + at[j4], &val[i], sizeof(Four));
+        else
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (ring[j4 + e] >= 0) vo[(head_ring(j4 + e) * v.D + d) * v.room + at[j4 + e]] = val[i].e[e];
     }
     __syncthreads();
-    const int d = tid % 64;
+    // 16 bytes of a key's row a thread
+    constexpr int kE = 16 / sizeof(T), kParts = 64 / kE;
+    const int d = tid % kParts * kE;
     if (d0 + d >= v.D16) return;
-    for (int j = tid / 64; j < 64; j += kBlock / 64) {
+    for (int j = tid / kParts; j < 64; j += kBlock / kParts) {
         if (ring[j] < 0) continue;
-        const int64_t r = ((head_of + ring[j]) * v.heads + head);
-        ko[(r * v.room + at[j]) * v.D16 + d0 + d] = tile[d][j];
+        alignas(16) T row[kE];
+#pragma unroll
+        for (int e = 0; e < kE; ++e) row[e] = tile[d + e][j];
+        *reinterpret_cast<uint4 *>(ko + (head_ring(j) * v.room + at[j]) * v.D16 + d0 + d) =
+            *reinterpret_cast<const uint4 *>(row);
     }
 }
 
@@ -155,7 +199,7 @@ __device__ __forceinline__ Commit commit_of(const CacheView &v, const int32_t *l
 // tokens lie anywhere among the drafted ones: the workgroup makes all pages, then moves what stays
 // open to the front, in pieces that are read before they are written.  (The list
 // ascends, so no piece is written over before a later one has been read.)
-template <typename T, bool kInt8>
+template <typename T, bool kInt8, bool kList>
 __global__ __launch_bounds__(kBlock) void k_cache_commit(CacheView v, const int32_t *lengths,
                                                          const int32_t *kept_offsets, const int32_t *kept,
                                                          int n_kept, int32_t *new_lengths) {
@@ -163,50 +207,84 @@ __global__ __launch_bounds__(kBlock) void k_cache_commit(CacheView v, const int3
     __shared__ int slots[128];
     const int b = blockIdx.x, is_v = blockIdx.y & 1, lh = blockIdx.y >> 1;   // layer * heads + head
     const int layer = lh / v.heads, head = lh % v.heads, tid = threadIdx.x;
-    const Commit k = commit_of(v, lengths, kept_offsets, kept != nullptr, n_kept, b);
+    const Commit k = commit_of(v, lengths, kept_offsets, kList, n_kept, b);
     if (blockIdx.y == 0 && blockIdx.z == 0 && tid == 0) new_lengths[b] = k.n + k.more;
     const int full = k.n - k.open;
     const int64_t ring = ((int64_t)layer * v.sequences + b) * v.heads + head;
     const T *open = static_cast<const T *>(is_v ? v.v_open : v.k_open) +
                     ring * v.room * (is_v ? v.D : v.D16);
-    const int first = kept ? max(0, min(kept_offsets[b], n_kept)) : 0;
+    const int first = kList ? max(0, min(kept_offsets[b], n_kept)) : 0;
     // slot of token u of the open list
     auto slot_of = [&](int u) {
         int at = full + u;
-        if (kept && u >= k.open) at = k.n + min(max(kept[first + u - k.open], 0), v.room - 1);
+        if (kList && u >= k.open) at = k.n + min(max(kept[first + u - k.open], 0), v.room - 1);
         return (int)((uint32_t)at % (uint32_t)v.room);
     };
     for (int j = blockIdx.z; j < k.whole; j += gridDim.z) {
-        __syncthreads();
-        if (tid < v.block) slots[tid] = slot_of(j * v.block + tid);
-        __syncthreads();
+        // without a list the block's slots follow one another
+        const int slot0 = slot_of(j * v.block);
+        if constexpr (kList) {
+            __syncthreads();
+            if (tid < v.block) slots[tid] = slot_of(j * v.block + tid);
+            __syncthreads();
+        }
         const int page = v.table[(int64_t)b * v.row + full / v.block + j];
         const int64_t of = ((int64_t)layer * v.pages + page) * v.heads + head;
-        // four neighbours of a row: of a key's features, of a feature's tokens
-        const int width = is_v ? v.block : v.D16, quads = (is_v ? v.D : v.block) * (width / 4);
-        auto four = [&](int i) {
-            const int r = i / (width / 4), e = i % (width / 4) * 4;
-            if (!is_v) return load4(open + (int64_t)slots[r] * v.D16 + e, 4, true);
+        // 16 bytes of neighbours: of a key's features, of a feature's tokens
+        constexpr int kE = 16 / sizeof(T);
+        struct alignas(16) Some { T e[kE]; };
+        const int width = is_v ? v.block : v.D16, units = (is_v ? v.D : v.block) * (width / kE);
+        auto some = [&](int i) {
+            if (!kList && !is_v)
+                return *reinterpret_cast<const Some *>(open + (int64_t)slot0 * v.D16 + i * kE);
+            const int r = i / (width / kE), e = i % (width / kE) * kE;
+            if (!is_v) return *reinterpret_cast<const Some *>(open + (int64_t)slots[r] * v.D16 + e);
             const T *row = open + (int64_t)r * v.room;
-            if (!kept) return load4(row + slots[e], 4, true);
-            return v4f{(float)row[slots[e]], (float)row[slots[e + 1]], (float)row[slots[e + 2]],
-                       (float)row[slots[e + 3]]};
-        };
-        uint32_t top = 0;
-        for (int i = tid; i < quads; i += kBlock) {
-            const v4f x = four(i);
+            if (!kList) return *reinterpret_cast<const Some *>(row + slot0 + e);
+            Some x;
 #pragma unroll
-            for (int m = 0; m < 4; ++m) top = max(top, __float_as_uint(x[m]) & 0x7fffffffu);
+            for (int m = 0; m < kE; ++m) x.e[m] = row[slots[e + m]];
+            return x;
+        };
+        // blocks of up to 16384 values stay in registers between their maximum and their codes
+        constexpr int kKeep = 64 / kE;
+        const bool keep = units <= kKeep * kBlock;
+        Some held[kKeep];
+        uint32_t top = 0;
+        auto look = [&](const Some &x) {
+#pragma unroll
+            for (int m = 0; m < kE; ++m) top = max(top, __float_as_uint((float)x.e[m]) & 0x7fffffffu);
+        };
+        if (keep) {
+            // (a thread past the end looks at the last unit once more)
+#pragma unroll
+            for (int h = 0; h < kKeep; ++h) held[h] = some(min(h * kBlock + tid, units - 1));
+#pragma unroll
+            for (int h = 0; h < kKeep; ++h) look(held[h]);
+        } else {
+            for (int i = tid; i < units; i += kBlock) look(some(i));
         }
         top = workgroup_max(top, most);
         float inverse, limit;
         const float scale = block_scale<T, kInt8>(top, &inverse, &limit);
         uint32_t *to = reinterpret_cast<uint32_t *>((is_v ? v.v_pages + of * v.D * v.block
                                                           : v.k_pages + of * v.block * v.D16));
-        for (int i = tid; i < quads; i += kBlock) to[i] = encode4<kInt8>(four(i), inverse, limit);
+        auto store = [&](int i, const Some &x) {
+#pragma unroll
+            for (int m = 0; m < kE; m += 4)
+                to[(i * kE + m) / 4] = encode4<kInt8>(v4f{(float)x.e[m], (float)x.e[m + 1], (float)x.e[m + 2],
+                                                          (float)x.e[m + 3]}, inverse, limit);
+        };
+        if (keep) {
+#pragma unroll
+            for (int h = 0; h < kKeep; ++h)
+                if (h * kBlock + tid < units) store(h * kBlock + tid, held[h]);
+        } else {
+            for (int i = tid; i < units; i += kBlock) store(i, some(i));
+        }
         if (tid == 0) (is_v ? v.v_scales : v.k_scales)[of] = scale;
     }
-    if (!kept) return;
+    if constexpr (!kList) return;
     T *ring_out = const_cast<T *>(open);
     const int from = max(k.whole * v.block, k.open), end = k.open + k.more;
     const int width = is_v ? v.D : v.D16;
@@ -475,8 +553,11 @@ nmg_status commit(const CacheView &c, const int32_t *lengths, const int32_t *kep
     if (y > 65535) return NMG_ERR_UNSUPPORTED;
     const int z = kept ? 1 : std::min(c.room / c.block, 65535);
     if ((int64_t)c.sequences * kBlock >= ((int64_t)1 << 32)) return NMG_ERR_UNSUPPORTED;
-    k_cache_commit<T, kInt8><<<dim3(c.sequences, (int)y, z), kBlock, 0, stream>>>(
-        c, lengths, kept_offsets, kept, n_kept, new_lengths);
+    const dim3 grid(c.sequences, (int)y, z);
+    if (kept)
+        k_cache_commit<T, kInt8, true><<<grid, kBlock, 0, stream>>>(c, lengths, kept_offsets, kept, n_kept, new_lengths);
+    else
+        k_cache_commit<T, kInt8, false><<<grid, kBlock, 0, stream>>>(c, lengths, kept_offsets, kept, n_kept, new_lengths);
     return launched();
 }
 

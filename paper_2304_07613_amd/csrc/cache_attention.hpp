@@ -625,9 +625,15 @@ __global__ __launch_bounds__(256, (attention_waves<T, VT, NT>())) void k_cache_a
 #pragma unroll
             for (int k = 0; k < KC; ++k) kk[s][k] = buf_load16(from, k_off[k], first + 4 * s * D16);
     };
-    int tile = begin + wave;
-    if (tile < paged_end) {
-        pages.look(a, t, tile, 4, paged_end);
+    // A wave's tiles: open ones from the last wave on, of the pages a run of as many as make the
+    // units of all waves about equal
+    const int opens = end - max(begin, min(kt.paged, end)), paged = max(0, paged_end - begin);
+    const int quota = (paged + 3 * opens + 3) / 4;
+    int tile = begin;
+    for (int w = 0; w < wave; ++w) tile += max(0, quota - 3 * ((opens + w) / 4));
+    const int mine_end = min(paged_end, tile + max(0, quota - 3 * ((opens + wave) / 4)));
+    if (tile < mine_end) {
+        pages.look(a, t, tile, 1, mine_end);
         load_keys(tile, 0);
     }
     // queries: the lane's features 64 k + 16 c + j of row x of every row tile
@@ -675,7 +681,7 @@ __global__ __launch_bounds__(256, (attention_waves<T, VT, NT>())) void k_cache_a
     const float factor = a.scale * kLog2e;
 
     // ---- whole pages
-    for (int at = 0; tile < paged_end; tile += 4, ++at) {
+    for (int at = 0; tile < mine_end; ++tile, ++at) {
         u4 vv[VT];
         const int i64 = at & 63;
         const buf_rsrc_t from = buf_rsrc(v.v_pages + pages.place(i64) * v_bytes, v_bytes);
@@ -686,35 +692,40 @@ __global__ __launch_bounds__(256, (attention_waves<T, VT, NT>())) void k_cache_a
         const float tile_ks = pages.scale(pages.ks, i64), vs = pages.scale(pages.vs, i64);
         const float tile_vs = vs < 0x1p-32f && !kF32 ? 0x1p-32f : vs;
         v4f s[4][NT];
+        // (products that follow one another are of different sums: none waits for the last)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < 4; ++i)
 #pragma unroll
             for (int n = 0; n < NT; ++n) s[i][n] = v4f{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int k = 0; k < KC; ++k) {
-                if constexpr (kF32) {
+        for (int k = 0; k < KC; ++k) {
+            if constexpr (kF32) {
 #pragma unroll
-                    for (int w = 0; w < 4; ++w) {
-                        const v4f f = decode4f<kInt8>(kk[i][k][w]);
+                for (int w = 0; w < 4; ++w) {
+                    v4f f[4];
 #pragma unroll
-                        for (int j = 0; j < 4; ++j)
+                    for (int i = 0; i < 4; ++i) f[i] = decode4f<kInt8>(kk[i][k][w]);
 #pragma unroll
-                            for (int n = 0; n < NT; ++n) s[i][n] = mfma_f32(f[j], q[n][k][4 * w + j], s[i][n]);
-                    }
-                } else {
-                    const h8 f0 = decode8<kInt8>(kk[i][k][0], kk[i][k][1]);
-                    const h8 f1 = decode8<kInt8>(kk[i][k][2], kk[i][k][3]);
+                    for (int j = 0; j < 4; ++j)
 #pragma unroll
-                    for (int n = 0; n < NT; ++n) {
-                        s[i][n] = mfma_f16(f0, q[n][k][0], s[i][n]);
-                        s[i][n] = mfma_f16(f1, q[n][k][1], s[i][n]);
-                    }
+                        for (int i = 0; i < 4; ++i)
+#pragma unroll
+                            for (int n = 0; n < NT; ++n) s[i][n] = mfma_f32(f[i][j], q[n][k][4 * w + j], s[i][n]);
                 }
+            } else {
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const h8 f = decode8<kInt8>(kk[i][k][2 * h], kk[i][k][2 * h + 1]);
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) s[i][n] = mfma_f16(f, q[n][k][h], s[i][n]);
+                    }
             }
         }
-        if (tile + 4 < paged_end) {
-            if (i64 == 63) pages.look(a, t, tile + 4, 4, paged_end);
-            load_keys(tile + 4, (at + 1) & 63);
+        if (tile + 1 < mine_end) {
+            if (i64 == 63) pages.look(a, t, tile + 1, 1, mine_end);
+            load_keys(tile + 1, (at + 1) & 63);
         }
         issued();
         if constexpr (kF32) {
@@ -733,14 +744,23 @@ __global__ __launch_bounds__(256, (attention_waves<T, VT, NT>())) void k_cache_a
         if constexpr (kF32) {
             const float f = tile_vs / r.unit;
 #pragma unroll
-            for (int d = 0; d < VT; ++d)
+            for (int w = 0; w < 4; ++w)
+#pragma unroll
+                for (int n = 0; n < NT; ++n) s[w][n] *= f;
+            // (four features at a time, so that products that follow one another are of different sums)
+#pragma unroll
+            for (int d4 = 0; d4 < VT; d4 += 4)
 #pragma unroll
                 for (int w = 0; w < 4; ++w) {
-                    const v4f g = decode4f<kInt8>(vv[d][w]);
+                    v4f g[4];
+#pragma unroll
+                    for (int d = d4; d < VT && d < d4 + 4; ++d) g[d - d4] = decode4f<kInt8>(vv[d][w]);
 #pragma unroll
                     for (int j = 0; j < 4; ++j)
 #pragma unroll
-                        for (int n = 0; n < NT; ++n) r.o[d][n] = mfma_f32(g[j], s[w][n][j] * f, r.o[d][n]);
+                        for (int d = d4; d < VT && d < d4 + 4; ++d)
+#pragma unroll
+                            for (int n = 0; n < NT; ++n) r.o[d][n] = mfma_f32(g[d - d4][j], s[w][n][j], r.o[d][n]);
                 }
         } else {
             h8 p[NT][2];
@@ -758,7 +778,8 @@ __global__ __launch_bounds__(256, (attention_waves<T, VT, NT>())) void k_cache_a
     }
 
     // ---- open tokens
-    for (; tile < end; tile += 4) {
+    // (a single tile is wave 0's, whose result is the workgroup's)
+    for (tile = max(begin, kt.paged) + (paged ? 3 - wave : wave); tile < end; tile += 4) {
         const int first = 64 * (tile - kt.paged);          // of the open tokens
         const int at_slot = (int)((uint32_t)(t.n - kt.kept + first) % (uint32_t)room);
         const int64_t ring = ((int64_t)a.layer * v.sequences + t.b) * heads + head;
@@ -796,32 +817,35 @@ __global__ __launch_bounds__(256, (attention_waves<T, VT, NT>())) void k_cache_a
             reload();
         }
 #pragma unroll
-        for (int m = 0; m < 4; ++m) {
+        for (int m = 0; m < 4; ++m)
 #pragma unroll
             for (int n = 0; n < NT; ++n) s[m][n] = v4f{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int k = 0; k < KC; ++k) {
+        for (int k = 0; k < KC; ++k)
+#pragma unroll
+            for (int w = 0; w < kWords; ++w) {
+                u4 y[4];
+#pragma unroll
+                for (int m = 0; m < 4; ++m) y[m] = key_word(m, k, w);
                 if constexpr (kF32) {
 #pragma unroll
-                    for (int w = 0; w < 4; ++w) {
-                        const u4 y = key_word(m, k, w);
+                    for (int e = 0; e < 4; ++e)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const float f = __builtin_ldexpf(__uint_as_float(y[e]), -ke);
+                        for (int m = 0; m < 4; ++m) {
+                            const float f = __builtin_ldexpf(__uint_as_float(y[m][e]), -ke);
 #pragma unroll
                             for (int n = 0; n < NT; ++n) s[m][n] = mfma_f32(f, q[n][k][4 * w + e], s[m][n]);
                         }
-                    }
                 } else {
-                    const h8 f0 = __builtin_bit_cast(h8, key_word(m, k, 0));
-                    const h8 f1 = __builtin_bit_cast(h8, key_word(m, k, 1));
 #pragma unroll
-                    for (int n = 0; n < NT; ++n) {
-                        s[m][n] = mfma_f16(f0, q[n][k][0], s[m][n]);
-                        s[m][n] = mfma_f16(f1, q[n][k][1], s[m][n]);
-                    }
+                    for (int m = 0; m < 4; ++m)
+#pragma unroll
+                        for (int n = 0; n < NT; ++n)
+                            s[m][n] = mfma_f16(__builtin_bit_cast(h8, y[m]), q[n][k][w], s[m][n]);
                 }
             }
+#pragma unroll
+        for (int m = 0; m < 4; ++m)
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -830,7 +854,6 @@ __global__ __launch_bounds__(256, (attention_waves<T, VT, NT>())) void k_cache_a
                     if constexpr (kF32) y = __builtin_ldexpf(y * factor, qe[n] + ke);
                     s[m][n][e] = seen[n] >> (4 * m + e) & 1 ? y : kMinusInf;
                 }
-        }
         r.softmax(s, kF32 ? 1.f : factor);
         // values: those behind the open tokens are whatever the ring held, so none are taken
         const int valid = kt.open - first - 16 * c;       // of the lane's 16
@@ -890,15 +913,19 @@ __global__ __launch_bounds__(256, (attention_waves<T, VT, NT>())) void k_cache_a
         } else if constexpr (kF32) {
             const float f = 1.f / r.unit;
 #pragma unroll
-            for (int d = 0; d < VT; ++d)
+            for (int d4 = 0; d4 < VT; d4 += 4)
 #pragma unroll
                 for (int w = 0; w < 4; ++w) {
-                    const u4 y = value_word(d, w);
+                    u4 y[4];
+#pragma unroll
+                    for (int d = d4; d < VT && d < d4 + 4; ++d) y[d - d4] = value_word(d, w);
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
 #pragma unroll
-                        for (int n = 0; n < NT; ++n)
-                            r.o[d][n] = mfma_f32(__uint_as_float(y[e]) * f, s[w][n][e], r.o[d][n]);
+                        for (int d = d4; d < VT && d < d4 + 4; ++d)
+#pragma unroll
+                            for (int n = 0; n < NT; ++n)
+                                r.o[d][n] = mfma_f32(__uint_as_float(y[d - d4][e]) * f, s[w][n][e], r.o[d][n]);
                 }
         } else {
             h8 p[NT][2];

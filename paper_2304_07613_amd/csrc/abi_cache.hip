@@ -26,7 +26,9 @@ nmg_status check_sizes(const nmg_cache *c, CacheView *v) {
     // positions and their slots in 31 bits, rows of heads in 31 bits, grids
     if (((int64_t)c->row + 1) * c->block + c->room > INT32_MAX) return NMG_ERR_UNSUPPORTED;
     if ((int64_t)c->kv_heads * c->head_dim > INT32_MAX) return NMG_ERR_PARAM;
-    if (2 * (int64_t)c->layers * c->kv_heads > 65535) return NMG_ERR_UNSUPPORTED;
+    if (2 * (int64_t)c->layers * c->kv_heads > 65535 ||
+        (int64_t)c->kv_heads * ((c->head_dim + 63) / 64) > 65535)
+        return NMG_ERR_UNSUPPORTED;
     if ((int64_t)c->sequences * kBlock >= ((int64_t)1 << 32)) return NMG_ERR_UNSUPPORTED;
     *v = CacheView{static_cast<uint8_t *>(c->k_pages), static_cast<uint8_t *>(c->v_pages), c->k_scales,
                    c->v_scales, c->k_open, c->v_open, c->table, c->references,

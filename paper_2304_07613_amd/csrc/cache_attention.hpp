@@ -730,14 +730,13 @@ __global__ __launch_bounds__(256, (attention_waves<T, VT, NT>())) void k_cache_a
         issued();
         if constexpr (kF32) {
             const int ke = exponent_of(tile_ks);
-            const float nan = tile_ks - tile_ks;       // of a block that is not finite
+            const float f = factor * __builtin_ldexpf(tile_ks, -ke);
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
 #pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        s[i][n][j] = __builtin_ldexpf(s[i][n][j] * factor, qe[n] + ke) + nan;
+                    for (int j = 0; j < 4; ++j) s[i][n][j] = __builtin_ldexpf(s[i][n][j] * f, qe[n] + ke);
         }
         r.softmax(s, kF32 ? 1.f : factor * tile_ks);
         r.new_unit(tile_vs);

@@ -400,7 +400,7 @@ __device__ __forceinline__ void release_row(const CacheView &v, int32_t *row, in
 
 // Sequence to[i] becomes a copy of from[i]: it shares the pages, which are never written
 // again, and has the open tokens for itself.  blockIdx.y 0: the row; others: 16
-// bytes a thread of the ring's block.
+// bytes a thread and turn of the ring's block.
 template <typename T>
 __global__ __launch_bounds__(kBlock) void k_cache_fork(CacheView v, int32_t *lengths, SlotList list) {
     const int a = list.from[blockIdx.x], b = list.to[blockIdx.x];
@@ -419,29 +419,31 @@ __global__ __launch_bounds__(kBlock) void k_cache_fork(CacheView v, int32_t *len
     }
     constexpr int kE = 16 / sizeof(T);
     const int k_units = v.block * v.D16 / kE, v_units = v.D * v.block / kE;
-    const int64_t unit = (int64_t)(blockIdx.y - 1) * kBlock + threadIdx.x;
-    const int lh = (int)(unit / (k_units + v_units)), at = (int)(unit % (k_units + v_units));
-    if (lh >= v.layers * v.heads) return;
-    const int layer = lh / v.heads, head = lh % v.heads;
     const int start = (int)((uint32_t)(n - open) % (uint32_t)v.room);
-    const int64_t ra = ((int64_t)layer * v.sequences + a) * v.heads + head,
-                  rb = ((int64_t)layer * v.sequences + b) * v.heads + head;
-    if (at < k_units) {
-        if (at >= open * v.D16 / kE) return;
-        T *k = static_cast<T *>(v.k_open);
-        const int64_t e = (int64_t)start * v.D16 + (int64_t)at * kE;
-        *reinterpret_cast<uint4 *>(k + rb * v.room * v.D16 + e) =
-            *reinterpret_cast<const uint4 *>(k + ra * v.room * v.D16 + e);
-    } else {
-        const int d = (at - k_units) / (v.block / kE), u = (at - k_units) % (v.block / kE) * kE;
-        if (u >= open) return;
-        T *values = static_cast<T *>(v.v_open);
-        const T *from = values + (ra * v.D + d) * v.room + start + u;
-        T *to = values + (rb * v.D + d) * v.room + start + u;
-        if (u + kE <= open)
-            *reinterpret_cast<uint4 *>(to) = *reinterpret_cast<const uint4 *>(from);
-        else
-            for (int i = 0; u + i < open; ++i) to[i] = from[i];
+    const int64_t units = (int64_t)v.layers * v.heads * (k_units + v_units);
+    for (int64_t unit = (int64_t)(blockIdx.y - 1) * kBlock + threadIdx.x; unit < units;
+         unit += (int64_t)(gridDim.y - 1) * kBlock) {
+        const int lh = (int)(unit / (k_units + v_units)), at = (int)(unit % (k_units + v_units));
+        const int layer = lh / v.heads, head = lh % v.heads;
+        const int64_t ra = ((int64_t)layer * v.sequences + a) * v.heads + head,
+                      rb = ((int64_t)layer * v.sequences + b) * v.heads + head;
+        if (at < k_units) {
+            if (at >= open * v.D16 / kE) continue;
+            T *k = static_cast<T *>(v.k_open);
+            const int64_t e = (int64_t)start * v.D16 + (int64_t)at * kE;
+            *reinterpret_cast<uint4 *>(k + rb * v.room * v.D16 + e) =
+                *reinterpret_cast<const uint4 *>(k + ra * v.room * v.D16 + e);
+        } else {
+            const int d = (at - k_units) / (v.block / kE), u = (at - k_units) % (v.block / kE) * kE;
+            if (u >= open) continue;
+            T *values = static_cast<T *>(v.v_open);
+            const T *from = values + (ra * v.D + d) * v.room + start + u;
+            T *to = values + (rb * v.D + d) * v.room + start + u;
+            if (u + kE <= open)
+                *reinterpret_cast<uint4 *>(to) = *reinterpret_cast<const uint4 *>(from);
+            else
+                for (int i = 0; u + i < open; ++i) to[i] = from[i];
+        }
     }
 }
 
@@ -540,7 +542,6 @@ template <typename T>
 nmg_status append(const CacheView &c, int32_t layer, const int32_t *q_offsets, const int32_t *lengths,
                   const void *K, int64_t ldk, const void *V, int64_t ldv, int32_t N, hipStream_t stream) {
     const int64_t y = (int64_t)c.heads * ((c.D16 + 63) / 64);
-    if (y > 65535) return NMG_ERR_UNSUPPORTED;
     k_cache_append<T><<<dim3((N + 63) / 64, (int)y), kBlock, 0, stream>>>(
         c, layer, q_offsets, lengths, static_cast<const T *>(K), ldk, static_cast<const T *>(V), ldv, N);
     return launched();
@@ -550,9 +551,7 @@ template <typename T, bool kInt8>
 nmg_status commit(const CacheView &c, const int32_t *lengths, const int32_t *kept_offsets,
                   const int32_t *kept, int32_t n_kept, int32_t *new_lengths, hipStream_t stream) {
     const int64_t y = 2 * (int64_t)c.layers * c.heads;
-    if (y > 65535) return NMG_ERR_UNSUPPORTED;
     const int z = kept ? 1 : std::min(c.room / c.block, 65535);
-    if ((int64_t)c.sequences * kBlock >= ((int64_t)1 << 32)) return NMG_ERR_UNSUPPORTED;
     const dim3 grid(c.sequences, (int)y, z);
     if (kept)
         k_cache_commit<T, kInt8, true><<<grid, kBlock, 0, stream>>>(c, lengths, kept_offsets, kept, n_kept, new_lengths);
@@ -565,8 +564,7 @@ template <typename T>
 nmg_status fork(const CacheView &c, int32_t *lengths, const SlotList &list, int32_t count, hipStream_t stream) {
     constexpr int kE = 16 / sizeof(T);
     const int64_t units = (int64_t)c.layers * c.heads * (c.block * c.D16 / kE + c.D * c.block / kE);
-    const int64_t y = 1 + (units + kBlock - 1) / kBlock;
-    if (y > 65535) return NMG_ERR_UNSUPPORTED;
+    const int64_t y = std::min<int64_t>(1 + (units + kBlock - 1) / kBlock, 65535);
     k_cache_fork<T><<<dim3(count, (int)y), kBlock, 0, stream>>>(c, lengths, list);
     return launched();
 }

@@ -291,12 +291,11 @@ class Both:
             got = getattr(c, name).float().cpu().numpy().astype(np.float64)
             assert np.array_equal(got, ref, equal_nan=True), name
         room, block = m.shape[6], m.shape[7]
+        k, v = (t.cpu().numpy() for t in (c.k_open, c.v_open))
         for b in range(m.shape[3]):
             slots = [p % room for p in range(m.n[b] // block * block, m.n[b])]
-            assert np.array_equal(c.k_open.cpu().numpy()[:, b][:, :, slots].astype(np.float64),
-                                  m.ko[:, b][:, :, slots], equal_nan=True)
-            assert np.array_equal(c.v_open.cpu().numpy()[:, b][..., slots].astype(np.float64),
-                                  m.vo[:, b][..., slots], equal_nan=True)
+            assert np.array_equal(k[:, b][:, :, slots].astype(np.float64), m.ko[:, b][:, :, slots], equal_nan=True)
+            assert np.array_equal(v[:, b][..., slots].astype(np.float64), m.vo[:, b][..., slots], equal_nan=True)
 
     def attend(self, heads, q, tree=None, layer=0, longest=None, scale=None, sharp=1.5, Q=None, out=None):
         D = self.model.shape[2]
@@ -579,6 +578,34 @@ def test_attention_over_long_caches(dev, fmt, dtype):
             print(fmt, dtype, counts, longest, flush=True)
             b.attend(4, q, longest=longest)
             b.attend(4, q, random_tree(3, counts), longest=longest)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
+@pytest.mark.parametrize("sequences", [64, 65, 200, 4500])
+def test_many_sequences(dev, sequences, dtype):
+    """Few with a draft among many, some of them long; the splits aim at more workgroups than
+    there are row tiles, or not."""
+    rng = np.random.default_rng(sequences)
+    b = Both(dev, 1, 1, 16, sequences, 60 + sequences // 64, 40, 256, 64, "int8", dtype)
+    grown = [0] * sequences
+    for s in rng.permutation(sequences)[:20]:
+        grown[s] = int(rng.integers(1, 100))
+    grown[3] = 1500
+    b.grow(grown)
+    for most in (1, 100):
+        counts = [0] * sequences
+        for s in rng.permutation(sequences)[:12]:
+            counts[s] = int(rng.integers(1, most + 1))
+        counts[3] = most
+        print(sequences, dtype, counts[:20], flush=True)
+        q = b.draft(counts)
+        b.attend(2, q)
+        b.attend(2, q, random_tree(1, counts), longest=1500)
+        kept = [list(range(0, n, 2)) for n in counts]
+        b.reserve([len(k) for k in kept])
+        b.keep(kept)
+        b.same()
 
 
 @gpu
@@ -951,7 +978,7 @@ def struct(**change):
 SIZES = [dict(layers=0), dict(kv_heads=0), dict(head_dim=0), dict(pages=0), dict(sequences=0), dict(row=0),
          dict(room=0), dict(room=96), dict(format=2), dict(format=-1)]
 UNSUPPORTED = [dict(head_dim=257), dict(block=32), dict(block=0), dict(block=-64), dict(row=1 << 25),
-               dict(layers=40000), dict(sequences=1 << 24)]
+               dict(layers=40000), dict(kv_heads=32767, head_dim=256), dict(sequences=1 << 24)]
 
 
 def calls(c):

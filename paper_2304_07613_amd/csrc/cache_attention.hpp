@@ -794,27 +794,9 @@ __global__ __launch_bounds__(256, (attention_waves<T, VT, NT>())) void k_cache_a
             const uint32_t at = k_off[k] == past ? past : k_off[k] * (uint32_t)sizeof(T);
             return buf_load16(key_tile, at, (4 * m * D16 + w * (16 / kWords)) * sizeof(T));
         };
-        int ke = 0;
-        if constexpr (kF32) {
-            // the tile's keys are scaled like codes, by its largest finite value
-            uint32_t top = 0;
-#pragma unroll KC == 1 ? 4 : KC == 2 ? 2 : 1
-            for (int m = 0; m < 4; ++m)
-#pragma unroll
-                for (int k = 0; k < KC; ++k)
-#pragma unroll
-                    for (int w = 0; w < 4; ++w) {
-                        const u4 y = key_word(m, k, w);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const uint32_t b = y[e] & 0x7fffffffu;
-                            top = b < 0x7f800000u && b > top ? b : top;
-                        }
-                    }
-            for (int d = 1; d < 64; d *= 2) top = max(top, (uint32_t)__shfl_xor((int)top, d));
-            ke = exponent_of(__uint_as_float(top));
-            reload();
-        }
+        // binary32 keys are scaled by 2^-10: 256 products with queries below 2 then stay in the
+        // range, and only keys below 2^-116 lose bits
+        constexpr int ke = kF32 ? 10 : 0;
 #pragma unroll
         for (int m = 0; m < 4; ++m)
 #pragma unroll
@@ -831,7 +813,7 @@ __global__ __launch_bounds__(256, (attention_waves<T, VT, NT>())) void k_cache_a
                     for (int e = 0; e < 4; ++e)
 #pragma unroll
                         for (int m = 0; m < 4; ++m) {
-                            const float f = __builtin_ldexpf(__uint_as_float(y[m][e]), -ke);
+                            const float f = __uint_as_float(y[m][e]) * 0x1p-10f;
 #pragma unroll
                             for (int n = 0; n < NT; ++n) s[m][n] = mfma_f32(f, q[n][k][4 * w + e], s[m][n]);
                         }

@@ -7,6 +7,14 @@
 // tile's part of a row is one run; the sums of a token go over lanes, then over
 // waves through LDS.  Rows may start on any element: the loads of kVec tokens do not
 // ask for more.
+//
+// 768 x 8: 7.5 us, one workgroup's chain of loads, two sums and stores.  768 x 4096
+// (residual, LayerNorm, 25 MB): 11.7 us, 256 workgroups, one a compute unit, so that a
+// chain stands beside no other.  Binary32 4096 x 4095, norms on both sides, gate and residual
+// (335 MB): 127 us, 2.6 TB/s: 8 tokens are all that fit the registers, 32 bytes a row, and
+// one workgroup a compute unit holds them, so reading, summing and writing alternate.
+// Measured there: 16 tokens of 1024 threads 227 us and of 512 threads with 128 values each
+// 156, 4 tokens 238 (runs of 16 bytes), two workgroups of 128 registers 170 to 207 (spills).
 #include "norm.hpp"
 
 namespace {

@@ -702,8 +702,9 @@ nmg_status nmg_cache_append(const nmg_cache *cache, int32_t layer, const int32_t
  * value changes times, not what is computed.  workspace (may be NULL; 256-byte
  * aligned): lets few queries over many keys be split over the GPU.  Too little of
  * it: fewer parts, one with 0.  The parts, and with them the order of sums, depend
- * on the sizes, `longest` and workspace_bytes alone.  nmg_cache_attention_workspace_bytes: the most a
- * call uses (pure host code; -1 for invalid arguments). */
+ * on the sizes, q_offsets, lengths, `longest` and workspace_bytes alone.
+ * nmg_cache_attention_workspace_bytes: the most a call uses (pure host code; -1 for
+ * invalid arguments). */
 nmg_status nmg_cache_attention(const nmg_cache *cache, int32_t layer, int32_t heads,
                                const int32_t *q_offsets, const int32_t *lengths, const void *Q,
                                int64_t ldq, int64_t Nq, const uint8_t *tree, int64_t ldtree,

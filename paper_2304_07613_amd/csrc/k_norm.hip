@@ -14,7 +14,8 @@
 // (335 MB): 127 us, 2.6 TB/s: 8 tokens are all that fit the registers, 32 bytes a row, and
 // one workgroup a compute unit holds them, so reading, summing and writing alternate.
 // Measured there: 16 tokens of 1024 threads 227 us and of 512 threads with 128 values each
-// 156, 4 tokens 238 (runs of 16 bytes), two workgroups of 128 registers 170 to 207 (spills).
+// 156, 4 tokens 238 (runs of 16 bytes), two workgroups of 128 registers 170 to 207 (spills),
+// half of the values in LDS 136.  Rows of 4128 values in place of 4096 take 109 us.
 #include "norm.hpp"
 
 namespace {
@@ -172,9 +173,10 @@ __device__ __forceinline__ void normed(float (&x)[kPer][kVec], const nmg_norm &n
 template <typename T, int kVec, int kPer, bool kWhole>
 __device__ __forceinline__ void residual_norm(const NormArgs &a, int tile, float *lds) {
     using P = Pack<T, kVec>;
-    // the gate, the residual and the weights are asked for with A where the registers
-    // hold them beside it
-    constexpr bool kEarly = kPer * kVec * (int)sizeof(T) <= 128, kWeights = kPer <= 4;
+    // The gate and the residual are asked for with A where they are 64 bytes a thread at most:
+    // more of them beside A cost registers that the loads of A lack (binary16 768 x 32768 101 us
+    // with a limit of 128 bytes, 82 with 64).
+    constexpr bool kEarly = kPer * kVec * (int)sizeof(T) <= 64, kWeights = kEarly && kPer <= 4;
     constexpr int kE = kEarly ? kPer : 1, kW = kWeights ? kPer : 1;
     const int lanes = a.lanes, step = kThreads / lanes, r0 = threadIdx.x / lanes;
     const int64_t n = (int64_t)tile * lanes * kVec + threadIdx.x % lanes * kVec;

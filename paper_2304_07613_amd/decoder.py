@@ -91,6 +91,9 @@ class SparseDecoder:
         self.branch_scale, self.max_draft, self.cache = branch_scale, max_draft, None
         if any(layer.before for layer in layers) != all(layer.before for layer in layers):
             raise ValueError("norms around the blocks of every layer or of none")
+        for layer in layers:
+            if (layer.before and set(layer.before) != set(BLOCKS)) or not set(layer.after) <= set(layer.before):
+                raise ValueError("a layer's norms are before every block or none, and after those alone")
         device = layers[0].packed["qkv"][0].device
         self.table = nmg.rotary_table(capacity, shape.head_dim, base, device=device, **scaling)
         rows = shape.kv_heads * shape.head_dim
@@ -279,18 +282,21 @@ class SparseDecoder:
         return self.cache
 
     def fork(self, sources: list, targets: list):
-        """Sequences `targets` go on as copies of `sources`; the last draft is gone."""
+        """Sequences `targets` go on as copies of `sources`, attending to the same encoder
+        columns; a target's last draft is gone, and a source's stays the source's alone."""
         nmg.cache_fork(self._paged(), self.lengths, sources, targets)
         for a, b in zip(sources, targets):
-            self.kept[b] = self.kept[a]
-        self.draft = [[] for _ in self.draft]
+            self.kept[b], self.draft[b] = self.kept[a], []
+        if self.encoder_begin is not None and len(targets):
+            to, of = (torch.tensor(v, device=self.begin.device) for v in (targets, sources))
+            self.encoder_begin, self.encoder_end = (
+                t.index_copy(0, to, t.index_select(0, of)) for t in (self.encoder_begin, self.encoder_end))
 
     def free(self, sequences: list):
-        """These sequences have no tokens any more, their pages are free; the last draft is gone."""
+        """These sequences have no tokens and no draft any more, their pages are free."""
         nmg.cache_free(self._paged(), self.lengths, sequences)
         for b in sequences:
-            self.kept[b] = 0
-        self.draft = [[] for _ in self.draft]
+            self.kept[b], self.draft[b] = 0, []
 
     def compact(self) -> int:
         """The pages in use move to the front of the pool: their number."""

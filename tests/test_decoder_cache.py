@@ -84,6 +84,7 @@ def test_drafts_over_pages(fmt, block, block_norms, dtype):
         for cache in (layer.keys, layer.values):
             cache[:, 2 * 300:3 * 300] = cache[:, :300]
     plain.lengths[2], plain.kept[2] = plain.lengths[0], plain.kept[0]
+    plain.encoder_begin, plain.encoder_end = i32(0, 30, 0), i32(30, 50, 30)     # and its encoder's columns
     step(chains([2, 2, 2]), [[0], [0, 1], [0, 1]])
     paged.free([0])
     plain.lengths[0], plain.kept[0] = 0, 0
@@ -109,6 +110,31 @@ def test_a_pool_that_runs_out():
     assert dec.kept == [71, 0] and dec.lengths.tolist() == [71, 0]
 
 
+def test_fork_and_free_leave_other_drafts():
+    """What an exhausted pool's error asks for: free a sequence, accept the draft again."""
+    make = lambda pages: SparseDecoder.random(shape_of(torch.float16), 1, sequences=3, capacity=200,  # noqa: E731
+                                              cache="e4m3", pages=pages)
+    few, many = make(1), make(9)
+    g = torch.Generator().manual_seed(8)
+    xs = [torch.randn(128, n, generator=g).half().to(DEV) for n in (150, 30, 2)]
+    for dec in (few, many):
+        dec.step(xs[0], chains([60, 60, 30]))
+        dec.accept([list(range(60)), list(range(60)), list(range(30))])
+        dec.step(xs[1], chains([10, 10, 10]))
+    with pytest.raises(RuntimeError):
+        few.accept([list(range(10))] * 2 + [[0]])
+    for dec in (few, many):
+        dec.free([0])
+        dec.fork([1], [2])
+        for path in ([[0], [], []], [[], [], [0]]):     # the drafts of a freed sequence and of a target are gone
+            with pytest.raises(ValueError):
+                dec.accept(path)
+        dec.accept([[], list(range(10)), []])
+        assert dec.kept == dec.lengths.tolist() == [0, 70, 60]
+    a, b = (dec.step(xs[2], chains([0, 1, 1])) for dec in (few, many))
+    assert torch.equal(a, b)
+
+
 def test_refusals():
     dec = SparseDecoder.random(shape_of(torch.float16), 1, sequences=2, capacity=200)
     for call in (lambda: dec.fork([0], [1]), lambda: dec.free([0]), dec.compact):
@@ -125,6 +151,14 @@ def test_refusals():
     dec.layers.append(SparseDecoder.random(shape_of(torch.float16), 1, 2, 200, block_norms="rms").layers[0])
     with pytest.raises(ValueError):
         SparseDecoder(dec.shape, dec.layers, 2, 200)
+    for name in BLOCKS:                                                      # some blocks without
+        layers = SparseDecoder.random(shape_of(torch.float16), 1, 2, 200, block_norms="rms").layers
+        del layers[0].before[name]
+        with pytest.raises(ValueError):
+            SparseDecoder(dec.shape, layers, 2, 200)
+    layers[0].before.clear()                                                 # norms after alone
+    with pytest.raises(ValueError):
+        SparseDecoder(dec.shape, layers, 2, 200)
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.float16])

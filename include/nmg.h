@@ -653,7 +653,7 @@ typedef enum nmg_cache_format {
  * aligned.  dim16 is head_dim rounded up to 16 (a key's row; the values behind
  * head_dim are zeros, written by the library).  NMG_ERR_UNSUPPORTED: head_dim > 256, another
  * block than 64 or 128, layers * kv_heads > 32767, kv_heads * ceil(head_dim / 64) >
- * 65535, (row + 1) block + room past 31 bits, or 2^24 sequences or more. */
+ * 65535, (row + 1) block + room or sequences * row past 31 bits, or 2^24 sequences or more. */
 typedef struct nmg_cache {
     int32_t layers, kv_heads, head_dim;
     nmg_dtype dtype;         /* of open tokens, and of the matrices that meet the cache */

@@ -30,6 +30,8 @@ nmg_status check_sizes(const nmg_cache *c, CacheView *v) {
         (int64_t)c->kv_heads * ((c->head_dim + 63) / 64) > 65535)
         return NMG_ERR_UNSUPPORTED;
     if ((int64_t)c->sequences * kBlock >= ((int64_t)1 << 32)) return NMG_ERR_UNSUPPORTED;
+    // pages that sequences ask for are counted in 31 bits
+    if ((int64_t)c->sequences * c->row > INT32_MAX) return NMG_ERR_UNSUPPORTED;
     *v = CacheView{static_cast<uint8_t *>(c->k_pages), static_cast<uint8_t *>(c->v_pages), c->k_scales,
                    c->v_scales, c->k_open, c->v_open, c->table, c->references,
                    c->layers, c->kv_heads, c->head_dim, (c->head_dim + 15) / 16 * 16,

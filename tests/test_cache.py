@@ -978,7 +978,8 @@ def struct(**change):
 SIZES = [dict(layers=0), dict(kv_heads=0), dict(head_dim=0), dict(pages=0), dict(sequences=0), dict(row=0),
          dict(room=0), dict(room=96), dict(format=2), dict(format=-1)]
 UNSUPPORTED = [dict(head_dim=257), dict(block=32), dict(block=0), dict(block=-64), dict(row=1 << 25),
-               dict(layers=40000), dict(kv_heads=32767, head_dim=256), dict(sequences=1 << 24)]
+               dict(layers=40000), dict(kv_heads=32767, head_dim=256), dict(sequences=1 << 24),
+               dict(sequences=1 << 20, row=1 << 12)]
 
 
 def calls(c):

@@ -292,9 +292,19 @@ __device__ __forceinline__ uint32_t seen_of(const CacheAttnArgs &a, const RowTil
 
 // ------------------------------------------------------------------ results
 
+// A factor that only underflowed is not 0: infinities and NaN of sums stay what they are however
+// far below the others their scores lie (what it leaves of finite sums is nothing to the others)
+__device__ __forceinline__ float not_zero(float f) { return f == 0.f ? 0x1p-149f : f; }
+// The root of 2^(m - top), m <= top.  Sums are multiplied by it twice: binary32 values times a
+// weight of 2^-140 may still be more than others.
+__device__ __forceinline__ float root_weight(float m, float top) {
+    return not_zero(exp2_fast(0.5f * (m - top)));
+}
+
 // A wave's result of 16 NT rows: sums o (features x rows as the matrix instructions
-// leave them), divided by the totals; maxima m and totals l per row
-template <int VT, int NT>
+// leave them), divided by the totals; maxima m and totals l per row.  A row without weight
+// (l = 0) has 0 or, of a weight 0 times infinity, NaN.
+template <bool kF32, int VT, int NT>
 struct Result {
     v4f o[VT][NT];
     float m[NT], l[NT];
@@ -303,16 +313,16 @@ struct Result {
     template <typename F>
     __device__ __forceinline__ void join(int n, float m2, float l2, F &&get) {
         const float top = fmaxf(m[n], m2), base = top == kMinusInf ? 0.f : top;
-        const float w1 = l[n] * exp2_fast(m[n] - base), w2 = l2 * exp2_fast(m2 - base);
+        // binary32: roots h, and t what is left of the factors
+        const float h1 = kF32 ? root_weight(m[n], base) : 1.f, h2 = kF32 ? root_weight(m2, base) : 1.f;
+        const float w1 = l[n] * (kF32 ? h1 * h1 : exp2_fast(m[n] - base)), w2 = l2 * (kF32 ? h2 * h2 : exp2_fast(m2 - base));
         const float all = w1 + w2, inv = all == 0.f ? 0.f : 1.f / all;
-        const float f1 = w1 * inv, f2 = w2 * inv;
-        // (a side without weight adds nothing, whatever it holds)
+        const float t1 = not_zero(kF32 ? l[n] * inv * h1 : w1 * inv), t2 = not_zero(kF32 ? l2 * inv * h2 : w2 * inv);
 #pragma unroll
         for (int d = 0; d < VT; ++d) {
             const v4f other = get(d, n);
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                o[d][n][i] = (f1 == 0.f ? 0.f : o[d][n][i] * f1) + (f2 == 0.f ? 0.f : other[i] * f2);
+            for (int i = 0; i < 4; ++i) o[d][n][i] = o[d][n][i] * h1 * t1 + other[i] * h2 * t2;
         }
         m[n] = top;
         l[n] = all;
@@ -320,8 +330,8 @@ struct Result {
 };
 
 // The four waves' results joined in wave 0, through LDS: two at a time
-template <int VT, int NT>
-__device__ __forceinline__ void join_waves(Result<VT, NT> &r, float *lds) {
+template <bool kF32, int VT, int NT>
+__device__ __forceinline__ void join_waves(Result<kF32, VT, NT> &r, float *lds) {
     constexpr int kO = VT * NT * 256, kWave = kO + NT * 128;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     auto put = [&](float *to) {
@@ -349,16 +359,17 @@ __device__ __forceinline__ void join_waves(Result<VT, NT> &r, float *lds) {
     __syncthreads();
     if (wave == 0) take(lds);
 }
+constexpr int kScores = 68;        // floats of a row of scores in LDS: 64, rows four banks apart
 template <int VT, int NT>
-constexpr int join_floats() { return std::max(2 * (VT * NT * 256 + NT * 128), 4 * 1024); }
+constexpr int join_floats() { return std::max(2 * (VT * NT * 256 + NT * 128), 4 * NT * 16 * kScores); }
 
 // Floats of one part's result: a row of sums for every feature, then maxima, then totals
 __host__ __device__ inline int64_t part_floats(int D, int rows) { return (int64_t)(D + 2) * rows; }
 
 // kRows: of the row tile, of which `at` and what follows are the wave's
-template <typename T, int kRows, int VT, int NT>
+template <typename T, int kRows, bool kF32, int VT, int NT>
 __device__ __forceinline__ void store_result(const CacheAttnArgs &a, const RowTile &t, int at,
-                                             const Result<VT, NT> &r) {
+                                             const Result<kF32, VT, NT> &r) {
     const int lane = threadIdx.x & 63, x = lane % 16, c = lane / 16, D = a.c.D;
     if (t.parts > 1) {
         float *to = a.part + (t.place + t.part) * part_floats(D, kRows);
@@ -388,7 +399,8 @@ __device__ __forceinline__ void store_result(const CacheAttnArgs &a, const RowTi
         for (int d = 0; d < VT; ++d)
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-                if (16 * d + 4 * c + i < D) to[(16 * d + 4 * c + i) * a.ldo] = (T)r.o[d][n][i];
+                if (16 * d + 4 * c + i < D)
+                    to[(16 * d + 4 * c + i) * a.ldo] = r.l[n] == 0.f ? (T)0.f : (T)r.o[d][n][i];
     }
 }
 
@@ -483,11 +495,13 @@ struct Pass {
         if (__any(up)) {
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
-                const float g = top[n] > m[n] ? exp2_fast(m[n] - top[n]) : 1.f;
+                const bool grows = top[n] > m[n];
+                const float h = kF32 && grows ? root_weight(m[n], top[n]) : 1.f;
+                const float g = kF32 ? h * h : grows ? not_zero(exp2_fast(m[n] - top[n])) : 1.f;
                 m[n] = fmaxf(m[n], top[n]);
                 total[n] *= g;
 #pragma unroll
-                for (int d = 0; d < VT; ++d) o[d][n] *= g;
+                for (int d = 0; d < VT; ++d) o[d][n] = kF32 ? o[d][n] * h * h : o[d][n] * g;
             }
         }
 #pragma unroll
@@ -498,11 +512,15 @@ struct Pass {
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    s[i][n][j] = exp2_fast(__builtin_fmaf(s[i][n][j], f, -base));
-                    if constexpr (kF32) total[n][0] += s[i][n][j];
-                }
+                for (int j = 0; j < 4; ++j) s[i][n][j] = exp2_fast(__builtin_fmaf(s[i][n][j], f, -base));
         }
+    }
+    // binary32: the lane's weights into the total
+    __device__ __forceinline__ void count(const v4f (&s)[4][NT]) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) total[n][0] += s[i / 4][n][i % 4];
     }
     // binary16: the lane's 16 weights as the matrix instructions take them, and their total
     __device__ __forceinline__ void weights(const v4f (&s)[4][NT], h8 (&p)[NT][2]) {
@@ -516,7 +534,7 @@ struct Pass {
         }
     }
     // the sums over their totals
-    __device__ __forceinline__ void finish(Result<VT, NT> &r) {
+    __device__ __forceinline__ void finish(Result<kF32, VT, NT> &r) {
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
             r.m[n] = m[n];
@@ -530,34 +548,55 @@ struct Pass {
     }
 };
 
-// Sums over a tile of open tokens some of whose values are not finite: every row takes the
-// values that it sees and no others, one by one: weights (-1: not seen) through the wave's
-// 4 KB of LDS.  `count`: the tile's tokens.
-template <typename T, bool kF32, int VT, int NT>
-__device__ __forceinline__ void odd_sums(Pass<kF32, VT, NT> &r, const v4f (&s)[4][NT], const uint32_t (&seen)[NT],
-                                         float *lds, const T *values, int D, int room, int count) {
+// Open values as the matrix instructions take them, without those that are not finite
+template <bool kF32>
+__device__ __forceinline__ u4 finite_word(u4 y) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        if constexpr (kF32) {
+            if ((y[e] & 0x7f800000u) == 0x7f800000u) y[e] = 0;
+        } else {
+            if ((y[e] & 0x7c00u) == 0x7c00u) y[e] &= 0xffff0000u;
+            if ((y[e] & 0x7c000000u) == 0x7c000000u) y[e] &= 0xffffu;
+        }
+    }
+    return y;
+}
+// Those that are not finite, one by one, to the sums of the 16 rows that see them: `scores` are the rows'
+// in LDS (NaN: not seen, or its row is NaN already), `stride` a row.  Their weights are no 0, however
+// small, but where the score is minus infinity; word(d, w): the tile's values.
+template <bool kF32, int VT, int NT, typename F>
+__device__ __forceinline__ void odd_values(v4f (&o)[VT][NT], int n, const float *scores, int stride, F &&word) {
     const int lane = threadIdx.x & 63, x = lane % 16, c = lane / 16;
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        wave_sync();
-#pragma unroll
-        for (int e = 0; e < 16; ++e)
-            lds[(16 * c + e) * 16 + x] = seen[n] >> e & 1 ? s[e / 4][n][e % 4] : -1.f;
-        wave_sync();
-#pragma unroll
-        for (int d = 0; d < VT; ++d)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                int f = 16 * d + 4 * c + e;
-                asm volatile("" : "+v"(f));      // (its address is not kept for the next n)
-                float o = r.o[d][n][e];
+    constexpr int kWords = kF32 ? 4 : 2, kPer = 16 / kWords;
 #pragma unroll 1
-                for (int key = 0; key < 64 && key < count; ++key) {
-                    const float p = lds[key * 16 + x];
-                    if (f < D && p != -1.f) o += p * ((float)values[(int64_t)f * room + key] / r.unit);
-                }
-                r.o[d][n][e] = o;
+    for (int dw = 0; dw < VT * kWords; ++dw) {
+        const u4 y = word(dw / kWords, dw % kWords);
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) {
+            float v;
+            if constexpr (kF32) {
+                const uint32_t bits = y[e];      // (a vector's element is no object of its own)
+                v = __uint_as_float(bits);
+            } else {
+                const uint16_t bits = (uint16_t)(y[e / 2] >> (16 * (e % 2)));
+                v = (float)__builtin_bit_cast(_Float16, bits);
             }
+            uint64_t left = __ballot(!(fabsf(v) < __builtin_inff()));
+            while (left) {
+                const int l = __ffsll((unsigned long long)left) - 1;
+                left &= left - 1;
+                const float value = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), l));
+                const float score = scores[x * stride + 16 * (l / 16) + kPer * (dw % kWords) + e];
+                const float term = score == kMinusInf ? 0.f * value : value;
+                const int mine = score == score ? 16 * (dw / kWords) + l % 16 - 4 * c : -1;
+#pragma unroll
+                for (int d = 0; d < VT; ++d)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (mine == 16 * d + i) o[d][n][i] += term;
+            }
+        }
     }
 }
 
@@ -754,6 +793,7 @@ __global__ __launch_bounds__(256, (attention_waves<T, VT, NT>())) void k_cache_a
                     for (int j = 0; j < 4; ++j) s[i][n][j] = __builtin_ldexpf(s[i][n][j] * f, qe[n] + ke);
         }
         r.softmax(s, kF32 ? 1.f : factor * tile_ks);
+        if constexpr (kF32) r.count(s);
         r.new_unit(tile_vs);
         if constexpr (kF32) {
             const float f = tile_vs / r.unit;
@@ -803,7 +843,6 @@ __global__ __launch_bounds__(256, (attention_waves<T, VT, NT>())) void k_cache_a
         uint32_t seen[NT];
 #pragma unroll
         for (int n = 0; n < NT; ++n) seen[n] = seen_of(a, t, kt, token[n], first + 16 * c);
-        v4f s[4][NT];
         const buf_rsrc_t key_tile = buf_rsrc(kf, 64 * D16 * sizeof(T));
         auto key_word = [&](int m, int k, int w) {
             const uint32_t at = k_off[k] == past ? past : k_off[k] * (uint32_t)sizeof(T);
@@ -812,6 +851,25 @@ __global__ __launch_bounds__(256, (attention_waves<T, VT, NT>())) void k_cache_a
         // binary32 keys are scaled by 2^-10: 256 products with queries below 2 then stay in the
         // range, and only keys below 2^-116 lose bits
         constexpr int ke = kF32 ? 10 : 0;
+        // values: those behind the open tokens are whatever the ring held, so none are taken
+        const int valid = kt.open - first - 16 * c;       // of the lane's 16
+        auto value_word = [&](int d, int w) {
+            u4 y = 16 * d + x < D && valid > w * (16 / kWords)
+                       ? *reinterpret_cast<const u4 *>(vf + (int64_t)(16 * d + x) * room + 16 * c +
+                                                       w * (16 / kWords))
+                       : u4{0, 0, 0, 0};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                if constexpr (kF32) {
+                    if (4 * w + e >= valid) y[e] = 0;
+                } else {
+                    if (8 * w + 2 * e >= valid) y[e] = 0;
+                    if (8 * w + 2 * e + 1 >= valid) y[e] &= 0xffffu;
+                }
+            }
+            return y;
+        };
+        v4f s[4][NT];
 #pragma unroll
         for (int m = 0; m < 4; ++m)
 #pragma unroll
@@ -848,29 +906,15 @@ __global__ __launch_bounds__(256, (attention_waves<T, VT, NT>())) void k_cache_a
                 for (int e = 0; e < 4; ++e) {
                     float y = s[m][n][e];
                     if constexpr (kF32) y = __builtin_ldexpf(y * factor, qe[n] + ke);
-                    s[m][n][e] = seen[n] >> (4 * m + e) & 1 ? y : kMinusInf;
+                    const bool sees = seen[n] >> (4 * m + e) & 1;
+                    s[m][n][e] = sees ? y : kMinusInf;
+                    y = sees ? y : __builtin_nanf("");
+                    // (kept for odd_values, which needs them once they are weights)
+                    lds[((wave * NT + n) * 16 + x) * kScores + 16 * c + 4 * m + e] = y;
                 }
         r.softmax(s, kF32 ? 1.f : factor);
-        // values: those behind the open tokens are whatever the ring held, so none are taken
-        const int valid = kt.open - first - 16 * c;       // of the lane's 16
-        auto value_word = [&](int d, int w) {
-            u4 y = 16 * d + x < D && valid > w * (16 / kWords)
-                       ? *reinterpret_cast<const u4 *>(vf + (int64_t)(16 * d + x) * room + 16 * c +
-                                                       w * (16 / kWords))
-                       : u4{0, 0, 0, 0};
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                if constexpr (kF32) {
-                    if (4 * w + e >= valid) y[e] = 0;
-                } else {
-                    if (8 * w + 2 * e >= valid) y[e] = 0;
-                    if (8 * w + 2 * e + 1 >= valid) y[e] &= 0xffffu;
-                }
-            }
-            return y;
-        };
         float tile_vs = 1.f;
-        bool odd = false;          // a value that is not finite
+        bool bad = false;          // a value that is not finite
         if constexpr (kF32) {
             uint32_t top = 0;
 #pragma unroll 4
@@ -881,7 +925,7 @@ __global__ __launch_bounds__(256, (attention_waves<T, VT, NT>())) void k_cache_a
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         const uint32_t b = y[e] & 0x7fffffffu;
-                        odd |= b >= 0x7f800000u;
+                        bad |= b >= 0x7f800000u;
                         top = b < 0x7f800000u && b > top ? b : top;
                     }
                 }
@@ -897,50 +941,63 @@ __global__ __launch_bounds__(256, (attention_waves<T, VT, NT>())) void k_cache_a
 #pragma unroll
                 for (int w = 0; w < 2; ++w) z = mfma_f16(__builtin_bit_cast(h8, value_word(d, w)), none, z);
             reload();
-            odd = z[0] != z[0] || z[1] != z[1] || z[2] != z[2] || z[3] != z[3];
+            bad = z[0] != z[0] || z[1] != z[1] || z[2] != z[2] || z[3] != z[3];
         }
+        const bool odd = __any(bad);
+        if constexpr (kF32) r.count(s);
         r.new_unit(tile_vs);
-        if (__any(odd)) {
-            if constexpr (!kF32) {      // (their total too)
+        // (a case of its own, so that the words of ordinary tiles are not looked at)
+        auto sums = [&](auto clean) {
+            auto word = [&](int d, int w) {
+                const u4 y = value_word(d, w);
+                return decltype(clean)::value ? finite_word<kF32>(y) : y;
+            };
+            if constexpr (kF32) {
+                const float f = 1.f / r.unit;
+#pragma unroll
+                for (int d4 = 0; d4 < VT; d4 += 4)
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) {
+                        u4 y[4];
+#pragma unroll
+                        for (int d = d4; d < VT && d < d4 + 4; ++d) y[d - d4] = word(d, w);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+#pragma unroll
+                            for (int d = d4; d < VT && d < d4 + 4; ++d)
+#pragma unroll
+                                for (int n = 0; n < NT; ++n)
+                                    r.o[d][n] = mfma_f32(__uint_as_float(y[d - d4][e]) * f, s[w][n][e], r.o[d][n]);
+                    }
+            } else {
                 h8 p[NT][2];
                 r.weights(s, p);
-            }
-            odd_sums<T>(r, s, seen, lds + wave * 1024, vf, D, room, kt.open - first);
-        } else if constexpr (kF32) {
-            const float f = 1.f / r.unit;
 #pragma unroll
-            for (int d4 = 0; d4 < VT; d4 += 4)
+                for (int d = 0; d < VT; ++d) {
+                    const h8 g0 = __builtin_bit_cast(h8, word(d, 0)), g1 = __builtin_bit_cast(h8, word(d, 1));
 #pragma unroll
-                for (int w = 0; w < 4; ++w) {
-                    u4 y[4];
-#pragma unroll
-                    for (int d = d4; d < VT && d < d4 + 4; ++d) y[d - d4] = value_word(d, w);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-#pragma unroll
-                        for (int d = d4; d < VT && d < d4 + 4; ++d)
-#pragma unroll
-                            for (int n = 0; n < NT; ++n)
-                                r.o[d][n] = mfma_f32(__uint_as_float(y[d - d4][e]) * f, s[w][n][e], r.o[d][n]);
+                    for (int n = 0; n < NT; ++n) {
+                        r.o[d][n] = mfma_f16(g0, p[n][0], r.o[d][n]);
+                        r.o[d][n] = mfma_f16(g1, p[n][1], r.o[d][n]);
+                    }
                 }
+            }
+        };
+        if (__builtin_expect(odd, 0)) {
+            sums(std::true_type{});
+            wave_sync();
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+                odd_values<kF32>(r.o, n, lds + (wave * NT + n) * 16 * kScores, kScores, value_word);
+            wave_sync();
         } else {
-            h8 p[NT][2];
-            r.weights(s, p);
-#pragma unroll
-            for (int d = 0; d < VT; ++d) {
-                const h8 g0 = __builtin_bit_cast(h8, value_word(d, 0)), g1 = __builtin_bit_cast(h8, value_word(d, 1));
-#pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    r.o[d][n] = mfma_f16(g0, p[n][0], r.o[d][n]);
-                    r.o[d][n] = mfma_f16(g1, p[n][1], r.o[d][n]);
-                }
-            }
+            sums(std::false_type{});
         }
     }
     if (end > kt.paged) __syncthreads();     // (the waves' parts of LDS are free again)
 
     // ---- the wave's sums over its totals, then the four waves'
-    Result<VT, NT> mine;
+    Result<kF32, VT, NT> mine;
     r.finish(mine);
     if (end - begin > 1) join_waves(mine, lds);
     if (wave == 0) store_result<T, 16 * NT>(a, t, 0, mine);
@@ -1106,14 +1163,29 @@ __global__ __launch_bounds__(256, VT == 16 ? 1 : 2) void k_cache_attention_share
     auto first_slot = [&](int tile) {
         return (int)((uint32_t)(t.n - kt.kept + 64 * (tile - kt.paged)) % (uint32_t)room);
     };
+    // 8 values of feature d, h of the lane's two words; what lies behind the open tokens is anything
+    auto raw_word = [&](int tile, int d, int h) {
+        const T *vf = static_cast<const T *>(v.v_open) + ring * D * room + first_slot(tile);
+        return d < D && kt.open - 64 * (tile - kt.paged) - 16 * c > 8 * h
+                   ? *reinterpret_cast<const u4 *>(vf + (int64_t)d * room + 16 * c + 8 * h)
+                   : u4{0, 0, 0, 0};
+    };
+    auto cut_word = [&](int tile, u4 y, int h) {
+        const int valid = kt.open - 64 * (tile - kt.paged) - 16 * c;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if (8 * h + 2 * e >= valid) y[e] = 0;
+            if (8 * h + 2 * e + 1 >= valid) y[e] &= 0xffffu;
+        }
+        return y;
+    };
+    auto open_word = [&](int tile, int d, int h) { return cut_word(tile, raw_word(tile, d, h), h); };
     u4 ko[KC][2], vo[VQ][2];
     uint32_t seen[NT];
     auto load_open = [&](int tile) {
-        const int first = 64 * (tile - kt.paged), at_slot = first_slot(tile);
+        const int at_slot = first_slot(tile);
         const buf_rsrc_t key_tile = buf_rsrc(static_cast<const T *>(v.k_open) + (ring * room + at_slot) * D16,
                                              64 * D16 * sizeof(T));
-        const T *vf = static_cast<const T *>(v.v_open) + ring * D * room + at_slot;
-        const int valid = kt.open - first - 16 * c;
 #pragma unroll
         for (int k = 0; k < KC; ++k)
 #pragma unroll
@@ -1124,47 +1196,39 @@ __global__ __launch_bounds__(256, VT == 16 ? 1 : 2) void k_cache_attention_share
 #pragma unroll
         for (int i = 0; i < VQ; ++i)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int d = 16 * (wave + 4 * i) + x;
-                vo[i][h] = d < D && valid > 8 * h
-                               ? *reinterpret_cast<const u4 *>(vf + (int64_t)d * room + 16 * c + 8 * h)
-                               : u4{0, 0, 0, 0};
-            }
+            for (int h = 0; h < 2; ++h) vo[i][h] = raw_word(tile, 16 * (wave + 4 * i) + x, h);
     };
     int tile = max(begin, kt.paged);
     if (tile < end) load_open(tile);
     for (; tile < end; ++tile) {
         const int first = 64 * (tile - kt.paged);
-        const T *vf = static_cast<const T *>(v.v_open) + ring * D * room + first_slot(tile);
 #pragma unroll
         for (int k = 0; k < KC; ++k)
 #pragma unroll
             for (int h = 0; h < 2; ++h)
                 frag[0][(wave * KC + k) * 2 + h][lane] = __builtin_bit_cast(h8, ko[k][h]);
-        const int valid = kt.open - first - 16 * c;
         v4f z = {0.f, 0.f, 0.f, 0.f};
+        auto put_values = [&](auto clean) {
 #pragma unroll
-        for (int i = 0; i < VQ; ++i) {
-            const int d = wave + 4 * i;
-            if (VT % 4 && d >= VT) continue;
+            for (int i = 0; i < VQ; ++i) {
+                const int d = wave + 4 * i;
+                if (VT % 4 && d >= VT) continue;
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                u4 y = vo[i][h];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    if (8 * h + 2 * e >= valid) y[e] = 0;
-                    if (8 * h + 2 * e + 1 >= valid) y[e] &= 0xffffu;
+                for (int h = 0; h < 2; ++h) {
+                    const u4 y = cut_word(tile, vo[i][h], h);
+                    const h8 g = __builtin_bit_cast(h8, decltype(clean)::value ? finite_word<false>(y) : y), none = {};
+                    frag[0][8 * KC + 2 * d + h][lane] = g;
+                    if constexpr (!decltype(clean)::value) z = mfma_f16(g, none, z);   // NaN where a value is not finite
                 }
-                const h8 g = __builtin_bit_cast(h8, y), none = {};
-                frag[0][8 * KC + 2 * d + h][lane] = g;
-                z = mfma_f16(g, none, z);            // NaN where a value is not finite
             }
-        }
+        };
+        put_values(std::false_type{});
+        const bool mine = __any(z[0] != z[0] || z[1] != z[1] || z[2] != z[2] || z[3] != z[3]);
+        if (__builtin_expect(mine, 0)) put_values(std::true_type{});
         if (rows)
 #pragma unroll
             for (int n = 0; n < NT; ++n) seen[n] = seen_of(a, t, kt, token[n], first + 16 * c);
         if (tile + 1 < end) load_open(tile + 1);
-        const bool mine = __any(z[0] != z[0] || z[1] != z[1] || z[2] != z[2] || z[3] != z[3]);
         if (lane == 0) odd_of[wave] = mine;
         lds_barrier();
         if (rows) {
@@ -1177,21 +1241,29 @@ __global__ __launch_bounds__(256, VT == 16 ? 1 : 2) void k_cache_attention_share
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
                         if (!(seen[n] >> (4 * i + e) & 1)) s[i][n][e] = kMinusInf;
+            if (__builtin_expect(odd_of[0] | odd_of[1] | odd_of[2] | odd_of[3], 0)) {
+                // (before the others, whose weights and units do not matter to them)
+                float *rows_of = reinterpret_cast<float *>(frag[1]) + wave * 1024;
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    wave_sync();
+#pragma unroll
+                    for (int e = 0; e < 16; ++e)
+                        rows_of[x * 64 + 16 * c + e] = seen[n] >> e & 1 ? s[e / 4][n][e % 4] : __builtin_nanf("");
+                    wave_sync();
+                    odd_values<false>(r.o, n, rows_of, 64, [&](int d, int w) {
+                        return open_word(tile, 16 * d + x, w);
+                    });
+                }
+            }
             r.softmax(s, factor);
             r.new_unit(1.f);
-            if (odd_of[0] | odd_of[1] | odd_of[2] | odd_of[3]) {
-                h8 p[NT][2];
-                r.weights(s, p);                     // (the total)
-                odd_sums<T>(r, s, seen, reinterpret_cast<float *>(frag[1]) + wave * 1024, vf, D, room,
-                            kt.open - first);
-            } else {
-                sums(0, s);
-            }
+            sums(0, s);
         }
         lds_barrier();
     }
     if (!rows) return;
-    Result<VT, NT> mine;
+    Result<false, VT, NT> mine;
     r.finish(mine);
     store_result<T, W>(a, t, 16 * NT * wave, mine);
 }
@@ -1201,7 +1273,7 @@ __global__ __launch_bounds__(256, VT == 16 ? 1 : 2) void k_cache_attention_share
 // 14 us, 16 parts of 16 rows of 32 (sequence, head): 6 us.
 template <typename T, int W>
 __global__ __launch_bounds__(256) void k_cache_join(CacheAttnArgs a) {
-    __shared__ float top_of[max_parts(W)][W], weight[max_parts(W)][W];
+    __shared__ float root[max_parts(W)][W], weight[max_parts(W)][W];   // (maxima, totals at first)
     RowTile t;
     if (!row_tile<W, true>(a, blockIdx.x, t) || t.parts == 1) return;
     const int used = t.parts;
@@ -1212,18 +1284,28 @@ __global__ __launch_bounds__(256) void k_cache_join(CacheAttnArgs a) {
     const float *from = a.part + t.place * size + row;
     for (int p = g; p < used; p += kGroups) {
         int begin, end;
-        kt.range(p, used, &begin, &end);             // (a part without tiles has left nothing)
-        top_of[p][row] = begin < end ? from[p * size + D * W] : kMinusInf;
-        weight[p][row] = begin < end ? from[p * size + (D + 1) * W] : 0.f;
+        kt.range(p, used, &begin, &end);             // (a part without tiles has left nothing: -1)
+        root[p][row] = begin < end ? from[p * size + D * W] : kMinusInf;
+        weight[p][row] = begin < end ? from[p * size + (D + 1) * W] : -1.f;
     }
     __syncthreads();
     float top = kMinusInf, all = 0.f;
-    for (int p = 0; p < used; ++p) top = fmaxf(top, top_of[p][row]);
+    for (int p = 0; p < used; ++p) top = fmaxf(top, root[p][row]);
     const float base = top == kMinusInf ? 0.f : top;
-    for (int p = 0; p < used; ++p) all += weight[p][row] * exp2_fast(top_of[p][row] - base);
+    // binary32: of a part's factor the root and the rest (root_weight)
+    constexpr bool kF32 = std::is_same<T, float>::value;
+    auto root_of = [&](int p) { return kF32 ? root_weight(root[p][row], base) : exp2_fast(root[p][row] - base); };
+    for (int p = 0; p < used; ++p) {
+        const float l = weight[p][row], r = root_of(p);
+        all += l < 0.f ? 0.f : l * r * (kF32 ? r : 1.f);
+    }
     const float inv = all == 0.f ? 0.f : 1.f / all;
     __syncthreads();
-    for (int p = g; p < used; p += kGroups) weight[p][row] *= exp2_fast(top_of[p][row] - base) * inv;
+    for (int p = g; p < used; p += kGroups) {
+        const float l = weight[p][row], r = root_of(p);
+        if (kF32) root[p][row] = r;
+        weight[p][row] = l < 0.f ? -1.f : not_zero(l * inv * r);
+    }
     __syncthreads();
     if (t.first + row >= t.rows) return;
     const int64_t h = t.head * a.share + (t.first + row) / t.T;
@@ -1245,14 +1327,15 @@ __global__ __launch_bounds__(256) void k_cache_join(CacheAttnArgs a) {
                 for (int i = 0; i < 2; ++i) asm volatile("" : "+v"(v[p][i]));   // (loaded, whatever the weight)
 #pragma unroll
             for (int p = 0; p < 8; ++p) {
-                const float w = p0 + p < used ? weight[p0 + p][row] : 0.f;
+                const float w = p0 + p < used ? weight[p0 + p][row] : -1.f;
+                const float r = kF32 ? root[min(p0 + p, used - 1)][row] : 1.f;
 #pragma unroll
-                for (int i = 0; i < 2; ++i) o[i] += w == 0.f ? 0.f : w * v[p][i];   // (what has no weight may be anything)
+                for (int i = 0; i < 2; ++i) o[i] += w < 0.f ? 0.f : v[p][i] * r * w;   // (what is not there may be anything)
             }
         }
 #pragma unroll
         for (int i = 0; i < 2; ++i)
-            if (d + i * kGroups < end) to[(d + i * kGroups) * a.ldo] = (T)o[i];
+            if (d + i * kGroups < end) to[(d + i * kGroups) * a.ldo] = all == 0.f ? (T)0.f : (T)o[i];
     }
 }
 

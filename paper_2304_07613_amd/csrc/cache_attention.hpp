@@ -363,14 +363,33 @@ constexpr int kScores = 68;        // floats of a row of scores in LDS: 64, rows
 template <int VT, int NT>
 constexpr int join_floats() { return std::max(2 * (VT * NT * 256 + NT * 128), 4 * NT * 16 * kScores); }
 
+// The lane's number, of which nothing that follows from it is kept over a loop's turns
+__device__ __forceinline__ int lane_here() {
+    int lane = threadIdx.x & 63;
+    asm volatile("" : "+v"(lane));
+    return lane;
+}
+
 // Floats of one part's result: a row of sums for every feature, then maxima, then totals
 __host__ __device__ inline int64_t part_floats(int D, int rows) { return (int64_t)(D + 2) * rows; }
 
-// kRows: of the row tile, of which `at` and what follows are the wave's
+// kRows: of the row tile, of which `at` and what follows are the wave's.  again: only in the
+// place of results that are not finite.  Whether the lane stored such.
 template <typename T, int kRows, bool kF32, int VT, int NT>
-__device__ __forceinline__ void store_result(const CacheAttnArgs &a, const RowTile &t, int at,
-                                             const Result<kF32, VT, NT> &r) {
-    const int lane = threadIdx.x & 63, x = lane % 16, c = lane / 16, D = a.c.D;
+__device__ __forceinline__ bool store_result(const CacheAttnArgs &a, const RowTile &t, int at,
+                                             const Result<kF32, VT, NT> &r, bool again = false) {
+    const int lane = lane_here(), x = lane % 16, c = lane / 16, D = a.c.D;
+    bool odd = false;
+    if constexpr (kF32)
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int d = 0; d < VT; ++d)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) odd |= !(fabsf(r.o[d][n][i]) < __builtin_inff());
+    auto put = [&](auto *to, float v) {
+        if (!kF32 || !again || !(fabsf((float)*to) < __builtin_inff())) *to = (std::decay_t<decltype(*to)>)v;
+    };
     if (t.parts > 1) {
         float *to = a.part + (t.place + t.part) * part_floats(D, kRows);
 #pragma unroll
@@ -380,13 +399,13 @@ __device__ __forceinline__ void store_result(const CacheAttnArgs &a, const RowTi
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
                     if (16 * d + 4 * c + i < D)
-                        to[(16 * d + 4 * c + i) * kRows + at + 16 * n + x] = r.o[d][n][i];
-            if (c == 0) {
+                        put(to + (16 * d + 4 * c + i) * kRows + at + 16 * n + x, r.o[d][n][i]);
+            if (c == 0 && !again) {     // (the first ones stay: another shift would only cost the join precision)
                 to[D * kRows + at + 16 * n + x] = r.m[n];
                 to[(D + 1) * kRows + at + 16 * n + x] = r.l[n];
             }
         }
-        return;
+        return odd;
     }
     T *O = static_cast<T *>(a.O);
 #pragma unroll
@@ -400,8 +419,9 @@ __device__ __forceinline__ void store_result(const CacheAttnArgs &a, const RowTi
 #pragma unroll
             for (int i = 0; i < 4; ++i)
                 if (16 * d + 4 * c + i < D)
-                    to[(16 * d + 4 * c + i) * a.ldo] = r.l[n] == 0.f ? (T)0.f : (T)r.o[d][n][i];
+                    put(to + (16 * d + 4 * c + i) * a.ldo, r.l[n] == 0.f ? 0.f : r.o[d][n][i]);
     }
+    return odd;
 }
 
 // ------------------------------------------------------------------ the pass
@@ -446,6 +466,18 @@ __device__ __forceinline__ void wave_sync() {
     __builtin_amdgcn_wave_barrier();
 }
 
+// Binary32 sums: any value of the type may meet any weight, and what is large may be what a row does not
+// see, or hardly weighs.  So values keep their size, and weights are 2^kShift times larger: products of
+// weights down to 2^-190 of the largest with values below 2^kLarge are whole.  Larger open values (there
+// are hardly ever any) take weights of their own, 2^(kLarge - 1) times larger still, and the values as many
+// times smaller; page scales from kLargeScale on go into the weights' exponents, with codes times 2^kCodes.
+// Those weights are cut at 2^127, where their products with all but zeros are past the range anyway.  A result
+// that passes the range -- of values above 2^64 or so, over the number of keys -- is made once more, with
+// weights times 2^kShiftAgain, where no sum of any values does.
+// (Beside the roundings there is left: 2^-125 a key, of weights below 2^-253; 2^-17 in results past 2^50.)
+constexpr int kShift = 64, kLarge = 64, kCodes = 10, kShiftAgain = -44;
+constexpr float kLargeScale = 0x1p55f;
+
 // What a wave carries from key tile to key tile, for 16 NT rows (lane (x, c): row x of
 // every 16, features 16 d + 4 c + i)
 template <bool kF32, int VT, int NT>
@@ -454,9 +486,8 @@ struct Pass {
     v4f total[NT];          // of the weights: binary16 by a matrix instruction with ones (four
                             // equal values), binary32 the lane's part
     float m[NT];            // the reference of the weights: no score so far is more than kSlack larger
-    // The sums are in units of a power of two.  binary16: of the tile at hand's values,
-    // since its weights leave no room for another factor.  binary32: of the largest
-    // scale so far, the weights take the rest.
+    // binary16: the sums are in units of the value scale of the tile at hand, since its weights leave
+    // no room for another factor.  binary32: see kShift.
     float unit;
 
     __device__ __forceinline__ void clear() {
@@ -467,10 +498,10 @@ struct Pass {
 #pragma unroll
             for (int d = 0; d < VT; ++d) o[d][n] = v4f{0.f, 0.f, 0.f, 0.f};
         }
-        unit = kF32 ? 0x1p-126f : 1.f;
+        unit = 1.f;
     }
     __device__ __forceinline__ void new_unit(float vs) {
-        if (kF32 ? !(vs <= unit) : vs != unit) {
+        if (vs != unit) {
             const float f = unit / vs;
 #pragma unroll
             for (int n = 0; n < NT; ++n)
@@ -479,8 +510,9 @@ struct Pass {
             unit = vs;
         }
     }
-    // Scores s * f (in units of log 2, f > 0) to weights, in place
-    __device__ __forceinline__ void softmax(v4f (&s)[4][NT], float f) {
+    // Scores s * f (in units of log 2, f > 0) to weights, in place.  binary32: f is 1; weights
+    // times 2^shift are counted into the total, those left in s are 2^more times larger.
+    __device__ __forceinline__ void softmax(v4f (&s)[4][NT], float f, float shift = 0.f, float more = 0.f) {
         float top[NT];
         bool up = false;
 #pragma unroll
@@ -490,6 +522,8 @@ struct Pass {
             for (int i = 1; i < 4; ++i)
                 t = larger(t, larger(larger(s[i][n][0], s[i][n][1]), larger(s[i][n][2], s[i][n][3])));
             top[n] = max_over_c(t) * f;
+            // (the reference of binary32's weights has the shift in it, as it is rounded)
+            if (kF32) top[n] -= shift;
             up |= top[n] > m[n] + kSlack;
         }
         if (__any(up)) {
@@ -509,18 +543,23 @@ struct Pass {
             // binary16 weights are 2^15 at most, so that the small ones stay normal down to
             // 2^-23 of the reference (totals have the same factor)
             const float base = (m[n] == kMinusInf ? 0.f : m[n]) - (kF32 ? 0.f : 15.f - kSlack);
+            if constexpr (!kF32) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+                for (int i = 0; i < 16; ++i) s[i / 4][n][i % 4] = exp2_fast(__builtin_fmaf(s[i / 4][n][i % 4], f, -base));
+            } else {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) s[i][n][j] = exp2_fast(__builtin_fmaf(s[i][n][j], f, -base));
+                for (int i = 0; i < 16; ++i) s[i / 4][n][i % 4] -= base;
+                if (__builtin_expect(more > 0.f, 0))
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        total[n][0] += exp2_fast(s[i / 4][n][i % 4]);
+                        s[i / 4][n][i % 4] = exp2_fast(fminf(s[i / 4][n][i % 4] + more, 127.f));
+                    }
+                else
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) total[n][0] += s[i / 4][n][i % 4] = exp2_fast(s[i / 4][n][i % 4]);
+            }
         }
-    }
-    // binary32: the lane's weights into the total
-    __device__ __forceinline__ void count(const v4f (&s)[4][NT]) {
-#pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) total[n][0] += s[i / 4][n][i % 4];
     }
     // binary16: the lane's 16 weights as the matrix instructions take them, and their total
     __device__ __forceinline__ void weights(const v4f (&s)[4][NT], h8 (&p)[NT][2]) {
@@ -543,22 +582,17 @@ struct Pass {
 #pragma unroll
             for (int d = 0; d < VT; ++d)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) r.o[d][n][i] = o[d][n][i] * inv * unit;
+                for (int i = 0; i < 4; ++i) r.o[d][n][i] = kF32 ? o[d][n][i] * inv : o[d][n][i] * inv * unit;
         }
     }
 };
 
-// Open values as the matrix instructions take them, without those that are not finite
-template <bool kF32>
+// Open values in binary16 as the matrix instructions take them, without those that are not finite
 __device__ __forceinline__ u4 finite_word(u4 y) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-        if constexpr (kF32) {
-            if ((y[e] & 0x7f800000u) == 0x7f800000u) y[e] = 0;
-        } else {
-            if ((y[e] & 0x7c00u) == 0x7c00u) y[e] &= 0xffff0000u;
-            if ((y[e] & 0x7c000000u) == 0x7c000000u) y[e] &= 0xffffu;
-        }
+        if ((y[e] & 0x7c00u) == 0x7c00u) y[e] &= 0xffff0000u;
+        if ((y[e] & 0x7c000000u) == 0x7c000000u) y[e] &= 0xffffu;
     }
     return y;
 }
@@ -679,302 +713,161 @@ __global__ __launch_bounds__(256, (attention_waves<T, VT, NT>())) void k_cache_a
 #pragma unroll
             for (int k = 0; k < KC; ++k) kk[s][k] = buf_load16(from, k_off[k], first + 4 * s * D16);
     };
-    // A wave's tiles: open ones from the last wave on, of the pages a run of as many as make the
-    // units of all waves about equal
-    const int opens = end - max(begin, min(kt.paged, end)), paged = max(0, paged_end - begin);
-    const int quota = (paged + 3 * opens + 3) / 4;
-    int tile = begin;
-    for (int w = 0; w < wave; ++w) tile += max(0, quota - 3 * ((opens + w) / 4));
-    const int mine_end = min(paged_end, tile + max(0, quota - 3 * ((opens + wave) / 4)));
-    if (tile < mine_end) {
-        pages.look(a, t, tile, 1, mine_end);
-        load_keys(tile, 0);
-    }
-    // queries: the lane's features 64 k + 16 c + j of row x of every row tile
-    std::conditional_t<kF32, float[NT][KC][16], h8[NT][KC][2]> q;
-    int qe[NT];
-    int token[NT];
-    {
-        const T *Q = static_cast<const T *>(a.Q);
+    // Whether the lane had results that are not finite.  again: those alone are made, with other weights.
+    auto pass = [&](const bool again) __attribute__((always_inline)) {
+        const int lane = lane_here(), x = lane % 16, c = lane / 16;
+        const int shift = again ? kShiftAgain : kShift;
+        // A wave's tiles: open ones from the last wave on, of the pages a run of as many as make the
+        // units of all waves about equal
+        const int opens = end - max(begin, min(kt.paged, end)), paged = max(0, paged_end - begin);
+        const int quota = (paged + 3 * opens + 3) / 4;
+        int tile = begin;
+        for (int w = 0; w < wave; ++w) tile += max(0, quota - 3 * ((opens + w) / 4));
+        const int mine_end = min(paged_end, tile + max(0, quota - 3 * ((opens + wave) / 4)));
+        if (tile < mine_end) {
+            pages.look(a, t, tile, 1, mine_end);
+            load_keys(tile, 0);
+        }
+        // queries: the lane's features 64 k + 16 c + j of row x of every row tile
+        std::conditional_t<kF32, float[NT][KC][16], h8[NT][KC][2]> q;
+        int qe[NT];
+        int token[NT];
+        {
+            const T *Q = static_cast<const T *>(a.Q);
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            const int row = min(t.first + 16 * n + x, t.rows - 1);
-            token[n] = row % t.T;
-            const T *from = Q + ((int64_t)(head * a.share + row / t.T) * D + 16 * c) * a.ldq + t.q0 + token[n];
-            float top = 0.f;
-#pragma unroll
-            for (int k = 0; k < KC; ++k)
-#pragma unroll
-                for (int j = 0; j < 16; ++j) {
-                    const int d = 64 * k + 16 * c + j;
-                    const T value = d < D ? *from : (T)0.f;
-                    from += j < 15 ? a.ldq : 49 * a.ldq;
-                    if constexpr (kF32) {
-                        q[n][k][j] = value;
-                        top = fmaxf(top, fabsf(value));
-                    } else {
-                        q[n][k][j / 8][j % 8] = value;
-                    }
-                }
-            qe[n] = 0;
-            if constexpr (kF32) {
-                // scaled by a power of two to below 2, so that no product with codes
-                // passes the range where the score itself does not
-                top = max_over_c(top);
-                if (top < __builtin_inff()) qe[n] = exponent_of(top);
+            for (int n = 0; n < NT; ++n) {
+                const int row = min(t.first + 16 * n + x, t.rows - 1);
+                token[n] = row % t.T;
+                const T *from = Q + ((int64_t)(head * a.share + row / t.T) * D + 16 * c) * a.ldq + t.q0 + token[n];
+                float top = 0.f;
 #pragma unroll
                 for (int k = 0; k < KC; ++k)
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) q[n][k][j] = __builtin_ldexpf(q[n][k][j], -qe[n]);
-            }
-        }
-    }
-
-    Pass<kF32, VT, NT> r;
-    r.clear();
-    const float factor = a.scale * kLog2e;
-
-    // ---- whole pages
-    for (int at = 0; tile < mine_end; ++tile, ++at) {
-        u4 vv[VT];
-        const int i64 = at & 63;
-        const buf_rsrc_t from = buf_rsrc(v.v_pages + pages.place(i64) * v_bytes, v_bytes);
-        const uint32_t first = (tile & two) * 64;
-#pragma unroll
-        for (int d = 0; d < VT; ++d) vv[d] = buf_load16(from, v_at + first + 16 * d * v.block, 0);
-        issued();        // before the scores: they are the time that the values have to come
-        const float tile_ks = pages.scale(pages.ks, i64), vs = pages.scale(pages.vs, i64);
-        const float tile_vs = vs < 0x1p-32f && !kF32 ? 0x1p-32f : vs;
-        v4f s[4][NT];
-        // (products that follow one another are of different sums: none waits for the last)
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int n = 0; n < NT; ++n) s[i][n] = v4f{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int k = 0; k < KC; ++k) {
-            if constexpr (kF32) {
-#pragma unroll
-                for (int w = 0; w < 4; ++w) {
-                    v4f f[4];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) f[i] = decode4f<kInt8>(kk[i][k][w]);
-#pragma unroll
-                    for (int j = 0; j < 4; ++j)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i)
-#pragma unroll
-                            for (int n = 0; n < NT; ++n) s[i][n] = mfma_f32(f[i][j], q[n][k][4 * w + j], s[i][n]);
-                }
-            } else {
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const h8 f = decode8<kInt8>(kk[i][k][2 * h], kk[i][k][2 * h + 1]);
-#pragma unroll
-                        for (int n = 0; n < NT; ++n) s[i][n] = mfma_f16(f, q[n][k][h], s[i][n]);
+                    for (int j = 0; j < 16; ++j) {
+                        const int d = 64 * k + 16 * c + j;
+                        const T value = d < D ? *from : (T)0.f;
+                        from += j < 15 ? a.ldq : 49 * a.ldq;
+                        if constexpr (kF32) {
+                            q[n][k][j] = value;
+                            top = fmaxf(top, fabsf(value));
+                        } else {
+                            q[n][k][j / 8][j % 8] = value;
+                        }
                     }
+                qe[n] = 0;
+                if constexpr (kF32) {
+                    // scaled by a power of two to below 2, so that no product with codes
+                    // passes the range where the score itself does not
+                    top = max_over_c(top);
+                    if (top < __builtin_inff()) qe[n] = exponent_of(top);
+#pragma unroll
+                    for (int k = 0; k < KC; ++k)
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) q[n][k][j] = __builtin_ldexpf(q[n][k][j], -qe[n]);
+                }
             }
         }
-        if (tile + 1 < mine_end) {
-            if (i64 == 63) pages.look(a, t, tile + 1, 1, mine_end);
-            load_keys(tile + 1, (at + 1) & 63);
-        }
-        issued();
-        if constexpr (kF32) {
-            const int ke = exponent_of(tile_ks);
-            const float f = factor * __builtin_ldexpf(tile_ks, -ke);
+
+        Pass<kF32, VT, NT> r;
+        r.clear();
+        const float factor = a.scale * kLog2e;
+
+        // ---- whole pages
+        for (int at = 0; tile < mine_end; ++tile, ++at) {
+            u4 vv[VT];
+            const int i64 = at & 63;
+            const buf_rsrc_t from = buf_rsrc(v.v_pages + pages.place(i64) * v_bytes, v_bytes);
+            const uint32_t first = (tile & two) * 64;
+#pragma unroll
+            for (int d = 0; d < VT; ++d) vv[d] = buf_load16(from, v_at + first + 16 * d * v.block, 0);
+            issued();        // before the scores: they are the time that the values have to come
+            const float tile_ks = pages.scale(pages.ks, i64), vs = pages.scale(pages.vs, i64);
+            const float tile_vs = vs < 0x1p-32f && !kF32 ? 0x1p-32f : vs;
+            v4f s[4][NT];
+            // (products that follow one another are of different sums: none waits for the last)
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
-                for (int n = 0; n < NT; ++n)
+                for (int n = 0; n < NT; ++n) s[i][n] = v4f{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) s[i][n][j] = __builtin_ldexpf(s[i][n][j] * f, qe[n] + ke);
-        }
-        r.softmax(s, kF32 ? 1.f : factor * tile_ks);
-        if constexpr (kF32) r.count(s);
-        r.new_unit(tile_vs);
-        if constexpr (kF32) {
-            const float f = tile_vs / r.unit;
-#pragma unroll
-            for (int w = 0; w < 4; ++w)
-#pragma unroll
-                for (int n = 0; n < NT; ++n) s[w][n] *= f;
-            // (four features at a time, so that products that follow one another are of different sums)
-#pragma unroll
-            for (int d4 = 0; d4 < VT; d4 += 4)
-#pragma unroll
-                for (int w = 0; w < 4; ++w) {
-                    v4f g[4];
-#pragma unroll
-                    for (int d = d4; d < VT && d < d4 + 4; ++d) g[d - d4] = decode4f<kInt8>(vv[d][w]);
-#pragma unroll
-                    for (int j = 0; j < 4; ++j)
-#pragma unroll
-                        for (int d = d4; d < VT && d < d4 + 4; ++d)
-#pragma unroll
-                            for (int n = 0; n < NT; ++n) r.o[d][n] = mfma_f32(g[d - d4][j], s[w][n][j], r.o[d][n]);
-                }
-        } else {
-            h8 p[NT][2];
-            r.weights(s, p);
-#pragma unroll
-            for (int d = 0; d < VT; ++d) {
-                const h8 g0 = decode8<kInt8>(vv[d][0], vv[d][1]), g1 = decode8<kInt8>(vv[d][2], vv[d][3]);
-#pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    r.o[d][n] = mfma_f16(g0, p[n][0], r.o[d][n]);
-                    r.o[d][n] = mfma_f16(g1, p[n][1], r.o[d][n]);
-                }
-            }
-        }
-    }
-
-    // ---- open tokens
-    // (a single tile is wave 0's, whose result is the workgroup's)
-    for (tile = max(begin, kt.paged) + (paged ? 3 - wave : wave); tile < end; tile += 4) {
-        const int first = 64 * (tile - kt.paged);          // of the open tokens
-        const int at_slot = (int)((uint32_t)(t.n - kt.kept + first) % (uint32_t)room);
-        const int64_t ring = ((int64_t)a.layer * v.sequences + t.b) * heads + head;
-        const T *kf = static_cast<const T *>(v.k_open) + (ring * room + at_slot) * D16;
-        const T *vf = static_cast<const T *>(v.v_open) + ring * D * room + at_slot;
-        // which of the lane's keys each of its rows sees
-        uint32_t seen[NT];
-#pragma unroll
-        for (int n = 0; n < NT; ++n) seen[n] = seen_of(a, t, kt, token[n], first + 16 * c);
-        const buf_rsrc_t key_tile = buf_rsrc(kf, 64 * D16 * sizeof(T));
-        auto key_word = [&](int m, int k, int w) {
-            const uint32_t at = k_off[k] == past ? past : k_off[k] * (uint32_t)sizeof(T);
-            return buf_load16(key_tile, at, (4 * m * D16 + w * (16 / kWords)) * sizeof(T));
-        };
-        // binary32 keys are scaled by 2^-10: 256 products with queries below 2 then stay in the
-        // range, and only keys below 2^-116 lose bits
-        constexpr int ke = kF32 ? 10 : 0;
-        // values: those behind the open tokens are whatever the ring held, so none are taken
-        const int valid = kt.open - first - 16 * c;       // of the lane's 16
-        auto value_word = [&](int d, int w) {
-            u4 y = 16 * d + x < D && valid > w * (16 / kWords)
-                       ? *reinterpret_cast<const u4 *>(vf + (int64_t)(16 * d + x) * room + 16 * c +
-                                                       w * (16 / kWords))
-                       : u4{0, 0, 0, 0};
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
+            for (int k = 0; k < KC; ++k) {
                 if constexpr (kF32) {
-                    if (4 * w + e >= valid) y[e] = 0;
-                } else {
-                    if (8 * w + 2 * e >= valid) y[e] = 0;
-                    if (8 * w + 2 * e + 1 >= valid) y[e] &= 0xffffu;
-                }
-            }
-            return y;
-        };
-        v4f s[4][NT];
-#pragma unroll
-        for (int m = 0; m < 4; ++m)
-#pragma unroll
-            for (int n = 0; n < NT; ++n) s[m][n] = v4f{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int k = 0; k < KC; ++k)
-#pragma unroll
-            for (int w = 0; w < kWords; ++w) {
-                u4 y[4];
-#pragma unroll
-                for (int m = 0; m < 4; ++m) y[m] = key_word(m, k, w);
-                if constexpr (kF32) {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-#pragma unroll
-                        for (int m = 0; m < 4; ++m) {
-                            const float f = __uint_as_float(y[m][e]) * 0x1p-10f;
-#pragma unroll
-                            for (int n = 0; n < NT; ++n) s[m][n] = mfma_f32(f, q[n][k][4 * w + e], s[m][n]);
-                        }
-                } else {
-#pragma unroll
-                    for (int m = 0; m < 4; ++m)
-#pragma unroll
-                        for (int n = 0; n < NT; ++n)
-                            s[m][n] = mfma_f16(__builtin_bit_cast(h8, y[m]), q[n][k][w], s[m][n]);
-                }
-            }
-#pragma unroll
-        for (int m = 0; m < 4; ++m)
-#pragma unroll
-            for (int n = 0; n < NT; ++n)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    float y = s[m][n][e];
-                    if constexpr (kF32) y = __builtin_ldexpf(y * factor, qe[n] + ke);
-                    const bool sees = seen[n] >> (4 * m + e) & 1;
-                    s[m][n][e] = sees ? y : kMinusInf;
-                    y = sees ? y : __builtin_nanf("");
-                    // (kept for odd_values, which needs them once they are weights)
-                    lds[((wave * NT + n) * 16 + x) * kScores + 16 * c + 4 * m + e] = y;
-                }
-        r.softmax(s, kF32 ? 1.f : factor);
-        float tile_vs = 1.f;
-        bool bad = false;          // a value that is not finite
-        if constexpr (kF32) {
-            uint32_t top = 0;
-#pragma unroll 4
-            for (int d = 0; d < VT; ++d)
-#pragma unroll
-                for (int w = 0; w < 4; ++w) {
-                    const u4 y = value_word(d, w);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const uint32_t b = y[e] & 0x7fffffffu;
-                        bad |= b >= 0x7f800000u;
-                        top = b < 0x7f800000u && b > top ? b : top;
-                    }
-                }
-            for (int d = 1; d < 64; d *= 2) top = max(top, (uint32_t)__shfl_xor((int)top, d));
-            tile_vs = __builtin_ldexpf(1.f, max(exponent_of(__uint_as_float(top)), -126));
-            reload();
-        } else {
-            // 0 times a value that is not finite is NaN
-            v4f z = {0.f, 0.f, 0.f, 0.f};
-            const h8 none = {};
-#pragma unroll
-            for (int d = 0; d < VT; ++d)
-#pragma unroll
-                for (int w = 0; w < 2; ++w) z = mfma_f16(__builtin_bit_cast(h8, value_word(d, w)), none, z);
-            reload();
-            bad = z[0] != z[0] || z[1] != z[1] || z[2] != z[2] || z[3] != z[3];
-        }
-        const bool odd = __any(bad);
-        if constexpr (kF32) r.count(s);
-        r.new_unit(tile_vs);
-        // (a case of its own, so that the words of ordinary tiles are not looked at)
-        auto sums = [&](auto clean) {
-            auto word = [&](int d, int w) {
-                const u4 y = value_word(d, w);
-                return decltype(clean)::value ? finite_word<kF32>(y) : y;
-            };
-            if constexpr (kF32) {
-                const float f = 1.f / r.unit;
-#pragma unroll
-                for (int d4 = 0; d4 < VT; d4 += 4)
 #pragma unroll
                     for (int w = 0; w < 4; ++w) {
-                        u4 y[4];
+                        v4f f[4];
 #pragma unroll
-                        for (int d = d4; d < VT && d < d4 + 4; ++d) y[d - d4] = word(d, w);
+                        for (int i = 0; i < 4; ++i) f[i] = decode4f<kInt8>(kk[i][k][w]);
 #pragma unroll
-                        for (int e = 0; e < 4; ++e)
+                        for (int j = 0; j < 4; ++j)
 #pragma unroll
-                            for (int d = d4; d < VT && d < d4 + 4; ++d)
+                            for (int i = 0; i < 4; ++i)
 #pragma unroll
-                                for (int n = 0; n < NT; ++n)
-                                    r.o[d][n] = mfma_f32(__uint_as_float(y[d - d4][e]) * f, s[w][n][e], r.o[d][n]);
+                                for (int n = 0; n < NT; ++n) s[i][n] = mfma_f32(f[i][j], q[n][k][4 * w + j], s[i][n]);
                     }
+                } else {
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const h8 f = decode8<kInt8>(kk[i][k][2 * h], kk[i][k][2 * h + 1]);
+#pragma unroll
+                            for (int n = 0; n < NT; ++n) s[i][n] = mfma_f16(f, q[n][k][h], s[i][n]);
+                        }
+                }
+            }
+            if (tile + 1 < mine_end) {
+                if (i64 == 63) pages.look(a, t, tile + 1, 1, mine_end);
+                load_keys(tile + 1, (at + 1) & 63);
+            }
+            issued();
+            if constexpr (kF32) {
+                const int ke = exponent_of(tile_ks);
+                const float f = factor * __builtin_ldexpf(tile_ks, -ke);
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) s[i][n][j] = __builtin_ldexpf(s[i][n][j] * f, qe[n] + ke);
+            }
+            if constexpr (kF32) {
+                const int large = tile_vs > kLargeScale ? exponent_of(tile_vs) - kCodes : 0;
+                r.softmax(s, 1.f, (float)shift, (float)large);
+                const float f = large ? __builtin_ldexpf(tile_vs, -large - kCodes) : tile_vs;
+#pragma unroll
+                for (int w = 0; w < 4; ++w)
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) s[w][n] *= f;
+                auto sums = [&](float by) {
+                    // (four features at a time, so that products that follow one another are of different sums)
+#pragma unroll
+                    for (int d4 = 0; d4 < VT; d4 += 4)
+#pragma unroll
+                        for (int w = 0; w < 4; ++w) {
+                            v4f g[4];
+#pragma unroll
+                            for (int d = d4; d < VT && d < d4 + 4; ++d) g[d - d4] = decode4f<kInt8>(vv[d][w]) * by;
+#pragma unroll
+                            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                                for (int d = d4; d < VT && d < d4 + 4; ++d)
+#pragma unroll
+                                    for (int n = 0; n < NT; ++n)
+                                        r.o[d][n] = mfma_f32(g[d - d4][j], s[w][n][j], r.o[d][n]);
+                        }
+                };
+                if (__builtin_expect(large != 0, 0))
+                    sums((float)(1 << kCodes));
+                else
+                    sums(1.f);
             } else {
+                r.softmax(s, factor * tile_ks);
+                r.new_unit(tile_vs);
                 h8 p[NT][2];
                 r.weights(s, p);
 #pragma unroll
                 for (int d = 0; d < VT; ++d) {
-                    const h8 g0 = __builtin_bit_cast(h8, word(d, 0)), g1 = __builtin_bit_cast(h8, word(d, 1));
+                    const h8 g0 = decode8<kInt8>(vv[d][0], vv[d][1]), g1 = decode8<kInt8>(vv[d][2], vv[d][3]);
 #pragma unroll
                     for (int n = 0; n < NT; ++n) {
                         r.o[d][n] = mfma_f16(g0, p[n][0], r.o[d][n]);
@@ -982,25 +875,200 @@ __global__ __launch_bounds__(256, (attention_waves<T, VT, NT>())) void k_cache_a
                     }
                 }
             }
-        };
-        if (__builtin_expect(odd, 0)) {
-            sums(std::true_type{});
-            wave_sync();
-#pragma unroll
-            for (int n = 0; n < NT; ++n)
-                odd_values<kF32>(r.o, n, lds + (wave * NT + n) * 16 * kScores, kScores, value_word);
-            wave_sync();
-        } else {
-            sums(std::false_type{});
         }
-    }
-    if (end > kt.paged) __syncthreads();     // (the waves' parts of LDS are free again)
 
-    // ---- the wave's sums over its totals, then the four waves'
-    Result<kF32, VT, NT> mine;
-    r.finish(mine);
-    if (end - begin > 1) join_waves(mine, lds);
-    if (wave == 0) store_result<T, 16 * NT>(a, t, 0, mine);
+        // ---- open tokens
+        // (a single tile is wave 0's, whose result is the workgroup's)
+        for (tile = max(begin, kt.paged) + (paged ? 3 - wave : wave); tile < end; tile += 4) {
+            const int first = 64 * (tile - kt.paged);          // of the open tokens
+            const int at_slot = (int)((uint32_t)(t.n - kt.kept + first) % (uint32_t)room);
+            const int64_t ring = ((int64_t)a.layer * v.sequences + t.b) * heads + head;
+            const T *kf = static_cast<const T *>(v.k_open) + (ring * room + at_slot) * D16;
+            const T *vf = static_cast<const T *>(v.v_open) + ring * D * room + at_slot;
+            // which of the lane's keys each of its rows sees
+            uint32_t seen[NT];
+#pragma unroll
+            for (int n = 0; n < NT; ++n) seen[n] = seen_of(a, t, kt, token[n], first + 16 * c);
+            const buf_rsrc_t key_tile = buf_rsrc(kf, 64 * D16 * sizeof(T));
+            auto key_word = [&](int m, int k, int w) {
+                const uint32_t at = k_off[k] == past ? past : k_off[k] * (uint32_t)sizeof(T);
+                return buf_load16(key_tile, at, (4 * m * D16 + w * (16 / kWords)) * sizeof(T));
+            };
+            // binary32 keys are scaled by 2^-10: 256 products with queries below 2 then stay in the
+            // range, and only keys below 2^-116 lose bits
+            constexpr int ke = kF32 ? 10 : 0;
+            // values: those behind the open tokens are whatever the ring held, so none are taken
+            const int valid = kt.open - first - 16 * c;       // of the lane's 16
+            int feature = x;
+            auto value_word = [&](int d, int w) {
+                u4 y = 16 * d + feature < D && valid > w * (16 / kWords)
+                           ? *reinterpret_cast<const u4 *>(vf + (int64_t)(16 * d + feature) * room + 16 * c +
+                                                           w * (16 / kWords))
+                           : u4{0, 0, 0, 0};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    if constexpr (kF32) {
+                        if (4 * w + e >= valid) y[e] = 0;
+                    } else {
+                        if (8 * w + 2 * e >= valid) y[e] = 0;
+                        if (8 * w + 2 * e + 1 >= valid) y[e] &= 0xffffu;
+                    }
+                }
+                return y;
+            };
+            v4f s[4][NT];
+#pragma unroll
+            for (int m = 0; m < 4; ++m)
+#pragma unroll
+                for (int n = 0; n < NT; ++n) s[m][n] = v4f{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int k = 0; k < KC; ++k)
+#pragma unroll
+                for (int w = 0; w < kWords; ++w) {
+                    u4 y[4];
+#pragma unroll
+                    for (int m = 0; m < 4; ++m) y[m] = key_word(m, k, w);
+                    if constexpr (kF32) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+#pragma unroll
+                            for (int m = 0; m < 4; ++m) {
+                                const float f = __uint_as_float(y[m][e]) * 0x1p-10f;
+#pragma unroll
+                                for (int n = 0; n < NT; ++n) s[m][n] = mfma_f32(f, q[n][k][4 * w + e], s[m][n]);
+                            }
+                    } else {
+#pragma unroll
+                        for (int m = 0; m < 4; ++m)
+#pragma unroll
+                            for (int n = 0; n < NT; ++n)
+                                s[m][n] = mfma_f16(__builtin_bit_cast(h8, y[m]), q[n][k][w], s[m][n]);
+                    }
+                }
+#pragma unroll
+            for (int m = 0; m < 4; ++m)
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        float y = s[m][n][e];
+                        if constexpr (kF32) y = __builtin_ldexpf(y * factor, qe[n] + ke);
+                        const bool sees = seen[n] >> (4 * m + e) & 1;
+                        s[m][n][e] = sees ? y : kMinusInf;
+                        y = sees ? y : __builtin_nanf("");
+                        // (kept for odd_values, which needs them once they are weights)
+                        lds[((wave * NT + n) * 16 + x) * kScores + 16 * c + 4 * m + e] = y;
+                    }
+            r.softmax(s, kF32 ? 1.f : factor, (float)shift);
+            // a value that is not finite, or larger than the weights are made for
+            bool odd = false;
+            constexpr uint32_t limit = (127 + kLarge) << 23;
+            if constexpr (kF32) {
+#pragma unroll 4
+                for (int d = 0; d < VT; ++d)
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) {
+                        const u4 y = value_word(d, w);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) odd |= (y[e] & 0x7fffffffu) >= limit;
+                    }
+                reload();
+            } else {
+                // 0 times a value that is not finite is NaN
+                v4f z = {0.f, 0.f, 0.f, 0.f};
+                const h8 none = {};
+#pragma unroll
+                for (int d = 0; d < VT; ++d)
+#pragma unroll
+                    for (int w = 0; w < 2; ++w) z = mfma_f16(__builtin_bit_cast(h8, value_word(d, w)), none, z);
+                reload();
+                odd = z[0] != z[0] || z[1] != z[1] || z[2] != z[2] || z[3] != z[3];
+                r.new_unit(1.f);
+            }
+            odd = __any(odd);
+            // (by the words and numbers that are taken: in ordinary tiles they are not looked at)
+            auto sums_f32 = [&](auto value_of) {
+#pragma unroll
+                for (int d4 = 0; d4 < VT; d4 += 4)
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) {
+                        u4 y[4];
+#pragma unroll
+                        for (int d = d4; d < VT && d < d4 + 4; ++d) y[d - d4] = value_word(d, w);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+#pragma unroll
+                            for (int d = d4; d < VT && d < d4 + 4; ++d)
+#pragma unroll
+                                for (int n = 0; n < NT; ++n)
+                                    r.o[d][n] = mfma_f32(value_of(y[d - d4][e]), s[w][n][e], r.o[d][n]);
+                    }
+            };
+            auto sums_f16 = [&](auto word_of) {
+                h8 p[NT][2];
+                r.weights(s, p);
+#pragma unroll
+                for (int d = 0; d < VT; ++d) {
+                    const h8 g0 = __builtin_bit_cast(h8, word_of(value_word(d, 0)));
+                    const h8 g1 = __builtin_bit_cast(h8, word_of(value_word(d, 1)));
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        r.o[d][n] = mfma_f16(g0, p[n][0], r.o[d][n]);
+                        r.o[d][n] = mfma_f16(g1, p[n][1], r.o[d][n]);
+                    }
+                }
+            };
+            float *scores = lds + wave * NT * 16 * kScores;
+            if (__builtin_expect(odd, 0)) {
+                if constexpr (kF32) {
+                    uint32_t from = 0, to = limit;
+                    float by = 1.f;
+#pragma unroll 1
+                    for (;;) {
+                        feature = lane_here() % 16;       // (no address is kept over the turns)
+                        sums_f32([&](uint32_t bits) {
+                            const uint32_t b = bits & 0x7fffffffu;
+                            return b >= from && b < to ? __uint_as_float(bits) * by : 0.f;
+                        });
+                        if (from) break;
+                        // the larger ones and their weights
+                        from = limit;
+                        to = 0x7f800000u;
+                        by = __builtin_ldexpf(1.f, 1 - kLarge);
+#pragma unroll
+                        for (int n = 0; n < NT; ++n)
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) {
+                                const float y = scores[(n * 16 + x) * kScores + 16 * c + e] - (r.m[n] == kMinusInf ? 0.f : r.m[n]);
+                                s[e / 4][n][e % 4] = y == y ? exp2_fast(fminf(y + (float)(kLarge - 1), 127.f)) : 0.f;
+                            }
+                    }
+                } else {
+                    sums_f16([](u4 y) { return finite_word(y); });
+                }
+                wave_sync();
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+                    odd_values<kF32>(r.o, n, scores + n * 16 * kScores, kScores, value_word);
+                wave_sync();
+            } else if constexpr (kF32) {
+                sums_f32([](uint32_t bits) { return __uint_as_float(bits); });
+            } else {
+                sums_f16([](u4 y) { return y; });
+            }
+        }
+        if (end > kt.paged) __syncthreads();     // (the waves' parts of LDS are free again)
+
+        // ---- the wave's sums over its totals, then the four waves'
+        Result<kF32, VT, NT> mine;
+        r.finish(mine);
+        if (end - begin > 1) join_waves(mine, lds);
+        return wave == 0 && store_result<T, 16 * NT>(a, t, 0, mine, again);
+    };
+    // (twice in the code: a loop around it kept registers from turn to turn, and spilled them)
+    const bool odd = pass(false);
+    if constexpr (kF32)
+        if (__builtin_expect(__syncthreads_or(odd), 0)) pass(true);
 }
 
 // ------------------------------------------------- many rows (binary16)
@@ -1216,7 +1284,7 @@ __global__ __launch_bounds__(256, VT == 16 ? 1 : 2) void k_cache_attention_share
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     const u4 y = cut_word(tile, vo[i][h], h);
-                    const h8 g = __builtin_bit_cast(h8, decltype(clean)::value ? finite_word<false>(y) : y), none = {};
+                    const h8 g = __builtin_bit_cast(h8, decltype(clean)::value ? finite_word(y) : y), none = {};
                     frag[0][8 * KC + 2 * d + h][lane] = g;
                     if constexpr (!decltype(clean)::value) z = mfma_f16(g, none, z);   // NaN where a value is not finite
                 }

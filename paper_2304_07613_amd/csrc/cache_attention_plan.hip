@@ -25,8 +25,12 @@ Plan plan(nmg_dtype dtype, const CacheAttnArgs &a, int64_t longest) {
     // the lengths are on the device: sequences with the same number of drafted tokens
     const int64_t rows = ((int64_t)a.Nq + a.c.sequences - 1) / a.c.sequences * a.share;
     const bool wide = a.c.D > 128;
+    // Binary32 heads of 65 to 96: 32 rows do not fit the registers of two waves a SIMD beside their
+    // six tiles of features.  8 sequences of 12 drafted tokens over 1032 to 2000, 8 / 4 heads of 96: 24.7 us with 16
+    // rows, 33.3 with 32 and one wave, 37.5 with 32 and spills; 200 tokens over 2000, 12 heads: 49, 64, 58.
+    const bool tight = a.c.D > 64 && a.c.D <= 96;
     if (dtype == NMG_F32)
-        p.rows = rows <= 16 || wide ? kRows16 : kRows32;
+        p.rows = rows <= 16 || wide || tight ? kRows16 : kRows32;
     else if (rows > (wide ? 16 : 64))
         p.rows = wide ? kRows64 : kRows128;
     else

@@ -11,9 +11,8 @@ nmg_status cache_attention_f32(nmg_cache_format format, const CacheAttnArgs &a, 
                : tiles > 6 ? run_cache_attention<float, 8, 1>(format, a, stream)
                : tiles > 4 ? run_cache_attention<float, 6, 1>(format, a, stream)
                            : run_cache_attention<float, 4, 1>(format, a, stream);
-    return tiles > 6   ? run_cache_attention<float, 8, 2>(format, a, stream)
-           : tiles > 4 ? run_cache_attention<float, 6, 2>(format, a, stream)
-                       : run_cache_attention<float, 4, 2>(format, a, stream);
+    return tiles > 4 ? run_cache_attention<float, 8, 2>(format, a, stream)
+                     : run_cache_attention<float, 4, 2>(format, a, stream);
 }
 
 }  // namespace nmg_internal

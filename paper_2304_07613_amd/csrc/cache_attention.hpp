@@ -756,10 +756,11 @@ __global__ __launch_bounds__(256, (attention_waves<T, VT, NT>())) void k_cache_a
                     }
                 qe[n] = 0;
                 if constexpr (kF32) {
-                    // scaled by a power of two to below 2, so that no product with codes
-                    // passes the range where the score itself does not
+                    // From 2^100 on scaled to 2^60, so that no product with codes passes the range where
+                    // the score itself does not.  (Others as they are: beside a large query
+                    // small ones count, where they meet large keys.)
                     top = max_over_c(top);
-                    if (top < __builtin_inff()) qe[n] = exponent_of(top);
+                    if (top >= 0x1p100f && top < __builtin_inff()) qe[n] = exponent_of(top) - 60;
 #pragma unroll
                     for (int k = 0; k < KC; ++k)
 #pragma unroll
@@ -894,9 +895,6 @@ __global__ __launch_bounds__(256, (attention_waves<T, VT, NT>())) void k_cache_a
                 const uint32_t at = k_off[k] == past ? past : k_off[k] * (uint32_t)sizeof(T);
                 return buf_load16(key_tile, at, (4 * m * D16 + w * (16 / kWords)) * sizeof(T));
             };
-            // binary32 keys are scaled by 2^-10: 256 products with queries below 2 then stay in the
-            // range, and only keys below 2^-116 lose bits
-            constexpr int ke = kF32 ? 10 : 0;
             // values: those behind the open tokens are whatever the ring held, so none are taken
             const int valid = kt.open - first - 16 * c;       // of the lane's 16
             int feature = x;
@@ -916,49 +914,64 @@ __global__ __launch_bounds__(256, (attention_waves<T, VT, NT>())) void k_cache_a
                 }
                 return y;
             };
+            // Binary32 sums of products that pass the range are made once more from keys 2^kKeys times smaller: the
+            // score may be inside it.  (All keys so would lose bits of the small ones.)
+            constexpr int kKeys = 112;
+            float *scores = lds + wave * NT * 16 * kScores;
             v4f s[4][NT];
+#pragma unroll 1
+            for (bool smaller = false;; smaller = true) {
+                if (kF32) reload();
+                const float keys_by = smaller ? __builtin_ldexpf(1.f, -kKeys) : 1.f;
+                bool past = false;
 #pragma unroll
-            for (int m = 0; m < 4; ++m)
+                for (int m = 0; m < 4; ++m)
 #pragma unroll
-                for (int n = 0; n < NT; ++n) s[m][n] = v4f{0.f, 0.f, 0.f, 0.f};
+                    for (int n = 0; n < NT; ++n) s[m][n] = v4f{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int k = 0; k < KC; ++k)
+                for (int k = 0; k < KC; ++k)
 #pragma unroll
-                for (int w = 0; w < kWords; ++w) {
-                    u4 y[4];
+                    for (int w = 0; w < kWords; ++w) {
+                        u4 y[4];
 #pragma unroll
-                    for (int m = 0; m < 4; ++m) y[m] = key_word(m, k, w);
-                    if constexpr (kF32) {
+                        for (int m = 0; m < 4; ++m) y[m] = key_word(m, k, w);
+                        if constexpr (kF32) {
 #pragma unroll
-                        for (int e = 0; e < 4; ++e)
+                            for (int e = 0; e < 4; ++e)
 #pragma unroll
-                            for (int m = 0; m < 4; ++m) {
-                                const float f = __uint_as_float(y[m][e]) * 0x1p-10f;
+                                for (int m = 0; m < 4; ++m) {
+                                    const float f = __uint_as_float(y[m][e]) * keys_by;
 #pragma unroll
-                                for (int n = 0; n < NT; ++n) s[m][n] = mfma_f32(f, q[n][k][4 * w + e], s[m][n]);
+                                    for (int n = 0; n < NT; ++n) s[m][n] = mfma_f32(f, q[n][k][4 * w + e], s[m][n]);
+                                }
+                        } else {
+#pragma unroll
+                            for (int m = 0; m < 4; ++m)
+#pragma unroll
+                                for (int n = 0; n < NT; ++n)
+                                    s[m][n] = mfma_f16(__builtin_bit_cast(h8, y[m]), q[n][k][w], s[m][n]);
+                        }
+                    }
+#pragma unroll
+                for (int m = 0; m < 4; ++m)
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            // (kept for odd_values and others, which need them once they are weights)
+                            float &kept = scores[(n * 16 + x) * kScores + 16 * c + 4 * m + e];
+                            const bool sees = seen[n] >> (4 * m + e) & 1;
+                            float y = s[m][n][e];
+                            if constexpr (kF32) {
+                                y = __builtin_ldexpf(y * factor, qe[n] + (smaller ? kKeys : 0));
+                                if (smaller && fabsf(kept) < __builtin_inff()) y = kept;
+                                past |= sees && !(fabsf(y) < __builtin_inff());
                             }
-                    } else {
-#pragma unroll
-                        for (int m = 0; m < 4; ++m)
-#pragma unroll
-                            for (int n = 0; n < NT; ++n)
-                                s[m][n] = mfma_f16(__builtin_bit_cast(h8, y[m]), q[n][k][w], s[m][n]);
-                    }
-                }
-#pragma unroll
-            for (int m = 0; m < 4; ++m)
-#pragma unroll
-                for (int n = 0; n < NT; ++n)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        float y = s[m][n][e];
-                        if constexpr (kF32) y = __builtin_ldexpf(y * factor, qe[n] + ke);
-                        const bool sees = seen[n] >> (4 * m + e) & 1;
-                        s[m][n][e] = sees ? y : kMinusInf;
-                        y = sees ? y : __builtin_nanf("");
-                        // (kept for odd_values, which needs them once they are weights)
-                        lds[((wave * NT + n) * 16 + x) * kScores + 16 * c + 4 * m + e] = y;
-                    }
+                            s[m][n][e] = sees ? y : kMinusInf;
+                            kept = sees ? y : __builtin_nanf("");
+                        }
+                if (!kF32 || smaller || !__builtin_expect(__any(past), 0)) break;
+            }
             r.softmax(s, kF32 ? 1.f : factor, (float)shift);
             // a value that is not finite, or larger than the weights are made for
             bool odd = false;
@@ -1018,7 +1031,6 @@ __global__ __launch_bounds__(256, (attention_waves<T, VT, NT>())) void k_cache_a
                     }
                 }
             };
-            float *scores = lds + wave * NT * 16 * kScores;
             if (__builtin_expect(odd, 0)) {
                 if constexpr (kF32) {
                     uint32_t from = 0, to = limit;

@@ -478,6 +478,10 @@ __device__ __forceinline__ void wave_sync() {
 constexpr int kShift = 64, kLarge = 64, kCodes = 10, kShiftAgain = -44;
 constexpr float kLargeScale = 0x1p55f;
 
+// binary16: the unit of a page's sums.  Codes times less than 2^-64 are nothing to the type, whose
+// smallest number is 2^-24; and 2^31 weights of 2^15 times its largest value are 2^126 in units of 2^-64.
+__device__ __forceinline__ float value_unit(float scale) { return scale < 0x1p-64f ? 0x1p-64f : scale; }
+
 // What a wave carries from key tile to key tile, for 16 NT rows (lane (x, c): row x of
 // every 16, features 16 d + 4 c + i)
 template <bool kF32, int VT, int NT>
@@ -783,7 +787,7 @@ __global__ __launch_bounds__(256, (attention_waves<T, VT, NT>())) void k_cache_a
             for (int d = 0; d < VT; ++d) vv[d] = buf_load16(from, v_at + first + 16 * d * v.block, 0);
             issued();        // before the scores: they are the time that the values have to come
             const float tile_ks = pages.scale(pages.ks, i64), vs = pages.scale(pages.vs, i64);
-            const float tile_vs = vs < 0x1p-32f && !kF32 ? 0x1p-32f : vs;
+            const float tile_vs = kF32 ? vs : value_unit(vs);
             v4f s[4][NT];
             // (products that follow one another are of different sums: none waits for the last)
 #pragma unroll
@@ -1221,7 +1225,7 @@ __global__ __launch_bounds__(256, VT == 16 ? 1 : 2) void k_cache_attention_share
         lds_barrier();
     }
     for (int tile = begin, buffer = 0; tile < paged_end; ++tile, buffer ^= 1) {
-        const float tile_ks = ks[0], tile_vs = vs[0] < 0x1p-32f ? 0x1p-32f : vs[0];
+        const float tile_ks = ks[0], tile_vs = value_unit(vs[0]);
         if (tile + 1 < paged_end) decode(buffer ^ 1);
         if (tile + 2 < paged_end) load(tile + 2, 2);
         ks[0] = ks[1];

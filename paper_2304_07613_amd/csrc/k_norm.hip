@@ -50,18 +50,18 @@ struct Pack {
 };
 
 // Sums (kMax: largest) of v over the threads of the same tokens.  Two buffers in turn, so that
-// one barrier a call is enough.
+// one barrier a call is enough.  kRare: in a few registers.
 template <int kVec>
 struct Reducer {
     static constexpr int kWaves = kThreads / 64;
-    float *lds;
+    double *lds;
     int lanes, turn = 0;
 
-    template <bool kMax>
-    __device__ __forceinline__ void operator()(float (&v)[kVec]) {
-        auto both = [](float a, float b) { return kMax ? fmaxf(a, b) : a + b; };
+    template <bool kMax, bool kRare = false, typename V>
+    __device__ __forceinline__ void operator()(V (&v)[kVec]) {
+        auto both = [](V a, V b) { return kMax ? (a > b ? a : b) : a + b; };
         const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, tokens = lanes * kVec;
-        float *here = lds + turn * kWaves * tokens;
+        V *here = reinterpret_cast<V *>(lds + turn * kWaves * tokens);
         turn ^= 1;
         if (kVec > 1 && lanes * kVec <= 64) {
             // halves are exchanged first: a lane ends up with one of its tokens, after 10
@@ -72,7 +72,7 @@ struct Reducer {
                 const bool up = lane & d;
 #pragma unroll
                 for (int e = 0; e < c; ++e) {
-                    const float send = up ? v[e] : v[e + c], keep = up ? v[e + c] : v[e];
+                    const V a = v[e], b = v[e + c], send = up ? a : b, keep = up ? b : a;
                     v[e] = both(keep, __shfl_xor(send, d));
                 }
                 token += up ? c : 0;
@@ -88,57 +88,74 @@ struct Reducer {
                 for (int e = 0; e < kVec; ++e) here[wave * tokens + lane * kVec + e] = v[e];
         }
         __syncthreads();
-        const float *mine = here + threadIdx.x % lanes * kVec;
+        const V *mine = here + threadIdx.x % lanes * kVec;
 #pragma unroll
         for (int e = 0; e < kVec; ++e) v[e] = mine[e];
+#pragma unroll kRare ? 1 : kWaves
         for (int w = 1; w < kWaves; ++w)
 #pragma unroll
             for (int e = 0; e < kVec; ++e) v[e] = both(v[e], mine[w * tokens + e]);
     }
 };
 
+// What the values of a norm may be: kSmall, binary16, whose squares and sums are in binary32's range.  kWide, what becomes
+// binary16 only afterwards (scale, weights and biases are binary32, so a sum with the residual may be of any size): sums in
+// binary64.  kAll, binary32: sums in binary32, and made once more where that range does not do.
+// (kWide so too would cost calls of 4096 rows a workgroup a compute unit, 8192 tokens 191 us in place of 148.)
+enum Range { kSmall, kWide, kAll };
+
 // x becomes its norm, without weight and bias
-template <typename T, int kVec, int kPer>
+template <Range kRange, int kVec, int kPer>
 __device__ __forceinline__ void normed(float (&x)[kPer][kVec], const nmg_norm &norm, int M,
                                        Reducer<kVec> &reduce) {
     if (norm.kind == NMG_NORM_NONE) return;
     const int step = kThreads / reduce.lanes, r0 = threadIdx.x / reduce.lanes;
     const float inv_m = 1.f / (float)M;
-    float mean[kVec], ss[kVec];
-    int ex[kVec] = {};
-    bool scaled = false;
-#pragma unroll 1
-    for (;;) {
+    using Sum = std::conditional_t<kRange == kWide, double, float>;
+    float mean[kVec], by[kVec];      // by: what a token is multiplied by first
+    Sum ss[kVec];
+#pragma unroll
+    for (int e = 0; e < kVec; ++e) by[e] = 1.f;
+    auto sums = [&](auto rare) __attribute__((always_inline)) {
+        constexpr bool kRare = decltype(rare)::value;
 #pragma unroll
         for (int e = 0; e < kVec; ++e) mean[e] = 0.f;
         if (norm.kind == NMG_NORM_LAYER) {
+            Sum sum[kVec] = {};
 #pragma unroll
             for (int i = 0; i < kPer; ++i)
 #pragma unroll
-                for (int e = 0; e < kVec; ++e) mean[e] += x[i][e];   // (rows past M hold 0)
-            reduce.template operator()<false>(mean);
+                for (int e = 0; e < kVec; ++e) sum[e] += (Sum)(x[i][e] * by[e]);   // (rows past M hold 0)
+            reduce.template operator()<false, kRare>(sum);
 #pragma unroll
-            for (int e = 0; e < kVec; ++e) mean[e] *= inv_m;
+            for (int e = 0; e < kVec; ++e) mean[e] = (float)(sum[e] * inv_m);
         }
 #pragma unroll
-        for (int e = 0; e < kVec; ++e) ss[e] = 0.f;
+        for (int e = 0; e < kVec; ++e) ss[e] = 0;
 #pragma unroll
         for (int i = 0; i < kPer; ++i)
 #pragma unroll
             for (int e = 0; e < kVec; ++e) {
-                const float d = r0 + i * step < M ? x[i][e] - mean[e] : 0.f;
+                const Sum d = r0 + i * step < M ? __builtin_fmaf(x[i][e], by[e], -mean[e]) : 0.f;
                 ss[e] += d * d;
             }
-        reduce.template operator()<false>(ss);
-        if constexpr (!std::is_same<T, float>::value) break;
-        // Squares or sums past the range, or below it where eps does not cover what is
-        // lost: the tokens are scaled by a power of two each to below 2 and summed again.
-        bool again = false;
+        reduce.template operator()<false, kRare>(ss);
+    };
+    sums(std::false_type{});
+    // Squares or sums past the range, or below it where eps does not cover what is lost: once more, of tokens
+    // times a power of two each that brings them to about 1
+    bool scaled = false;
+    if constexpr (kRange == kAll) {
 #pragma unroll
         for (int e = 0; e < kVec; ++e)
-            again |= !(ss[e] < __builtin_inff()) || (ss[e] < 0x1p-80f && norm.eps < 0x1p-60f);
-        if (scaled || !__syncthreads_or(again)) break;
-        scaled = true;
+            scaled |= !(ss[e] < __builtin_inff()) || (ss[e] < 0x1p-80f && norm.eps < 0x1p-60f);
+        // (every wave has all tokens of the tile, with the same sums: all agree without a barrier)
+        scaled = __any(scaled);
+    }
+    float *factors = reinterpret_cast<float *>(reduce.lds + 2 * Reducer<kVec>::kWaves * reduce.lanes * kVec);
+    float *scales = factors + reduce.lanes * kVec;
+    const int at = threadIdx.x % reduce.lanes * kVec;
+    if (__builtin_expect(scaled, 0)) {
         float top[kVec];
 #pragma unroll
         for (int e = 0; e < kVec; ++e) {
@@ -149,29 +166,36 @@ __device__ __forceinline__ void normed(float (&x)[kPer][kVec], const nmg_norm &n
                 if (v < __builtin_inff()) top[e] = fmaxf(top[e], v);
             }
         }
-        reduce.template operator()<true>(top);
+        reduce.template operator()<true, true>(top);
 #pragma unroll
-        for (int e = 0; e < kVec; ++e) {
-            ex[e] = top[e] == 0.f ? 0 : __builtin_amdgcn_frexp_expf(top[e]) - 1;
+        for (int e = 0; e < kVec; ++e)
+            by[e] = top[e] == 0.f ? 1.f : __builtin_ldexpf(1.f, min(max(1 - __builtin_amdgcn_frexp_expf(top[e]), -126), 126));
+        sums(std::true_type{});
+        // the factors of the differences: 1 / sqrt(mean square + eps by^2), by a thread each
+        if ((int)threadIdx.x < reduce.lanes)
 #pragma unroll
-            for (int i = 0; i < kPer; ++i) x[i][e] = __builtin_ldexpf(x[i][e], -ex[e]);
-        }
+            for (int e = 0; e < kVec; ++e) {
+                factors[at + e] = ss[e];
+                scales[at + e] = by[e];
+            }
+        __syncthreads();
+        if (const int t = threadIdx.x; t < reduce.lanes * kVec)
+            factors[t] = (float)(1.0 / sqrt((double)factors[t] / M + (double)norm.eps * scales[t] * scales[t]));
+        __syncthreads();
     }
 #pragma unroll
     for (int e = 0; e < kVec; ++e) {
-        float inv;
-        if (std::is_same<T, float>::value && scaled)    // x / sqrt(mean square + eps), both over 2^ex
-            inv = (float)(1.0 / sqrt((double)ss[e] / M + __builtin_ldexp((double)norm.eps, -2 * ex[e])));
-        else
-            inv = 1.f / sqrtf(ss[e] * inv_m + norm.eps);
+        const float inv = scaled             ? factors[at + e]
+                          : kRange == kWide ? (float)(1.0 / sqrt(ss[e] * inv_m + norm.eps))
+                                            : 1.f / sqrtf(ss[e] * inv_m + norm.eps);
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) x[i][e] = (x[i][e] - mean[e]) * inv;
+        for (int i = 0; i < kPer; ++i) x[i][e] = __builtin_fmaf(x[i][e], by[e], -mean[e]) * inv;
     }
 }
 
 // kWhole: every token of the tile is inside
 template <typename T, int kVec, int kPer, bool kWhole>
-__device__ __forceinline__ void residual_norm(const NormArgs &a, int tile, float *lds) {
+__device__ __forceinline__ void residual_norm(const NormArgs &a, int tile, double *lds) {
     using P = Pack<T, kVec>;
     // The gate and the residual are asked for with A where they are 64 bytes a thread at most:
     // more of them beside A cost registers that the loads of A lack (binary16 768 x 32768 101 us
@@ -223,7 +247,7 @@ __device__ __forceinline__ void residual_norm(const NormArgs &a, int tile, float
             }
         }
     Reducer<kVec> reduce{lds, lanes};
-    normed<T, kVec, kPer>(x, a.after, a.M, reduce);
+    normed<std::is_same<T, float>::value ? kAll : kSmall, kVec, kPer>(x, a.after, a.M, reduce);
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
         const int r = r0 + i * step;
@@ -248,7 +272,7 @@ __device__ __forceinline__ void residual_norm(const NormArgs &a, int tile, float
         if (a.H) h.template store<kWhole>(const_cast<T *>(at_row(a.H, a.ldh, i)), valid);
     }
     if (!a.Y) return;
-    normed<T, kVec, kPer>(x, a.before, a.M, reduce);
+    normed<std::is_same<T, float>::value ? kAll : kWide, kVec, kPer>(x, a.before, a.M, reduce);
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
         const int r = r0 + i * step;
@@ -262,9 +286,11 @@ __device__ __forceinline__ void residual_norm(const NormArgs &a, int tile, float
     }
 }
 
+// (binary16 of up to 4096 rows: two workgroups a compute unit, at 10 spilled registers.  148 us for 8192 tokens;
+// one workgroup with 134 registers, 188.)
 template <typename T, int kVec, int kPer>
-__global__ __launch_bounds__(kThreads, 2) void k_residual_norm(NormArgs a, int tiles) {
-    extern __shared__ float lds[];
+__global__ __launch_bounds__(kThreads, (kVec == 8 && kPer == 8 ? 4 : 2)) void k_residual_norm(NormArgs a, int tiles) {
+    extern __shared__ double lds[];
     const int tile = xcd_tile(blockIdx.x, tiles);
     if (((int64_t)tile + 1) * a.lanes * kVec <= a.N)
         residual_norm<T, kVec, kPer, true>(a, tile, lds);
@@ -278,7 +304,7 @@ nmg_status run(NormArgs a, int tokens, hipStream_t stream) {
     const int tiles = (int)(((int64_t)a.N + tokens - 1) / tokens);
     if ((int64_t)tiles * kThreads >= ((int64_t)1 << 32)) return NMG_ERR_UNSUPPORTED;
     const int step = kThreads / a.lanes, per = (a.M + step - 1) / step;
-    const size_t room = 2 * (kThreads / 64) * tokens * sizeof(float);
+    const size_t room = (2 * (kThreads / 64) + 1) * tokens * sizeof(double);
     auto go = [&](auto k) {
         constexpr int kPer = decltype(k)::value;
         k_residual_norm<T, kVec, kPer><<<tiles, kThreads, room, stream>>>(a, tiles);

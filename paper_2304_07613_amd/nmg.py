@@ -16,6 +16,7 @@ import ctypes
 import importlib.util
 import os
 import re
+import types
 
 import torch
 
@@ -677,9 +678,22 @@ def tree_attention(Q, K, V, heads: int, kv_heads: int, q_offsets, kv_begin, kv_e
 
 # ------------------------------------------------------------ a cache in 8 bits
 
-class Cache:
+class _Fixed:
+    """What the library knows by the addresses of its tensors: once it is made, its attributes stay."""
+
+    def __setattr__(self, name, value):
+        if self.__dict__.get("made"):
+            raise AttributeError(f"a {type(self).__name__} stays as it was made: calls know its tensors by address")
+        super().__setattr__(name, value)
+
+    def __delattr__(self, name):
+        raise AttributeError(f"a {type(self).__name__} stays as it was made: calls know its tensors by address")
+
+
+class Cache(_Fixed):
     """Buffers of a cache in 8 bits for several sequences and layers (``nmg_cache``);
-    they are read by the attribute names below and not exchanged afterwards.
+    they are read by the attribute names below and cannot be exchanged afterwards (calls
+    know their addresses).
 
         k_pages     layers x pages x kv_heads x block x dim16   float8_e4m3fn or int8
         v_pages     layers x pages x kv_heads x head_dim x block
@@ -716,16 +730,16 @@ class Cache:
                 raise ValueError(f"{name} must be contiguous {shape}")
             if not t.is_cuda or t.device != v_pages.device:
                 raise ValueError("a cache's tensors must be on one GPU")
-        self.buffers = {name: given[name] for name in want}
+        self.buffers = types.MappingProxyType({name: given[name] for name in want})
         self.format, code = by_code[v_pages.dtype]
         self.layers, self.pages, self.kv_heads, self.head_dim, self.block = v_pages.shape
         self.sequences, self.row, self.room, self.dtype = sequences, row, room, v_open.dtype
         self.device, self.index = v_pages.device, v_pages.get_device()
         self.c = _Cache(layers, heads, dim, _DTYPE_CODE[v_open.dtype], code, block, pages, sequences,
                         row, room, *(t.data_ptr() for t in self.buffers.values()))
-        self.address = ctypes.addressof(self.c)
         if lib().nmg_cache_compact_workspace_bytes(self.c) < 0:
             raise NmgError(ERR_UNSUPPORTED, "nmg_cache")
+        self.address, self.made = ctypes.addressof(self.c), True
 
     def __getattr__(self, name):
         try:
@@ -836,9 +850,10 @@ def cache_compact(cache: Cache, table=None, references=None) -> torch.Tensor:
 
 # ------------------------------------------------------- norms around a block
 
-class Norm:
+class Norm(_Fixed):
     """A norm over features (``nmg_norm``): kind "rms", "layer" or "none", weight and
-    bias float32 with a value for every feature, or None."""
+    bias float32 with a value for every feature, or None.  Their values may change, the
+    tensors and numbers themselves not: that is another Norm."""
 
     def __init__(self, kind: str = "rms", weight=None, bias=None, eps: float = 1e-6):
         if kind not in NORMS:
@@ -857,7 +872,7 @@ class Norm:
         self.kind, self.weight, self.bias, self.eps = kind, weight, bias, eps
         self.c = _Norm(NORMS[kind], None if weight is None else weight.data_ptr(),
                        None if bias is None else bias.data_ptr(), eps)
-        self.args = (ctypes.addressof(self.c), rows, device)
+        self.args, self.made = (ctypes.addressof(self.c), rows, device), True
 
 
 def residual_norm(A, R=None, gate=None, scale: float = 1.0, after: Norm | None = None,

@@ -458,6 +458,13 @@ __device__ __forceinline__ int exponent_of(float v) {
 }
 // What was loaded before is loaded again, rather than kept in registers
 __device__ __forceinline__ void reload() { asm volatile("" ::: "memory"); }
+// 2^(x + e), 2^127 at most.  Whole powers go into the exponent: beside them x would lose bits, and below 2^-126 the
+// instruction knows no numbers.
+__device__ __forceinline__ float weight_at(float x, int e) {
+    x = x < -1000.f ? -1000.f : x;       // (NaN stays)
+    const float whole = floorf(x);
+    return fminf(__builtin_ldexpf(exp2_fast(x - whole), (int)whole + e), 0x1p127f);
+}
 // No instruction is moved across
 __device__ __forceinline__ void issued() { __builtin_amdgcn_sched_barrier(0); }
 // LDS that the wave's lanes wrote is read by its other lanes
@@ -467,14 +474,13 @@ __device__ __forceinline__ void wave_sync() {
 }
 
 // Binary32 sums: any value of the type may meet any weight, and what is large may be what a row does not
-// see, or hardly weighs.  So values keep their size, and weights are 2^kShift times larger: products of
-// weights down to 2^-190 of the largest with values below 2^kLarge are whole.  Larger open values (there
-// are hardly ever any) take weights of their own, 2^(kLarge - 1) times larger still, and the values as many
+// see, or hardly weighs.  So values keep their size, and weights are 2^kShift times larger: of their
+// products with values below 2^kLarge none is lost that is 2^-148 or more.  Larger open values (there are
+// hardly ever any) take weights of their own, 2^(kLarge - 1) times larger still, and the values as many
 // times smaller; page scales from kLargeScale on go into the weights' exponents, with codes times 2^kCodes.
 // Those weights are cut at 2^127, where their products with all but zeros are past the range anyway.  A result
 // that passes the range -- of values above 2^64 or so, over the number of keys -- is made once more, with
-// weights times 2^kShiftAgain, where no sum of any values does.
-// (Beside the roundings there is left: 2^-125 a key, of weights below 2^-253; 2^-17 in results past 2^50.)
+// weights times 2^kShiftAgain, where no sum of any values does (and products below 2^-40 are lost).
 constexpr int kShift = 64, kLarge = 64, kCodes = 10, kShiftAgain = -44;
 constexpr float kLargeScale = 0x1p55f;
 
@@ -514,9 +520,9 @@ struct Pass {
             unit = vs;
         }
     }
-    // Scores s * f (in units of log 2, f > 0) to weights, in place.  binary32: f is 1; weights
-    // times 2^shift are counted into the total, those left in s are 2^more times larger.
-    __device__ __forceinline__ void softmax(v4f (&s)[4][NT], float f, float shift = 0.f, float more = 0.f) {
+    // Scores s * f (in units of log 2, f > 0) to weights, in place.  binary32 (f is 1): to their differences
+    // from the reference, of which weigh makes weights.
+    __device__ __forceinline__ void softmax(v4f (&s)[4][NT], float f) {
         float top[NT];
         bool up = false;
 #pragma unroll
@@ -526,8 +532,6 @@ struct Pass {
             for (int i = 1; i < 4; ++i)
                 t = larger(t, larger(larger(s[i][n][0], s[i][n][1]), larger(s[i][n][2], s[i][n][3])));
             top[n] = max_over_c(t) * f;
-            // (the reference of binary32's weights has the shift in it, as it is rounded)
-            if (kF32) top[n] -= shift;
             up |= top[n] > m[n] + kSlack;
         }
         if (__any(up)) {
@@ -547,22 +551,46 @@ struct Pass {
             // binary16 weights are 2^15 at most, so that the small ones stay normal down to
             // 2^-23 of the reference (totals have the same factor)
             const float base = (m[n] == kMinusInf ? 0.f : m[n]) - (kF32 ? 0.f : 15.f - kSlack);
-            if constexpr (!kF32) {
 #pragma unroll
-                for (int i = 0; i < 16; ++i) s[i / 4][n][i % 4] = exp2_fast(__builtin_fmaf(s[i / 4][n][i % 4], f, -base));
-            } else {
-#pragma unroll
-                for (int i = 0; i < 16; ++i) s[i / 4][n][i % 4] -= base;
-                if (__builtin_expect(more > 0.f, 0))
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        total[n][0] += exp2_fast(s[i / 4][n][i % 4]);
-                        s[i / 4][n][i % 4] = exp2_fast(fminf(s[i / 4][n][i % 4] + more, 127.f));
-                    }
-                else
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) total[n][0] += s[i / 4][n][i % 4] = exp2_fast(s[i / 4][n][i % 4]);
+            for (int i = 0; i < 16; ++i) {
+                const float v = s[i / 4][n][i % 4];
+                s[i / 4][n][i % 4] = kF32 ? v - base : exp2_fast(__builtin_fmaf(v, f, -base));
             }
+        }
+    }
+    // binary32: whether a row's difference is below -120, where exp2_fast may not do, and not minus infinity
+    __device__ __forceinline__ static bool deep(const v4f (&s)[4][NT]) {
+        uint32_t most = 0;       // of the bits of negative numbers the largest are the smallest; minus infinity, NaN become 0
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const float x = s[i / 4][n][i % 4];
+                most = max(most, __float_as_uint(x) + 0x800000u);
+            }
+        return __any(most > 0xc2f00000u + 0x800000u);
+    }
+    // binary32: the lane's differences to weights, those counted into the total: times f where all are plain,
+    // else times f2 2^e
+    __device__ __forceinline__ void weigh(v4f (&s)[4][NT], bool plain, float f, float f2, int e) {
+        if (__builtin_expect(plain, 1)) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const float w = exp2_fast(s[i / 4][n][i % 4]);
+                    total[n][0] += w;
+                    s[i / 4][n][i % 4] = w * f;
+                }
+        } else {
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const float x = s[i / 4][n][i % 4];
+                    total[n][0] += exp2_fast(x);
+                    s[i / 4][n][i % 4] = weight_at(x, e) * f2;
+                }
         }
     }
     // binary16: the lane's 16 weights as the matrix instructions take them, and their total
@@ -577,7 +605,7 @@ struct Pass {
         }
     }
     // the sums over their totals
-    __device__ __forceinline__ void finish(Result<kF32, VT, NT> &r) {
+    __device__ __forceinline__ void finish(Result<kF32, VT, NT> &r, int shift = 0) {
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
             r.m[n] = m[n];
@@ -586,7 +614,7 @@ struct Pass {
 #pragma unroll
             for (int d = 0; d < VT; ++d)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) r.o[d][n][i] = kF32 ? o[d][n][i] * inv : o[d][n][i] * inv * unit;
+                for (int i = 0; i < 4; ++i) r.o[d][n][i] = o[d][n][i] * inv * (kF32 ? __builtin_ldexpf(1.f, -shift) : unit);
         }
     }
 };
@@ -837,12 +865,9 @@ __global__ __launch_bounds__(256, (attention_waves<T, VT, NT>())) void k_cache_a
             }
             if constexpr (kF32) {
                 const int large = tile_vs > kLargeScale ? exponent_of(tile_vs) - kCodes : 0;
-                r.softmax(s, 1.f, (float)shift, (float)large);
-                const float f = large ? __builtin_ldexpf(tile_vs, -large - kCodes) : tile_vs;
-#pragma unroll
-                for (int w = 0; w < 4; ++w)
-#pragma unroll
-                    for (int n = 0; n < NT; ++n) s[w][n] *= f;
+                r.softmax(s, 1.f);
+                r.weigh(s, large == 0 && !r.deep(s), tile_vs * __builtin_ldexpf(1.f, shift),
+                        large ? __builtin_ldexpf(tile_vs, -large - kCodes) : tile_vs, shift + large);
                 auto sums = [&](float by) {
                     // (four features at a time, so that products that follow one another are of different sums)
 #pragma unroll
@@ -976,7 +1001,8 @@ __global__ __launch_bounds__(256, (attention_waves<T, VT, NT>())) void k_cache_a
                         }
                 if (!kF32 || smaller || !__builtin_expect(__any(past), 0)) break;
             }
-            r.softmax(s, kF32 ? 1.f : factor, (float)shift);
+            r.softmax(s, kF32 ? 1.f : factor);
+            if constexpr (kF32) r.weigh(s, !r.deep(s), __builtin_ldexpf(1.f, shift), 1.f, shift);
             // a value that is not finite, or larger than the weights are made for
             bool odd = false;
             constexpr uint32_t limit = (127 + kLarge) << 23;
@@ -1056,7 +1082,7 @@ __global__ __launch_bounds__(256, (attention_waves<T, VT, NT>())) void k_cache_a
 #pragma unroll
                             for (int e = 0; e < 16; ++e) {
                                 const float y = scores[(n * 16 + x) * kScores + 16 * c + e] - (r.m[n] == kMinusInf ? 0.f : r.m[n]);
-                                s[e / 4][n][e % 4] = y == y ? exp2_fast(fminf(y + (float)(kLarge - 1), 127.f)) : 0.f;
+                                s[e / 4][n][e % 4] = y == y ? weight_at(y, shift + kLarge - 1) : 0.f;
                             }
                     }
                 } else {
@@ -1077,7 +1103,7 @@ __global__ __launch_bounds__(256, (attention_waves<T, VT, NT>())) void k_cache_a
 
         // ---- the wave's sums over its totals, then the four waves'
         Result<kF32, VT, NT> mine;
-        r.finish(mine);
+        r.finish(mine, shift);
         if (end - begin > 1) join_waves(mine, lds);
         return wave == 0 && store_result<T, 16 * NT>(a, t, 0, mine, again);
     };

@@ -1,7 +1,6 @@
 """Binary32 values of very different sizes in one cache: what a row does not see, or hardly weighs,
 costs no precision of what it sees.  References and bounds as in ``test_cache.py``: relative to
-sum_j p_j |v_j| of the row and feature.  A weight below 2^-253 or so is no number any more; what it
-leaves out, 2^-125 at most, is less than the bounds of the values here."""
+sum_j p_j |v_j| of the row and feature."""
 import numpy as np
 import pytest
 

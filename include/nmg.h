@@ -778,7 +778,7 @@ typedef struct nmg_norm {
  * size, also where their squares are past the range.  H and Y may each be A, G or R
  * (with its leading dimension), not both the same.  In binary16 too scale, weights and biases may
  * be of any size, and H in binary32 with them, as long as the root of the mean square (LAYER:
- * of the differences) of a token of H is 0 or from 2^-126 to 2^126.  NMG_ERR_UNSUPPORTED: M >
+ * of the differences) of a token of H is 0 or from 2^-100 to 2^126.  NMG_ERR_UNSUPPORTED: M >
  * 32768, or more tokens than one launch holds (2^32 threads, 512 for 64 tokens or fewer). */
 nmg_status nmg_residual_norm(nmg_dtype dtype, int64_t M, int64_t N, const void *A, int64_t lda,
                              const nmg_norm *after, const void *G, int64_t ldg, float scale,

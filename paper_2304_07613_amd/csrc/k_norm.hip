@@ -8,10 +8,10 @@
 // waves through LDS.  Rows may start on any element: the loads of kVec tokens do not
 // ask for more.
 //
-// 768 x 8: 7.5 us, one workgroup's chain of loads, two sums and stores.  768 x 4096
-// (residual, LayerNorm, 25 MB): 11.7 us, 256 workgroups, one a compute unit, so that a
+// 768 x 8: 7.6 us, one workgroup's chain of loads, two sums and stores.  768 x 4096
+// (residual, LayerNorm, 25 MB): 11.5 us, 256 workgroups, one a compute unit, so that a
 // chain stands beside no other.  Binary32 4096 x 4095, norms on both sides, gate and residual
-// (335 MB): 127 us, 2.6 TB/s: 8 tokens are all that fit the registers, 32 bytes a row, and
+// (335 MB): 122 us, 2.7 TB/s: 8 tokens are all that fit the registers, 32 bytes a row, and
 // one workgroup a compute unit holds them, so reading, summing and writing alternate.
 // Measured there: 16 tokens of 1024 threads 227 us and of 512 threads with 128 values each
 // 156, 4 tokens 238 (runs of 16 bytes), two workgroups of 128 registers 170 to 207 (spills),
@@ -99,9 +99,9 @@ struct Reducer {
 };
 
 // What the values of a norm may be: kSmall, binary16, whose squares and sums are in binary32's range.  kWide, what becomes
-// binary16 only afterwards (scale, weights and biases are binary32, so a sum with the residual may be of any size): sums in
-// binary64.  kAll, binary32: sums in binary32, and made once more where that range does not do.
-// (kWide so too would cost calls of 4096 rows a workgroup a compute unit, 8192 tokens 191 us in place of 148.)
+// binary16 only afterwards (scale, weights and biases are binary32, so a sum with the residual may be of any size): sums of
+// squares in binary64.  kAll, binary32: sums in binary32, and made once more where that range does not do.
+// (kWide as kAll would cost calls of 4096 rows a workgroup a compute unit, 8192 tokens 191 us in place of 147.)
 enum Range { kSmall, kWide, kAll };
 
 // x becomes its norm, without weight and bias
@@ -121,14 +121,15 @@ __device__ __forceinline__ void normed(float (&x)[kPer][kVec], const nmg_norm &n
 #pragma unroll
         for (int e = 0; e < kVec; ++e) mean[e] = 0.f;
         if (norm.kind == NMG_NORM_LAYER) {
-            Sum sum[kVec] = {};
+            // (kWide: 2^15 values of any size times 2^-16 stay in the range; rows past M hold 0)
+            constexpr float down = kRange == kWide ? 0x1p-16f : 1.f;
 #pragma unroll
             for (int i = 0; i < kPer; ++i)
 #pragma unroll
-                for (int e = 0; e < kVec; ++e) sum[e] += (Sum)(x[i][e] * by[e]);   // (rows past M hold 0)
-            reduce.template operator()<false, kRare>(sum);
+                for (int e = 0; e < kVec; ++e) mean[e] = __builtin_fmaf(x[i][e], down * by[e], mean[e]);
+            reduce.template operator()<false, kRare>(mean);
 #pragma unroll
-            for (int e = 0; e < kVec; ++e) mean[e] = (float)(sum[e] * inv_m);
+            for (int e = 0; e < kVec; ++e) mean[e] *= inv_m * (1.f / down);
         }
 #pragma unroll
         for (int e = 0; e < kVec; ++e) ss[e] = 0;
@@ -286,8 +287,8 @@ __device__ __forceinline__ void residual_norm(const NormArgs &a, int tile, doubl
     }
 }
 
-// (binary16 of up to 4096 rows: two workgroups a compute unit, at 10 spilled registers.  148 us for 8192 tokens;
-// one workgroup with 134 registers, 188.)
+// (binary16 of up to 4096 rows: two workgroups a compute unit, 128 registers.  147 us for 8192 tokens; one
+// workgroup of 134 registers, 188.)
 template <typename T, int kVec, int kPer>
 __global__ __launch_bounds__(kThreads, (kVec == 8 && kPer == 8 ? 4 : 2)) void k_residual_norm(NormArgs a, int tiles) {
     extern __shared__ double lds[];

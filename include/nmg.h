@@ -692,8 +692,12 @@ nmg_status nmg_cache_append(const nmg_cache *cache, int32_t layer, const int32_t
  * slots, pages and codes hold never matters.  A token that sees nothing, or all of whose scores are minus
  * infinity, gives 0; drafted tokens past the room are seen by none.  Infinities and
  * NaN of open tokens and queries reach the outputs that the formula makes them reach, and no
- * others.  Statistics and sums are binary32; binary16 weights are rounded
- * to binary16 for the product with V.  scale > 0.  O overlaps no input; columns
+ * others: a weight is 0 only where the score is minus infinity, however far below the others a
+ * score lies.  Statistics and sums are binary32; binary16 weights are rounded
+ * to binary16 for the product with V, and binary16 counts value scales below 2^-64 as 2^-64.
+ * Binary32 keys, values and queries may be of any size, and cost others no bits (but a query of
+ * 2^100 or more costs those of its token and head below 2^-59 some); a product q . k that
+ * is past the range times scale is infinite.  scale > 0.  O overlaps no input; columns
  * of no sequence are not written.  NMG_ERR_UNSUPPORTED: Nq * heads / kv_heads past 31
  * bits, or more row tiles and heads than one launch holds.
  *

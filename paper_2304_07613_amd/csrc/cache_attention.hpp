@@ -24,12 +24,15 @@
 // sums (Pass).
 //
 // What bounds it (MI355X, e4m3 unless said): a cache of many tokens, the memory -- 4 sequences
-// of 32768 tokens, 32 / 8 heads of 128, a token each: 54 us, 5.0 TB/s, and 6 of join.  A
-// short one, the chain of a workgroup -- 8 of 512, 12 heads of 64: 8.9 us, of which
+// of 32768 tokens, 32 / 8 heads of 128, a token each: 54 us, 5.0 TB/s, and 7 of join.  A
+// short one, the chain of a workgroup -- 8 of 512, 12 heads of 64: 9.0 us, of which
 // places 1.4, queries beside the first pages 1.6, three key tiles a wave 2.1, the waves' join 1.7,
 // stores 1.1.  Many rows, the vector instructions -- 63 drafted tokens over 8 caches of
-// 4307 to 8191, 16 / 4 heads of 128, int8: 55 us, 480 TFLOP/s, and 14 of join; they run
-// in 57% of the cycles of a busy compute unit, the matrix ones in 27%.
+// 4307 to 8191, 16 / 4 heads of 128, int8: 56 us, 470 TFLOP/s, and 14 of join; they run
+// in 52% of the cycles of a busy compute unit, the matrix ones in 28%.
+//
+// Spilled vector registers of the variants (row tiles of 16: features / 16, row tiles): few rows, binary16
+// 8, 2: 9; binary32 8, 1: 1 and 4, 2: 23; many rows 8, 2: 40 and 6, 2: 5; the others none.
 #pragma once
 
 #include "cache.hpp"
@@ -145,8 +148,9 @@ struct RowTile {
 struct KeyTiles {
     int paged, all;         // tiles of pages, and of both
     int open, kept;         // open tokens, and how many of them are kept ones
-    // In units of a page's tile, a tile of open tokens is three.  (It takes 7 us beside 2.5
-    // where many rows meet it.)
+    // In units of a page's tile, a tile of open tokens is three.  With 1 / 2 / 3 / 4: 8 single tokens over 500,
+    // 12 heads of 64, 9.9 / 9.1 / 9.3 / 9.4 us; 63 over 3000, 8 heads of 128, 37.6 / 35.2 / 34.4 / 33.6; binary32
+    // 5 over up to 701, 12 heads of 64, 18.7 / 18.3 / 16.9 / 19.4; others differ by 1%.
     __device__ __forceinline__ int units() const { return paged + 3 * (all - paged); }
     __device__ __forceinline__ int tile_at(int unit) const {
         return unit <= paged ? unit : paged + (unit - paged + 1) / 3;
@@ -696,15 +700,15 @@ struct Ahead {
 // Waves of a SIMD that the registers are to leave room for
 template <typename T, int VT, int NT>
 constexpr int attention_waves() {
-    return VT == 16 || NT == 4 || (std::is_same<T, float>::value && VT * NT == 16) ? 1 : 2;
+    return VT == 16 || (std::is_same<T, float>::value && VT * NT == 16) ? 1 : 2;
 }
 
 // Few rows: 16 or 32 of a workgroup, whose waves have key tiles of their own and join at the
 // end.  Keys of the next tile are on their way while one is multiplied, its values from before the
 // scores on.  The features of a workgroup's rows stay in registers; binary32 runs on the binary32
 // matrix instructions, whose rate a single row a sequence does not reach (8 sequences of
-// up to 701 tokens, 12 heads of 64, 5 drafted: 17 us, 8.5 of them the tile of open tokens,
-// whose largest value is looked up before its sums).
+// up to 701 tokens, 12 heads of 64, 5 drafted: 17.3 us, half of them the tile of open tokens,
+// whose values are looked at before its sums).
 template <typename T, int VT, int NT, bool kInt8>
 __global__ __launch_bounds__(256, (attention_waves<T, VT, NT>())) void k_cache_attention(CacheAttnArgs a) {
     constexpr bool kF32 = std::is_same<T, float>::value;
@@ -1127,8 +1131,8 @@ __device__ __forceinline__ void lds_barrier() {
 // tile's vector work -- and leaves it in LDS as the matrix instructions take it, 16 bytes a
 // lane, so that neither side has a bank conflict.  Two buffers: while tile i is multiplied,
 // tile i + 1 is decoded and tile i + 2 on its way.  Against the waves with keys of their own, 32
-// rows each: 548 vector instructions a tile and wave in place of 884, 75 us in place of 88 for the
-// 63 drafted tokens above.  From 65 rows of a (sequence, key head) on.
+// rows each: 75 us in place of 88 for the 63 drafted tokens above, whose (sequence, key head) have 252
+// rows each (when both were measured; 474 vector instructions a tile and wave now).
 template <int VT, int NT, bool kInt8>
 __global__ __launch_bounds__(256, VT == 16 ? 1 : 2) void k_cache_attention_shared(CacheAttnArgs a) {
     using T = _Float16;

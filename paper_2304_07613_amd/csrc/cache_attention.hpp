@@ -32,7 +32,7 @@
 // in 52% of the cycles of a busy compute unit, the matrix ones in 28%.
 //
 // Spilled vector registers of the variants (row tiles of 16: features / 16, row tiles): few rows, binary16
-// 8, 2: 9; binary32 8, 1: 1 and 4, 2: 23; many rows 8, 2: 40 and 6, 2: 5; the others none.
+// 8, 2: 34; binary32 16, 1: 4, 8, 1: 5 and 4, 2: 33; the others none.
 #pragma once
 
 #include "cache.hpp"
@@ -471,11 +471,6 @@ __device__ __forceinline__ float weight_at(float x, int e) {
 }
 // No instruction is moved across
 __device__ __forceinline__ void issued() { __builtin_amdgcn_sched_barrier(0); }
-// LDS that the wave's lanes wrote is read by its other lanes
-__device__ __forceinline__ void wave_sync() {
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-}
 
 // Binary32 sums: any value of the type may meet any weight, and what is large may be what a row does not
 // see, or hardly weighs.  So values keep their size, and weights are 2^kShift times larger: of their
@@ -632,41 +627,46 @@ __device__ __forceinline__ u4 finite_word(u4 y) {
     }
     return y;
 }
-// Those that are not finite, one by one, to the sums of the 16 rows that see them: `scores` are the rows'
-// in LDS (NaN: not seen, or its row is NaN already), `stride` a row.  Their weights are no 0, however
-// small, but where the score is minus infinity; word(d, w): the tile's values.
+// What a key's score makes of its values that are not finite: nothing where it is not seen (NaN; or the row is NaN
+// already), NaN where the weight is 0, themselves else, however small the weight
+__device__ __forceinline__ _Float16 odd_weight(float score) {
+    return (_Float16)(score == score ? score == kMinusInf ? 16384.f : 1.f : 0.f);
+}
+// Those values, to the sums: by matrix instructions on numbers that tell them apart -- 1, 128 and 16384 for plus and minus
+// infinity and NaN, whose sums over 64 keys do too.  w: the lane's 16 odd_weights; word(d, i): the tile's values.
 template <bool kF32, int VT, int NT, typename F>
-__device__ __forceinline__ void odd_values(v4f (&o)[VT][NT], int n, const float *scores, int stride, F &&word) {
-    const int lane = threadIdx.x & 63, x = lane % 16, c = lane / 16;
-    constexpr int kWords = kF32 ? 4 : 2, kPer = 16 / kWords;
+__device__ __forceinline__ void odd_values(v4f (&o)[VT][NT], int n, const h8 (&w)[2], F &&word) {
 #pragma unroll 1
-    for (int dw = 0; dw < VT * kWords; ++dw) {
-        const u4 y = word(dw / kWords, dw % kWords);
+    for (int d = 0; d < VT; ++d) {               // (a loop, since all at once would cost registers)
+        h8 kind[2];
+        bool some = false;
 #pragma unroll
-        for (int e = 0; e < kPer; ++e) {
-            float v;
-            if constexpr (kF32) {
-                const uint32_t bits = y[e];      // (a vector's element is no object of its own)
-                v = __uint_as_float(bits);
-            } else {
-                const uint16_t bits = (uint16_t)(y[e / 2] >> (16 * (e % 2)));
-                v = (float)__builtin_bit_cast(_Float16, bits);
-            }
-            uint64_t left = __ballot(!(fabsf(v) < __builtin_inff()));
-            while (left) {
-                const int l = __ffsll((unsigned long long)left) - 1;
-                left &= left - 1;
-                const float value = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), l));
-                const float score = scores[x * stride + 16 * (l / 16) + kPer * (dw % kWords) + e];
-                const float term = score == kMinusInf ? 0.f * value : value;
-                const int mine = score == score ? 16 * (dw / kWords) + l % 16 - 4 * c : -1;
+        for (int i = 0; i < (kF32 ? 4 : 2); ++i) {
+            const u4 y = word(d, i);
 #pragma unroll
-                for (int d = 0; d < VT; ++d)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if (mine == 16 * d + i) o[d][n][i] += term;
+            for (int e = 0; e < (kF32 ? 4 : 8); ++e) {
+                const uint32_t b = kF32 ? y[e] : y[e / 2] >> (16 * (e % 2)) << 16;      // (16 bits as the upper ones)
+                const uint32_t size = b & 0x7fffffffu, infinite = kF32 ? 0x7f800000u : 0x7c000000u;
+                const float k = size < infinite ? 0.f : size > infinite ? 16384.f : b >> 31 ? 128.f : 1.f;
+                some |= size >= infinite;
+                kind[kF32 ? i / 2 : i][kF32 ? 4 * (i % 2) + e : e] = (_Float16)k;
             }
         }
+        if (!__any(some)) continue;
+        v4f sum = {0.f, 0.f, 0.f, 0.f};
+        sum = mfma_f16(kind[0], w[0], sum);
+        sum = mfma_f16(kind[1], w[1], sum);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float minus = floorf(sum[i] * 0x1p-7f), plus = sum[i] - 128.f * minus;
+            sum[i] = sum[i] >= 16384.f || (minus > 0.f && plus > 0.f) ? __builtin_nanf("")
+                     : plus > 0.f  ? __builtin_inff()
+                     : minus > 0.f ? kMinusInf
+                                   : 0.f;
+        }
+#pragma unroll
+        for (int to = 0; to < VT; ++to)
+            if (to == d) o[to][n] += sum;
     }
 }
 
@@ -1092,11 +1092,13 @@ __global__ __launch_bounds__(256, (attention_waves<T, VT, NT>())) void k_cache_a
                 } else {
                     sums_f16([](u4 y) { return finite_word(y); });
                 }
-                wave_sync();
 #pragma unroll
-                for (int n = 0; n < NT; ++n)
-                    odd_values<kF32>(r.o, n, scores + n * 16 * kScores, kScores, value_word);
-                wave_sync();
+                for (int n = 0; n < NT; ++n) {
+                    h8 w[2];
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) w[e / 8][e % 8] = odd_weight(scores[(n * 16 + x) * kScores + 16 * c + e]);
+                    odd_values<kF32>(r.o, n, w, value_word);
+                }
             } else if constexpr (kF32) {
                 sums_f32([](uint32_t bits) { return __uint_as_float(bits); });
             } else {
@@ -1355,24 +1357,25 @@ __global__ __launch_bounds__(256, VT == 16 ? 1 : 2) void k_cache_attention_share
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
                         if (!(seen[n] >> (4 * i + e) & 1)) s[i][n][e] = kMinusInf;
-            if (__builtin_expect(odd_of[0] | odd_of[1] | odd_of[2] | odd_of[3], 0)) {
-                // (before the others, whose weights and units do not matter to them)
-                float *rows_of = reinterpret_cast<float *>(frag[1]) + wave * 1024;
+            const bool odd = odd_of[0] | odd_of[1] | odd_of[2] | odd_of[3];
+            uint32_t dead[NT] = {};          // (seen keys whose weight is 0: only scores tell)
+            if (__builtin_expect(odd, 0))
 #pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    wave_sync();
+                for (int n = 0; n < NT; ++n)
 #pragma unroll
-                    for (int e = 0; e < 16; ++e)
-                        rows_of[x * 64 + 16 * c + e] = seen[n] >> e & 1 ? s[e / 4][n][e % 4] : __builtin_nanf("");
-                    wave_sync();
-                    odd_values<false>(r.o, n, rows_of, 64, [&](int d, int w) {
-                        return open_word(tile, 16 * d + x, w);
-                    });
-                }
-            }
+                    for (int e = 0; e < 16; ++e) dead[n] |= (uint32_t)(s[e / 4][n][e % 4] == kMinusInf) << e;
             r.softmax(s, factor);
             r.new_unit(1.f);
             sums(0, s);
+            if (__builtin_expect(odd, 0))
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    h8 w[2];
+#pragma unroll
+                    for (int e = 0; e < 16; ++e)
+                        w[e / 8][e % 8] = odd_weight(!(seen[n] >> e & 1) ? __builtin_nanf("") : dead[n] >> e & 1 ? kMinusInf : 0.f);
+                    odd_values<false>(r.o, n, w, [&](int d, int i) { return open_word(tile, 16 * d + x, i); });
+                }
         }
         lds_barrier();
     }

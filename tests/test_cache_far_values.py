@@ -148,3 +148,29 @@ def test_scratch_memory_and_splits_change_nothing(dev, dtype):  # noqa: F811
                                    torch.cuda.current_stream().cuda_stream)
         assert st == 0
         check(out, ref, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
+@pytest.mark.parametrize("heads,dim", [(2, 64), (3, 80), (1, 200), (4, 128)])
+def test_many_values_that_are_not_finite(dev, heads, dim, dtype):  # noqa: F811
+    """Features with infinities of one sign, of both, NaN, and none, keys whose score is minus
+    infinity among them, seen by some."""
+    rng = np.random.default_rng(11)
+    for counts in ([7, 1, 40], [130, 255, 70]):
+        b = Both(dev, 1, 1, dim, 3, 30, 6, 384, 64, "e4m3", dtype)
+        b.grow([100, 0, 70])
+
+        def change(K, V, q):
+            some = rng.random(V.shape) < 0.05
+            kinds = np.array([math.inf, -math.inf, math.nan, 1.0, math.inf])[np.arange(dim) % 5]
+            signs = np.where(rng.random(V.shape) < 0.5, -1, 1)
+            V[:] = np.where(some, np.where((np.arange(dim) % 5 == 4)[:, None], signs, 1) * kinds[:, None], V)
+            K[0, rng.random(V.shape[1]) < 0.1] = -math.inf
+        q = b.draft(counts, change)
+        Q = np.random.default_rng(5).standard_normal((heads * dim, int(q[-1])))
+        Q[::dim] = 0.5
+        Q = Q.astype(np.float16 if dtype == "f16" else np.float32)
+        print(heads, dim, counts, dtype, flush=True)
+        b.attend(heads, q, random_tree(3, counts), Q=Q)
+        b.attend(heads, q, Q=Q)
+        b.attend(heads, q, random_tree(4, counts), Q=Q, longest=4000)

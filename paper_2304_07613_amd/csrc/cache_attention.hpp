@@ -25,10 +25,10 @@
 //
 // What bounds it (MI355X, e4m3 unless said): a cache of many tokens, the memory -- 4 sequences
 // of 32768 tokens, 32 / 8 heads of 128, a token each: 54 us, 5.0 TB/s, and 7 of join.  A
-// short one, the chain of a workgroup -- 8 of 512, 12 heads of 64: 9.0 us, of which
+// short one, the chain of a workgroup -- 8 of 512, 12 heads of 64: 8.6 us, of which
 // places 1.4, queries beside the first pages 1.6, three key tiles a wave 2.1, the waves' join 1.7,
 // stores 1.1.  Many rows, the vector instructions -- 63 drafted tokens over 8 caches of
-// 4307 to 8191, 16 / 4 heads of 128, int8: 56 us, 470 TFLOP/s, and 14 of join; they run
+// 4307 to 8191, 16 / 4 heads of 128, int8: 54 us, 490 TFLOP/s, and 14 of join; they run
 // in 52% of the cycles of a busy compute unit, the matrix ones in 28%.
 //
 // Spilled vector registers of the variants (row tiles of 16: features / 16, row tiles): few rows, binary16
